@@ -24,6 +24,11 @@
  *   dlm_loop_*               repeat a recorded pass on the GPU until no
  *                            confident edit remains (one graph launch)
  *
+ * Training and scoring the refiner's last layer (the paper takes trained
+ * refiners as they are; these have no counterpart in it):
+ *   dlm_layer_norm, dlm_layer_norm_grad    the norm in front of the projection
+ *   dlm_clip_grad_norm                     the norm over all gradients, clipping
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Tensors are passed as dlm_tensor descriptors: a DEVICE pointer of the
@@ -259,6 +264,71 @@ int dlm_refine_update_ranked(const dlm_tensor* tokens, const dlm_tensor* mask, c
                              const dlm_tensor* conf, const dlm_tensor* tok_prob,
                              const dlm_refine_params* params, dlm_tensor* new_tokens,
                              dlm_tensor* new_mask, dlm_tensor* n_edits);
+
+/*
+ * Layer norm over the last dimension, the norm in front of an output
+ * projection (dlm_lmhead_confidence):
+ *   mean[r] = sum_c x[r, c] / d
+ *   rstd[r] = 1 / sqrt(sum_c (x[r, c] - mean[r])^2 / d + eps)
+ *   out[r, c] = (x[r, c] - mean[r]) * rstd[r] * weight[c] + bias[c]
+ *
+ *   x, out        [N, d] or [B, L, d], BF16 or F32 (both the same dtype); innermost
+ *                 contiguous, rows evenly strided; any d >= 1, any alignment (16-byte
+ *                 aligned rows are faster)
+ *   weight, bias  d entries, BF16 or F32 (both the same dtype), contiguous; bias may be
+ *                 NULL
+ *   mean, rstd    N F32, contiguous: what dlm_layer_norm_grad reads; either may be NULL
+ *   eps           finite, >= 0
+ * Sums in fp32 over the centred values; one rounding to the output's dtype. out may
+ * not overlap x. A row with a NaN or an infinity gives NaN.
+ */
+int dlm_layer_norm(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* bias, float eps, dlm_tensor* out,
+                   dlm_tensor* mean, dlm_tensor* rstd);
+
+/*
+ * Gradients of dlm_layer_norm given dout, the gradient of out: with
+ * xhat = (x - mean) rstd and a = dout weight,
+ *   dx[r, c]   = rstd[r] (a[r, c] - (sum_k a[r, k] + xhat[r, c] sum_k a[r, k] xhat[r, k]) / d)
+ *   dweight[c] = sum_r dout[r, c] xhat[r, c]
+ *   dbias[c]   = sum_r dout[r, c]
+ *
+ *   dout, dx        the shape and dtype of x, rows evenly strided
+ *   mean, rstd      N F32, as dlm_layer_norm wrote them
+ *   dweight, dbias  d entries of weight's dtype, contiguous; either may be NULL. With no
+ *                   rows they are 0.
+ *   workspace       >= dlm_layer_norm_grad_workspace_bytes(N, d) bytes, 16-byte aligned,
+ *                   no initial contents needed; not used where dweight and dbias are both
+ *                   NULL. Calls sharing it must not overlap on the GPU.
+ * All sums in fp32 and in a fixed order: the same inputs give the same bits. No output
+ * may overlap another tensor.
+ */
+int dlm_layer_norm_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* mean,
+                        const dlm_tensor* rstd, dlm_tensor* dx, dlm_tensor* dweight, dlm_tensor* dbias, void* workspace,
+                        size_t workspace_bytes);
+size_t dlm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t d);
+
+/*
+ * The norm over all gradients of a step, and clipping by it:
+ *   norm = sqrt(sum over every element of every tensor of x^2)
+ *   outs[i] = grads[i] * min(1, max_norm / (norm + 1e-6))
+ *
+ *   grads, outs  arrays of `count` descriptors (host memory, read during the call):
+ *                contiguous tensors of any rank and size (empty ones too), BF16 or F32 each,
+ *                outs[i] of the shape and dtype of grads[i]. outs[i] may be grads[i] itself
+ *                (in place); no other overlap with an output is allowed, so a tensor listed
+ *                twice is refused where it is written. outs NULL: the norm alone.
+ *   count        0 .. 15360
+ *   max_norm     >= 0; infinity leaves the gradients as they are
+ *   norm         1 F32
+ *   workspace    >= dlm_clip_grad_norm_workspace_bytes() bytes, 8-byte aligned, no initial
+ *                contents needed; calls sharing it must not overlap on the GPU.
+ * The norm is exact to fp32 rounding over the whole range of the inputs (squares that
+ * leave fp32's range are summed in fp64) and summed in a fixed order. A NaN makes norm
+ * and every output NaN; an infinity makes norm infinite and finite elements 0.
+ */
+int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t count, float max_norm, dlm_tensor* norm,
+                       void* workspace, size_t workspace_bytes);
+size_t dlm_clip_grad_norm_workspace_bytes(void);
 
 /*
  * Steps A2 and A3 in one call (the per-position reduction of the confidences

@@ -31,6 +31,9 @@ remain).
 the output weights) followed by ``vocab.vocab_confidence``, the operation of
 the fused projection + reduction kernel.
 
+``train`` states the training and scoring of the refiner's last layer: layer
+norm, the cross entropy under the projection, their gradients, and clipping.
+
 Floating point is fp64 unless a comparison is defined in fp32 (edit threshold,
 remask order), where the fp32 values are compared exactly.
 
@@ -43,3 +46,5 @@ from .vocab import token_prob, vocab_confidence  # noqa: F401
 from .update import refine_update, remask_count  # noqa: F401
 from .lmhead import lm_head_confidence, lm_head_logits  # noqa: F401
 from .loop import refine_passes  # noqa: F401
+from .train import (clip_grad_norm, layer_norm, layer_norm_grad, lm_head_loss, lm_head_loss_grad,  # noqa: F401
+                    scored_rows)

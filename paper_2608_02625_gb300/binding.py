@@ -59,13 +59,20 @@ def _load():
     lib.dlm_lmhead_confidence.argtypes = [P, P, P, P, P, ctypes.c_void_p, ctypes.c_size_t]
     lib.dlm_lmhead_workspace_bytes.argtypes = [ctypes.c_int64]
     lib.dlm_lmhead_workspace_bytes.restype = ctypes.c_size_t
+    lib.dlm_layer_norm.argtypes = [P, P, P, ctypes.c_float, P, P, P]
+    lib.dlm_layer_norm_grad.argtypes = [P] * 8 + [ctypes.c_void_p, ctypes.c_size_t]
+    lib.dlm_layer_norm_grad_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64]
+    lib.dlm_clip_grad_norm.argtypes = [P, P, ctypes.c_int32, ctypes.c_float, P, ctypes.c_void_p, ctypes.c_size_t]
+    lib.dlm_clip_grad_norm_workspace_bytes.argtypes = []
+    for f in ("dlm_layer_norm_grad_workspace_bytes", "dlm_clip_grad_norm_workspace_bytes"):
+        getattr(lib, f).restype = ctypes.c_size_t
     lib.dlm_refine_update_ranked.argtypes = [P, P, P, P, P, ctypes.POINTER(DlmRefineParams), P, P, P]
     lib.dlm_refine_step_static.argtypes = [P, P, P, ctypes.POINTER(DlmRefineParams), P, P, P, P, P, P]
     lib.dlm_refine_step_workspace_bytes.argtypes = [ctypes.c_int64]
     lib.dlm_refine_step_workspace_bytes.restype = ctypes.c_size_t
     for f in ("dlm_bidir_attn", "dlm_attn_masked", "dlm_vocab_confidence", "dlm_refine_update", "dlm_refine_step",
               "dlm_refine_step_static", "dlm_token_prob", "dlm_refine_update_ranked", "dlm_lmhead_confidence",
-              "dlm_set_stream", "dlm_set_attn_tiles_per_unit",
+              "dlm_layer_norm", "dlm_layer_norm_grad", "dlm_clip_grad_norm", "dlm_set_stream", "dlm_set_attn_tiles_per_unit",
               "dlm_version", "dlm_get_device_error"):
         getattr(lib, f).restype = ctypes.c_int
     lib.dlm_loop_begin.argtypes = [ctypes.c_void_p]
@@ -250,6 +257,62 @@ def dlm_lmhead_confidence(hidden, weight, argmax, conf, lse, workspace):
     _check(lib.dlm_lmhead_confidence(*[_ref(d) for d in ds], ctypes.c_void_p(workspace.data_ptr() if nbytes else None),
                                      ctypes.c_size_t(nbytes)))
     return argmax, conf, lse
+
+
+def _workspace(workspace):
+    """(address, bytes) of a workspace tensor; (None, 0) for None."""
+    if workspace is None:
+        return ctypes.c_void_p(None), ctypes.c_size_t(0)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    nbytes = workspace.numel() * workspace.element_size()
+    return ctypes.c_void_p(workspace.data_ptr() if nbytes else None), ctypes.c_size_t(nbytes)
+
+
+def dlm_layer_norm(x, weight, bias, eps: float, out, mean, rstd):
+    """out = (x - mean) * rstd * weight + bias over the last dimension. bias, mean
+    and rstd may be None (mean and rstd are what dlm_layer_norm_grad reads)."""
+    if _done(_marshal.layer_norm(x, weight, bias, eps, out, mean, rstd)):
+        return out, mean, rstd
+    _prepare(x, weight, bias, out, mean, rstd)
+    dx, dw, db, do, dm, dr = (describe(t) for t in (x, weight, bias, out, mean, rstd))
+    _check(lib.dlm_layer_norm(_ref(dx), _ref(dw), _ref(db), float(eps), _ref(do), _ref(dm), _ref(dr)))
+    return out, mean, rstd
+
+
+def dlm_layer_norm_grad_workspace_bytes(rows: int, d: int) -> int:
+    return lib.dlm_layer_norm_grad_workspace_bytes(int(rows), int(d))
+
+
+def dlm_layer_norm_grad(dout, x, weight, mean, rstd, dx, dweight, dbias, workspace):
+    """Gradients of dlm_layer_norm. dweight and dbias may be None; the workspace too
+    where both are."""
+    if _done(_marshal.layer_norm_grad(dout, x, weight, mean, rstd, dx, dweight, dbias, workspace)):
+        return dx, dweight, dbias
+    _prepare(dout, x, weight, mean, rstd, dx, dweight, dbias, workspace)
+    ds = [describe(t) for t in (dout, x, weight, mean, rstd, dx, dweight, dbias)]
+    _check(lib.dlm_layer_norm_grad(*[_ref(d) for d in ds], *_workspace(workspace)))
+    return dx, dweight, dbias
+
+
+def dlm_clip_grad_norm_workspace_bytes() -> int:
+    return lib.dlm_clip_grad_norm_workspace_bytes()
+
+
+def dlm_clip_grad_norm(grads, outs, max_norm: float, norm, workspace):
+    """norm: over every element of every tensor of `grads`; outs[i] = grads[i] scaled so
+    that the norm is at most max_norm (outs may be grads: in place; None: the norm alone)."""
+    if _done(_marshal.clip_grad_norm(grads, outs, max_norm, norm, workspace)):
+        return outs, norm
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError("outs must have one tensor per gradient")
+    _prepare(norm, workspace, *grads, *(outs or ()))
+    n = len(grads)
+    dg = (DlmTensor * max(1, n))(*[describe(t) for t in grads])
+    do = None if outs is None else (DlmTensor * max(1, n))(*[describe(t) for t in outs])
+    dn = describe(norm)
+    _check(lib.dlm_clip_grad_norm(dg, do, n, float(max_norm), _ref(dn), *_workspace(workspace)))
+    return outs, norm
 
 
 def dlm_token_prob(logits, tokens, lse, prob):

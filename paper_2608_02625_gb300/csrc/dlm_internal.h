@@ -184,4 +184,54 @@ constexpr int kLmMaxSplits = 64;  // parts per row in the workspace
 inline size_t lmhead_workspace_bytes(int64_t N) { return static_cast<size_t>(N) * kLmMaxSplits * 12; }
 int launch_lmhead(const LmArgs& a, cudaStream_t stream);
 
+// Layer norm over the last dimension of [N, d] rows, and its gradients.
+struct NormArgs {
+  const void* x;
+  const void* weight;
+  const void* bias;      // may be null
+  void* out;
+  float* mean;           // written by the norm (may be null there), read by its gradients
+  float* rstd;
+  int64_t N, d, s_x, s_out;  // row strides in elements
+  int is_bf16, weight_bf16;
+  float eps;
+  const void* dout;      // gradients only, from here on
+  void* dx;
+  int64_t s_dout, s_dx;
+  void* dweight;         // may be null
+  void* dbias;           // may be null
+  void* workspace;       // norm_grad_workspace_bytes(N, d)
+};
+
+// CTAs that leave sums of the columns: four, or for wide rows two, on each SM.
+inline int norm_max_parts(int64_t d) { return d <= 2048 ? 608 : 304; }
+inline size_t norm_grad_workspace_bytes(int64_t N, int64_t d) {
+  const int64_t most = norm_max_parts(d), parts = N < most ? N : most;
+  return static_cast<size_t>(parts) * 2 * static_cast<size_t>(d) * sizeof(float);
+}
+int launch_layer_norm(const NormArgs& a, cudaStream_t stream);
+int launch_layer_norm_grad(const NormArgs& a, cudaStream_t stream);
+
+// The norm over all gradients, and their clipping.
+struct GradTensor {
+  const void* in;
+  void* out;
+  int64_t n;
+  bool is_bf16;
+};
+struct GradArgs {
+  const GradTensor* grads;
+  int count;
+  bool scale;            // write the scaled gradients (else the norm alone)
+  float max_norm;
+  float* norm;
+  double* workspace;     // clip_grad_norm_workspace_bytes()
+  int parts;             // set by the launcher
+};
+constexpr int kGradParts = 608;      // sums (CTAs) a launch
+constexpr int kGradTable = 960;      // tensors a launch
+constexpr int kMaxGradTensors = 16 * kGradTable;
+inline size_t clip_grad_norm_workspace_bytes() { return sizeof(double) * kGradParts * (kMaxGradTensors / kGradTable); }
+int launch_clip_grad_norm(const GradArgs& a, cudaStream_t stream);
+
 }  // namespace dlm

@@ -18,6 +18,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <vector>
 
 #include "dlmrefine.h"
 
@@ -41,21 +42,7 @@ class Call {
     at::Tensor* t = nullptr;
     if (!plain(o, &t)) return false;
     dlm_tensor& d = desc_[n_];
-    switch (t->scalar_type()) {
-      case at::kBFloat16: d.dtype = DLM_BF16; break;
-      case at::kFloat: d.dtype = DLM_F32; break;
-      case at::kInt: d.dtype = DLM_I32; break;
-      case at::kByte: d.dtype = DLM_U8; break;
-      default: return false;
-    }
-    const int64_t nd = t->dim();
-    if (nd < 1 || nd > 4) return false;
-    d.data = t->numel() ? t->data_ptr() : nullptr;
-    d.ndim = static_cast<int32_t>(nd);
-    for (int i = 0; i < 4; ++i) {
-      d.shape[i] = i < nd ? t->size(i) : 0;
-      d.stride[i] = i < nd ? t->stride(i) : 0;
-    }
+    if (!describe(*t, &d)) return false;
     ptr_[n_++] = &d;
     return true;
   }
@@ -91,7 +78,38 @@ class Call {
 
   dlm_tensor* operator[](int i) { return ptr_[i]; }
 
+  // Descriptors of a list or tuple of tensors.
+  bool list(PyObject* o, std::vector<dlm_tensor>* out) {
+    if (!PyList_CheckExact(o) && !PyTuple_CheckExact(o)) return false;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    out->resize(static_cast<size_t>(n));
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      at::Tensor* t = nullptr;
+      if (!plain(PySequence_Fast_GET_ITEM(o, i), &t) || !describe(*t, &(*out)[static_cast<size_t>(i)])) return false;
+    }
+    return true;
+  }
+
  private:
+  static bool describe(const at::Tensor& t, dlm_tensor* d) {
+    switch (t.scalar_type()) {
+      case at::kBFloat16: d->dtype = DLM_BF16; break;
+      case at::kFloat: d->dtype = DLM_F32; break;
+      case at::kInt: d->dtype = DLM_I32; break;
+      case at::kByte: d->dtype = DLM_U8; break;
+      default: return false;
+    }
+    const int64_t nd = t.dim();
+    if (nd < 1 || nd > 4) return false;
+    d->data = t.numel() ? t.data_ptr() : nullptr;
+    d->ndim = static_cast<int32_t>(nd);
+    for (int i = 0; i < 4; ++i) {
+      d->shape[i] = i < nd ? t.size(i) : 0;
+      d->stride[i] = i < nd ? t.stride(i) : 0;
+    }
+    return true;
+  }
+
   bool plain(PyObject* o, at::Tensor** out) {
     if (!THPVariable_CheckExact(o)) return false;
     const at::Tensor& t = THPVariable_Unpack(o);
@@ -141,6 +159,14 @@ bool as_int32(PyObject* o, int32_t* v) {
   const long x = PyLong_AsLong(o);
   if (PyErr_Occurred() || x < INT32_MIN || x > INT32_MAX) return false;
   *v = static_cast<int32_t>(x);
+  return true;
+}
+
+bool as_float(PyObject* o, float* v) {
+  if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return false;
+  const double x = PyFloat_AsDouble(o);
+  if (x == -1.0 && PyErr_Occurred()) return false;
+  *v = static_cast<float>(x);
   return true;
 }
 
@@ -269,6 +295,52 @@ PyObject* lmhead_confidence(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// x, weight, bias, eps, out, mean, rstd
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 7, [&](Call& c, int* st) {
+    float eps;
+    if (!add_all(c, a, 0, 2) || !c.add(a[2], true) || !as_float(a[3], &eps) || !c.add(a[4]) || !c.add(a[5], true) ||
+        !c.add(a[6], true) || !c.stream())
+      return false;
+    *st = unlocked([&] { return dlm_layer_norm(c[0], c[1], c[2], eps, c[3], c[4], c[5]); });
+    return true;
+  });
+}
+
+// dout, x, weight, mean, rstd, dx, dweight, dbias, workspace (None where nothing needs it)
+PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 9, [&](Call& c, int* st) {
+    void* ws = nullptr;
+    size_t bytes = 0;
+    if (!add_all(c, a, 0, 6) || !c.add(a[6], true) || !c.add(a[7], true) ||
+        (a[8] != Py_None && !c.workspace(a[8], &ws, &bytes)) || !c.stream())
+      return false;
+    *st = unlocked([&] { return dlm_layer_norm_grad(c[0], c[1], c[2], c[3], c[4], c[5], c[6], c[7], ws, bytes); });
+    return true;
+  });
+}
+
+// grads, outs (None: the norm alone), max_norm, norm, workspace
+PyObject* clip_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 5, [&](Call& c, int* st) {
+    std::vector<dlm_tensor> grads, outs;
+    float max_norm;
+    void* ws;
+    size_t bytes;
+    const bool scale = a[1] != Py_None;
+    if (!c.list(a[0], &grads) || (scale && (!c.list(a[1], &outs) || outs.size() != grads.size())) ||
+        grads.size() > INT32_MAX || !as_float(a[2], &max_norm) || !c.add(a[3]) || !c.workspace(a[4], &ws, &bytes) || !c.stream())
+      return false;
+    // An empty list has no descriptors, but still outputs.
+    dlm_tensor none;
+    *st = unlocked([&] {
+      return dlm_clip_grad_norm(grads.empty() ? &none : grads.data(), !scale ? nullptr : outs.empty() ? &none : outs.data(),
+                                static_cast<int32_t>(grads.size()), max_norm, c[0], ws, bytes);
+    });
+    return true;
+  });
+}
+
 // handle (a non-zero int), device index
 PyObject* loop_launch(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(n, 2, [&](Call&, int* st) {
@@ -299,6 +371,9 @@ PyMethodDef methods[] = {FAST(bidir_attn),
                          FAST(refine_step),
                          FAST(refine_step_static),
                          FAST(lmhead_confidence),
+                         FAST(layer_norm),
+                         FAST(layer_norm_grad),
+                         FAST(clip_grad_norm),
                          FAST(loop_launch),
                          {"set_params_type", set_params_type, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,243 @@
+// libdlmrefine C ABI: the entry points of training the refiner's last layer
+// (argument validation, dispatch). The rules of the other entry points hold: a
+// nonzero status means that nothing was launched.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+#include <vector>
+
+#include "dlm_checks.h"
+#include "dlm_internal.h"
+#include "dlmrefine.h"
+
+namespace {
+
+using namespace dlm;
+
+// Rows of a [N, d] or [B, L, d] tensor: their number, width and (even) stride.
+int rows_of(const dlm_tensor* t, const char* name, int dtype_mask, int64_t* N, int64_t* d, int64_t* stride) {
+  int st;
+  if ((st = check_tensor(t, name, dtype_mask, 2, 3))) return st;
+  const int nd = t->ndim;
+  *d = t->shape[nd - 1];
+  *N = 1;
+  for (int i = 0; i < nd - 1; ++i) *N *= t->shape[i];
+  *stride = t->stride[nd - 2];
+  if (nd == 3 && t->shape[1] == 1) *stride = t->stride[0];
+  if (*N > 0x7FFFFFFFLL) return fail(DLM_ERR_SHAPE, "%s: more than 2^31 - 1 rows", name);
+  if (nd == 3 && t->shape[0] > 1 && t->shape[1] > 1 && t->stride[0] != t->shape[1] * t->stride[1])
+    return fail(DLM_ERR_STRIDE, "%s: rows must be evenly strided ([B, L, d] with stride[0] = L * stride[1])", name);
+  if (*N > 1 && *d > 0 && *stride < *d) return fail(DLM_ERR_STRIDE, "%s: rows overlap", name);
+  if (*N <= 1) *stride = *d;
+  return DLM_OK;
+}
+
+bool same_shape(const dlm_tensor* a, const dlm_tensor* b) {
+  if (a->ndim != b->ndim) return false;
+  for (int i = 0; i < a->ndim; ++i)
+    if (a->shape[i] != b->shape[i]) return false;
+  return true;
+}
+
+// A vector of n contiguous entries, any rank; null allowed where `optional`.
+int check_vector(const dlm_tensor* t, const char* name, int dtype_mask, int64_t n, bool optional) {
+  if (!t && optional) return DLM_OK;
+  int st;
+  if ((st = check_tensor(t, name, dtype_mask, 1, 3))) return st;
+  if (numel(t) != n) return fail(DLM_ERR_SHAPE, "%s: %lld entries expected", name, (long long)n);
+  if (!is_dense(t)) return fail(DLM_ERR_STRIDE, "%s must be contiguous", name);
+  return DLM_OK;
+}
+
+// No output may overlap an input or another output. Null descriptors are skipped.
+int check_disjoint(const dlm_tensor* const* outs, int n_outs, const dlm_tensor* const* ins, int n_ins) {
+  for (int i = 0; i < n_outs; ++i) {
+    if (!outs[i]) continue;
+    for (int j = 0; j < n_ins; ++j)
+      if (ins[j] && overlaps(outs[i], ins[j])) return fail(DLM_ERR_ARG, "an output overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (outs[j] && overlaps(outs[i], outs[j])) return fail(DLM_ERR_ARG, "outputs overlap each other");
+  }
+  return DLM_OK;
+}
+
+// The caller's workspace: present, aligned, large enough and apart from every tensor.
+int check_workspace(const void* workspace, size_t bytes, size_t need, uintptr_t align, const dlm_tensor* const* all, int n) {
+  if (need == 0) return DLM_OK;
+  if (!workspace) return fail(DLM_ERR_NULL, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(workspace) % align != 0)
+    return fail(DLM_ERR_ALIGN, "workspace not %d-byte aligned", static_cast<int>(align));
+  if (bytes < need) return fail(DLM_ERR_ARG, "workspace too small: %zu bytes, %zu needed", bytes, need);
+  const uintptr_t wlo = reinterpret_cast<uintptr_t>(workspace), whi = wlo + need;
+  for (int i = 0; i < n; ++i) {
+    if (!all[i] || numel(all[i]) == 0) continue;
+    uintptr_t lo, hi;
+    byte_span(all[i], &lo, &hi);
+    if (lo < whi && wlo < hi) return fail(DLM_ERR_ARG, "workspace overlaps a tensor");
+  }
+  return DLM_OK;
+}
+
+// Every kernel records device-side failures in the error word; refuse to launch without it.
+int require_error_word() {
+  if (!device_error_word()) return fail(DLM_ERR_CUDA, "device error word unavailable on this device");
+  return DLM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dlm_layer_norm(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* bias, float eps, dlm_tensor* out,
+                   dlm_tensor* mean, dlm_tensor* rstd) {
+  clear_error();
+  NormArgs a = {};
+  int64_t N2, d2;
+  int st;
+  if ((st = rows_of(x, "x", kMaskBF16F32, &a.N, &a.d, &a.s_x))) return st;
+  if ((st = rows_of(out, "out", 1 << x->dtype, &N2, &d2, &a.s_out))) return st;
+  if (!same_shape(x, out)) return fail(DLM_ERR_SHAPE, "out must have the shape of x");
+  if (a.d < 1) return fail(DLM_ERR_SHAPE, "rows must have at least one element");
+  if ((st = check_vector(weight, "weight", kMaskBF16F32, a.d, false))) return st;
+  if ((st = check_vector(bias, "bias", 1 << weight->dtype, a.d, true))) return st;
+  if ((st = check_vector(mean, "mean", 1 << DLM_F32, a.N, true))) return st;
+  if ((st = check_vector(rstd, "rstd", 1 << DLM_F32, a.N, true))) return st;
+  if (!(eps >= 0.f) || std::isinf(eps)) return fail(DLM_ERR_ARG, "eps must be finite and not negative");
+  const dlm_tensor* outs[3] = {out, mean, rstd};
+  const dlm_tensor* ins[3] = {x, weight, bias};
+  if ((st = check_disjoint(outs, 3, ins, 3))) return st;
+  if (a.N == 0) return DLM_OK;
+  a.x = x->data;
+  a.weight = weight->data;
+  a.bias = bias ? bias->data : nullptr;
+  a.out = out->data;
+  a.mean = mean ? static_cast<float*>(mean->data) : nullptr;
+  a.rstd = rstd ? static_cast<float*>(rstd->data) : nullptr;
+  a.is_bf16 = x->dtype == DLM_BF16;
+  a.weight_bf16 = weight->dtype == DLM_BF16;
+  a.eps = eps;
+  return launch_layer_norm(a, current_stream());
+}
+
+size_t dlm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t d) {
+  return rows > 0 && d > 0 ? norm_grad_workspace_bytes(rows, d) : 0;
+}
+
+int dlm_layer_norm_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* mean,
+                        const dlm_tensor* rstd, dlm_tensor* dx, dlm_tensor* dweight, dlm_tensor* dbias, void* workspace,
+                        size_t workspace_bytes) {
+  clear_error();
+  NormArgs a = {};
+  int64_t N2, d2;
+  int st;
+  if ((st = rows_of(x, "x", kMaskBF16F32, &a.N, &a.d, &a.s_x))) return st;
+  if ((st = rows_of(dout, "dout", 1 << x->dtype, &N2, &d2, &a.s_dout))) return st;
+  if ((st = rows_of(dx, "dx", 1 << x->dtype, &N2, &d2, &a.s_dx))) return st;
+  if (!same_shape(x, dout) || !same_shape(x, dx)) return fail(DLM_ERR_SHAPE, "dout and dx must have the shape of x");
+  if (a.d < 1) return fail(DLM_ERR_SHAPE, "rows must have at least one element");
+  if ((st = check_vector(weight, "weight", kMaskBF16F32, a.d, false))) return st;
+  if ((st = check_vector(mean, "mean", 1 << DLM_F32, a.N, false))) return st;
+  if ((st = check_vector(rstd, "rstd", 1 << DLM_F32, a.N, false))) return st;
+  if ((st = check_vector(dweight, "dweight", 1 << weight->dtype, a.d, true))) return st;
+  if ((st = check_vector(dbias, "dbias", 1 << weight->dtype, a.d, true))) return st;
+  const dlm_tensor* outs[3] = {dx, dweight, dbias};
+  const dlm_tensor* ins[5] = {dout, x, weight, mean, rstd};
+  if ((st = check_disjoint(outs, 3, ins, 5))) return st;
+  const dlm_tensor* all[8] = {dout, x, weight, mean, rstd, dx, dweight, dbias};
+  if ((dweight || dbias) &&
+      (st = check_workspace(workspace, workspace_bytes, dlm_layer_norm_grad_workspace_bytes(a.N, a.d), 16, all, 8)))
+    return st;
+  if (a.N == 0 && !dweight && !dbias) return DLM_OK;
+  a.dout = dout->data;
+  a.x = x->data;
+  a.weight = weight->data;
+  a.mean = static_cast<float*>(mean->data);
+  a.rstd = static_cast<float*>(rstd->data);
+  a.dx = dx->data;
+  a.dweight = dweight ? dweight->data : nullptr;
+  a.dbias = dbias ? dbias->data : nullptr;
+  a.is_bf16 = x->dtype == DLM_BF16;
+  a.weight_bf16 = weight->dtype == DLM_BF16;
+  a.workspace = workspace;
+  return launch_layer_norm_grad(a, current_stream());
+}
+
+size_t dlm_clip_grad_norm_workspace_bytes(void) { return clip_grad_norm_workspace_bytes(); }
+
+int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t count, float max_norm, dlm_tensor* norm,
+                       void* workspace, size_t workspace_bytes) {
+  clear_error();
+  int st;
+  if (count < 0 || count > kMaxGradTensors) return fail(DLM_ERR_ARG, "count must be in [0, %d]", kMaxGradTensors);
+  if (count > 0 && !grads) return fail(DLM_ERR_NULL, "grads is NULL");
+  if (!(max_norm >= 0.f)) return fail(DLM_ERR_ARG, "max_norm must not be negative or NaN");
+  if ((st = check_vector(norm, "norm", 1 << DLM_F32, 1, false))) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, clip_grad_norm_workspace_bytes(), 8, nullptr, 0))) return st;
+  struct Span {
+    uintptr_t lo, hi;
+    int tensor;   // index of its gradient; -1: the norm, -2: the workspace
+    bool written;
+  };
+  // Nothing thrown leaves a C entry point: the only throwing calls are these vectors'.
+  try {
+    std::vector<GradTensor> list;
+    std::vector<Span> spans;
+    list.reserve(count);
+    spans.reserve(2 * static_cast<size_t>(count) + 2);
+    for (int i = 0; i < count; ++i) {
+      const dlm_tensor* g = grads + i;
+      const dlm_tensor* o = outs ? outs + i : g;
+      if ((st = check_tensor(g, "gradient", kMaskBF16F32, 1, 4))) return st;
+      if (o != g) {
+        if ((st = check_tensor(o, "scaled gradient", 1 << g->dtype, 1, 4))) return st;
+        if (!same_shape(g, o)) return fail(DLM_ERR_SHAPE, "tensor %d: the output must have the gradient's shape", i);
+      }
+      double n = 1;
+      for (int k = 0; k < g->ndim; ++k) n *= static_cast<double>(g->shape[k]);
+      if (n > 0x1p40) return fail(DLM_ERR_SHAPE, "tensor %d: more than 2^40 elements", i);
+      if (!is_dense(g) || !is_dense(o)) return fail(DLM_ERR_STRIDE, "tensor %d must be contiguous", i);
+      const int64_t size = numel(g);
+      if (size == 0) continue;
+      list.push_back({g->data, o->data, size, g->dtype == DLM_BF16});
+      Span s = {0, 0, i, false};
+      byte_span(g, &s.lo, &s.hi);
+      const bool in_place = outs && o->data == g->data;
+      s.written = in_place;
+      spans.push_back(s);
+      if (outs && !in_place) {
+        byte_span(o, &s.lo, &s.hi);
+        s.written = true;
+        spans.push_back(s);
+      }
+    }
+    Span s = {0, 0, -1, true};
+    byte_span(norm, &s.lo, &s.hi);
+    spans.push_back(s);
+    s.tensor = -2;
+    s.lo = reinterpret_cast<uintptr_t>(workspace);
+    s.hi = s.lo + clip_grad_norm_workspace_bytes();
+    spans.push_back(s);
+    // A written range may overlap no other: each range against the furthest end so far.
+    std::sort(spans.begin(), spans.end(), [](const Span& p, const Span& q) { return p.lo < q.lo; });
+    uintptr_t end = 0, written_end = 0;
+    for (const Span& p : spans) {
+      if (p.lo < (p.written ? end : written_end))
+        return fail(DLM_ERR_ARG, "an output overlaps a gradient, another output, norm or the workspace");
+      end = std::max(end, p.hi);
+      if (p.written) written_end = std::max(written_end, p.hi);
+    }
+    GradArgs a = {};
+    a.grads = list.data();
+    a.count = static_cast<int>(list.size());
+    a.scale = outs != nullptr;
+    a.max_norm = max_norm;
+    a.norm = static_cast<float*>(norm->data);
+    a.workspace = static_cast<double*>(workspace);
+    return launch_clip_grad_norm(a, current_stream());
+  } catch (const std::bad_alloc&) {
+    return fail(DLM_ERR_ARG, "out of host memory for the list of gradients");
+  }
+}
+
+}  // extern "C"
