@@ -26,6 +26,8 @@
  *
  * Training and scoring the refiner's last layer (the paper takes trained
  * refiners as they are; these have no counterpart in it):
+ *   dlm_lmhead_loss, dlm_lmhead_loss_grad  cross entropy of given tokens under the
+ *                                          projection, logits never stored
  *   dlm_layer_norm, dlm_layer_norm_grad    the norm in front of the projection
  *   dlm_clip_grad_norm                     the norm over all gradients, clipping
  *
@@ -264,6 +266,58 @@ int dlm_refine_update_ranked(const dlm_tensor* tokens, const dlm_tensor* mask, c
                              const dlm_tensor* conf, const dlm_tensor* tok_prob,
                              const dlm_refine_params* params, dlm_tensor* new_tokens,
                              dlm_tensor* new_mask, dlm_tensor* n_edits);
+
+/*
+ * Cross entropy of given tokens under the vocabulary projection, without writing
+ * the N x V logits to memory (dlm_lmhead_confidence for a token that is known):
+ *   logits[r, v] = sum_k hidden[r, k] * weight[v, k]
+ *   lse[r]  = ln sum_v exp(logits[r, v])
+ *   loss[r] = lse[r] - logits[r, targets[r]]        (-ln of the token's probability)
+ * A row whose target is outside [0, V) (-1, say, or a mask token) is not scored: its
+ * loss and lse are 0, its hidden state is not read, and it takes no part in the
+ * product, whose time goes by the scored rows.
+ *
+ *   hidden      [N, d] or [B, L, d] BF16, rows evenly strided, any alignment; d a multiple
+ *               of 8
+ *   weight      [V, d] BF16; base pointer and row stride multiples of 16 bytes
+ *   targets     N I32, contiguous (any rank with N elements, like loss and lse)
+ *   loss, lse   N F32, contiguous
+ *   workspace   >= dlm_lmhead_loss_workspace_bytes(N, d) bytes, 16-byte aligned, no initial
+ *               contents needed; calls sharing it must not overlap on the GPU.
+ * bf16 products, fp32 accumulation and sums (a few 1e-6 of sum_k |hidden weight| in a
+ * logit). A scored row with a NaN logit, or without a finite maximum, gives NaN.
+ */
+int dlm_lmhead_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_tensor* targets, dlm_tensor* loss,
+                    dlm_tensor* lse, void* workspace, size_t workspace_bytes);
+size_t dlm_lmhead_loss_workspace_bytes(int64_t rows, int64_t d);
+
+/*
+ * Gradients of sum_r dloss[r] loss[r]:
+ *   g[r, v]  = dloss[r] (exp(logits[r, v] - lse[r]) - [v = targets[r]])
+ *   d_hidden = g weight,   d_weight = g^T hidden
+ * Rows that are not scored get 0 in d_hidden and add nothing to d_weight; neither their
+ * hidden state nor their lse and dloss are read.
+ *
+ *   hidden, weight, targets, lse   as dlm_lmhead_loss took and wrote them
+ *   dloss       N F32, contiguous: the gradient of each row's loss (1 / n for a mean over n
+ *               scored rows; a weight per row for a masked diffusion loss)
+ *   d_hidden    the shape of hidden, BF16, rows evenly strided, any alignment; or NULL
+ *   d_weight    [V, d] BF16; base pointer and row stride multiples of 16 bytes; or NULL
+ *               (a frozen projection), not both
+ *   workspace   16-byte aligned, no initial contents needed. The call works through the
+ *               vocabulary in pieces, as large as the workspace allows (multiples of 256
+ *               columns): dlm_lmhead_loss_grad_workspace_bytes(N, V, d, piece) bytes allow
+ *               pieces of `piece` columns, and of about 2 GB with piece = 0, which is
+ *               as fast as it gets; the least is what piece = 256 needs. Calls sharing it
+ *               must not overlap on the GPU.
+ * g is rounded to bf16 for the tensor cores (at most 2^-8 relative in each term), all sums
+ * are fp32, the results are rounded to bf16. The same inputs and workspace size give the
+ * same bits. No output may overlap another tensor.
+ */
+int dlm_lmhead_loss_grad(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_tensor* targets, const dlm_tensor* lse,
+                         const dlm_tensor* dloss, dlm_tensor* d_hidden, dlm_tensor* d_weight, void* workspace,
+                         size_t workspace_bytes);
+size_t dlm_lmhead_loss_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int64_t piece);
 
 /*
  * Layer norm over the last dimension, the norm in front of an output

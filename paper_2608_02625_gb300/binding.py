@@ -59,12 +59,17 @@ def _load():
     lib.dlm_lmhead_confidence.argtypes = [P, P, P, P, P, ctypes.c_void_p, ctypes.c_size_t]
     lib.dlm_lmhead_workspace_bytes.argtypes = [ctypes.c_int64]
     lib.dlm_lmhead_workspace_bytes.restype = ctypes.c_size_t
+    lib.dlm_lmhead_loss.argtypes = [P] * 5 + [ctypes.c_void_p, ctypes.c_size_t]
+    lib.dlm_lmhead_loss_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64]
+    lib.dlm_lmhead_loss_grad.argtypes = [P] * 7 + [ctypes.c_void_p, ctypes.c_size_t]
+    lib.dlm_lmhead_loss_grad_workspace_bytes.argtypes = [ctypes.c_int64] * 4
     lib.dlm_layer_norm.argtypes = [P, P, P, ctypes.c_float, P, P, P]
     lib.dlm_layer_norm_grad.argtypes = [P] * 8 + [ctypes.c_void_p, ctypes.c_size_t]
     lib.dlm_layer_norm_grad_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64]
     lib.dlm_clip_grad_norm.argtypes = [P, P, ctypes.c_int32, ctypes.c_float, P, ctypes.c_void_p, ctypes.c_size_t]
     lib.dlm_clip_grad_norm_workspace_bytes.argtypes = []
-    for f in ("dlm_layer_norm_grad_workspace_bytes", "dlm_clip_grad_norm_workspace_bytes"):
+    for f in ("dlm_lmhead_loss_workspace_bytes", "dlm_lmhead_loss_grad_workspace_bytes",
+              "dlm_layer_norm_grad_workspace_bytes", "dlm_clip_grad_norm_workspace_bytes"):
         getattr(lib, f).restype = ctypes.c_size_t
     lib.dlm_refine_update_ranked.argtypes = [P, P, P, P, P, ctypes.POINTER(DlmRefineParams), P, P, P]
     lib.dlm_refine_step_static.argtypes = [P, P, P, ctypes.POINTER(DlmRefineParams), P, P, P, P, P, P]
@@ -72,7 +77,7 @@ def _load():
     lib.dlm_refine_step_workspace_bytes.restype = ctypes.c_size_t
     for f in ("dlm_bidir_attn", "dlm_attn_masked", "dlm_vocab_confidence", "dlm_refine_update", "dlm_refine_step",
               "dlm_refine_step_static", "dlm_token_prob", "dlm_refine_update_ranked", "dlm_lmhead_confidence",
-              "dlm_layer_norm", "dlm_layer_norm_grad", "dlm_clip_grad_norm", "dlm_set_stream", "dlm_set_attn_tiles_per_unit",
+              "dlm_lmhead_loss", "dlm_lmhead_loss_grad", "dlm_layer_norm", "dlm_layer_norm_grad", "dlm_clip_grad_norm", "dlm_set_stream", "dlm_set_attn_tiles_per_unit",
               "dlm_version", "dlm_get_device_error"):
         getattr(lib, f).restype = ctypes.c_int
     lib.dlm_loop_begin.argtypes = [ctypes.c_void_p]
@@ -267,6 +272,37 @@ def _workspace(workspace):
         raise ValueError("workspace must be contiguous")
     nbytes = workspace.numel() * workspace.element_size()
     return ctypes.c_void_p(workspace.data_ptr() if nbytes else None), ctypes.c_size_t(nbytes)
+
+
+def dlm_lmhead_loss_workspace_bytes(rows: int, d: int) -> int:
+    return lib.dlm_lmhead_loss_workspace_bytes(int(rows), int(d))
+
+
+def dlm_lmhead_loss(hidden, weight, targets, loss, lse, workspace):
+    """loss / lse per row: the cross entropy of targets under hidden @ weight^T, without
+    materialising the logits; 0 for rows whose target is outside [0, V)."""
+    if _done(_marshal.lmhead_loss(hidden, weight, targets, loss, lse, workspace)):
+        return loss, lse
+    _prepare(hidden, weight, targets, loss, lse, workspace)
+    ds = [describe(t) for t in (hidden, weight, targets, loss, lse)]
+    _check(lib.dlm_lmhead_loss(*[_ref(d) for d in ds], *_workspace(workspace)))
+    return loss, lse
+
+
+def dlm_lmhead_loss_grad_workspace_bytes(rows: int, vocab: int, d: int, piece: int = 0) -> int:
+    """Bytes that let dlm_lmhead_loss_grad take `piece` columns of the vocabulary at a time
+    (0: about 2 GB of them)."""
+    return lib.dlm_lmhead_loss_grad_workspace_bytes(int(rows), int(vocab), int(d), int(piece))
+
+
+def dlm_lmhead_loss_grad(hidden, weight, targets, lse, dloss, d_hidden, d_weight, workspace):
+    """Gradients of sum(dloss * loss) of dlm_lmhead_loss; d_hidden or d_weight may be None."""
+    if _done(_marshal.lmhead_loss_grad(hidden, weight, targets, lse, dloss, d_hidden, d_weight, workspace)):
+        return d_hidden, d_weight
+    _prepare(hidden, weight, targets, lse, dloss, d_hidden, d_weight, workspace)
+    ds = [describe(t) for t in (hidden, weight, targets, lse, dloss, d_hidden, d_weight)]
+    _check(lib.dlm_lmhead_loss_grad(*[_ref(d) for d in ds], *_workspace(workspace)))
+    return d_hidden, d_weight
 
 
 def dlm_layer_norm(x, weight, bias, eps: float, out, mean, rstd):

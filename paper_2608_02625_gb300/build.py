@@ -32,12 +32,13 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 LIBS = {
     "libdlmrefine.so": ["dlm_api.cu", "attn_tc.cu", "attn_f32.cu", "vocab.cu", "update.cu", "loop.cu", "lmhead.cu",
-                        "selftest.cu", "train_api.cu", "layernorm.cu", "gradnorm.cu"],
+                        "selftest.cu", "train_api.cu", "lmloss.cu", "layernorm.cu",
+                        "gradnorm.cu"],
     "libdlmsynth.so": ["synth.cu"],
 }
 # The Python binding's marshalling: host code against torch's headers, beside the library it calls.
 MARSHAL, MARSHAL_SRC = "_marshal.so", "marshal.cpp"
-HEADERS = ["dlm_common.cuh", "dlm_internal.h", "dlm_checks.h", "update_impl.cuh"]
+HEADERS = ["dlm_common.cuh", "dlm_internal.h", "dlm_checks.h", "dlm_tmap.h", "update_impl.cuh"]
 
 
 def nvcc() -> str:

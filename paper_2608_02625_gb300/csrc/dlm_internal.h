@@ -184,6 +184,30 @@ constexpr int kLmMaxSplits = 64;  // parts per row in the workspace
 inline size_t lmhead_workspace_bytes(int64_t N) { return static_cast<size_t>(N) * kLmMaxSplits * 12; }
 int launch_lmhead(const LmArgs& a, cudaStream_t stream);
 
+// Cross entropy of given tokens under the output projection, and its gradients.
+struct LossArgs {
+  const void* hidden;     // bf16 [N, d], any alignment
+  const void* weight;     // bf16 [V, d], 16-byte aligned rows
+  const int32_t* targets; // a row whose target is outside [0, V) is not scored
+  int64_t N, V, d, s_hidden, s_weight;
+  float* loss;            // the loss only
+  float* lse_out;
+  const float* lse;       // the gradients only, from here on
+  const float* dloss;
+  void* d_hidden;         // may be null; any alignment
+  void* d_weight;         // may be null; 16-byte aligned rows
+  int64_t s_dhidden, s_dweight;
+  void* workspace;        // loss_workspace_bytes or loss_grad_workspace_bytes
+  size_t workspace_bytes;
+};
+
+constexpr int kLossMaxParts = 152;  // parts of the vocabulary a row's sums are kept in
+size_t loss_workspace_bytes(int64_t N, int64_t d);
+// piece: columns of the vocabulary at a time (0: as many as need 2 GB).
+size_t loss_grad_workspace_bytes(int64_t N, int64_t V, int64_t d, int64_t piece);
+int launch_loss(const LossArgs& a, cudaStream_t stream);
+int launch_loss_grad(const LossArgs& a, cudaStream_t stream);
+
 // Layer norm over the last dimension of [N, d] rows, and its gradients.
 struct NormArgs {
   const void* x;

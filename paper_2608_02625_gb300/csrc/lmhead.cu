@@ -38,10 +38,10 @@
 
 #include <cmath>
 #include <cstdint>
-#include <mutex>
 
 #include "dlm_common.cuh"
 #include "dlm_internal.h"
+#include "dlm_tmap.h"
 
 namespace cg = cooperative_groups;
 
@@ -400,39 +400,6 @@ __global__ void __launch_bounds__(kCombineThreads)
   }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
-            cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(ptr);
-  });
-  return fn;
-}
-
-// 2-D map over a [rows, d] bf16 matrix (row stride in elements), box d 64 x box_rows.
-int make_map_2d(CUtensorMap* map, const void* base, int64_t rows, int d, int64_t row_stride, int box_rows) {
-  EncodeTiledFn enc = encode_fn();
-  if (!enc) return fail(DLM_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-  cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows)};
-  cuuint64_t strides[1] = {static_cast<cuuint64_t>(row_stride) * 2};
-  cuuint32_t box[2] = {static_cast<cuuint32_t>(kBK), static_cast<cuuint32_t>(box_rows)};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(DLM_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
-  return DLM_OK;
-}
-
 }  // namespace
 
 namespace {
@@ -503,8 +470,8 @@ int launch_tiles(const LmArgs& a, const Split& sp, int sms, cudaStream_t stream)
   p.wait_ns = wait_budget_ns();
   CUtensorMap mh, mw;
   int st;
-  if ((st = make_map_2d(&mh, a.hidden, a.N, p.d, a.s_hidden, p.a_rows)) != DLM_OK) return st;
-  if ((st = make_map_2d(&mw, a.weight, a.V, p.d, a.s_weight, kBN)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&mh, a.hidden, true, a.N, p.d, a.s_hidden, p.a_rows)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&mw, a.weight, true, a.V, p.d, a.s_weight, kBN)) != DLM_OK) return st;
   const int grid = sp.csize > 1 ? p.items * sp.csize : (p.items < sms ? p.items : sms);
   cudaError_t e = launch_overlapped(lmhead_kernel<kBN>, dim3(static_cast<unsigned>(grid)), kThreads, smem_bytes<kBN>(), stream,
                                     sp.csize, true, mh, mw, p);

@@ -295,6 +295,29 @@ PyObject* lmhead_confidence(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// hidden, weight, targets, loss, lse, workspace
+PyObject* lmhead_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 6, [&](Call& c, int* st) {
+    void* ws;
+    size_t bytes;
+    if (!add_all(c, a, 0, 5) || !c.workspace(a[5], &ws, &bytes) || !c.stream()) return false;
+    *st = unlocked([&] { return dlm_lmhead_loss(c[0], c[1], c[2], c[3], c[4], ws, bytes); });
+    return true;
+  });
+}
+
+// hidden, weight, targets, lse, dloss, d_hidden, d_weight, workspace
+PyObject* lmhead_loss_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 8, [&](Call& c, int* st) {
+    void* ws;
+    size_t bytes;
+    if (!add_all(c, a, 0, 5) || !c.add(a[5], true) || !c.add(a[6], true) || !c.workspace(a[7], &ws, &bytes) || !c.stream())
+      return false;
+    *st = unlocked([&] { return dlm_lmhead_loss_grad(c[0], c[1], c[2], c[3], c[4], c[5], c[6], ws, bytes); });
+    return true;
+  });
+}
+
 // x, weight, bias, eps, out, mean, rstd
 PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(n, 7, [&](Call& c, int* st) {
@@ -371,6 +394,8 @@ PyMethodDef methods[] = {FAST(bidir_attn),
                          FAST(refine_step),
                          FAST(refine_step_static),
                          FAST(lmhead_confidence),
+                         FAST(lmhead_loss),
+                         FAST(lmhead_loss_grad),
                          FAST(layer_norm),
                          FAST(layer_norm_grad),
                          FAST(clip_grad_norm),

@@ -85,9 +85,113 @@ int require_error_word() {
   return DLM_OK;
 }
 
+bool aligned_rows(const dlm_tensor* t) {
+  if (reinterpret_cast<uintptr_t>(t->data) % 16 != 0) return false;
+  return t->shape[0] <= 1 || (t->stride[0] * elem_size(t->dtype)) % 16 == 0;
+}
+
+constexpr int64_t kMostRows = int64_t{1} << 30, kMostWidth = int64_t{1} << 20;
+
+// The arguments that the loss and its gradients share.
+int prepare_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_tensor* targets, LossArgs* a) {
+  int st;
+  if ((st = rows_of(hidden, "hidden", 1 << DLM_BF16, &a->N, &a->d, &a->s_hidden))) return st;
+  if ((st = check_tensor(weight, "weight", 1 << DLM_BF16, 2, 2))) return st;
+  if ((st = check_vector(targets, "targets", 1 << DLM_I32, a->N, false))) return st;
+  a->V = weight->shape[0];
+  if (weight->shape[1] != a->d) return fail(DLM_ERR_SHAPE, "weight must be [V, d] with the d of hidden");
+  if (a->d < 8 || a->d % 8 != 0) return fail(DLM_ERR_SHAPE, "d must be a positive multiple of 8 (got %lld)", (long long)a->d);
+  if (a->V < 1) return fail(DLM_ERR_SHAPE, "V must be >= 1");
+  if (a->N > kMostRows || a->V > kMostRows || a->d > kMostWidth)
+    return fail(DLM_ERR_SHAPE, "at most 2^30 rows and tokens and a width of 2^20");
+  if (a->V > 1 && weight->stride[0] < a->d) return fail(DLM_ERR_STRIDE, "weight rows overlap");
+  if (!aligned_rows(weight)) return fail(DLM_ERR_ALIGN, "weight rows must start at multiples of 16 bytes");
+  a->hidden = hidden->data;
+  a->weight = weight->data;
+  a->targets = static_cast<const int32_t*>(targets->data);
+  a->s_weight = a->V > 1 ? weight->stride[0] : a->d;
+  return DLM_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t dlm_lmhead_loss_workspace_bytes(int64_t rows, int64_t d) {
+  return rows > 0 && rows <= kMostRows && d > 0 && d <= kMostWidth ? loss_workspace_bytes(rows, d) : 0;
+}
+
+int dlm_lmhead_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_tensor* targets, dlm_tensor* loss,
+                    dlm_tensor* lse, void* workspace, size_t workspace_bytes) {
+  clear_error();
+  LossArgs a = {};
+  int st;
+  if ((st = prepare_loss(hidden, weight, targets, &a))) return st;
+  if ((st = check_vector(loss, "loss", 1 << DLM_F32, a.N, false))) return st;
+  if ((st = check_vector(lse, "lse", 1 << DLM_F32, a.N, false))) return st;
+  const dlm_tensor* outs[2] = {loss, lse};
+  const dlm_tensor* ins[3] = {hidden, weight, targets};
+  if ((st = check_disjoint(outs, 2, ins, 3))) return st;
+  if (a.N == 0) return DLM_OK;
+  const dlm_tensor* all[5] = {hidden, weight, targets, loss, lse};
+  if ((st = check_workspace(workspace, workspace_bytes, loss_workspace_bytes(a.N, a.d), 16, all, 5))) return st;
+  if ((st = require_error_word())) return st;
+  a.loss = static_cast<float*>(loss->data);
+  a.lse_out = static_cast<float*>(lse->data);
+  a.workspace = workspace;
+  return launch_loss(a, current_stream());
+}
+
+size_t dlm_lmhead_loss_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int64_t piece) {
+  const bool fine = rows > 0 && rows <= kMostRows && vocab > 0 && vocab <= kMostRows && d > 0 && d <= kMostWidth && piece >= 0;
+  return fine ? loss_grad_workspace_bytes(rows, vocab, d, piece) : 0;
+}
+
+int dlm_lmhead_loss_grad(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_tensor* targets, const dlm_tensor* lse,
+                         const dlm_tensor* dloss, dlm_tensor* d_hidden, dlm_tensor* d_weight, void* workspace,
+                         size_t workspace_bytes) {
+  clear_error();
+  LossArgs a = {};
+  int64_t N2, d2;
+  int st;
+  if ((st = prepare_loss(hidden, weight, targets, &a))) return st;
+  if ((st = check_vector(lse, "lse", 1 << DLM_F32, a.N, false))) return st;
+  if ((st = check_vector(dloss, "dloss", 1 << DLM_F32, a.N, false))) return st;
+  if (!d_hidden && !d_weight) return fail(DLM_ERR_NULL, "d_hidden and d_weight are both NULL");
+  if (d_hidden) {
+    if ((st = rows_of(d_hidden, "d_hidden", 1 << DLM_BF16, &N2, &d2, &a.s_dhidden))) return st;
+    if (!same_shape(hidden, d_hidden)) return fail(DLM_ERR_SHAPE, "d_hidden must have the shape of hidden");
+    a.d_hidden = d_hidden->data;
+  }
+  if (d_weight) {
+    if ((st = check_tensor(d_weight, "d_weight", 1 << DLM_BF16, 2, 2))) return st;
+    if (!same_shape(weight, d_weight)) return fail(DLM_ERR_SHAPE, "d_weight must have the shape of weight");
+    if (a.V > 1 && d_weight->stride[0] < a.d) return fail(DLM_ERR_STRIDE, "d_weight rows overlap");
+    if (!aligned_rows(d_weight)) return fail(DLM_ERR_ALIGN, "d_weight rows must start at multiples of 16 bytes");
+    a.d_weight = d_weight->data;
+    a.s_dweight = a.V > 1 ? d_weight->stride[0] : a.d;
+  }
+  const dlm_tensor* outs[2] = {d_hidden, d_weight};
+  const dlm_tensor* ins[5] = {hidden, weight, targets, lse, dloss};
+  if ((st = check_disjoint(outs, 2, ins, 5))) return st;
+  if (a.N == 0) {  // the gradient of no rows
+    if (!d_weight) return DLM_OK;
+    const cudaError_t e = cudaMemset2DAsync(a.d_weight, static_cast<size_t>(a.s_dweight) * 2, 0, static_cast<size_t>(a.d) * 2,
+                                            static_cast<size_t>(a.V), current_stream());
+    return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "d_weight: %s", cudaGetErrorString(e));
+  }
+  const dlm_tensor* all[7] = {hidden, weight, targets, lse, dloss, d_hidden, d_weight};
+  // At least pieces of 256 columns; all that is given is used, up to the whole vocabulary.
+  const size_t most = loss_grad_workspace_bytes(a.N, a.V, a.d, a.V), least = loss_grad_workspace_bytes(a.N, a.V, a.d, 256);
+  if ((st = check_workspace(workspace, workspace_bytes, least, 16, nullptr, 0))) return st;
+  a.workspace_bytes = workspace_bytes < most ? workspace_bytes : most;
+  if ((st = check_workspace(workspace, workspace_bytes, a.workspace_bytes, 16, all, 7))) return st;
+  if ((st = require_error_word())) return st;
+  a.lse = static_cast<const float*>(lse->data);
+  a.dloss = static_cast<const float*>(dloss->data);
+  a.workspace = workspace;
+  return launch_loss_grad(a, current_stream());
+}
 
 int dlm_layer_norm(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* bias, float eps, dlm_tensor* out,
                    dlm_tensor* mean, dlm_tensor* rstd) {

@@ -111,3 +111,67 @@ def test_workspace_sizes():
     assert B.dlm_layer_norm_grad_workspace_bytes(6, 64) == 6 * 2 * 64 * 4
     assert B.dlm_layer_norm_grad_workspace_bytes(10 ** 6, 64) == B.dlm_layer_norm_grad_workspace_bytes(10 ** 7, 64)
     assert B.dlm_clip_grad_norm_workspace_bytes() > 0
+
+
+def loss_args(N=6, V=50, d=64):
+    return dict(h=T(BF16, [N, d], 1 * MB), w=T(BF16, [V, d], 2 * MB), t=T(I32, [N], 3 * MB), loss=T(F32, [N], 4 * MB),
+                lse=T(F32, [N], 5 * MB), ws=ctypes.c_void_p(6 * MB), nbytes=ctypes.c_size_t(1 << 24))
+
+
+SHARED = {
+    "null_hidden": (dict(h=None), -1), "null_weight": (dict(w=None), -1), "null_targets": (dict(t=None), -1),
+    "null_lse": (dict(lse=None), -1), "null_workspace": (dict(ws=None), -1),
+    "hidden_f32": (dict(h=T(F32, [6, 64], MB)), -2), "weight_f32": (dict(w=T(F32, [50, 64], 2 * MB)), -2),
+    "targets_u8": (dict(t=T(U8, [6], 3 * MB)), -2), "lse_bf16": (dict(lse=T(BF16, [6], 5 * MB)), -2),
+    "width": (dict(w=T(BF16, [50, 72], 2 * MB)), -3), "targets_length": (dict(t=T(I32, [5], 3 * MB)), -3),
+    "no_vocabulary": (dict(w=T(BF16, [0, 64], 2 * MB)), -3),
+    "width_not_8": (dict(h=T(BF16, [6, 60], MB), w=T(BF16, [50, 60], 2 * MB, [64, 1])), -3),
+    "hidden_apart": (dict(h=T(BF16, [6, 64], MB, [128, 2])), -4), "weight_overlap": (dict(w=T(BF16, [50, 64], 2 * MB, [8, 1])), -4),
+    "targets_apart": (dict(t=T(I32, [6], 3 * MB, [2])), -4), "weight_base": (dict(w=T(BF16, [50, 64], 2 * MB + 2)), -5),
+    "weight_stride": (dict(w=T(BF16, [50, 64], 2 * MB, [65, 1])), -5), "workspace_misaligned": (dict(ws=ctypes.c_void_p(6 * MB + 8)), -5),
+    "workspace_small": (dict(nbytes=ctypes.c_size_t(1000)), -6), "workspace_on_weight": (dict(ws=ctypes.c_void_p(2 * MB)), -6),
+}
+LOSS = {
+    "loss_on_lse": (dict(loss=T(F32, [6], 5 * MB + 4)), -6), "loss_on_hidden": (dict(loss=T(F32, [6], 1 * MB + 16)), -6),
+    "loss_on_targets": (dict(loss=T(F32, [6], 3 * MB)), -6), "loss_length": (dict(loss=T(F32, [7], 4 * MB)), -3),
+}
+
+
+@pytest.mark.parametrize("case", [*SHARED, *LOSS])
+def test_loss_refuses(case):
+    over, status = {**SHARED, **LOSS}[case]
+    assert call("dlm_lmhead_loss", *{**loss_args(), **over}.values()) == status
+
+
+def loss_grad_args(N=6, V=50, d=64):
+    a = loss_args(N, V, d)
+    return dict(h=a["h"], w=a["w"], t=a["t"], lse=a["lse"], dloss=T(F32, [N], 4 * MB), dh=T(BF16, [N, d], 10 * MB),
+                dw=T(BF16, [V, d], 11 * MB), ws=a["ws"], nbytes=a["nbytes"])
+
+
+LOSS_GRAD = {
+    "null_dloss": (dict(dloss=None), -1), "no_gradient": (dict(dh=None, dw=None), -1),
+    "dh_f32": (dict(dh=T(F32, [6, 64], 10 * MB)), -2), "dw_f32": (dict(dw=T(F32, [50, 64], 11 * MB)), -2),
+    "dh_shape": (dict(dh=T(BF16, [2, 3, 64], 10 * MB)), -3), "dw_shape": (dict(dw=T(BF16, [49, 64], 11 * MB)), -3),
+    "dh_rows_overlap": (dict(dh=T(BF16, [6, 64], 10 * MB, [32, 1])), -4), "dw_base": (dict(dw=T(BF16, [50, 64], 11 * MB + 8)), -5),
+    "dw_rows_overlap": (dict(dw=T(BF16, [50, 64], 11 * MB, [56, 1])), -4), "dh_on_hidden": (dict(dh=T(BF16, [6, 64], MB)), -6),
+    "dw_on_weight": (dict(dw=T(BF16, [50, 64], 2 * MB)), -6), "dw_on_dh": (dict(dw=T(BF16, [50, 64], 10 * MB)), -6),
+    "workspace_on_dw": (dict(ws=ctypes.c_void_p(11 * MB)), -6),
+}
+
+
+@pytest.mark.parametrize("case", [*SHARED, *LOSS_GRAD])
+def test_loss_grad_refuses(case):
+    over, status = {**SHARED, **LOSS_GRAD}[case]
+    assert call("dlm_lmhead_loss_grad", *{**loss_grad_args(), **over}.values()) == status
+
+
+def test_loss_workspace_sizes():
+    from paper_2608_02625_gb300 import binding as B
+    assert B.dlm_lmhead_loss_workspace_bytes(0, 64) == B.dlm_lmhead_loss_workspace_bytes(5, 0) == 0
+    size = B.dlm_lmhead_loss_grad_workspace_bytes
+    assert size(0, 10, 64) == size(5, 0, 64) == size(5, 10, 64, -1) == 0
+    assert size(128, 10 ** 5, 64, 512) - size(128, 10 ** 5, 64, 256) == 128 * 256 * 2
+    assert size(128, 10 ** 5, 64, 257) == size(128, 10 ** 5, 64, 512)
+    assert size(128, 300, 64, 10 ** 6) == size(128, 300, 64, 300)
+    assert size(16384, 151552, 2048) < 3 * 2 ** 30
