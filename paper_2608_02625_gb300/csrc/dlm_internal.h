@@ -227,8 +227,9 @@ struct NormArgs {
   void* workspace;       // norm_grad_workspace_bytes(N, d)
 };
 
-// CTAs that leave sums of the columns: four, or for wide rows two, on each SM.
-inline int norm_max_parts(int64_t d) { return d <= 2048 ? 608 : 304; }
+// CTAs that leave sums of the columns, at most: four on each of 152 SMs for rows up to
+// 2048 wide, two for wider ones.
+inline int norm_max_parts(int64_t d) { return 152 * (d <= 2048 ? 4 : 2); }
 inline size_t norm_grad_workspace_bytes(int64_t N, int64_t d) {
   const int64_t most = norm_max_parts(d), parts = N < most ? N : most;
   return static_cast<size_t>(parts) * 2 * static_cast<size_t>(d) * sizeof(float);

@@ -5,19 +5,26 @@
 //   dx   = rstd (a - (sum a + xhat sum a xhat) / d)      with a = dout w
 //   dw   = sum over rows of dout xhat,   db = sum over rows of dout
 //
-// One pass over the rows: a row lives in the registers of a group of threads (a
-// part of a warp, a warp, or a CTA), which takes its two sums over the centred
-// values (not from sums of x and x^2, which cancel where the mean is large). Every
-// group walks rows a grid apart, its weights kept in registers, the next row's
-// loads issued before the sums of this one. In the gradient each thread also
-// keeps the sums of its columns over the rows of its group; the CTAs' sums go to
-// the caller's workspace and a second launch adds them in a fixed order, so the
-// results do not depend on scheduling. All sums are fp32. Rows too wide for the
-// registers of a CTA are read once for each sum, their columns' sums by a launch
-// of their own.
+// One pass over the rows: a row lives in the registers of a group of threads (a part
+// of a warp, a warp, or several), which takes its two sums over the centred values
+// (not from sums of x and x^2, which cancel where the mean is large). The groups of a
+// persistent grid walk the rows, the rows to come on their way to shared memory, the
+// weights there in fp32. In the gradient each thread also keeps the sums of its columns
+// over the rows of its group; the CTAs' sums go to the caller's workspace and a second
+// launch adds them in a fixed order, so the results do not depend on scheduling. All
+// sums are fp32. Rows too wide for that are read once for each sum, their columns' sums
+// by a launch of their own.
+//
+// What bounds it is HBM, then the issue slots: what a row costs whatever a thread holds
+// (two sums over the group, the root and its reciprocal, the loop) was most of the
+// instructions with 8 elements a thread, so a thread holds 32. 16384 x 2048 bf16, among
+// other calls: 25.1 us, 5.3 TB/s (8 elements, a CTA a row: 41.8; 64 elements, a warp a
+// row, too few warps: 37), the gradients 41.4 us, 4.9 TB/s (98 before; 55 % of the issue
+// slots busy at 16 warps an SM, whose registers hold the columns' sums).
 #include <cuda_bf16.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "dlm_common.cuh"
 #include "dlm_internal.h"
@@ -27,7 +34,7 @@ namespace {
 
 constexpr int kRowThreads = 256;    // a CTA of the kernels that hold rows in registers
 constexpr int kWideThreads = 1024;  // a CTA of those that read a row again
-constexpr int kHeldWidth = 8192;    // widest row held: 32 values of each kind a thread
+constexpr int kHeldWidth = 8192;    // widest row held: 32 elements a thread
 
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Pack {
@@ -47,25 +54,32 @@ __device__ __forceinline__ float load_param(const void* p, int bf16, int i) {
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
 }
 
-// The sums of v over the G threads of a row. G: a power of two up to 32 (groups
-// inside a warp), or the whole block (a multiple of 32). `red` is not written
-// again before every thread of the block has passed another barrier.
+__device__ __forceinline__ void group_barrier(int G) {
+  if (G <= 32)
+    __syncwarp();
+  else
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + static_cast<int>(threadIdx.x) / G), "r"(G) : "memory");
+}
+
+// The sums of v over the G threads of a row: a power of two, side by side. Whole warps
+// call it. `red` is not written again before the group has passed another barrier.
 template <int NS>
 __device__ __forceinline__ void row_sums(float (&v)[NS], int G, float (*red)[32]) {
   const int top = G < 32 ? G : 32;
-  for (int o = top >> 1; o > 0; o >>= 1)
 #pragma unroll
-    for (int k = 0; k < NS; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+  for (int o = 16; o > 0; o >>= 1)
+    if (o < top)
+#pragma unroll
+      for (int k = 0; k < NS; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
   if (G <= 32) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = G >> 5;
   if (lane == 0)
 #pragma unroll
     for (int k = 0; k < NS; ++k) red[k][warp] = v[k];
-  __syncthreads();
+  group_barrier(G);
 #pragma unroll
-  for (int k = 0; k < NS; ++k) v[k] = lane < warps ? red[k][lane] : 0.f;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
+  for (int k = 0; k < NS; ++k) v[k] = red[k][(warp & ~(warps - 1)) + (lane & (warps - 1))];
+  for (int o = warps >> 1; o > 0; o >>= 1)
 #pragma unroll
     for (int k = 0; k < NS; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
 }
@@ -84,182 +98,344 @@ struct NormParams {
   float eps;
 };
 
-template <typename T, int VEC, int NV>
-__device__ __forceinline__ void load_row(Pack<T, VEC> (&r)[NV], const void* base, int64_t off, int tid, int G, int d, bool any) {
-  const T* p = static_cast<const T*>(base) + off;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int e = (tid + i * G) * VEC;
-    if (any && e < d)
-      r[i] = *reinterpret_cast<const Pack<T, VEC>*>(p + e);
+// A ring of a thread's own vectors of the rows to come, in shared memory: fetched with
+// cp.async and read back by the thread that fetched them, so no barrier is needed. A
+// vector of two bytes, which cp.async does not copy, comes with the aligned four bytes
+// around it.
+template <typename P>
+struct Slot {
+  static constexpr bool kHalf = sizeof(P) == 2;
+  using Type = typename std::conditional<kHalf, uint32_t, P>::type;
+  static __device__ __forceinline__ void fetch(Type* slot, const void* src) {
+    if constexpr (sizeof(Type) == 16)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot)), "l"(src) : "memory");
     else
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(slot)),
+                   "l"(reinterpret_cast<uintptr_t>(src) & ~static_cast<uintptr_t>(3))
+                   : "memory");
+  }
+  static __device__ __forceinline__ void zero(Type* slot) {
+    if constexpr (sizeof(Type) == 16)
+      *reinterpret_cast<uint4*>(slot) = make_uint4(0, 0, 0, 0);
+    else
+      *reinterpret_cast<uint32_t*>(slot) = 0;
+  }
+  // The values of a slot that was fetched from an address with this bit 1 (two-byte vectors).
+  static __device__ __forceinline__ void get(const Type* slot, uint32_t odd, float* v) {
+    if constexpr (kHalf) {
+      v[0] = __uint_as_float(odd ? *slot & 0xFFFF0000u : *slot << 16);
+    } else if constexpr (sizeof(P) == 16 && sizeof(P::e[0]) == 2) {
+      const uint4 u = *reinterpret_cast<const uint4*>(slot);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) r[i].e[k] = from_f32<T>(0.f);
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = __uint_as_float(w[k] << 16);
+        v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      }
+    } else {
+      const P u = *slot;
+#pragma unroll
+      for (int k = 0; k < static_cast<int>(sizeof(P) / sizeof(float)); ++k) v[k] = to_f32(u.e[k]);
+    }
+  }
+};
+__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void fetch_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void store(T* dst, const float* v) {
+  if constexpr (VEC == 8) {
+    *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                                pack_bf16x2(v[6], v[7]));
+  } else if constexpr (VEC == 4) {
+    *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    *dst = from_f32<T>(v[0]);
   }
 }
 
-// VEC: elements per load (16 bytes, or one where a base, a stride or d is not a
-// multiple of that); NV: loads per thread and row.
+// The parameters of vector i (of width / VEC) in shared memory: eight of them lie apart
+// in two runs of four, so that neighbouring threads' 16-byte loads meet different banks.
+template <int VEC>
+__device__ __forceinline__ void load_params(const float* src, int i, int width, float* v) {
+  if constexpr (VEC >= 4) {
+#pragma unroll
+    for (int k = 0; k < VEC; k += 4) {
+      const float4 u = *reinterpret_cast<const float4*>(src + (k ? width / 2 : 0) + i * 4);
+      v[k] = u.x;
+      v[k + 1] = u.y;
+      v[k + 2] = u.z;
+      v[k + 3] = u.w;
+    }
+  } else {
+    v[0] = src[i];
+  }
+}
+template <int VEC>
+__device__ __forceinline__ int param_place(int e, int width) {
+  return VEC == 8 ? (e & 4 ? width / 2 : 0) + (e >> 3) * 4 + (e & 3) : e;
+}
+
+// VEC: elements per load (16 bytes, or one where a base, a stride or d is not a multiple
+// of that); NV: loads per thread, row and tensor. CTAs on an SM by the registers that the
+// elements a thread holds take; the ring's depth by the shared memory of each.
+template <typename T, int VEC, int NV, bool kGradient>
+struct Held {
+  using S = Slot<Pack<T, VEC>>;
+  static constexpr int kElems = VEC * NV;
+  static constexpr int kTensors = kGradient ? 2 : 1;
+  static constexpr int kStage = kRowThreads * NV * kTensors * static_cast<int>(sizeof(typename S::Type));  // bytes
+  static constexpr int kShared = (kGradient ? 192 : 144) * 1024;
+  static constexpr int kCtas = kElems <= 8 ? 4 : !kGradient && kStage <= 16384 ? 3 : kShared / 2 / kStage >= 2 ? 2 : 1;
+  static constexpr int kRoom = kShared / kCtas / kStage;
+  static constexpr int kDepth = kRoom > 6 ? 6 : kRoom;
+  static constexpr int kRing = kDepth * kStage;
+  static_assert(kDepth >= 2, "a ring of one row waits for every load");
+  static_assert(kRing >= kRowThreads * kElems * 4 || !kGradient, "the columns' sums of every group");
+};
+
+// The columns a group's threads hold, a multiple of what d needs.
+__host__ __device__ inline int held_width(int G, int elems) { return G * elems; }
+
+// The weight (and bias) in fp32 behind the ring, zeros past d.
+template <int VEC>
+__device__ __forceinline__ void stage_params(const NormParams& p, float* w, float* b, int width) {
+  for (int e = threadIdx.x; e < width; e += kRowThreads) {
+    const int at = param_place<VEC>(e, width);
+    w[at] = e < p.d ? load_param(p.w, p.w_bf16, e) : 0.f;
+    if (b) b[at] = e < p.d && p.b ? load_param(p.b, p.w_bf16, e) : 0.f;
+  }
+  __syncthreads();
+}
+
 template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kRowThreads) norm_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, false>::kCtas)) norm_kernel(const NormParams p) {
+  using H = Held<T, VEC, NV, false>;
+  using S = typename H::S;
+  constexpr int kElems = H::kElems, kDepth = H::kDepth;
+  extern __shared__ __align__(16) uint8_t smem[];
+  typename S::Type* ring = reinterpret_cast<typename S::Type*>(smem) + threadIdx.x;  // [kDepth][NV][thread]
   __shared__ float red[2][1][32];
-  const int G = p.G, R = blockDim.x / G, g = threadIdx.x / G, tid = threadIdx.x % G, d = p.d;
+  const int G = p.G, R = kRowThreads / G, tid = threadIdx.x % G, d = p.d, width = held_width(G, kElems);
+  float* w = reinterpret_cast<float*>(smem + H::kRing);
+  float* b = w + width;
   const float inv_d = 1.f / static_cast<float>(d);
+  const bool full = width == d;  // every element held is one of the row
+  if (!full)
+#pragma unroll
+    for (int i = 0; i < kDepth * NV; ++i)
+      if ((tid + i % NV * G) * VEC >= d) S::zero(&ring[i * kRowThreads]);
   wait_for_previous();
-  float w[NV * VEC], b[NV * VEC];
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const int e = (tid + i * G) * VEC + k;
-      w[i * VEC + k] = e < d ? load_param(p.w, p.w_bf16, e) : 0.f;
-      b[i * VEC + k] = e < d && p.b ? load_param(p.b, p.w_bf16, e) : 0.f;
-    }
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
-  int64_t row = static_cast<int64_t>(blockIdx.x) * R + g;
-  Pack<T, VEC> x[NV], next[NV];
-  load_row<T, VEC, NV>(x, p.x, row * p.s_x, tid, G, d, row < p.N);
-  for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < p.N; first += step, row += step) {
-    load_row<T, VEC, NV>(next, p.x, (row + step) * p.s_x, tid, G, d, row + step < p.N);
-    float s[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) s[0] += to_f32(x[i].e[k]);
-    row_sums<1>(s, G, red[0]);
-    const float mean = s[0] * inv_d;
-    s[0] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if ((tid + i * G) * VEC < d)
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          const float c = to_f32(x[i].e[k]) - mean;
-          s[0] = fmaf(c, c, s[0]);
-        }
-    row_sums<1>(s, G, red[1]);
-    const float rstd = 1.f / sqrtf(s[0] * inv_d + p.eps);
-    if (row < p.N) {
-      T* o = static_cast<T*>(p.out) + row * p.s_out;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int e = (tid + i * G) * VEC;
-        if (e < d) {
-          Pack<T, VEC> y;
-#pragma unroll
-          for (int k = 0; k < VEC; ++k)
-            y.e[k] = from_f32<T>(fmaf((to_f32(x[i].e[k]) - mean) * rstd, w[i * VEC + k], b[i * VEC + k]));
-          *reinterpret_cast<Pack<T, VEC>*>(o + e) = y;
-        }
-      }
-      if (tid == 0) {
-        if (p.mean) p.mean[row] = mean;
-        if (p.rstd) p.rstd[row] = rstd;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) x[i] = next[i];
-  }
-}
-
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kRowThreads) norm_grad_kernel(const NormParams p) {
-  extern __shared__ float cols[];  // G <= 32: [2][R][G * NV * VEC]
-  __shared__ float red[2][2][32];
-  const int G = p.G, R = blockDim.x / G, g = threadIdx.x / G, tid = threadIdx.x % G, d = p.d;
-  const float inv_d = 1.f / static_cast<float>(d);
-  wait_for_previous();
-  float w[NV * VEC], dw[NV * VEC], db[NV * VEC];
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const int e = (tid + i * G) * VEC + k;
-      w[i * VEC + k] = e < d ? load_param(p.w, p.w_bf16, e) : 0.f;
-      dw[i * VEC + k] = db[i * VEC + k] = 0.f;
-    }
-  const int64_t step = static_cast<int64_t>(gridDim.x) * R;
-  int64_t row = static_cast<int64_t>(blockIdx.x) * R + g;
-  Pack<T, VEC> x[NV], dy[NV], next_x[NV], next_dy[NV];
-  load_row<T, VEC, NV>(x, p.x, row * p.s_x, tid, G, d, row < p.N);
-  load_row<T, VEC, NV>(dy, p.dy, row * p.s_dy, tid, G, d, row < p.N);
-  float mean = row < p.N ? p.mean[row] : 0.f, rstd = row < p.N ? p.rstd[row] : 0.f;
-  int parity = 0;
-  for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < p.N; first += step, row += step, parity ^= 1) {
-    const int64_t after = row + step;
-    load_row<T, VEC, NV>(next_x, p.x, after * p.s_x, tid, G, d, after < p.N);
-    load_row<T, VEC, NV>(next_dy, p.dy, after * p.s_dy, tid, G, d, after < p.N);
-    const float next_mean = after < p.N ? p.mean[after] : 0.f, next_rstd = after < p.N ? p.rstd[after] : 0.f;
-    float s[2] = {0.f, 0.f};
-    if (row < p.N) {  // a group without a row adds nothing
+  int64_t row = static_cast<int64_t>(blockIdx.x) * R + threadIdx.x / G;
+  // Whole warps stay together: the first row of a warp's groups says when it ends.
+  int64_t warp_row = static_cast<int64_t>(blockIdx.x) * R + (threadIdx.x & ~31) / G;
+  const auto ask = [&](int64_t r, int stage) {
+    if (r < p.N) {
+      const T* src = static_cast<const T*>(p.x) + r * p.s_x + tid * VEC;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if ((tid + i * G) * VEC < d)
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) {
-            const float xhat = (to_f32(x[i].e[k]) - mean) * rstd, t = to_f32(dy[i].e[k]), a = t * w[i * VEC + k];
-            s[0] += a;
-            s[1] = fmaf(a, xhat, s[1]);
-            dw[i * VEC + k] = fmaf(t, xhat, dw[i * VEC + k]);
-            db[i * VEC + k] += t;
-          }
+        if (full || (tid + i * G) * VEC < d) S::fetch(&ring[(stage * NV + i) * kRowThreads], src + i * G * VEC);
     }
-    row_sums<2>(s, G, red[parity]);
-    const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
-    if (row < p.N) {
-      T* o = static_cast<T*>(p.out) + row * p.s_out;
+    fetch_commit();
+  };
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int e = (tid + i * G) * VEC;
-        if (e < d) {
-          Pack<T, VEC> y;
+  for (int k = 0; k < kDepth; ++k) ask(row + k * step, k);
+  stage_params<VEC>(p, w, b, width);
+  int stage = 0;
+  for (; warp_row < p.N; warp_row += step, row += step) {
+    fetch_wait<kDepth - 1>();
+    float x[kElems];
+    const uint32_t odd = S::kHalf ? (reinterpret_cast<uintptr_t>(static_cast<const T*>(p.x) + row * p.s_x + tid) >> 1) & 1 : 0;
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) {
-            const float xhat = (to_f32(x[i].e[k]) - mean) * rstd, a = to_f32(dy[i].e[k]) * w[i * VEC + k];
-            y.e[k] = from_f32<T>(rstd * (a - fmaf(xhat, c2, c1)));
-          }
-          *reinterpret_cast<Pack<T, VEC>*>(o + e) = y;
+    for (int i = 0; i < NV; ++i)  // G is even: the elements of a thread have one parity
+      S::get(&ring[(stage * NV + i) * kRowThreads], odd, x + i * VEC);
+    float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < kElems; j += 2) s2 = fadd2(s2, make_float2(x[j], x[j + 1]));
+    float s[1] = {s2.x + s2.y};
+    row_sums<1>(s, G, red[0]);
+    ask(row + kDepth * step, stage);
+    stage = stage + 1 == kDepth ? 0 : stage + 1;
+    const float mean = s[0] * inv_d;
+    const float2 m2 = make_float2(-mean, -mean);
+    s2 = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < kElems; j += 2) {
+      const float2 c = fadd2(make_float2(x[j], x[j + 1]), m2);
+      x[j] = c.x;
+      x[j + 1] = c.y;
+    }
+    if (!full)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if ((tid + i * G) * VEC >= d)
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) x[i * VEC + k] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kElems; j += 2) s2 = ffma2(make_float2(x[j], x[j + 1]), make_float2(x[j], x[j + 1]), s2);
+    s[0] = s2.x + s2.y;
+    row_sums<1>(s, G, red[1]);
+    const float rstd = 1.f / sqrtf(s[0] * inv_d + p.eps);
+    if (row >= p.N) continue;
+    T* o = static_cast<T*>(p.out) + row * p.s_out + tid * VEC;
+    const float2 r2 = make_float2(rstd, rstd);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (!full && (tid + i * G) * VEC >= d) continue;
+      float wv[VEC], bv[VEC];
+      load_params<VEC>(w, tid + i * G, width, wv);
+      load_params<VEC>(b, tid + i * G, width, bv);
+      if constexpr (VEC == 1) {
+        wv[0] = fmaf(x[i] * rstd, wv[0], bv[0]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; k += 2) {
+          const float2 y = ffma2(fmul2(make_float2(x[i * VEC + k], x[i * VEC + k + 1]), r2), make_float2(wv[k], wv[k + 1]),
+                                 make_float2(bv[k], bv[k + 1]));
+          wv[k] = y.x;
+          wv[k + 1] = y.y;
+        }
+      }
+      store<T, VEC>(o + i * G * VEC, wv);
+    }
+    if (tid == 0) {
+      if (p.mean) p.mean[row] = mean;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
+  }
+  fetch_wait<0>();
+}
+
+template <typename T, int VEC, int NV>
+__global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, true>::kCtas)) norm_grad_kernel(const NormParams p) {
+  using H = Held<T, VEC, NV, true>;
+  using S = typename H::S;
+  constexpr int kElems = H::kElems, kDepth = H::kDepth;
+  extern __shared__ __align__(16) uint8_t smem[];
+  typename S::Type* ring = reinterpret_cast<typename S::Type*>(smem) + threadIdx.x;  // [kDepth][x, dy][NV][thread]
+  __shared__ float red[2][2][32];
+  const int G = p.G, R = kRowThreads / G, g = threadIdx.x / G, tid = threadIdx.x % G, d = p.d, width = held_width(G, kElems);
+  float* w = reinterpret_cast<float*>(smem + H::kRing);
+  const float inv_d = 1.f / static_cast<float>(d);
+  const bool full = width == d;
+  if (!full)
+#pragma unroll
+    for (int i = 0; i < kDepth * 2 * NV; ++i)
+      if ((tid + i % NV * G) * VEC >= d) S::zero(&ring[i * kRowThreads]);
+  wait_for_previous();
+  const int64_t step = static_cast<int64_t>(gridDim.x) * R;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * R + g;
+  int64_t warp_row = static_cast<int64_t>(blockIdx.x) * R + (threadIdx.x & ~31) / G;
+  const auto ask = [&](int64_t r, int stage) {
+    if (r < p.N) {
+      const T* x = static_cast<const T*>(p.x) + r * p.s_x + tid * VEC;
+      const T* dy = static_cast<const T*>(p.dy) + r * p.s_dy + tid * VEC;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (full || (tid + i * G) * VEC < d) {
+          S::fetch(&ring[(stage * 2 * NV + i) * kRowThreads], x + i * G * VEC);
+          S::fetch(&ring[((stage * 2 + 1) * NV + i) * kRowThreads], dy + i * G * VEC);
+        }
+    }
+    fetch_commit();
+  };
+#pragma unroll
+  for (int k = 0; k < kDepth; ++k) ask(row + k * step, k);
+  stage_params<VEC>(p, w, nullptr, width);
+  float2 dw[kElems / 2], db[kElems / 2];
+#pragma unroll
+  for (int j = 0; j < kElems / 2; ++j) dw[j] = db[j] = make_float2(0.f, 0.f);
+  float mean = row < p.N ? p.mean[row] : 0.f, rstd = row < p.N ? p.rstd[row] : 0.f;
+  int parity = 0, stage = 0;
+  for (; warp_row < p.N; warp_row += step, row += step, parity ^= 1) {
+    const int64_t after = row + step;
+    const float next_mean = after < p.N ? p.mean[after] : 0.f, next_rstd = after < p.N ? p.rstd[after] : 0.f;
+    const float2 m2 = make_float2(-mean, -mean), r2 = make_float2(rstd, rstd);
+    const uint32_t odd_x = S::kHalf ? (reinterpret_cast<uintptr_t>(static_cast<const T*>(p.x) + row * p.s_x + tid) >> 1) & 1 : 0;
+    const uint32_t odd_dy = S::kHalf ? (reinterpret_cast<uintptr_t>(static_cast<const T*>(p.dy) + row * p.s_dy + tid) >> 1) & 1 : 0;
+    // kPair elements at a time: a vector, or two loads of one element. Past d x, dy and w
+    // are 0, and so is all that is added up.
+    constexpr int kPair = VEC == 1 ? 2 : VEC;
+    const auto get = [&](int j, float* x, float* dy, float* wv) {
+      constexpr int kLoads = kPair / VEC;
+#pragma unroll
+      for (int l = 0; l < kLoads; ++l) {
+        const int i = j / VEC + l;
+        S::get(&ring[(stage * 2 * NV + i) * kRowThreads], odd_x, x + l);
+        S::get(&ring[((stage * 2 + 1) * NV + i) * kRowThreads], odd_dy, dy + l);
+        load_params<VEC>(w, tid + i * G, width, wv + l);
+      }
+    };
+    fetch_wait<kDepth - 1>();
+    float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+    if (row < p.N) {  // a group without a row adds nothing
+#pragma unroll
+      for (int j = 0; j < kElems; j += kPair) {
+        float x[kPair], dy[kPair], wv[kPair];
+        get(j, x, dy, wv);
+#pragma unroll
+        for (int k = 0; k < kPair; k += 2) {
+          const float2 xhat = fmul2(fadd2(make_float2(x[k], x[k + 1]), m2), r2), t = make_float2(dy[k], dy[k + 1]);
+          const float2 a = fmul2(t, make_float2(wv[k], wv[k + 1]));
+          s0 = fadd2(s0, a);
+          s1 = ffma2(a, xhat, s1);
+          dw[(j + k) / 2] = ffma2(t, xhat, dw[(j + k) / 2]);
+          db[(j + k) / 2] = fadd2(db[(j + k) / 2], t);
         }
       }
     }
+    float s[2] = {s0.x + s0.y, s1.x + s1.y};
+    row_sums<2>(s, G, red[parity]);
+    if (row < p.N) {
+      const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
+      const float2 n1 = make_float2(-c1, -c1), n2 = make_float2(-c2, -c2);
+      T* o = static_cast<T*>(p.out) + row * p.s_out + tid * VEC;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      x[i] = next_x[i];
-      dy[i] = next_dy[i];
+      for (int j = 0; j < kElems; j += kPair) {
+        float x[kPair], dy[kPair], wv[kPair];
+        get(j, x, dy, wv);
+#pragma unroll
+        for (int k = 0; k < kPair; k += 2) {
+          const float2 xhat = fmul2(fadd2(make_float2(x[k], x[k + 1]), m2), r2);
+          const float2 a = fmul2(make_float2(dy[k], dy[k + 1]), make_float2(wv[k], wv[k + 1]));
+          const float2 y = fmul2(r2, fadd2(a, ffma2(xhat, n2, n1)));
+          x[k] = y.x;
+          x[k + 1] = y.y;
+        }
+#pragma unroll
+        for (int l = 0; l < kPair / VEC; ++l) {
+          const int i = j / VEC + l;
+          if (full || (tid + i * G) * VEC < d) store<T, VEC>(o + i * G * VEC, x + l);
+        }
+      }
     }
+    ask(row + kDepth * step, stage);
+    stage = stage + 1 == kDepth ? 0 : stage + 1;
     mean = next_mean;
     rstd = next_rstd;
   }
+  fetch_wait<0>();
   if (!p.part) return;
+  // The groups' sums of each column, dw's and then db's, joined through the ring's memory.
   float* part = p.part + static_cast<int64_t>(blockIdx.x) * 2 * d;
-  if (R == 1) {
+  float* cols = reinterpret_cast<float*>(smem);
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        const int e = (tid + i * G) * VEC + k;
-        if (e < d) {
-          part[e] = dw[i * VEC + k];
-          part[d + e] = db[i * VEC + k];
-        }
-      }
-    return;
-  }
-  const int width = G * NV * VEC;  // at least d
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const int e = (tid + i * G) * VEC + k;
-      cols[g * width + e] = dw[i * VEC + k];
-      cols[(R + g) * width + e] = db[i * VEC + k];
+    for (int j = 0; j < kElems; ++j) {
+      const float2 v = which ? db[j / 2] : dw[j / 2];
+      cols[g * width + (tid + j / VEC * G) * VEC + j % VEC] = j & 1 ? v.y : v.x;
     }
-  __syncthreads();
-  for (int e = threadIdx.x; e < 2 * d; e += blockDim.x) {
-    const float* c = cols + (e < d ? e : R * width + e - d);
-    float sum = 0.f;
-    for (int r = 0; r < R; ++r) sum += c[r * width];
-    part[e] = sum;
+    __syncthreads();
+    for (int e = threadIdx.x; e < d; e += kRowThreads) {
+      float sum = 0.f;
+      for (int r = 0; r < R; ++r) sum += cols[r * width + e];
+      part[which * d + e] = sum;
+    }
   }
 }
 
@@ -362,93 +538,130 @@ __global__ void __launch_bounds__(kRowThreads) norm_columns_kernel(const NormPar
   part[p.d + c] = db;
 }
 
-// Adds the parts of 32 columns (blockIdx.x) of dw or db (blockIdx.y), in a fixed order.
-constexpr int kReduceRows = 16;
-__global__ void __launch_bounds__(32 * kReduceRows)
+// Adds the parts of 8 columns (a sector; blockIdx.x) of dw or db (blockIdx.y) in a fixed
+// order, 32 threads a column, each with its loads in flight at once. (32 columns and 1024
+// threads a CTA: 7.5 us instead of 4.)
+constexpr int kReduceThreads = 256;
+__global__ void __launch_bounds__(kReduceThreads)
     norm_reduce_kernel(const float* part, int parts, int d, int bf16, void* dw, void* db) {
-  __shared__ float sums[kReduceRows][33];
+  __shared__ float sums[kReduceThreads / 32][8];
   void* out = blockIdx.y ? db : dw;
   if (!out) return;
   wait_for_previous();
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 8 + (lane & 7);
   float s = 0.f;
-  if (c < d)
-#pragma unroll 4
-    for (int i = ty; i < parts; i += kReduceRows) s += part[(static_cast<int64_t>(i) * 2 + blockIdx.y) * d + c];
-  sums[ty][tx] = s;
+  const float* src = part + static_cast<int64_t>(blockIdx.y) * d + c;
+  for (int i = warp * 4 + (lane >> 3); i < parts; i += kReduceThreads) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int at = i + k * (kReduceThreads / 8);
+      v[k] = c < d && at < parts ? src[static_cast<int64_t>(at) * 2 * d] : 0.f;
+    }
+    s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  }
+  s += __shfl_xor_sync(0xffffffffu, s, 8);
+  s += __shfl_xor_sync(0xffffffffu, s, 16);
+  if (lane < 8) sums[warp][lane] = s;
   __syncthreads();
-  if (ty || c >= d) return;
+  if (threadIdx.x >= 8 || c >= d) return;
   s = 0.f;
 #pragma unroll
-  for (int i = 0; i < kReduceRows; ++i) s += sums[i][tx];
+  for (int i = 0; i < kReduceThreads / 32; ++i) s += sums[i][lane];
   if (bf16)
     static_cast<__nv_bfloat16*>(out)[c] = __float2bfloat16_rn(s);
   else
     static_cast<float*>(out)[c] = s;
 }
 
-// Threads a row, rows a CTA and loads a thread: the fewest loads whose threads fit
-// in a CTA; a row of few loads shares a CTA, and a warp, with others.
+// Threads a row and loads a thread. Many rows: a warp, or the fewest warps that hold the
+// row, so that few threads pay for each row; rows of few loads share a warp. Few rows:
+// more threads each, while half of them still find a place at once, for the chain of
+// loads and sums is what a call then waits for (512 x 2048 bf16: 6.8 us).
 struct Shape {
-  int G, R, nv;
+  int G, nv;
 };
 
-Shape shape_of(int64_t loads, const int* nvs) {
-  int nv = *nvs;
-  while ((loads + nv - 1) / nv > kRowThreads) nv = *++nvs;
-  const int64_t need = (loads + nv - 1) / nv;
-  if (need > 32) return {static_cast<int>((need + 31) / 32 * 32), 1, nv};
-  int G = 8;
-  while (G < need) G *= 2;
-  return {G, kRowThreads / G, nv};
+Shape shape_of(int64_t N, int64_t loads, int most_nv, int sms) {
+  int G = 8, nv = 1;
+  while (G < 32 && G < loads) G *= 2;
+  while (static_cast<int64_t>(G) * nv < loads) {
+    if (nv < most_nv)
+      nv *= 2;
+    else
+      G *= 2;
+  }
+  while (nv > 1 && G < kRowThreads && N * G * 2 <= static_cast<int64_t>(sms) * 512) {
+    G *= 2;
+    nv /= 2;
+  }
+  return {G, nv};
 }
 
 bool by_vectors(const void* p, int64_t stride, int esz) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * esz % 16 == 0;
 }
 
+// One CTA for every place on the SMs, or fewer: each walks rows.
+template <typename T, int VEC, int NV, bool kGradient>
+cudaError_t launch_held(const NormParams& p, int sms, int* parts, cudaStream_t stream) {
+  using H = Held<T, VEC, NV, kGradient>;
+  const auto kernel = kGradient ? norm_grad_kernel<T, VEC, NV> : norm_kernel<T, VEC, NV>;
+  const size_t smem = H::kRing + static_cast<size_t>(held_width(p.G, H::kElems)) * 4 * (kGradient ? 1 : 2);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  // The weights of wide rows leave room for fewer CTAs than the registers do.
+  const int fit = static_cast<int>(224 * 1024 / (smem + 1536));
+  const int R = kRowThreads / p.G, most = norm_max_parts(p.d);
+  int places = sms * (fit < 1 ? 1 : fit < H::kCtas ? fit : H::kCtas);
+  if (kGradient && places > most) places = most;
+  const int64_t want = (p.N + R - 1) / R;
+  *parts = static_cast<int>(want < places ? want : places);
+  return launch_overlapped(kernel, dim3(static_cast<unsigned>(*parts)), kRowThreads, smem, stream, 1, true, p);
+}
+
 template <typename T, int VEC, int NV>
-cudaError_t launch_shape(bool grad, const NormParams& p, const Shape& s, int ctas, cudaStream_t stream) {
-  const size_t smem = grad && s.R > 1 ? static_cast<size_t>(2) * s.R * s.G * NV * VEC * 4 : 0;
-  return launch_overlapped(grad ? norm_grad_kernel<T, VEC, NV> : norm_kernel<T, VEC, NV>, dim3(static_cast<unsigned>(ctas)),
-                           s.G * s.R, smem, stream, 1, true, p);
+cudaError_t launch_shape(bool grad, const NormParams& p, int sms, int* parts, cudaStream_t stream) {
+  return grad ? launch_held<T, VEC, NV, true>(p, sms, parts, stream) : launch_held<T, VEC, NV, false>(p, sms, parts, stream);
 }
 
 template <typename T, int VEC>
-cudaError_t launch_wide(bool grad, const NormParams& p, int max_ctas, int* parts, cudaStream_t stream) {
-  const int64_t most = p.N < 304 ? p.N : 304;  // two CTAs of 1024 threads an SM
+cudaError_t launch_wide(bool grad, const NormParams& p, int sms, int* parts, cudaStream_t stream) {
+  const int64_t most = p.N < 2 * sms ? p.N : 2 * sms;
   cudaError_t e = launch_overlapped(grad ? norm_grad_wide_kernel<T, VEC> : norm_wide_kernel<T, VEC>,
                                     dim3(static_cast<unsigned>(most)), kWideThreads, 0, stream, 1, true, p);
   if (e != cudaSuccess || !p.part) return e;
-  *parts = static_cast<int>(p.N < max_ctas ? p.N : max_ctas);
+  const int64_t room = norm_max_parts(p.d) < sms ? norm_max_parts(p.d) : sms;
+  *parts = static_cast<int>(p.N < room ? p.N : room);
   return launch_overlapped(norm_columns_kernel<T>, dim3(static_cast<unsigned>((p.d + kRowThreads - 1) / kRowThreads), *parts),
                            kRowThreads, 0, stream, 1, true, p);
 }
 
 // *parts: the parts of dw and db that the launches write.
 template <typename T>
-int launch_typed(bool grad, NormParams p, int max_ctas, int* parts, cudaStream_t stream) {
+int launch_typed(bool grad, NormParams p, int* parts, cudaStream_t stream) {
   constexpr int kVec = 16 / static_cast<int>(sizeof(T));
   const bool vec = p.d % kVec == 0 && by_vectors(p.x, p.s_x, sizeof(T)) && by_vectors(p.out, p.s_out, sizeof(T)) &&
                    (!grad || by_vectors(p.dy, p.s_dy, sizeof(T)));
+  int dev = 0, sms = 0;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   cudaError_t e;
   if (p.d > kHeldWidth) {
-    e = vec ? launch_wide<T, kVec>(grad, p, max_ctas, parts, stream) : launch_wide<T, 1>(grad, p, max_ctas, parts, stream);
+    e = vec ? launch_wide<T, kVec>(grad, p, sms, parts, stream) : launch_wide<T, 1>(grad, p, sms, parts, stream);
   } else {
-    static const int kVecLoads[] = {1, 2, 4, 8}, kLoads[] = {8, 32};
-    constexpr int kMost = 32 / kVec;  // loads a thread of the widest row held
-    const Shape s = vec ? shape_of(p.d / kVec, kVecLoads) : shape_of(p.d, kLoads);
+    const Shape s = vec ? shape_of(p.N, p.d / kVec, 32 / kVec, sms) : shape_of(p.N, (p.d + 3) / 4 * 4, 32, sms);
     p.G = s.G;
-    const int64_t want = (p.N + s.R - 1) / s.R;
-    *parts = static_cast<int>(want < max_ctas ? want : max_ctas);
-    if (!vec)
-      e = s.nv == 8 ? launch_shape<T, 1, 8>(grad, p, s, *parts, stream) : launch_shape<T, 1, 32>(grad, p, s, *parts, stream);
-    else if (s.nv == 1)
-      e = launch_shape<T, kVec, 1>(grad, p, s, *parts, stream);
-    else if (s.nv == 2)
-      e = launch_shape<T, kVec, 2>(grad, p, s, *parts, stream);
+    if (vec)
+      e = s.nv == 1   ? launch_shape<T, kVec, 1>(grad, p, sms, parts, stream)
+          : s.nv == 2 ? launch_shape<T, kVec, 2>(grad, p, sms, parts, stream)
+          : s.nv == 4 ? launch_shape<T, kVec, 4>(grad, p, sms, parts, stream)
+                      : launch_shape<T, kVec, 32 / kVec>(grad, p, sms, parts, stream);
     else
-      e = s.nv == kMost ? launch_shape<T, kVec, kMost>(grad, p, s, *parts, stream) : launch_shape<T, kVec, 4>(grad, p, s, *parts, stream);
+      e = s.nv <= 4    ? launch_shape<T, 1, 4>(grad, p, sms, parts, stream)
+          : s.nv <= 8  ? launch_shape<T, 1, 8>(grad, p, sms, parts, stream)
+          : s.nv <= 16 ? launch_shape<T, 1, 16>(grad, p, sms, parts, stream)
+                       : launch_shape<T, 1, 32>(grad, p, sms, parts, stream);
   }
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "layer norm launch: %s", cudaGetErrorString(e));
 }
@@ -474,9 +687,8 @@ int launch_layer_norm(const NormArgs& a, cudaStream_t stream) {
   p.out = a.out;
   p.s_out = a.s_out;
   p.eps = a.eps;
-  int ctas;
-  return a.is_bf16 ? launch_typed<__nv_bfloat16>(false, p, 152 * 8, &ctas, stream)
-                   : launch_typed<float>(false, p, 152 * 8, &ctas, stream);
+  int parts;
+  return a.is_bf16 ? launch_typed<__nv_bfloat16>(false, p, &parts, stream) : launch_typed<float>(false, p, &parts, stream);
 }
 
 int launch_layer_norm_grad(const NormArgs& a, cudaStream_t stream) {
@@ -486,16 +698,15 @@ int launch_layer_norm_grad(const NormArgs& a, cudaStream_t stream) {
   p.out = a.dx;
   p.s_out = a.s_dx;
   p.part = a.dweight || a.dbias ? static_cast<float*>(a.workspace) : nullptr;
-  int ctas = 0;
+  int parts = 0;
   if (a.N > 0) {
-    const int most = norm_max_parts(a.d);
-    const int st = a.is_bf16 ? launch_typed<__nv_bfloat16>(true, p, most, &ctas, stream) : launch_typed<float>(true, p, most, &ctas, stream);
+    const int st = a.is_bf16 ? launch_typed<__nv_bfloat16>(true, p, &parts, stream) : launch_typed<float>(true, p, &parts, stream);
     if (st != DLM_OK) return st;
   }
   if (!a.dweight && !a.dbias) return DLM_OK;
   const cudaError_t e =
-      launch_overlapped(norm_reduce_kernel, dim3(static_cast<unsigned>((a.d + 31) / 32), 2), 32 * kReduceRows, 0, stream, 1,
-                        true, static_cast<const float*>(a.workspace), ctas, p.d, a.weight_bf16, a.dweight, a.dbias);
+      launch_overlapped(norm_reduce_kernel, dim3(static_cast<unsigned>((a.d + 7) / 8), 2), kReduceThreads, 0, stream, 1,
+                        true, static_cast<const float*>(a.workspace), parts, p.d, a.weight_bf16, a.dweight, a.dbias);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "layer norm reduction launch: %s", cudaGetErrorString(e));
 }
 

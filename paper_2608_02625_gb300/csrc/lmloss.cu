@@ -474,22 +474,33 @@ struct GatherParams {
 constexpr int kGatherThreads = 256;
 
 // The K splits of dh that leave the busiest CTA the fewest steps: a tile also costs
-// about 16 steps (of 64, 128 x 256: 0.34 us) for writing and reading its fp32 sums.
+// about 16 steps (of 64, 128 x 256: 0.34 us) for writing and reading its fp32 sums. A
+// lane of a warp looks at two numbers of splits (one thread at all of them: 8 us).
 __device__ int choose_splits(const GatherParams& p, int n) {
-  const int per = (n + kBM - 1) / kBM * p.tiles;
-  if (per == 0) return 1;
-  int best = 1;
-  long long best_cost = -1;
-  for (int s = 1; s <= 64 && s <= p.kblocks; ++s) {
-    if (s > 1 && static_cast<long long>(s) * ((n + kBM - 1) / kBM) * kBM > p.max_rows) break;
-    const long long rounds = (static_cast<long long>(per) * s + p.ctas - 1) / p.ctas;
-    const long long cost = rounds * ((p.kblocks + s - 1) / s + 16);
-    if (best_cost < 0 || cost < best_cost) {
-      best_cost = cost;
-      best = s;
+  const int lane = threadIdx.x & 31, blocks = (n + kBM - 1) / kBM;
+  unsigned best = 0xFFFFFFFFu;
+  int splits = 1;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = lane + 32 * k + 1;
+    const bool fits = s == 1 || (s <= p.kblocks && blocks <= p.max_rows / kBM / s);
+    const unsigned rounds = (static_cast<unsigned>(blocks) * p.tiles * s + p.ctas - 1) / p.ctas;
+    const unsigned cost = fits ? rounds * ((p.kblocks + s - 1) / s + 16) : 0xFFFFFFFFu;
+    if (cost < best) {
+      best = cost;
+      splits = s;
     }
   }
-  return best;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const unsigned c = __shfl_xor_sync(0xffffffffu, best, o);
+    const int s = __shfl_xor_sync(0xffffffffu, splits, o);
+    if (c < best || (c == best && s < splits)) {
+      best = c;
+      splits = s;
+    }
+  }
+  return splits;
 }
 
 __device__ int block_count(int v, int* sums) {
@@ -572,9 +583,12 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
   }
   if (blockIdx.x != gridDim.x - 1) return;
   const int n = before, end = (n + kBM - 1) / kBM * kBM;
-  if (threadIdx.x == 0) {
-    p.plan->n = n;
-    p.plan->splits = p.tiles ? choose_splits(p, n) : 1;
+  if (warp == 0) {
+    const int splits = p.tiles ? choose_splits(p, n) : 1;
+    if (lane == 0) {
+      p.plan->n = n;
+      p.plan->splits = splits;
+    }
   }
   for (int r = n + threadIdx.x; r < end; r += kGatherThreads) {
     p.to_target[r] = -1;
@@ -619,41 +633,42 @@ __global__ void __launch_bounds__(kCombineThreads)
   }
 }
 
-// d_hidden: the splits' sums of each scored row, zeros for the others.
-constexpr int kFinishThreads = 256;
+// d_hidden: the splits' sums of each scored row, zeros for the others; four columns a
+// thread, eight splits' loads in flight.
+constexpr int kFinishThreads = 128;
 __global__ void __launch_bounds__(kFinishThreads)
     loss_dhidden_kernel(const Plan* plan, const int* place, const float* part, int N, int d, int d_pad, __nv_bfloat16* out,
                         int64_t s_out, int aligned) {
   wait_for_previous();
-  const int vecs = d / 8, splits = plan->splits;
+  const int vecs = d / 4, splits = plan->splits;
   const int64_t step = static_cast<int64_t>((plan->n + kBM - 1) / kBM) * kBM * d_pad;
   const int64_t total = static_cast<int64_t>(N) * vecs;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x; i < total;
        i += static_cast<int64_t>(gridDim.x) * kFinishThreads) {
     const int64_t r = i / vecs;
-    const int col = static_cast<int>(i - r * vecs) * 8, c = place[r];
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    const int col = static_cast<int>(i - r * vecs) * 4, c = place[r];
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c >= 0) {
       const float* src = part + static_cast<int64_t>(c) * d_pad + col;
-#pragma unroll 4
-      for (int s = 0; s < splits; ++s, src += step) {
-        const float4 u = reinterpret_cast<const float4*>(src)[0], w = reinterpret_cast<const float4*>(src)[1];
-        a = make_float4(a.x + u.x, a.y + u.y, a.z + u.z, a.w + u.w);
-        b = make_float4(b.x + w.x, b.y + w.y, b.z + w.z, b.w + w.w);
+      for (int s = 0; s < splits; s += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          v[k] = s + k < splits ? *reinterpret_cast<const float4*>(src + (s + k) * step) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) a = make_float4(a.x + v[k].x, a.y + v[k].y, a.z + v[k].z, a.w + v[k].w);
       }
     }
-    const uint4 o = make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w));
+    const uint2 o = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
     __nv_bfloat16* dst = out + r * s_out + col;
     if (aligned) {
-      *reinterpret_cast<uint4*>(dst) = o;
+      *reinterpret_cast<uint2*>(dst) = o;
     } else {
       unsigned short* e = reinterpret_cast<unsigned short*>(dst);
-      const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        e[2 * k] = static_cast<unsigned short>(w[k] & 0xFFFFu);
-        e[2 * k + 1] = static_cast<unsigned short>(w[k] >> 16);
-      }
+      e[0] = static_cast<unsigned short>(o.x & 0xFFFFu);
+      e[1] = static_cast<unsigned short>(o.x >> 16);
+      e[2] = static_cast<unsigned short>(o.y & 0xFFFFu);
+      e[3] = static_cast<unsigned short>(o.y >> 16);
     }
   }
 }
@@ -873,9 +888,9 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
     }
   }
   if (!a.d_hidden) return DLM_OK;
-  const int64_t vecs = a.N * (a.d / 8);
-  const int64_t want = (vecs + kFinishThreads - 1) / kFinishThreads, most = static_cast<int64_t>(sms) * 8;
-  const bool aligned = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 15) == 0;
+  const int64_t vecs = a.N * (a.d / 4);
+  const int64_t want = (vecs + kFinishThreads - 1) / kFinishThreads, most = static_cast<int64_t>(sms) * 16;
+  const bool aligned = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 7) == 0;
   const cudaError_t e = launch_overlapped(
       loss_dhidden_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), kFinishThreads, 0, stream, 1, true, base.plan,
       reinterpret_cast<const int*>(ws + l.place), reinterpret_cast<const float*>(ws + l.sums), static_cast<int>(a.N),
