@@ -253,7 +253,7 @@ struct GradArgs {
   double* workspace;     // clip_grad_norm_workspace_bytes()
   int parts;             // set by the launcher
 };
-constexpr int kGradParts = 608;      // sums (CTAs) a launch
+constexpr int kGradParts = 1216;     // sums (CTAs) a launch: eight on each of 152 SMs
 constexpr int kGradTable = 960;      // tensors a launch
 constexpr int kMaxGradTensors = 16 * kGradTable;
 inline size_t clip_grad_norm_workspace_bytes() { return sizeof(double) * kGradParts * (kMaxGradTensors / kGradTable); }

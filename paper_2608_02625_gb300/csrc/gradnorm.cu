@@ -6,12 +6,18 @@
 // Two launches over the same chunks of the tensors. The first sums squares: a
 // thread adds a chunk's in fp32 (up to 256, in eight sums) and the chunks' in fp64,
 // and each CTA leaves one fp64 sum in the caller's workspace. The second adds those
-// in a fixed order (every CTA for itself: a few hundred numbers) and scales,
-// walking the chunks from the last to the first, so that what the first launch read
-// last is still in L2; where nothing changes (no clipping, in place) it ends there.
+// in a fixed order (every CTA for itself: a thousand numbers) and scales, walking the
+// chunks from the last to the first, so that what the first launch read last may still
+// be in L2; where nothing changes (no clipping, in place) it ends there. (Both in one
+// launch, a cluster of 16 CTAs for a few small tensors, took 9.9 us for 48 of 2000 fp32
+// elements, the two launches 8.9.)
 // A chunk whose fp32 squares may have over- or underflowed (|x| above about 2^60,
 // or all of it below 2^-40) is summed again in fp64. The tensors' addresses travel
 // as kernel parameters, so a captured call needs no copy of a table.
+//
+// HBM bounds it: two reads and a write of everything. 310 M bf16 elements (621 MB): the
+// squares 91 us, the scaling 190 (eight CTAs an SM; four: 98 and 199), of 274 at the
+// copy rate.
 #include <cuda_bf16.h>
 
 #include <cstdint>
@@ -72,22 +78,27 @@ __device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x)
 // This thread's share of the squares of x[0, n).
 template <typename T>
 __device__ double squares(const T* x, int64_t n, bool vectors) {
-  constexpr int kPer = 16 / sizeof(T);
+  constexpr int kPer = 16 / sizeof(T), kLoads = 4;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   uint32_t any = 0;
-  const int64_t whole = vectors ? n / kPer * kPer : 0;
-#pragma unroll 4
-  for (int64_t i = static_cast<int64_t>(threadIdx.x) * kPer; i < whole; i += kThreads * kPer) {
-    const Vec<T> v = *reinterpret_cast<const Vec<T>*>(x + i);
+  const int vecs = vectors ? static_cast<int>(n / kPer) : 0, whole = vecs * kPer;
+  const Vec<T>* xv = reinterpret_cast<const Vec<T>*>(x);
+  for (int i = threadIdx.x; i < vecs; i += kThreads * kLoads) {
+    Vec<T> v[kLoads] = {};
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const float f = f32_of(v.e[k]);
-      acc[k] = fmaf(f, f, acc[k]);
-      any |= bits_of(f);
-    }
+    for (int k = 0; k < kLoads; ++k)
+      if (i + k * kThreads < vecs) v[k] = xv[i + k * kThreads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const float f = f32_of(v[k].e[e]);
+        acc[e] = fmaf(f, f, acc[e]);
+        any |= bits_of(f);
+      }
   }
 #pragma unroll 4
-  for (int64_t i = whole + threadIdx.x; i < n; i += kThreads) {
+  for (int i = whole + threadIdx.x; i < n; i += kThreads) {
     const float f = f32_of(x[i]);
     acc[0] = fmaf(f, f, acc[0]);
     any |= bits_of(f);
@@ -95,25 +106,46 @@ __device__ double squares(const T* x, int64_t n, bool vectors) {
   const float s = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
   if (any == 0 || (s >= 0x1p-80f && s <= 0x1p120f)) return s;
   double t = 0.0;
-  for (int64_t i = static_cast<int64_t>(threadIdx.x) * kPer; i < whole; i += kThreads * kPer)
-    for (int k = 0; k < kPer; ++k) t += static_cast<double>(f32_of(x[i + k])) * f32_of(x[i + k]);
-  for (int64_t i = whole + threadIdx.x; i < n; i += kThreads) t += static_cast<double>(f32_of(x[i])) * f32_of(x[i]);
+  for (int i = threadIdx.x; i < vecs; i += kThreads)
+    for (int e = 0; e < kPer; ++e) t += static_cast<double>(f32_of(x[i * kPer + e])) * f32_of(x[i * kPer + e]);
+  for (int i = whole + threadIdx.x; i < n; i += kThreads) t += static_cast<double>(f32_of(x[i])) * f32_of(x[i]);
   return t;
+}
+
+__device__ __forceinline__ Vec<float> scaled(const Vec<float>& v, float c1, float c2) {
+  Vec<float> o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o.e[e] = v.e[e] * c1 * c2;
+  return o;
+}
+__device__ __forceinline__ Vec<__nv_bfloat16> scaled(const Vec<__nv_bfloat16>& v, float c1, float c2) {
+  Vec<__nv_bfloat16> o;
+  uint32_t* w = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) w[e / 2] = pack_bf16x2(f32_of(v.e[e]) * c1 * c2, f32_of(v.e[e + 1]) * c1 * c2);
+  return o;
 }
 
 // Scales x[0, n) by c1 c2 (c2 = 1 unless the factor is below fp32's normal range).
 template <typename T>
 __device__ void scale(const T* x, T* out, int64_t n, bool vectors, float c1, float c2) {
-  constexpr int kPer = 16 / sizeof(T);
-  const int64_t whole = vectors ? n / kPer * kPer : 0;
-#pragma unroll 4
-  for (int64_t i = static_cast<int64_t>(threadIdx.x) * kPer; i < whole; i += kThreads * kPer) {
-    Vec<T> v = *reinterpret_cast<const Vec<T>*>(x + i);
+  constexpr int kPer = 16 / sizeof(T), kLoads = 8;
+  const int vecs = vectors ? static_cast<int>(n / kPer) : 0, whole = vecs * kPer;
+  const float4* xv = reinterpret_cast<const float4*>(x);
+  float4* ov = reinterpret_cast<float4*>(out);
+  for (int i = threadIdx.x; i < vecs; i += kThreads * kLoads) {
+    float4 v[kLoads];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) v.e[k] = static_cast<T>(f32_of(v.e[k]) * c1 * c2);
-    *reinterpret_cast<Vec<T>*>(out + i) = v;
+    for (int k = 0; k < kLoads; ++k)
+      if (i + k * kThreads < vecs) v[k] = __ldcs(xv + i + k * kThreads);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      if (i + k * kThreads < vecs) {
+        const Vec<T> o = scaled(*reinterpret_cast<const Vec<T>*>(&v[k]), c1, c2);
+        __stcs(ov + i + k * kThreads, *reinterpret_cast<const float4*>(&o));
+      }
   }
-  for (int64_t i = whole + threadIdx.x; i < n; i += kThreads) out[i] = static_cast<T>(f32_of(x[i]) * c1 * c2);
+  for (int i = whole + threadIdx.x; i < n; i += kThreads) out[i] = static_cast<T>(f32_of(x[i]) * c1 * c2);
 }
 
 // The sum of v over the block, in every thread.
@@ -129,17 +161,43 @@ __device__ double block_sum(double v) {
   return v;
 }
 
+// The squares of chunk c.
+template <typename Tab>
+__device__ double chunk_squares(const Tab& tab, int c) {
+  const Tensor& t = find(tab, c);
+  const int64_t at = static_cast<int64_t>(c - t.first) * tab.chunk;
+  const int64_t n = t.n - at < tab.chunk ? t.n - at : tab.chunk;
+  return t.flags & kBf16 ? squares(static_cast<const __nv_bfloat16*>(t.in) + at, n, t.flags & kVectors)
+                         : squares(static_cast<const float*>(t.in) + at, n, t.flags & kVectors);
+}
+
+// The factor as two numbers: below 2^-100 it may be below fp32's normal range.
+struct Factor {
+  float c1, c2;
+};
+__device__ __forceinline__ Factor factor_of(double norm, float max_norm) {
+  double c = static_cast<double>(max_norm) / (norm + 1e-6);
+  if (c >= 1.0) c = 1.0;  // a NaN stays one
+  return {static_cast<float>(c < 0x1p-100 ? c * 0x1p100 : c), c < 0x1p-100 ? 0x1p-100f : 1.f};
+}
+
+template <typename Tab>
+__device__ void chunk_scale(const Tab& tab, int c, const Factor& f) {
+  const Tensor& t = find(tab, c);
+  if (f.c1 == 1.f && t.in == t.out) return;
+  const int64_t at = static_cast<int64_t>(c - t.first) * tab.chunk;
+  const int64_t n = t.n - at < tab.chunk ? t.n - at : tab.chunk;
+  if (t.flags & kBf16)
+    scale(static_cast<const __nv_bfloat16*>(t.in) + at, static_cast<__nv_bfloat16*>(t.out) + at, n, t.flags & kVectors, f.c1, f.c2);
+  else
+    scale(static_cast<const float*>(t.in) + at, static_cast<float*>(t.out) + at, n, t.flags & kVectors, f.c1, f.c2);
+}
+
 template <int kTensors>
 __global__ void __launch_bounds__(kThreads) grad_squares_kernel(const __grid_constant__ Table<kTensors> tab) {
   wait_for_previous();
   double s = 0.0;
-  for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
-    const Tensor& t = find(tab, c);
-    const int64_t at = static_cast<int64_t>(c - t.first) * tab.chunk;
-    const int64_t n = t.n - at < tab.chunk ? t.n - at : tab.chunk;
-    s += t.flags & kBf16 ? squares(static_cast<const __nv_bfloat16*>(t.in) + at, n, t.flags & kVectors)
-                         : squares(static_cast<const float*>(t.in) + at, n, t.flags & kVectors);
-  }
+  for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) s += chunk_squares(tab, c);
   s = block_sum(s);
   if (threadIdx.x == 0) tab.part[blockIdx.x] = s;
 }
@@ -151,20 +209,8 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const __grid_const
   for (int i = threadIdx.x; i < tab.n_parts; i += kThreads) s += tab.parts[i];
   const double norm = sqrt(block_sum(s));
   if (tab.norm && blockIdx.x == 0 && threadIdx.x == 0) *tab.norm = static_cast<float>(norm);
-  double c = static_cast<double>(tab.max_norm) / (norm + 1e-6);
-  if (c >= 1.0) c = 1.0;  // a NaN stays one
-  // A factor below 2^-100 as two: it may be below fp32's normal range.
-  const float c2 = c < 0x1p-100 ? 0x1p-100f : 1.f, c1 = static_cast<float>(c < 0x1p-100 ? c * 0x1p100 : c);
-  for (int k = tab.chunks - 1 - static_cast<int>(blockIdx.x); k >= 0; k -= gridDim.x) {
-    const Tensor& t = find(tab, k);
-    if (c1 == 1.f && t.in == t.out) continue;
-    const int64_t at = static_cast<int64_t>(k - t.first) * tab.chunk;
-    const int64_t n = t.n - at < tab.chunk ? t.n - at : tab.chunk;
-    if (t.flags & kBf16)
-      scale(static_cast<const __nv_bfloat16*>(t.in) + at, static_cast<__nv_bfloat16*>(t.out) + at, n, t.flags & kVectors, c1, c2);
-    else
-      scale(static_cast<const float*>(t.in) + at, static_cast<float*>(t.out) + at, n, t.flags & kVectors, c1, c2);
-  }
+  const Factor f = factor_of(norm, tab.max_norm);
+  for (int c = tab.chunks - 1 - static_cast<int>(blockIdx.x); c >= 0; c -= gridDim.x) chunk_scale(tab, c, f);
 }
 
 template <int kTensors>
@@ -174,7 +220,7 @@ void fill(const GradArgs& a, int first, Table<kTensors>* tab, int64_t target) {
   for (int i = 0; i < tab->count; ++i) total += a.grads[first + i].n;
   int64_t chunk = (total / target + kUnit - 1) / kUnit * kUnit;
   if (chunk < kUnit) chunk = kUnit;
-  if (chunk > 32 * kUnit) chunk = 32 * kUnit;
+  if (chunk > 16 * kUnit) chunk = 16 * kUnit;
   int64_t chunks = 0;
   for (;; chunk *= 2) {  // until the chunks' number is an int
     chunks = 0;
@@ -199,7 +245,7 @@ int launch_phase(const GradArgs& a, bool scale_phase, cudaStream_t stream) {
   int written = 0;
   Table<kTensors> tab;
   for (int l = 0; l < launches; ++l) {
-    fill(a, l * kTensors, &tab, 4 * kGradParts);
+    fill(a, l * kTensors, &tab, 2 * kGradParts);
     int ctas = tab.chunks < kGradParts ? tab.chunks : kGradParts;
     if (ctas < 1) ctas = 1;
     tab.part = a.workspace + written;
