@@ -6,25 +6,29 @@
 //   d_hidden = g weight,   d_weight = g^T hidden
 //
 // Rows without a target (outside [0, V)) are not scored: the first launch copies the
-// hidden states of the others, in their order, to the workspace (n rows, then rows of
-// zeros to a multiple of 128), so the products take time for scored rows alone -- of a
+// hidden states of the others, in their order, to the workspace (n rows), so the products take time for scored rows alone -- of a
 // masked diffusion batch a quarter, say -- and their number stays on the GPU.
 //
-// Four products run through one persistent kernel, a CTA an SM, 128 x bn output tiles
-// (bn up to 256), K steps of 64 through a ring of four stages of 48 KB:
+// The products run through one persistent kernel in three modes, 128 x bn output tiles a
+// CTA (bn up to 256), K steps of 64 through a ring of 192 KB:
 //   stats  x = H W^T     per row and part of the vocabulary: maximum, sum of e^(x - m),
 //                        and the target's logit; loss_combine_kernel joins the parts
 //   grad   x = H W^T     g of one piece of the vocabulary, rounded to bf16, to the workspace
-//   dw     g^T H         a piece of d_weight, bf16
-//   dh     g W           fp32 sums over the piece, added to those of the pieces before it;
-//                        split over K where there are too few tiles for every SM
+//   back   g^T H         dw: a piece of d_weight, bf16, and
+//          g W           dh: fp32 sums over the piece, added to those of the pieces before
+//                        it; split over K where there are too few tiles for every SM
+// With many rows two CTAs share a tile of 256 rows (cta_group::2): each loads half of B,
+// which an MMA of one CTA's reads whole, and shared memory feeds the MMAs with fewer
+// pauses (4096 x 20000 x 2048: grad 203 -> 175 us, 90 % of the tensor pipe's cycles; dw
+// 247 -> 207, dh 250 -> 207).
 // g is rounded to bf16 because the tensor cores take it so: every term of d_hidden and
 // d_weight is off by at most 2^-8 relative, as the result is by its own rounding to bf16;
 // all sums are fp32. Warp 0 loads by TMA, warp 1 issues tcgen05.mma (both operands in
 // shared memory, K-major or MN-major as their matrix lies in memory, so nothing is
-// transposed), warps 4-7 read the fp32 accumulators (two, so a tile's epilogue runs
+// transposed), warps 4-11 read the fp32 accumulators (two, so a tile's epilogue runs
 // under the next one's K loop) and write their tiles through shared memory by TMA.
 // Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, drains and exits.
+#include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -35,37 +39,49 @@
 #include "dlm_internal.h"
 #include "dlm_tmap.h"
 
+namespace cg = cooperative_groups;
+
 namespace dlm {
 namespace {
 
-constexpr int kBM = 128;          // rows of an output tile = TMEM lanes
+constexpr int kBM = 128;          // a CTA's rows of an output tile = TMEM lanes
 constexpr int kBK = 64;           // K of a stage: 128 bytes of bf16
 constexpr int kMaxBN = 256;
-constexpr int kStages = 4;
-constexpr int kThreads = 256;     // warp 0 TMA, warp 1 MMA, warps 4-7 epilogue
-constexpr int kEpiWarp0 = 4;
+constexpr int kThreads = 384;     // warp 0 TMA, warp 1 MMA, warps 4-11 epilogue
+constexpr int kEpiWarp0 = 4, kEpiWarps = 8;
 constexpr int kABytes = kBM * kBK * 2;
-constexpr int kBBytes = kMaxBN * kBK * 2;
 constexpr int kBoxBytes = 64 * 128;          // an MN-major box: 64 K rows of 64 columns
 constexpr uint32_t kTmemCols = 2 * kMaxBN;   // two accumulators
 constexpr float kLog2e = 1.4426950408889634f;
+// From how many rows, and which width, CTAs work in pairs. V = 151552, graph us, single and
+// pairs: loss 512 x 2048 225, 214; 4096 x 1024 778, 741; 4096 x 512 400, 419 (the epilogues
+// of both wait for the slower); gradients 256 x 2048 460, 574 (tiles of 256 rows leave too
+// few); 512 x 2048 779, 716; 4096 x 512 1452, 1383; 4096 x 64 661, 718.
+constexpr int64_t kPairRows = 512, kPairLossWidth = 1024, kPairGradWidth = 512;
 
-enum Mode { kStats, kGrad, kDw, kDh };
+enum Mode { kStats, kGrad, kBack };
 
+// kCtas: CTAs that share a tile, 1 or 2 (a pair holds half of B each).
+template <int kCtas>
 struct Smem {
+  static constexpr int kStages = kCtas == 2 ? 6 : 4;  // 192 KB
+  static constexpr int kBBytes = kMaxBN / kCtas * kBK * 2;
   alignas(1024) uint8_t a[kStages][kABytes];
   alignas(1024) uint8_t b[kStages][kBBytes];
-  alignas(1024) uint8_t out[4][2][32 * 128];  // per epilogue warp, two buffers of 32 rows x 128 bytes
-  uint64_t full[kStages];   // stage loaded            (TMA -> MMA)
+  alignas(1024) uint8_t out[kEpiWarps][32 * 128];  // per epilogue warp, 32 rows x 128 bytes
+  uint64_t full[kStages];   // stage loaded            (TMA -> MMA; a pair's: in the leader)
   uint64_t empty[kStages];  // stage read by its MMAs  (MMA -> TMA)
   uint64_t acc_full[2];     // accumulator complete    (MMA -> epilogue)
-  uint64_t acc_empty[2];    // accumulator read out    (epilogue -> MMA)
+  uint64_t acc_empty[2];    // accumulator read out    (epilogue -> MMA; a pair's: in the leader)
   uint64_t done;            // every MMA completed     (teardown)
   uint32_t tmem_base;
   int abort;
 };
-constexpr size_t kSmemBytes = sizeof(Smem) + 1024;
-static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
+template <int kCtas>
+constexpr size_t smem_bytes() {
+  return sizeof(Smem<kCtas>) + 1024;
+}
+static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "shared memory of a CTA");
 
 // What the first launch leaves for the others.
 struct Plan {
@@ -76,18 +92,20 @@ struct Plan {
 struct Params {
   const Plan* plan;
   int V;
-  int kblocks;          // stats, grad: K steps (of d);  dh: of the piece
+  int kblocks;          // stats, grad: K steps (of d);  back: those of dh (of the piece)
   int bn;               // columns of a tile
-  int tiles;            // stats, grad: vocabulary tiles;  dw, dh: tiles of d
-  int parts;            // stats: parts of the vocabulary;  dw: tiles of the piece's rows
+  int tiles;            // stats, grad: vocabulary tiles;  back: tiles of d
+  int parts;            // stats: parts of the vocabulary;  back: dw's tiles of the piece's rows
   int v0;               // first vocabulary column of the piece
+  int n_pad;            // rows of a panel of g
   int a_rows;           // stats: rows of the hidden box
+  int want_dw, want_dh;
   int add;              // dh: add to what the pieces before left
-  int rows_out, cols_out;  // dw, dh: extents of what is written
+  int dw_rows, dw_cols, dh_cols;  // extents of what is written
   const int* target;    // of each scored row
   const float* lse2;    // lse log2(e)
   const float* dloss;
-  float2* part;         // stats: (maximum, sum) [part][row]
+  float2* part;         // stats: (maximum, sum) [half of the warps][part][row]
   float* x_target;      // stats: the target's logit
   int* err;
   uint64_t wait_ns;
@@ -113,25 +131,62 @@ __device__ __forceinline__ void tma_add_2d(const void* tmap, const void* src, in
                : "memory");
 }
 
-// One output tile and its K steps [k0, k1). m, n: its row and column tiles.
+// One output tile and its K steps [k0, k1). m, n: its row and column tiles; dw: of
+// d_weight (else, in back, of d_hidden).
 struct Tile {
   int m, n, k0, k1, split;
+  bool dw;
 };
 
-// The work of a launch: items, each a run of tiles [t0, t1) (one tile but for stats).
-template <int kMode>
-struct Work {
-  int items, row_blocks, k, splits;
+// What tiles cost, in K steps fed from L2 (of 64; 0.27 to 0.34 us). A step of dh waits for
+// HBM where few row blocks share the weight that it reads; its tile is written and read
+// as fp32 sums. dw's takes no less than writing it.
+__device__ __forceinline__ float dh_cost(int steps, int row_blocks) { return steps * fmaxf(1.f, 2.f / row_blocks) + 16.f; }
+__device__ __forceinline__ float dw_cost(int steps) { return max(steps, 4) + 1.f; }
 
-  __device__ Work(const Params& p) {
+// The work of a launch: items, each a run of tiles [t0, t1) (one tile but for stats).
+//
+// back: every worker takes tiles of dh, one round of all workers after another; those
+// without one in the last round turn to dw meanwhile, the others when they are done. The
+// rounds of each phase keep the workers on neighbouring tiles, which share their operands
+// in L2. (dw and dh in launches of their own leave workers without a tile in both last
+// rounds: 4096 x 65536 x 2048 dh 85 % of the SM cycles used.)
+template <int kMode, int kCtas>
+struct Work {
+  static constexpr int kRows = kBM * kCtas;  // rows of a tile
+  int items, row_blocks, k, splits;
+  int k_dw, dh, dw, left, meanwhile;  // back: tiles of each, dh's in its last round, dw's a worker meanwhile
+
+  __device__ Work(const Params& p, int workers) {
     const int n = p.plan->n;
-    row_blocks = (n + kBM - 1) / kBM;
+    row_blocks = (n + kRows - 1) / kRows;
     splits = p.plan->splits;
-    k = kMode == kDw ? (n + kBK - 1) / kBK : p.kblocks;
-    items = kMode == kStats  ? p.parts * row_blocks
-            : kMode == kGrad ? p.tiles * row_blocks
-            : kMode == kDw   ? p.parts * p.tiles
-                             : splits * row_blocks * p.tiles;
+    k = p.kblocks;
+    items = kMode == kStats ? p.parts * row_blocks : p.tiles * row_blocks;
+    if (kMode != kBack) return;
+    k_dw = (n + kBK - 1) / kBK;
+    dh = p.want_dh ? splits * row_blocks * p.tiles : 0;
+    dw = p.want_dw ? p.parts * p.tiles : 0;
+    left = dh % workers;
+    meanwhile = left ? static_cast<int>(dh_cost(k / splits, row_blocks) / dw_cost(k_dw)) : 0;
+  }
+  // The worker's j-th item, -1: none.
+  __device__ __forceinline__ int item(int worker, int workers, int j) const {
+    if (kMode != kBack) {
+      const int i = worker + j * workers;
+      return i < items ? i : -1;
+    }
+    const int own = dh / workers + (worker < left ? 1 : 0);
+    if (j < own) return j * workers + worker;
+    j -= own;
+    int t;
+    if (left && worker >= left && j < meanwhile) {
+      t = j * (workers - left) + worker - left;
+    } else {
+      if (left && worker >= left) j -= meanwhile;
+      t = meanwhile * (workers - left) + j * workers + worker;
+    }
+    return t < dw ? dh + t : -1;
   }
   __device__ __forceinline__ int first(const Params& p, int item) const {
     return kMode == kStats ? static_cast<int>(static_cast<long long>(p.tiles) * (item / row_blocks) / p.parts) : 0;
@@ -140,26 +195,32 @@ struct Work {
     return kMode == kStats ? static_cast<int>(static_cast<long long>(p.tiles) * (item / row_blocks + 1) / p.parts) : 1;
   }
   // Items that run at the same time share vocabulary tiles (stats, grad: the row block
-  // changes first) or the rows of g (dw, dh: the tile of d changes first).
+  // changes first) or the rows of g (back: the tile of d changes first).
   __device__ __forceinline__ Tile tile(const Params& p, int item, int t) const {
-    if (kMode == kStats) return {item % row_blocks, t, 0, k, 0};
-    if (kMode == kGrad) return {item % row_blocks, item / row_blocks, 0, k, 0};
-    if (kMode == kDw) return {item / p.tiles, item % p.tiles, 0, k, 0};
+    if (kMode == kStats) return {item % row_blocks, t, 0, k, 0, false};
+    if (kMode == kGrad) return {item % row_blocks, item / row_blocks, 0, k, 0, false};
+    if (item >= dh) return {(item - dh) / p.tiles, (item - dh) % p.tiles, 0, k_dw, 0, true};
     const int per = row_blocks * p.tiles, split = item / per, rest = item % per;
     return {rest / p.tiles, rest % p.tiles, static_cast<int>(static_cast<long long>(k) * split / splits),
-            static_cast<int>(static_cast<long long>(k) * (split + 1) / splits), split};
+            static_cast<int>(static_cast<long long>(k) * (split + 1) / splits), split, false};
   }
 };
 
-// ma, mb: the operands' maps; mo: the map written (none for stats).
-template <int kMode>
+// ma, mb: the operands' maps; mo: the map written (none for stats). back: those of dh, and
+// mda, mdb, mdo of dw.
+template <int kMode, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1)
     loss_product_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
-                        const __grid_constant__ CUtensorMap mo, const Params p) {
+                        const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mda,
+                        const __grid_constant__ CUtensorMap mdb, const __grid_constant__ CUtensorMap mdo, const Params p) {
+  using Sm = Smem<kCtas>;
+  constexpr int kStages = Sm::kStages, kBBytes = Sm::kBBytes, kRows = kBM * kCtas;
   extern __shared__ uint8_t smem_raw[];
-  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
+  const int rank = kCtas == 2 ? static_cast<int>(blockIdx.x & 1) : 0;  // in the pair
+  const int worker = static_cast<int>(blockIdx.x) / kCtas, workers = static_cast<int>(gridDim.x) / kCtas;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -168,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.acc_full[i], 1);
-      mbar_init(&sm.acc_empty[i], 128);
+      mbar_init(&sm.acc_empty[i], kEpiWarps * kCtas);
     }
     mbar_init(&sm.done, 1);
     sm.abort = 0;
@@ -176,17 +237,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_proxy_async_smem();
   }
   if (warp == 1) {
-    tmem_alloc(&sm.tmem_base, kTmemCols);
-    tmem_relinquish();
+    if (kCtas == 2) {
+      tmem_alloc_pair(&sm.tmem_base, kTmemCols);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(&sm.tmem_base, kTmemCols);
+      tmem_relinquish();
+    }
   }
   tc_fence_before();
-  __syncthreads();
+  if (kCtas == 2)
+    cg::this_cluster().sync();  // the other CTA's barriers and tensor memory are there too
+  else
+    __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   volatile int* abort = &sm.abort;
   wait_for_previous();
-  const Work<kMode> work(p);
-  const int boxes = p.bn / 64;  // MN-major boxes of B
+  const Work<kMode, kCtas> work(p, workers);
+  const int bn_own = p.bn / kCtas;  // this CTA's columns of B
+  const int boxes = bn_own / 64;    // its MN-major boxes
 
   if (warp == 0) {
     // ================================================================ TMA producer
@@ -194,13 +264,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       prefetch_tmap(&ma);
       prefetch_tmap(&mb);
     }
-    const uint32_t stage_bytes = (kMode == kStats ? p.a_rows * 128 : kABytes) + p.bn * 128;
+    const uint32_t stage_bytes = kCtas * ((kMode == kStats && kCtas == 1 ? p.a_rows * 128 : kABytes) + bn_own * 128);
     int fill = 0;
     bool ok = true;
-    for (int item = blockIdx.x; ok && item < work.items; item += gridDim.x) {
+    for (int j = 0, item; ok && (item = work.item(worker, workers, j)) >= 0; ++j) {
       const int t1 = work.last(p, item);
       for (int t = work.first(p, item); ok && t < t1; ++t) {
         const Tile tl = work.tile(p, item, t);
+        const int m0 = tl.m * kRows + rank * kBM, n0 = tl.n * p.bn + rank * bn_own;
         for (int kb = tl.k0; kb < tl.k1; ++kb, ++fill) {
           const int st = fill % kStages;
           if (fill >= kStages && !warp_wait(&sm.empty[st], ((fill / kStages) - 1) & 1, abort, p.err, p.wait_ns)) {
@@ -208,43 +279,60 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           if (lane == 0) {
-            mbar_arrive_expect_tx(&sm.full[st], stage_bytes);
+            uint64_t* bar = &sm.full[st];
+            const uint32_t pair_bar = kCtas == 2 ? smem_of_rank(bar, 0) : 0;  // the leader's
+            const auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1) {
+              if (kCtas == 2)
+                tma_load_2d_pair(dst, map, pair_bar, c0, c1);
+              else
+                tma_load_2d(dst, map, bar, c0, c1);
+            };
+            if (rank == 0) mbar_arrive_expect_tx(bar, stage_bytes);
             if (kMode == kStats || kMode == kGrad) {
-              tma_load_2d(sm.a[st], &ma, &sm.full[st], kb * kBK, tl.m * kBM);
-              tma_load_2d(sm.b[st], &mb, &sm.full[st], kb * kBK, p.v0 + tl.n * p.bn);
-            } else if (kMode == kDw) {
-              for (int j = 0; j < 2; ++j)
-                tma_load_2d(sm.a[st] + j * kBoxBytes, &ma, &sm.full[st], tl.m * kBM + 64 * j, kb * kBK);
-              for (int j = 0; j < boxes; ++j)
-                tma_load_2d(sm.b[st] + j * kBoxBytes, &mb, &sm.full[st], tl.n * p.bn + 64 * j, kb * kBK);
+              load(sm.a[st], &ma, kb * kBK, m0);
+              load(sm.b[st], &mb, kb * kBK, p.v0 + n0);
+            } else if (tl.dw) {
+              for (int i = 0; i < 2; ++i) load(sm.a[st] + i * kBoxBytes, &mda, 0, (m0 / 64 + i) * p.n_pad + kb * kBK);
+              for (int i = 0; i < boxes; ++i) load(sm.b[st] + i * kBoxBytes, &mdb, n0 + 64 * i, kb * kBK);
             } else {
-              tma_load_2d(sm.a[st], &ma, &sm.full[st], kb * kBK, tl.m * kBM);
-              for (int j = 0; j < boxes; ++j)
-                tma_load_2d(sm.b[st] + j * kBoxBytes, &mb, &sm.full[st], tl.n * p.bn + 64 * j, p.v0 + kb * kBK);
+              load(sm.a[st], &ma, 0, kb * p.n_pad + m0);
+              for (int i = 0; i < boxes; ++i) load(sm.b[st] + i * kBoxBytes, &mb, n0 + 64 * i, p.v0 + kb * kBK);
             }
           }
         }
       }
     }
-    // Teardown: every copy issued lands before the block exits.
-    if (lane == 0) {
+    // Teardown: every copy issued lands before the block exits (a pair's leader waits for
+    // both CTAs' copies, the other CTA for it).
+    if (lane == 0 && rank == 0) {
       for (int s = 0; s < kStages; ++s) {
         const int n_s = fill > s ? (fill - s + kStages - 1) / kStages : 0;
         if (n_s) mbar_drain(&sm.full[s], (n_s - 1) & 1);
       }
     }
+    if (kCtas == 2 && !ok) {
+      // Given up: copies that no barrier accounts for any more get a millisecond to land.
+      const uint64_t t0 = global_timer_ns();
+      while (global_timer_ns() - t0 < 1000000) {
+      }
+    }
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp == 1 && rank == 0) {
     // ================================================================ MMA issuer
-    constexpr bool a_mn = kMode == kDw, b_mn = kMode == kDw || kMode == kDh;
-    // A step of 16 in K: 32 bytes of each row (K-major), or 16 rows of 128 bytes (MN-major).
-    constexpr uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
-    const uint32_t idesc = idesc_bf16_f32(kBM, p.bn, a_mn, b_mn);
-    const uint64_t a_desc0 = sdesc_sw128(smem_u32(sm.a[0]), a_mn ? kBoxBytes : 16, 1024);
+    const auto commit = [](uint64_t* bar) {
+      if (kCtas == 2)
+        mma_commit_pair_elect(bar);
+      else
+        mma_commit_elect(bar);
+    };
+    // A step of 16 in K: 32 bytes of each row (K-major), or 16 rows of 128 bytes (MN-major:
+    // back's operands but for dh's A).
+    constexpr bool b_mn = kMode == kBack;
+    constexpr uint32_t b_step = b_mn ? 128 : 2;
     const uint64_t b_desc0 = sdesc_sw128(smem_u32(sm.b[0]), b_mn ? kBoxBytes : 16, 1024);
     int fill = 0, tile = 0;
     bool ok = true;
-    for (int item = blockIdx.x; ok && item < work.items; item += gridDim.x) {
+    for (int j = 0, item; ok && (item = work.item(worker, workers, j)) >= 0; ++j) {
       const int t1 = work.last(p, item);
       for (int t = work.first(p, item); ok && t < t1; ++t, ++tile) {
         const Tile tl = work.tile(p, item, t);
@@ -256,6 +344,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
         const uint32_t d_tmem = tmem + acc * kMaxBN;
+        const bool a_mn = kMode == kBack && tl.dw;
+        const uint32_t a_step = a_mn ? 128 : 2;
+        const uint32_t idesc = idesc_bf16_f32(kRows, p.bn, a_mn, b_mn);
+        const uint64_t a_desc0 = sdesc_sw128(smem_u32(sm.a[0]), a_mn ? kBoxBytes : 16, 1024);
         for (int kb = tl.k0; kb < tl.k1; ++kb, ++fill) {
           const int st = fill % kStages;
           if (!warp_wait(&sm.full[st], (fill / kStages) & 1, abort, p.err, p.wait_ns)) {
@@ -267,30 +359,47 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(st) * (kBBytes >> 4);
 #pragma unroll
           for (int kk = 0; kk < kBK / 16; ++kk)
-            mma_ss_elect(d_tmem, a_desc + kk * a_step, b_desc + kk * b_step, idesc, (kb > tl.k0 || kk > 0) ? 1u : 0u);
-          mma_commit_elect(&sm.empty[st]);
+            if (kCtas == 2)
+              mma_ss_pair_elect(d_tmem, a_desc + kk * a_step, b_desc + kk * b_step, idesc, (kb > tl.k0 || kk > 0) ? 1u : 0u);
+            else
+              mma_ss_elect(d_tmem, a_desc + kk * a_step, b_desc + kk * b_step, idesc, (kb > tl.k0 || kk > 0) ? 1u : 0u);
+          commit(&sm.empty[st]);
         }
         if (!ok) break;
-        mma_commit_elect(&sm.acc_full[acc]);
+        commit(&sm.acc_full[acc]);
       }
     }
-    mma_commit_elect(&sm.done);
+    commit(&sm.done);
     mbar_drain(&sm.done, 0);
     __syncwarp();
   } else if (warp >= kEpiWarp0) {
     // ================================================================ epilogue
-    const int qw = warp - kEpiWarp0;                 // TMEM lanes 32 qw .. 32 qw + 31
+    // Two warps for each 32 rows, which take the tile's groups of 64 columns in turn. (One
+    // warp: with d = 200 or 512 the epilogue is what a tile waits for.)
+    const int qw = warp & 3;                         // TMEM lanes 32 qw .. 32 qw + 31
+    const int half = (warp - kEpiWarp0) >> 2;
     const int t_row = qw * 32 + lane;                // row within the tile
     const uint32_t lane_base = static_cast<uint32_t>(qw * 32) << 16;
-    int tile = 0, chunk = 0;
+    uint8_t* buf = sm.out[warp - kEpiWarp0];
+    const auto release = [&](int acc) {  // every column of the accumulator has been read
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (kCtas == 2)
+          mbar_arrive_at(smem_of_rank(&sm.acc_empty[acc], 0));
+        else
+          mbar_arrive(&sm.acc_empty[acc]);
+      }
+    };
+    int tile = 0;
     bool ok = true;
-    for (int item = blockIdx.x; ok && item < work.items; item += gridDim.x) {
+    for (int j = 0, item; ok && (item = work.item(worker, workers, j)) >= 0; ++j) {
       const int t1 = work.last(p, item);
       float m = -INFINITY, s = 0.f;  // stats: over the item's tiles
       int target = -1;
       float lse2 = 0.f, dloss = 0.f;
       if (kMode == kStats || kMode == kGrad) {
-        const int row = (item % work.row_blocks) * kBM + t_row;
+        const int row = (item % work.row_blocks) * kRows + rank * kBM + t_row;
         target = p.target[row];
         if (kMode == kGrad) {
           lse2 = p.lse2[row];
@@ -306,17 +415,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
         const uint32_t base = tmem + lane_base + acc * kMaxBN;
-        const int row = tl.m * kBM + t_row;
+        const int row = tl.m * kRows + rank * kBM + t_row;
         float ts = 0.f;  // stats: this tile's terms, relative to m
+        const int chunks = p.bn / 32;
+        if (2 * half >= chunks) release(acc);
 #pragma unroll 1
-        for (int c = 0; c < p.bn / 32; ++c) {
+        for (int c = 2 * half; c < chunks; c += c & 1 ? 3 : 1) {
           uint32_t v[32];
           tmem_ld32(base + 32 * c, v);
           tmem_wait_ld();
-          if (c == p.bn / 32 - 1) {
-            tc_fence_before();
-            mbar_arrive(&sm.acc_empty[acc]);  // every column of the accumulator has been read
-          }
+          if ((c & 1) && c + 3 >= chunks) release(acc);
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
@@ -376,27 +484,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int e = 0; e < 32; ++e)
                   if (col0 + e >= p.V) x[e] = 0.f;
               }
+              // Rows behind the scored ones hold anything: their g is 0.
               const float2 d2 = make_float2(dloss, dloss);
 #pragma unroll
               for (int e = 0; e < 32; e += 2) {
                 const float2 y = fmul2(make_float2(x[e], x[e + 1]), d2);
-                x[e] = y.x;
-                x[e + 1] = y.y;
+                x[e] = target >= 0 ? y.x : 0.f;
+                x[e + 1] = target >= 0 ? y.y : 0.f;
               }
             }
-            if (kMode == kDw && work.k == 0) {  // no scored row: nothing was multiplied
+            if (kMode == kBack && tl.k1 == tl.k0) {  // no scored row: nothing was multiplied
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[e] = 0.f;
             }
             // 128 bytes of a row a buffer: 32 columns of fp32, 64 of bf16 (two chunks).
-            const bool opens = kMode == kDh || (c & 1) == 0, closes = kMode == kDh || (c & 1) == 1;
-            uint8_t* buf = sm.out[qw][chunk & 1];
+            const bool wide = kMode == kBack && !tl.dw;
+            const bool opens = wide || (c & 1) == 0, closes = wide || (c & 1) == 1;
             if (opens) {
-              if (lane == 0) bulk_wait_read<1>();  // the store before the last has left this buffer
+              if (lane == 0) bulk_wait_read<0>();  // the store before has left the buffer
               __syncwarp();
             }
             uint8_t* dst = buf + lane * 128;
-            if (kMode == kDh) {
+            if (wide) {
 #pragma unroll
               for (int e = 0; e < 8; ++e)
                 *reinterpret_cast<float4*>(dst + ((e ^ (lane & 7)) << 4)) =
@@ -412,24 +521,21 @@ __global__ void __launch_bounds__(kThreads, 1)
               fence_proxy_async_smem();
               __syncwarp();
               if (lane == 0) {
-                const int r0 = tl.m * kBM + qw * 32;
-                if (kMode == kGrad) tma_store_2d(&mo, buf, tl.n * p.bn + 32 * (c - 1), r0);
-                if (kMode == kDw) {
-                  const int col = tl.n * p.bn + 32 * (c - 1);
-                  if (p.v0 + r0 < p.rows_out && col < p.cols_out) tma_store_2d(&mo, buf, col, p.v0 + r0);
-                }
-                if (kMode == kDh) {
-                  const int y = tl.split * work.row_blocks * kBM + r0, col = tl.n * p.bn + 32 * c;
-                  if (col < p.cols_out) {
-                    if (!p.add)
-                      tma_store_2d(&mo, buf, col, y);
-                    else if (tl.k1 > tl.k0)
-                      tma_add_2d(&mo, buf, col, y);
-                  }
+                const int r0 = tl.m * kRows + rank * kBM + qw * 32;
+                const int col = tl.n * p.bn + 32 * (wide ? c : c - 1);
+                if (kMode == kGrad) {
+                  tma_store_2d(&mo, buf, 0, col / 64 * p.n_pad + r0);
+                } else if (tl.dw) {
+                  if (p.v0 + r0 < p.dw_rows && col < p.dw_cols) tma_store_2d(&mdo, buf, col, p.v0 + r0);
+                } else if (col < p.dh_cols) {
+                  const int y = tl.split * work.row_blocks * kRows + r0;
+                  if (!p.add)
+                    tma_store_2d(&mo, buf, col, y);
+                  else if (tl.k1 > tl.k0)
+                    tma_add_2d(&mo, buf, col, y);
                 }
                 bulk_commit();
               }
-              ++chunk;
             }
           }
         }
@@ -437,17 +543,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (kMode == kStats)
-        p.part[static_cast<int64_t>(item) * kBM + t_row] = make_float2(m, s);
+        p.part[(static_cast<int64_t>(item) + static_cast<int64_t>(half) * work.items) * kRows + rank * kBM + t_row] = make_float2(m, s);
     }
     if (kMode != kStats && lane == 0) bulk_wait_all();
     __syncwarp();
   }
 
   tc_fence_before();
-  __syncthreads();
+  if (kCtas == 2)
+    cg::this_cluster().sync();  // neither CTA's memory goes while the pair's copies and MMAs may use it
+  else
+    __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, kTmemCols);
+    if (kCtas == 2)
+      tmem_dealloc_pair(tmem, kTmemCols);
+    else
+      tmem_dealloc(tmem, kTmemCols);
   }
 }
 
@@ -468,24 +580,28 @@ struct GatherParams {
   uint4* to_hidden;     // [., d_pad]
   float* loss;          // loss only: 0 for rows that are not scored
   float* lse_out;
-  int tiles, kblocks, ctas, max_rows;  // gradients: what the K splits of dh depend on
+  int block_rows;       // rows of a tile
+  int tiles, kblocks, workers, max_rows, dw_tiles;  // gradients: what the K splits of dh depend on
 };
 
 constexpr int kGatherThreads = 256;
 
-// The K splits of dh that leave the busiest CTA the fewest steps: a tile also costs
-// about 16 steps (of 64, 128 x 256: 0.34 us) for writing and reading its fp32 sums. A
-// lane of a warp looks at two numbers of splits (one thread at all of them: 8 us).
+// The K splits of dh that end the launch first: no worker is done before its rounds of dh,
+// nor before its share of dh and dw. A lane of a warp looks at two numbers of splits (one
+// thread at all of them: 8 us).
 __device__ int choose_splits(const GatherParams& p, int n) {
-  const int lane = threadIdx.x & 31, blocks = (n + kBM - 1) / kBM;
-  unsigned best = 0xFFFFFFFFu;
+  const int lane = threadIdx.x & 31, blocks = (n + p.block_rows - 1) / p.block_rows;
+  const float c_dw = dw_cost((n + kBK - 1) / kBK);
+  float best = INFINITY;
   int splits = 1;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int s = lane + 32 * k + 1;
-    const bool fits = s == 1 || (s <= p.kblocks && blocks <= p.max_rows / kBM / s);
-    const unsigned rounds = (static_cast<unsigned>(blocks) * p.tiles * s + p.ctas - 1) / p.ctas;
-    const unsigned cost = fits ? rounds * ((p.kblocks + s - 1) / s + 16) : 0xFFFFFFFFu;
+    const bool fits = s == 1 || (s <= p.kblocks && blocks <= p.max_rows / p.block_rows / s);
+    const int dh = blocks * p.tiles * s, rounds = (dh + p.workers - 1) / p.workers;
+    const float c_dh = dh_cost((p.kblocks + s - 1) / s, max(blocks, 1));
+    const float share = (static_cast<float>(dh) * c_dh + static_cast<float>(p.dw_tiles) * c_dw) / static_cast<float>(p.workers);
+    const float cost = fits ? fmaxf(static_cast<float>(rounds) * c_dh, share) : INFINITY;
     if (cost < best) {
       best = cost;
       splits = s;
@@ -493,7 +609,7 @@ __device__ int choose_splits(const GatherParams& p, int n) {
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const unsigned c = __shfl_xor_sync(0xffffffffu, best, o);
+    const float c = __shfl_xor_sync(0xffffffffu, best, o);
     const int s = __shfl_xor_sync(0xffffffffu, splits, o);
     if (c < best || (c == best && s < splits)) {
       best = c;
@@ -516,7 +632,7 @@ __device__ int block_count(int v, int* sums) {
 }
 
 // Each CTA counts the scored rows before its own and copies its own behind them; the
-// last one knows their number and fills the last block of 128 rows with zeros.
+// last one knows their number and what has to be behind them.
 __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const GatherParams p) {
   __shared__ int sums[kGatherThreads / 32];
   __shared__ int source[kGatherThreads];
@@ -582,7 +698,7 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
     before += total;
   }
   if (blockIdx.x != gridDim.x - 1) return;
-  const int n = before, end = (n + kBM - 1) / kBM * kBM;
+  const int n = before, end = (n + p.block_rows - 1) / p.block_rows * p.block_rows;
   if (warp == 0) {
     const int splits = p.tiles ? choose_splits(p, n) : 1;
     if (lane == 0) {
@@ -594,7 +710,10 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
     p.to_target[r] = -1;
     if (p.to_lse2) p.to_lse2[r] = p.to_dloss[r] = 0.f;
   }
-  for (int64_t i = static_cast<int64_t>(n) * vecs + threadIdx.x; i < static_cast<int64_t>(end) * vecs; i += kGatherThreads)
+  // dw's last K step multiplies the hidden states behind the scored rows by 0.
+  const int64_t rows_end = (n + kBK - 1) / kBK * kBK;
+#pragma unroll 4
+  for (int64_t i = static_cast<int64_t>(n) * vecs + threadIdx.x; i < rows_end * vecs; i += kGatherThreads)
     p.to_hidden[i] = make_uint4(0, 0, 0, 0);
 }
 
@@ -603,16 +722,16 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
 // Joins the parts of each scored row, a warp a row.
 constexpr int kCombineThreads = 256;
 __global__ void __launch_bounds__(kCombineThreads)
-    loss_combine_kernel(const Plan* plan, const int* place, const float2* part, const float* x_target, int N, int parts,
-                        float* loss, float* lse) {
+    loss_combine_kernel(const Plan* plan, const int* place, const float2* part, const float* x_target, int N, int block_rows,
+                        int parts, float* loss, float* lse) {
   wait_for_previous();
   const int64_t r = (static_cast<int64_t>(blockIdx.x) * kCombineThreads + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
   if (r >= N) return;
   const int c = place[r];
   if (c < 0) return;  // written by the first launch
-  const int64_t step = static_cast<int64_t>((plan->n + kBM - 1) / kBM) * kBM;
-  constexpr int kPer = (kLossMaxParts + 31) / 32;
+  const int64_t step = static_cast<int64_t>((plan->n + block_rows - 1) / block_rows) * block_rows;
+  constexpr int kPer = (2 * kLossMaxParts + 31) / 32;
   float2 v[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) v[j] = lane + 32 * j < parts ? part[(lane + 32 * j) * step + c] : make_float2(-INFINITY, 0.f);
@@ -637,11 +756,11 @@ __global__ void __launch_bounds__(kCombineThreads)
 // thread, eight splits' loads in flight.
 constexpr int kFinishThreads = 128;
 __global__ void __launch_bounds__(kFinishThreads)
-    loss_dhidden_kernel(const Plan* plan, const int* place, const float* part, int N, int d, int d_pad, __nv_bfloat16* out,
-                        int64_t s_out, int aligned) {
+    loss_dhidden_kernel(const Plan* plan, const int* place, const float* part, int N, int block_rows, int d, int d_pad,
+                        __nv_bfloat16* out, int64_t s_out, int aligned) {
   wait_for_previous();
   const int vecs = d / 4, splits = plan->splits;
-  const int64_t step = static_cast<int64_t>((plan->n + kBM - 1) / kBM) * kBM * d_pad;
+  const int64_t step = static_cast<int64_t>((plan->n + block_rows - 1) / block_rows) * block_rows * d_pad;
   const int64_t total = static_cast<int64_t>(N) * vecs;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x; i < total;
        i += static_cast<int64_t>(gridDim.x) * kFinishThreads) {
@@ -682,15 +801,15 @@ int sm_count() {
   return sms;
 }
 
-// Columns of a tile: 256, or 128 or 64 where 256 leave SMs without a tile or much of the
-// last tile empty (narrow tiles read their other operand more often: a column counts
-// 1.12 and 1.36 times, as in the projection's own choice). With one CTA: by the last
-// tile alone (dw has tiles enough, dh is split).
-int choose_bn(int64_t cols, int64_t row_tiles, int ctas) {
+// Columns of a tile: 256, or 128 or 64 (single CTAs) where 256 leave SMs without a tile or
+// much of the last tile empty (narrow tiles read their other operand more often: a column
+// counts 1.12 and 1.36 times, as in the projection's own choice). With one worker: by the
+// last tile alone (dw has tiles enough, dh is split).
+int choose_bn(int64_t cols, int64_t row_tiles, int workers, int ctas) {
   int best = 256;
   double best_cost = 1e300;
-  for (int bn = 256; bn >= 64; bn /= 2) {
-    const int64_t tiles = (cols + bn - 1) / bn * row_tiles, rounds = (tiles + ctas - 1) / ctas;
+  for (int bn = 256; bn >= 64 * ctas; bn /= 2) {
+    const int64_t tiles = (cols + bn - 1) / bn * row_tiles, rounds = (tiles + workers - 1) / workers;
     const double cost = static_cast<double>(rounds) * (bn / 256.0 * 0.88 + 0.12);
     if (cost < best_cost - 1e-9) {
       best_cost = cost;
@@ -700,16 +819,43 @@ int choose_bn(int64_t cols, int64_t row_tiles, int ctas) {
   return best;
 }
 
-template <int kMode>
-int launch_product(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mo, const Params& p, int64_t items, int sms,
-                   cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(loss_product_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(kSmemBytes));
-  const int64_t grid = items < sms ? items : sms;
+// The maps of a launch: operands and result, and back's of dw.
+struct Maps {
+  CUtensorMap a, b, out, dw_a, dw_b, dw_out;
+};
+
+template <int kMode, int kCtas>
+int launch_product(const Maps& m, const Params& p, int64_t items, int workers, cudaStream_t stream) {
+  const auto kernel = loss_product_kernel<kMode, kCtas>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<kCtas>()));
+  const int64_t run = items < workers ? items : workers;
   if (e == cudaSuccess)
-    e = launch_overlapped(loss_product_kernel<kMode>, dim3(static_cast<unsigned>(grid)), kThreads, kSmemBytes, stream, 1, true, ma,
-                          mb, mo, p);
+    e = launch_overlapped(kernel, dim3(static_cast<unsigned>(run * kCtas)), kThreads, smem_bytes<kCtas>(), stream, kCtas, true, m.a,
+                          m.b, m.out, m.dw_a, m.dw_b, m.dw_out, p);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "projection loss launch: %s", cudaGetErrorString(e));
+}
+
+template <int kMode>
+int launch_product(int ctas, const Maps& m, const Params& p, int64_t items, int workers, cudaStream_t stream) {
+  return ctas == 2 ? launch_product<kMode, 2>(m, p, items, workers, stream) : launch_product<kMode, 1>(m, p, items, workers, stream);
+}
+
+// CTAs that share a tile, and how many such groups run at once.
+struct Team {
+  int ctas, workers;
+};
+
+Team team_for(int64_t N, int64_t d, int64_t least_d) {
+  const int sms = sm_count();
+  if (N >= kPairRows && d >= least_d) {
+    const auto kernel = loss_product_kernel<kBack, 2>;  // the same shared memory in every mode
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<2>())) == cudaSuccess) {
+      const int pairs = active_clusters(reinterpret_cast<const void*>(kernel), 2, kThreads, smem_bytes<2>());
+      if (pairs > 0) return {2, pairs < sms / 2 ? pairs : sms / 2};
+    }
+    cudaGetLastError();
+  }
+  return {1, sms};
 }
 
 // Places of the workspace, from its start.
@@ -727,7 +873,7 @@ size_t take(size_t* at, size_t bytes) {
 
 Layout layout_of(int64_t N, int64_t d, bool grad) {
   Layout l = {};
-  l.n_pad = (N + kBM - 1) / kBM * kBM;
+  l.n_pad = (N + 2 * kBM - 1) / (2 * kBM) * (2 * kBM);
   l.d_pad = (d + kBK - 1) / kBK * kBK;
   size_t at = 0;
   l.plan = take(&at, sizeof(Plan));
@@ -736,12 +882,12 @@ Layout layout_of(int64_t N, int64_t d, bool grad) {
   l.hidden = take(&at, l.n_pad * l.d_pad * 2);
   if (!grad) {
     l.x_target = take(&at, l.n_pad * 4);
-    l.part = take(&at, static_cast<size_t>(kLossMaxParts) * l.n_pad * 8);
+    l.part = take(&at, static_cast<size_t>(2 * kLossMaxParts) * l.n_pad * 8);
   } else {
     l.lse2 = take(&at, l.n_pad * 4);
     l.dloss = take(&at, l.n_pad * 4);
     // Room for splits of dh: up to 32 of them, 192 MB, and one in any case.
-    const int64_t most = (int64_t{192} << 20) / (l.d_pad * 4) / kBM * kBM;
+    const int64_t most = (int64_t{192} << 20) / (l.d_pad * 4) / (2 * kBM) * (2 * kBM);
     int64_t rows = 32 * l.n_pad < most ? 32 * l.n_pad : most;
     if (rows < l.n_pad) rows = l.n_pad;
     l.sums_rows = static_cast<size_t>(rows);
@@ -800,100 +946,108 @@ size_t loss_grad_workspace_bytes(int64_t N, int64_t V, int64_t d, int64_t piece)
 
 int launch_loss(const LossArgs& a, cudaStream_t stream) {
   const Layout l = layout_of(a.N, a.d, false);
-  const int sms = sm_count();
+  const Team team = team_for(a.N, a.d, kPairLossWidth);
+  const int block_rows = kBM * team.ctas;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   GatherParams g = {};
+  g.block_rows = block_rows;
   g.loss = a.loss;
   g.lse_out = a.lse_out;
   int st;
   if ((st = launch_gather(a, l, g, stream)) != DLM_OK) return st;
   Params p = common_params(a, l);
-  const int64_t row_blocks = l.n_pad / kBM;
+  const int64_t row_blocks = (a.N + block_rows - 1) / block_rows;
   p.kblocks = static_cast<int>(l.d_pad / kBK);
-  p.bn = choose_bn(a.V, row_blocks, sms);
+  p.bn = choose_bn(a.V, row_blocks, team.workers, team.ctas);
   p.tiles = static_cast<int>((a.V + p.bn - 1) / p.bn);
   p.parts = p.tiles < kLossMaxParts ? p.tiles : kLossMaxParts;
-  p.a_rows = a.N < kBM ? static_cast<int>((a.N + 7) / 8 * 8) : kBM;
+  p.a_rows = team.ctas == 1 && a.N < kBM ? static_cast<int>((a.N + 7) / 8 * 8) : kBM;
   p.part = reinterpret_cast<float2*>(ws + l.part);
   p.x_target = reinterpret_cast<float*>(ws + l.x_target);
-  CUtensorMap mh, mw;
-  if ((st = make_matrix_map(&mh, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, p.a_rows)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&mw, a.weight, true, a.V, a.d, a.s_weight, p.bn)) != DLM_OK) return st;
-  if ((st = launch_product<kStats>(mh, mw, mw, p, p.parts * row_blocks, sms, stream)) != DLM_OK) return st;
+  Maps m = {};
+  if ((st = make_matrix_map(&m.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, p.a_rows)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&m.b, a.weight, true, a.V, a.d, a.s_weight, p.bn / team.ctas)) != DLM_OK) return st;
+  if ((st = launch_product<kStats>(team.ctas, m, p, p.parts * row_blocks, team.workers, stream)) != DLM_OK) return st;
   const cudaError_t e = launch_overlapped(
       loss_combine_kernel, dim3(static_cast<unsigned>((a.N * 32 + kCombineThreads - 1) / kCombineThreads)), kCombineThreads, 0, stream,
       1, true, p.plan, reinterpret_cast<const int*>(ws + l.place), static_cast<const float2*>(p.part),
-      static_cast<const float*>(p.x_target), static_cast<int>(a.N), p.parts, a.loss, a.lse_out);
+      static_cast<const float*>(p.x_target), static_cast<int>(a.N), block_rows, 2 * p.parts, a.loss, a.lse_out);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "loss combine launch: %s", cudaGetErrorString(e));
 }
 
 int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   const Layout l = layout_of(a.N, a.d, true);
-  const int sms = sm_count();
+  const Team team = team_for(a.N, a.d, kPairGradWidth);
+  const int block_rows = kBM * team.ctas;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   const int64_t all = (a.V + 255) / 256 * 256;
   int64_t cols = static_cast<int64_t>((a.workspace_bytes - l.g) / (static_cast<size_t>(l.n_pad) * 2)) / 256 * 256;
+  // g lies in panels of 64 columns, whose rows follow each other: a box of any operand is
+  // one run of memory. Their number times n_pad is a coordinate.
+  const int64_t most_cols = int64_t{0x7FFFFF00} / l.n_pad * 64 / 256 * 256;
+  if (cols > most_cols) cols = most_cols;
   if (cols > all) cols = all;
-  const int64_t row_blocks = l.n_pad / kBM;
-  const int bn_d = choose_bn(a.d, 1, 1);
+  const int64_t row_blocks = (a.N + block_rows - 1) / block_rows, first = cols < a.V ? cols : a.V;
+  const int bn_d = choose_bn(a.d, 1, 1, team.ctas);
+  const int bn_v = choose_bn(first, row_blocks, team.workers, team.ctas);
+  const int d_tiles = static_cast<int>((a.d + bn_d - 1) / bn_d);
 
   GatherParams g = {};
+  g.block_rows = block_rows;
   g.lse = a.lse;
   g.dloss = a.dloss;
   g.to_lse2 = reinterpret_cast<float*>(ws + l.lse2);
   g.to_dloss = reinterpret_cast<float*>(ws + l.dloss);
-  g.tiles = static_cast<int>((a.d + bn_d - 1) / bn_d);
-  g.kblocks = static_cast<int>(((cols < a.V ? cols : a.V) + kBK - 1) / kBK);
-  g.ctas = sms;
+  g.tiles = d_tiles;
+  g.kblocks = static_cast<int>((first + kBK - 1) / kBK);
+  g.dw_tiles = a.d_weight ? static_cast<int>((first + block_rows - 1) / block_rows) * d_tiles : 0;
+  g.workers = team.workers;
   g.max_rows = l.sums_rows > 0x7FFFFFFF ? 0x7FFFFFFF : static_cast<int>(l.sums_rows);
   int st;
   if ((st = launch_gather(a, l, g, stream)) != DLM_OK) return st;
 
-  CUtensorMap h_k, h_mn, w_k, w_mn, g_k, g_mn, g_out, dw_out, dh_out;
-  const Params base = common_params(a, l);
-  const int bn_v = choose_bn(a.V < cols ? a.V : cols, row_blocks, sms);
-  if ((st = make_matrix_map(&h_k, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, kBM)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&h_mn, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, 64)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&w_k, a.weight, true, a.V, a.d, a.s_weight, bn_v)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&w_mn, a.weight, true, a.V, a.d, a.s_weight, 64)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&g_k, ws + l.g, true, l.n_pad, cols, cols, kBM)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&g_mn, ws + l.g, true, l.n_pad, cols, cols, 64)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&g_out, ws + l.g, true, l.n_pad, cols, cols, 32)) != DLM_OK) return st;
-  if (a.d_weight && (st = make_matrix_map(&dw_out, a.d_weight, true, a.V, a.d, a.s_dweight, 32)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&dh_out, ws + l.sums, false, static_cast<int64_t>(l.sums_rows), l.d_pad, l.d_pad, 32)) != DLM_OK) return st;
+  Maps grad = {}, back = {};
+  const int64_t panel_rows = l.n_pad * (cols / 64);
+  if ((st = make_matrix_map(&grad.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, kBM)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&grad.b, a.weight, true, a.V, a.d, a.s_weight, bn_v / team.ctas)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&grad.out, ws + l.g, true, panel_rows, 64, 64, 32)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&back.a, ws + l.g, true, panel_rows, 64, 64, kBM)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&back.b, a.weight, true, a.V, a.d, a.s_weight, 64)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&back.out, ws + l.sums, false, static_cast<int64_t>(l.sums_rows), l.d_pad, l.d_pad, 32)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&back.dw_a, ws + l.g, true, panel_rows, 64, 64, 64)) != DLM_OK) return st;
+  if ((st = make_matrix_map(&back.dw_b, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, 64)) != DLM_OK) return st;
+  if (a.d_weight && (st = make_matrix_map(&back.dw_out, a.d_weight, true, a.V, a.d, a.s_dweight, 32)) != DLM_OK) return st;
 
+  Params p = common_params(a, l);
+  p.n_pad = static_cast<int>(l.n_pad);
+  p.lse2 = g.to_lse2;
+  p.dloss = g.to_dloss;
+  p.want_dw = a.d_weight != nullptr;
+  p.want_dh = a.d_hidden != nullptr;
+  p.dw_rows = p.V;
+  p.dw_cols = static_cast<int>(a.d);
+  p.dh_cols = static_cast<int>(l.d_pad);
   for (int64_t v0 = 0; v0 < a.V; v0 += cols) {
     const int64_t vc = a.V - v0 < cols ? a.V - v0 : cols;
-    Params p = base;
     p.v0 = static_cast<int>(v0);
     p.kblocks = static_cast<int>(l.d_pad / kBK);
     p.bn = bn_v;
     p.tiles = static_cast<int>((vc + bn_v - 1) / bn_v);
-    p.lse2 = g.to_lse2;
-    p.dloss = g.to_dloss;
-    if ((st = launch_product<kGrad>(h_k, w_k, g_out, p, p.tiles * row_blocks, sms, stream)) != DLM_OK) return st;
+    if ((st = launch_product<kGrad>(team.ctas, grad, p, p.tiles * row_blocks, team.workers, stream)) != DLM_OK) return st;
     p.bn = bn_d;
-    p.tiles = g.tiles;
-    if (a.d_weight) {
-      p.rows_out = p.V;
-      p.cols_out = static_cast<int>(a.d);
-      p.parts = static_cast<int>((vc + kBM - 1) / kBM);
-      if ((st = launch_product<kDw>(g_mn, h_mn, dw_out, p, static_cast<int64_t>(p.parts) * p.tiles, sms, stream)) != DLM_OK) return st;
-    }
-    if (a.d_hidden) {
-      p.kblocks = static_cast<int>((vc + kBK - 1) / kBK);
-      p.add = v0 > 0;
-      p.cols_out = static_cast<int>(l.d_pad);
-      if ((st = launch_product<kDh>(g_k, w_mn, dh_out, p, sms, sms, stream)) != DLM_OK) return st;
-    }
+    p.tiles = d_tiles;
+    p.parts = static_cast<int>((vc + block_rows - 1) / block_rows);
+    p.kblocks = static_cast<int>((vc + kBK - 1) / kBK);
+    p.add = v0 > 0;
+    if ((st = launch_product<kBack>(team.ctas, back, p, team.workers, team.workers, stream)) != DLM_OK) return st;
   }
   if (!a.d_hidden) return DLM_OK;
   const int64_t vecs = a.N * (a.d / 4);
-  const int64_t want = (vecs + kFinishThreads - 1) / kFinishThreads, most = static_cast<int64_t>(sms) * 16;
+  const int64_t want = (vecs + kFinishThreads - 1) / kFinishThreads, most = static_cast<int64_t>(sm_count()) * 16;
   const bool aligned = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 7) == 0;
   const cudaError_t e = launch_overlapped(
-      loss_dhidden_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), kFinishThreads, 0, stream, 1, true, base.plan,
-      reinterpret_cast<const int*>(ws + l.place), reinterpret_cast<const float*>(ws + l.sums), static_cast<int>(a.N),
+      loss_dhidden_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), kFinishThreads, 0, stream, 1, true, p.plan,
+      reinterpret_cast<const int*>(ws + l.place), reinterpret_cast<const float*>(ws + l.sums), static_cast<int>(a.N), block_rows,
       static_cast<int>(a.d), static_cast<int>(l.d_pad), static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden, aligned ? 1 : 0);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "hidden gradient launch: %s", cudaGetErrorString(e));
 }

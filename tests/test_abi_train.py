@@ -171,7 +171,7 @@ def test_loss_workspace_sizes():
     assert B.dlm_lmhead_loss_workspace_bytes(0, 64) == B.dlm_lmhead_loss_workspace_bytes(5, 0) == 0
     size = B.dlm_lmhead_loss_grad_workspace_bytes
     assert size(0, 10, 64) == size(5, 0, 64) == size(5, 10, 64, -1) == 0
-    assert size(128, 10 ** 5, 64, 512) - size(128, 10 ** 5, 64, 256) == 128 * 256 * 2
+    assert size(256, 10 ** 5, 64, 512) - size(256, 10 ** 5, 64, 256) == 256 * 256 * 2
     assert size(128, 10 ** 5, 64, 257) == size(128, 10 ** 5, 64, 512)
     assert size(128, 300, 64, 10 ** 6) == size(128, 300, 64, 300)
     assert size(16384, 151552, 2048) < 3 * 2 ** 30
