@@ -155,7 +155,8 @@ template <int kMode, int kCtas>
 struct Work {
   static constexpr int kRows = kBM * kCtas;  // rows of a tile
   int items, row_blocks, k, splits;
-  int k_dw, dh, dw, left, meanwhile;  // back: tiles of each, dh's in its last round, dw's a worker meanwhile
+  int k_dw, k_tail;               // back: dw's K steps, and the 16s of the last
+  int dh, dw, left, meanwhile;    // back: tiles of each, dh's in its last round, dw's a worker meanwhile
 
   __device__ Work(const Params& p, int workers) {
     const int n = p.plan->n;
@@ -165,6 +166,7 @@ struct Work {
     items = kMode == kStats ? p.parts * row_blocks : p.tiles * row_blocks;
     if (kMode != kBack) return;
     k_dw = (n + kBK - 1) / kBK;
+    k_tail = (n - (k_dw - 1) * kBK + 15) / 16;
     dh = p.want_dh ? splits * row_blocks * p.tiles : 0;
     dw = p.want_dw ? p.parts * p.tiles : 0;
     left = dh % workers;
@@ -222,6 +224,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int rank = kCtas == 2 ? static_cast<int>(blockIdx.x & 1) : 0;  // in the pair
   const int worker = static_cast<int>(blockIdx.x) / kCtas, workers = static_cast<int>(gridDim.x) / kCtas;
 
+  if (threadIdx.x == 32 * kEpiWarp0) {  // parameters, not memory that another kernel writes
+    prefetch_tmap(&ma);
+    prefetch_tmap(&mb);
+    if (kMode != kStats) prefetch_tmap(&mo);
+    if (kMode == kBack) {
+      prefetch_tmap(&mda);
+      prefetch_tmap(&mdb);
+      prefetch_tmap(&mdo);
+    }
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sm.full[s], 1);
@@ -260,10 +272,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     // ================================================================ TMA producer
-    if (lane == 0) {
-      prefetch_tmap(&ma);
-      prefetch_tmap(&mb);
-    }
     const uint32_t stage_bytes = kCtas * ((kMode == kStats && kCtas == 1 ? p.a_rows * 128 : kABytes) + bn_own * 128);
     int fill = 0;
     bool ok = true;
@@ -357,12 +365,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_after();
           const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(st) * (kABytes >> 4);
           const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(st) * (kBBytes >> 4);
+          // Of dw's last step only the scored rows' 16s: past those g is 0, the hidden states are
+          // not.
+          const int kks = kMode == kBack && tl.dw && kb == tl.k1 - 1 ? work.k_tail : kBK / 16;
 #pragma unroll
-          for (int kk = 0; kk < kBK / 16; ++kk)
+          for (int kk = 0; kk < kBK / 16; ++kk) {
+            if (kMode == kBack && kk >= kks) break;
             if (kCtas == 2)
               mma_ss_pair_elect(d_tmem, a_desc + kk * a_step, b_desc + kk * b_step, idesc, (kb > tl.k0 || kk > 0) ? 1u : 0u);
             else
               mma_ss_elect(d_tmem, a_desc + kk * a_step, b_desc + kk * b_step, idesc, (kb > tl.k0 || kk > 0) ? 1u : 0u);
+          }
           commit(&sm.empty[st]);
         }
         if (!ok) break;
@@ -677,23 +690,29 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
       }
     }
     __syncthreads();
-    for (int k = warp; k < total; k += kGatherThreads / 32) {
-      const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.hidden) + (base + source[k]) * p.s_hidden;
-      uint4* dst = p.to_hidden + static_cast<int64_t>(before + k) * vecs;
-#pragma unroll 4
-      for (int i = lane; i < vecs; i += 32) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (i < full) {
-          if (aligned) {
-            v = reinterpret_cast<const uint4*>(src)[i];
-          } else {
-            const unsigned short* e = reinterpret_cast<const unsigned short*>(src) + 8 * i;
-            v = make_uint4(e[0] | static_cast<uint32_t>(e[1]) << 16, e[2] | static_cast<uint32_t>(e[3]) << 16,
-                           e[4] | static_cast<uint32_t>(e[5]) << 16, e[6] | static_cast<uint32_t>(e[7]) << 16);
-          }
+    constexpr int kLoads = 4;  // of 16 bytes, in flight
+    const int64_t words = static_cast<int64_t>(total) * vecs;
+    for (int64_t i0 = threadIdx.x; i0 < words; i0 += kGatherThreads * kLoads) {
+      uint4 v[kLoads];
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) {
+        const int64_t i = i0 + k * kGatherThreads;
+        v[k] = make_uint4(0, 0, 0, 0);
+        if (i >= words) continue;
+        const int row = static_cast<int>(i / vecs), col = static_cast<int>(i - static_cast<int64_t>(row) * vecs);
+        if (col >= full) continue;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.hidden) + (base + source[row]) * p.s_hidden + 8 * col;
+        if (aligned) {
+          v[k] = *reinterpret_cast<const uint4*>(src);
+        } else {
+          const unsigned short* e = reinterpret_cast<const unsigned short*>(src);
+          v[k] = make_uint4(e[0] | static_cast<uint32_t>(e[1]) << 16, e[2] | static_cast<uint32_t>(e[3]) << 16,
+                            e[4] | static_cast<uint32_t>(e[5]) << 16, e[6] | static_cast<uint32_t>(e[7]) << 16);
         }
-        dst[i] = v;
       }
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k)
+        if (i0 + k * kGatherThreads < words) p.to_hidden[static_cast<int64_t>(before) * vecs + i0 + k * kGatherThreads] = v[k];
     }
     before += total;
   }
@@ -710,8 +729,9 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
     p.to_target[r] = -1;
     if (p.to_lse2) p.to_lse2[r] = p.to_dloss[r] = 0.f;
   }
-  // dw's last K step multiplies the hidden states behind the scored rows by 0.
-  const int64_t rows_end = (n + kBK - 1) / kBK * kBK;
+  if (!p.to_lse2) return;
+  // dw's last 16 rows multiply the hidden states behind the scored ones by 0.
+  const int64_t rows_end = (n + 15) / 16 * 16;
 #pragma unroll 4
   for (int64_t i = static_cast<int64_t>(n) * vecs + threadIdx.x; i < rows_end * vecs; i += kGatherThreads)
     p.to_hidden[i] = make_uint4(0, 0, 0, 0);
@@ -910,9 +930,9 @@ int launch_gather(const LossArgs& a, const Layout& l, GatherParams g, cudaStream
   g.place = reinterpret_cast<int*>(ws + l.place);
   g.to_target = reinterpret_cast<int*>(ws + l.target);
   g.to_hidden = reinterpret_cast<uint4*>(ws + l.hidden);
-  // 16 rows a CTA, more where every CTA would otherwise count very many rows before its own.
-  int64_t rows = 16;
-  while (rows < kGatherThreads && a.N > rows * 2048) rows *= 2;
+  // As many CTAs as run at once, but 256 rows each at most: every CTA counts the rows before its own.
+  int64_t rows = 1;
+  while (rows < kGatherThreads && a.N > rows * 1024) rows *= 2;
   g.rows_per_cta = static_cast<int>(rows);
   const cudaError_t e = launch_overlapped(loss_gather_kernel, dim3(static_cast<unsigned>((a.N + rows - 1) / rows)), kGatherThreads, 0,
                                           stream, 1, true, g);
