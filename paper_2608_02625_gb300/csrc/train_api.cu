@@ -280,15 +280,14 @@ int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t 
   if ((st = check_workspace(workspace, workspace_bytes, clip_grad_norm_workspace_bytes(), 8, nullptr, 0))) return st;
   struct Span {
     uintptr_t lo, hi;
-    int tensor;   // index of its gradient; -1: the norm, -2: the workspace
-    bool written;
   };
   // Nothing thrown leaves a C entry point: the only throwing calls are these vectors'.
   try {
     std::vector<GradTensor> list;
-    std::vector<Span> spans;
+    std::vector<Span> read, written;  // by address, once checked
     list.reserve(count);
-    spans.reserve(2 * static_cast<size_t>(count) + 2);
+    read.reserve(count);
+    written.reserve(static_cast<size_t>(count) + 2);
     for (int i = 0; i < count; ++i) {
       const dlm_tensor* g = grads + i;
       const dlm_tensor* o = outs ? outs + i : g;
@@ -304,32 +303,30 @@ int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t 
       const int64_t size = numel(g);
       if (size == 0) continue;
       list.push_back({g->data, o->data, size, g->dtype == DLM_BF16});
-      Span s = {0, 0, i, false};
-      byte_span(g, &s.lo, &s.hi);
+      const uintptr_t bytes = static_cast<uintptr_t>(size) * elem_size(g->dtype), at = reinterpret_cast<uintptr_t>(g->data);
       const bool in_place = outs && o->data == g->data;
-      s.written = in_place;
-      spans.push_back(s);
-      if (outs && !in_place) {
-        byte_span(o, &s.lo, &s.hi);
-        s.written = true;
-        spans.push_back(s);
+      if (!in_place) read.push_back({at, at + bytes});
+      if (outs) {
+        const uintptr_t to = reinterpret_cast<uintptr_t>(o->data);
+        written.push_back({to, to + bytes});
       }
     }
-    Span s = {0, 0, -1, true};
-    byte_span(norm, &s.lo, &s.hi);
-    spans.push_back(s);
-    s.tensor = -2;
-    s.lo = reinterpret_cast<uintptr_t>(workspace);
-    s.hi = s.lo + clip_grad_norm_workspace_bytes();
-    spans.push_back(s);
-    // A written range may overlap no other: each range against the furthest end so far.
-    std::sort(spans.begin(), spans.end(), [](const Span& p, const Span& q) { return p.lo < q.lo; });
-    uintptr_t end = 0, written_end = 0;
-    for (const Span& p : spans) {
-      if (p.lo < (p.written ? end : written_end))
+    const uintptr_t norm_at = reinterpret_cast<uintptr_t>(norm->data), ws_at = reinterpret_cast<uintptr_t>(workspace);
+    written.push_back({norm_at, norm_at + sizeof(float)});
+    written.push_back({ws_at, ws_at + clip_grad_norm_workspace_bytes()});
+    // A written range may overlap no other: both lists walked together in the order of their
+    // addresses (which tensors allocated one after another often have already).
+    const auto before = [](const Span& p, const Span& q) { return p.lo < q.lo; };
+    for (std::vector<Span>* v : {&read, &written})
+      if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
+    uintptr_t end = 0, written_end = 0;  // the furthest end so far, of any and of a written range
+    for (size_t i = 0, j = 0; i < read.size() || j < written.size();) {
+      const bool write = i == read.size() || (j < written.size() && written[j].lo < read[i].lo);
+      const Span& p = write ? written[j++] : read[i++];
+      if (p.lo < (write ? end : written_end))
         return fail(DLM_ERR_ARG, "an output overlaps a gradient, another output, norm or the workspace");
       end = std::max(end, p.hi);
-      if (p.written) written_end = std::max(written_end, p.hi);
+      if (write) written_end = std::max(written_end, p.hi);
     }
     GradArgs a = {};
     a.grads = list.data();
