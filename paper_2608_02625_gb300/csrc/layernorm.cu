@@ -24,7 +24,6 @@
 #include <cuda_bf16.h>
 
 #include <cstdint>
-#include <type_traits>
 
 #include "dlm_common.cuh"
 #include "dlm_internal.h"
@@ -95,55 +94,65 @@ struct NormParams {
   float* part;      // gradient: [CTAs][2][d]; null where neither dw nor db is wanted
   int64_t N, s_x, s_dy, s_out;
   int d, G, w_bf16;
+  int ring;         // bytes of the ring, and of what else lies there
   float eps;
 };
 
-// A ring of a thread's own vectors of the rows to come, in shared memory: fetched with
-// cp.async and read back by the thread that fetched them, so no barrier is needed. A
-// vector of two bytes, which cp.async does not copy, comes with the aligned four bytes
-// around it.
-template <typename P>
-struct Slot {
-  static constexpr bool kHalf = sizeof(P) == 2;
-  using Type = typename std::conditional<kHalf, uint32_t, P>::type;
-  static __device__ __forceinline__ void fetch(Type* slot, const void* src) {
-    if constexpr (sizeof(Type) == 16)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot)), "l"(src) : "memory");
-    else
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(slot)),
-                   "l"(reinterpret_cast<uintptr_t>(src) & ~static_cast<uintptr_t>(3))
-                   : "memory");
+// The rows to come lie in a ring in shared memory, fetched with cp.async, 16 bytes a copy.
+//
+// Vectors (VEC > 1: bases, strides and d multiples of 16 bytes): a thread reads back the
+// vectors that it fetched itself, so no barrier is needed. Slot (stage, load, thread).
+//
+// Single elements (anything else): the group fetches the aligned 16 bytes around its row
+// (never a byte outside a 16-byte block of which the row has a part) and, behind a
+// barrier, each thread takes the columns tid, tid + G, ... (An aligned four bytes for each
+// element, fetched by the thread itself: 16384 x 1001 bf16 36 us, 70 in the gradient.)
+__device__ __forceinline__ void fetch16(void* slot, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void fetch_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
+// One tensor's part of a stage. `at`: the thread's first slot, or the group's row.
+template <typename T, int VEC, int NV>
+struct Row {
+  static __device__ __forceinline__ void fetch(uint8_t* at, const T* src, int tid, int G, int d) {
+    if constexpr (VEC > 1) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if ((tid + i * G) * VEC < d) fetch16(at + i * 16 * kRowThreads, src + (tid + i * G) * VEC);
+    } else {
+      const uint8_t* first = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(src) & ~static_cast<uintptr_t>(15));
+      const int blocks = (static_cast<int>(reinterpret_cast<uintptr_t>(src) & 15) + d * static_cast<int>(sizeof(T)) + 15) / 16;
+      for (int q = tid; q < blocks; q += G) fetch16(at + 16 * q, first + 16 * q);
+    }
   }
-  static __device__ __forceinline__ void zero(Type* slot) {
-    if constexpr (sizeof(Type) == 16)
-      *reinterpret_cast<uint4*>(slot) = make_uint4(0, 0, 0, 0);
-    else
-      *reinterpret_cast<uint32_t*>(slot) = 0;
-  }
-  // The values of a slot that was fetched from an address with this bit 1 (two-byte vectors).
-  static __device__ __forceinline__ void get(const Type* slot, uint32_t odd, float* v) {
-    if constexpr (kHalf) {
-      v[0] = __uint_as_float(odd ? *slot & 0xFFFF0000u : *slot << 16);
-    } else if constexpr (sizeof(P) == 16 && sizeof(P::e[0]) == 2) {
-      const uint4 u = *reinterpret_cast<const uint4*>(slot);
+  // Load i's values. Past d: what the slot was set to, or 0.
+  static __device__ __forceinline__ void get(const uint8_t* at, const T* src, int i, int tid, int G, int d, float* v) {
+    if constexpr (VEC == 8) {
+      const uint4 u = *reinterpret_cast<const uint4*>(at + i * 16 * kRowThreads);
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         v[2 * k] = __uint_as_float(w[k] << 16);
         v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
       }
+    } else if constexpr (VEC == 4) {
+      const float4 u = *reinterpret_cast<const float4*>(at + i * 16 * kRowThreads);
+      v[0] = u.x;
+      v[1] = u.y;
+      v[2] = u.z;
+      v[3] = u.w;
     } else {
-      const P u = *slot;
-#pragma unroll
-      for (int k = 0; k < static_cast<int>(sizeof(P) / sizeof(float)); ++k) v[k] = to_f32(u.e[k]);
+      const int c = tid + i * G;
+      const T* row = reinterpret_cast<const T*>(at + (reinterpret_cast<uintptr_t>(src) & 15));
+      v[0] = c < d ? to_f32(row[c]) : 0.f;
     }
   }
 };
-__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void fetch_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
-}
 
 template <typename T, int VEC>
 __device__ __forceinline__ void store(T* dst, const float* v) {
@@ -182,20 +191,21 @@ __device__ __forceinline__ int param_place(int e, int width) {
 // VEC: elements per load (16 bytes, or one where a base, a stride or d is not a multiple
 // of that); NV: loads per thread, row and tensor. CTAs on an SM by the registers that the
 // elements a thread holds take; the ring's depth by the shared memory of each.
-template <typename T, int VEC, int NV, bool kGradient>
+template <int VEC, int NV, bool kGradient>
 struct Held {
-  using S = Slot<Pack<T, VEC>>;
   static constexpr int kElems = VEC * NV;
   static constexpr int kTensors = kGradient ? 2 : 1;
-  static constexpr int kStage = kRowThreads * NV * kTensors * static_cast<int>(sizeof(typename S::Type));  // bytes
+  static constexpr int kStage = 16 * NV * kRowThreads * kTensors;  // bytes (vectors)
   static constexpr int kShared = (kGradient ? 192 : 144) * 1024;
-  static constexpr int kCtas = kElems <= 8 ? 4 : !kGradient && kStage <= 16384 ? 3 : kShared / 2 / kStage >= 2 ? 2 : 1;
+  static constexpr int kCtas = VEC == 1 ? (kElems <= 8 ? 4 : 2)
+                               : kElems <= 8 ? 4 : !kGradient && kStage <= 16384 ? 3 : kShared / 2 / kStage >= 2 ? 2 : 1;
   static constexpr int kRoom = kShared / kCtas / kStage;
-  static constexpr int kDepth = kRoom > 6 ? 6 : kRoom;
-  static constexpr int kRing = kDepth * kStage;
+  static constexpr int kDepth = VEC == 1 ? (NV <= 4 ? 6 : NV <= 8 ? 4 : 3) : kRoom > 6 ? 6 : kRoom;
   static_assert(kDepth >= 2, "a ring of one row waits for every load");
-  static_assert(kRing >= kRowThreads * kElems * 4 || !kGradient, "the columns' sums of every group");
 };
+
+// Bytes of a row's part of a stage (single elements): its length and up to 15 at either end.
+__host__ __device__ inline int row_room(int d, int esz) { return (d * esz + 15) / 16 * 16 + 16; }
 
 // The columns a group's threads hold, a multiple of what d needs.
 __host__ __device__ inline int held_width(int G, int elems) { return G * elems; }
@@ -212,34 +222,31 @@ __device__ __forceinline__ void stage_params(const NormParams& p, float* w, floa
 }
 
 template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, false>::kCtas)) norm_kernel(const NormParams p) {
-  using H = Held<T, VEC, NV, false>;
-  using S = typename H::S;
+__global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) norm_kernel(const NormParams p) {
+  using H = Held<VEC, NV, false>;
+  using Src = Row<T, VEC, NV>;
   constexpr int kElems = H::kElems, kDepth = H::kDepth;
   extern __shared__ __align__(16) uint8_t smem[];
-  typename S::Type* ring = reinterpret_cast<typename S::Type*>(smem) + threadIdx.x;  // [kDepth][NV][thread]
   __shared__ float red[2][1][32];
   const int G = p.G, R = kRowThreads / G, tid = threadIdx.x % G, d = p.d, width = held_width(G, kElems);
-  float* w = reinterpret_cast<float*>(smem + H::kRing);
+  const int stage_bytes = p.ring / kDepth;
+  uint8_t* ring = smem + (VEC > 1 ? 16 * threadIdx.x : threadIdx.x / G * row_room(d, sizeof(T)));
+  float* w = reinterpret_cast<float*>(smem + p.ring);
   float* b = w + width;
   const float inv_d = 1.f / static_cast<float>(d);
   const bool full = width == d;  // every element held is one of the row
-  if (!full)
+  if (VEC > 1 && !full)
 #pragma unroll
     for (int i = 0; i < kDepth * NV; ++i)
-      if ((tid + i % NV * G) * VEC >= d) S::zero(&ring[i * kRowThreads]);
+      if ((tid + i % NV * G) * VEC >= d) *reinterpret_cast<uint4*>(ring + i * 16 * kRowThreads) = make_uint4(0, 0, 0, 0);
   wait_for_previous();
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
   int64_t row = static_cast<int64_t>(blockIdx.x) * R + threadIdx.x / G;
   // Whole warps stay together: the first row of a warp's groups says when it ends.
   int64_t warp_row = static_cast<int64_t>(blockIdx.x) * R + (threadIdx.x & ~31) / G;
+  const T* src = static_cast<const T*>(p.x);
   const auto ask = [&](int64_t r, int stage) {
-    if (r < p.N) {
-      const T* src = static_cast<const T*>(p.x) + r * p.s_x + tid * VEC;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (full || (tid + i * G) * VEC < d) S::fetch(&ring[(stage * NV + i) * kRowThreads], src + i * G * VEC);
-    }
+    if (r < p.N) Src::fetch(ring + stage * stage_bytes, src + r * p.s_x, tid, G, d);
     fetch_commit();
   };
 #pragma unroll
@@ -248,16 +255,16 @@ __global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, false>::kCtas))
   int stage = 0;
   for (; warp_row < p.N; warp_row += step, row += step) {
     fetch_wait<kDepth - 1>();
+    if (VEC == 1) group_barrier(G);  // the whole row is there
     float x[kElems];
-    const uint32_t odd = S::kHalf ? (reinterpret_cast<uintptr_t>(static_cast<const T*>(p.x) + row * p.s_x + tid) >> 1) & 1 : 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)  // G is even: the elements of a thread have one parity
-      S::get(&ring[(stage * NV + i) * kRowThreads], odd, x + i * VEC);
+    for (int i = 0; i < NV; ++i) Src::get(ring + stage * stage_bytes, src + row * p.s_x, i, tid, G, d, x + i * VEC);
     float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < kElems; j += 2) s2 = fadd2(s2, make_float2(x[j], x[j + 1]));
     float s[1] = {s2.x + s2.y};
     row_sums<1>(s, G, red[0]);
+    if (VEC == 1) group_barrier(G);  // the row has been read
     ask(row + kDepth * step, stage);
     stage = stage + 1 == kDepth ? 0 : stage + 1;
     const float mean = s[0] * inv_d;
@@ -311,35 +318,32 @@ __global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, false>::kCtas))
 }
 
 template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, true>::kCtas)) norm_grad_kernel(const NormParams p) {
-  using H = Held<T, VEC, NV, true>;
-  using S = typename H::S;
+__global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) norm_grad_kernel(const NormParams p) {
+  using H = Held<VEC, NV, true>;
+  using Src = Row<T, VEC, NV>;
   constexpr int kElems = H::kElems, kDepth = H::kDepth;
   extern __shared__ __align__(16) uint8_t smem[];
-  typename S::Type* ring = reinterpret_cast<typename S::Type*>(smem) + threadIdx.x;  // [kDepth][x, dy][NV][thread]
   __shared__ float red[2][2][32];
   const int G = p.G, R = kRowThreads / G, g = threadIdx.x / G, tid = threadIdx.x % G, d = p.d, width = held_width(G, kElems);
-  float* w = reinterpret_cast<float*>(smem + H::kRing);
+  const int stage_bytes = p.ring / kDepth;
+  uint8_t* ring = smem + (VEC > 1 ? 16 * threadIdx.x : g * row_room(d, sizeof(T)));  // x, and dy half a stage on
+  float* w = reinterpret_cast<float*>(smem + p.ring);
   const float inv_d = 1.f / static_cast<float>(d);
   const bool full = width == d;
-  if (!full)
+  if (VEC > 1 && !full)
 #pragma unroll
     for (int i = 0; i < kDepth * 2 * NV; ++i)
-      if ((tid + i % NV * G) * VEC >= d) S::zero(&ring[i * kRowThreads]);
+      if ((tid + i % NV * G) * VEC >= d) *reinterpret_cast<uint4*>(ring + i * 16 * kRowThreads) = make_uint4(0, 0, 0, 0);
   wait_for_previous();
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
   int64_t row = static_cast<int64_t>(blockIdx.x) * R + g;
   int64_t warp_row = static_cast<int64_t>(blockIdx.x) * R + (threadIdx.x & ~31) / G;
+  const T* src_x = static_cast<const T*>(p.x);
+  const T* src_dy = static_cast<const T*>(p.dy);
   const auto ask = [&](int64_t r, int stage) {
     if (r < p.N) {
-      const T* x = static_cast<const T*>(p.x) + r * p.s_x + tid * VEC;
-      const T* dy = static_cast<const T*>(p.dy) + r * p.s_dy + tid * VEC;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (full || (tid + i * G) * VEC < d) {
-          S::fetch(&ring[(stage * 2 * NV + i) * kRowThreads], x + i * G * VEC);
-          S::fetch(&ring[((stage * 2 + 1) * NV + i) * kRowThreads], dy + i * G * VEC);
-        }
+      Src::fetch(ring + stage * stage_bytes, src_x + r * p.s_x, tid, G, d);
+      Src::fetch(ring + stage * stage_bytes + stage_bytes / 2, src_dy + r * p.s_dy, tid, G, d);
     }
     fetch_commit();
   };
@@ -355,8 +359,6 @@ __global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, true>::kCtas)) 
     const int64_t after = row + step;
     const float next_mean = after < p.N ? p.mean[after] : 0.f, next_rstd = after < p.N ? p.rstd[after] : 0.f;
     const float2 m2 = make_float2(-mean, -mean), r2 = make_float2(rstd, rstd);
-    const uint32_t odd_x = S::kHalf ? (reinterpret_cast<uintptr_t>(static_cast<const T*>(p.x) + row * p.s_x + tid) >> 1) & 1 : 0;
-    const uint32_t odd_dy = S::kHalf ? (reinterpret_cast<uintptr_t>(static_cast<const T*>(p.dy) + row * p.s_dy + tid) >> 1) & 1 : 0;
     // kPair elements at a time: a vector, or two loads of one element. Past d x, dy and w
     // are 0, and so is all that is added up.
     constexpr int kPair = VEC == 1 ? 2 : VEC;
@@ -365,12 +367,13 @@ __global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, true>::kCtas)) 
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) {
         const int i = j / VEC + l;
-        S::get(&ring[(stage * 2 * NV + i) * kRowThreads], odd_x, x + l);
-        S::get(&ring[((stage * 2 + 1) * NV + i) * kRowThreads], odd_dy, dy + l);
+        Src::get(ring + stage * stage_bytes, src_x + row * p.s_x, i, tid, G, d, x + l);
+        Src::get(ring + stage * stage_bytes + stage_bytes / 2, src_dy + row * p.s_dy, i, tid, G, d, dy + l);
         load_params<VEC>(w, tid + i * G, width, wv + l);
       }
     };
     fetch_wait<kDepth - 1>();
+    if (VEC == 1) group_barrier(G);
     float2 s0 = make_float2(0.f, 0.f), s1 = s0;
     if (row < p.N) {  // a group without a row adds nothing
 #pragma unroll
@@ -413,6 +416,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<T, VEC, NV, true>::kCtas)) 
         }
       }
     }
+    if (VEC == 1) group_barrier(G);
     ask(row + kDepth * step, stage);
     stage = stage + 1 == kDepth ? 0 : stage + 1;
     mean = next_mean;
@@ -604,15 +608,20 @@ bool by_vectors(const void* p, int64_t stride, int esz) {
 
 // One CTA for every place on the SMs, or fewer: each walks rows.
 template <typename T, int VEC, int NV, bool kGradient>
-cudaError_t launch_held(const NormParams& p, int sms, int* parts, cudaStream_t stream) {
-  using H = Held<T, VEC, NV, kGradient>;
+cudaError_t launch_held(NormParams p, int sms, int* parts, cudaStream_t stream) {
+  using H = Held<VEC, NV, kGradient>;
   const auto kernel = kGradient ? norm_grad_kernel<T, VEC, NV> : norm_kernel<T, VEC, NV>;
-  const size_t smem = H::kRing + static_cast<size_t>(held_width(p.G, H::kElems)) * 4 * (kGradient ? 1 : 2);
+  const int width = held_width(p.G, H::kElems), R = kRowThreads / p.G;
+  p.ring = H::kDepth * (VEC > 1 ? H::kStage : R * row_room(p.d, sizeof(T)) * H::kTensors);
+  // The groups' column sums take the ring's place at the end, in stages of whole 16 bytes.
+  const int unit = H::kDepth * 32;
+  if (kGradient && p.ring < R * width * 4) p.ring = (R * width * 4 + unit - 1) / unit * unit;
+  const size_t smem = p.ring + static_cast<size_t>(width) * 4 * (kGradient ? 1 : 2);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   // The weights of wide rows leave room for fewer CTAs than the registers do.
   const int fit = static_cast<int>(224 * 1024 / (smem + 1536));
-  const int R = kRowThreads / p.G, most = norm_max_parts(p.d);
+  const int most = norm_max_parts(p.d);
   int places = sms * (fit < 1 ? 1 : fit < H::kCtas ? fit : H::kCtas);
   if (kGradient && places > most) places = most;
   const int64_t want = (p.N + R - 1) / R;
