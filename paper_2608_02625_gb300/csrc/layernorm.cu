@@ -103,10 +103,11 @@ struct NormParams {
 // Vectors (VEC > 1: bases, strides and d multiples of 16 bytes): a thread reads back the
 // vectors that it fetched itself, so no barrier is needed. Slot (stage, load, thread).
 //
-// Single elements (anything else): the group fetches the aligned 16 bytes around its row
-// (never a byte outside a 16-byte block of which the row has a part) and, behind a
-// barrier, each thread takes the columns tid, tid + G, ... (An aligned four bytes for each
-// element, fetched by the thread itself: 16384 x 1001 bf16 36 us, 70 in the gradient.)
+// Single elements (anything else): the group fetches the aligned blocks of 16 bytes around
+// its row (never a byte outside a block of which the row has a part) and, behind a
+// barrier, each thread takes the columns tid, tid + G, ... (An aligned four bytes for each element, fetched by
+// the thread itself: 16384 x 1001 bf16 36 us, 70 in the gradient. A test of each column
+// against d costs as many instructions as its arithmetic.)
 __device__ __forceinline__ void fetch16(void* slot, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot)), "l"(src) : "memory");
 }
@@ -119,6 +120,20 @@ __device__ __forceinline__ void fetch_wait() {
 // One tensor's part of a stage. `at`: the thread's first slot, or the group's row.
 template <typename T, int VEC, int NV>
 struct Row {
+  // Loads whose columns all lie below d: of single elements the first half, for a row is
+  // wider than half of what its threads hold (launch_typed).
+  static constexpr int kSure = VEC == 1 && NV > 4 ? NV / 2 : 0;
+  static __device__ __forceinline__ int offset(const T* src) {
+    return VEC == 1 ? static_cast<int>(reinterpret_cast<uintptr_t>(src) & 15) : 0;
+  }
+  // Vectors past d, which no fetch writes: zeros, in every stage of the ring.
+  static __device__ __forceinline__ void clear(uint8_t* ring, int bytes, int tid, int G, int d) {
+    if (VEC == 1 || G * NV * VEC == d) return;
+    for (int k = 0; k < bytes; k += 16 * NV * kRowThreads)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if ((tid + i * G) * VEC >= d) *reinterpret_cast<uint4*>(ring + k + (i * kRowThreads + threadIdx.x) * 16) = make_uint4(0, 0, 0, 0);
+  }
   static __device__ __forceinline__ void fetch(uint8_t* at, const T* src, int tid, int G, int d) {
     if constexpr (VEC > 1) {
 #pragma unroll
@@ -130,8 +145,8 @@ struct Row {
       for (int q = tid; q < blocks; q += G) fetch16(at + 16 * q, first + 16 * q);
     }
   }
-  // Load i's values. Past d: what the slot was set to, or 0.
-  static __device__ __forceinline__ void get(const uint8_t* at, const T* src, int i, int tid, int G, int d, float* v) {
+  // Load i's values; past d 0. off: the row's offset in its first block.
+  static __device__ __forceinline__ void get(const uint8_t* at, int off, int i, int tid, int G, int d, float* v) {
     if constexpr (VEC == 8) {
       const uint4 u = *reinterpret_cast<const uint4*>(at + i * 16 * kRowThreads);
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -147,9 +162,9 @@ struct Row {
       v[2] = u.z;
       v[3] = u.w;
     } else {
-      const int c = tid + i * G;
-      const T* row = reinterpret_cast<const T*>(at + (reinterpret_cast<uintptr_t>(src) & 15));
-      v[0] = c < d ? to_f32(row[c]) : 0.f;
+      // What lies behind a row in shared memory (other rows, the weights) is read and dropped.
+      const float x = to_f32(reinterpret_cast<const T*>(at + off)[tid + i * G]);
+      v[0] = i < kSure || tid + i * G < d ? x : 0.f;
     }
   }
 };
@@ -235,10 +250,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) no
   float* b = w + width;
   const float inv_d = 1.f / static_cast<float>(d);
   const bool full = width == d;  // every element held is one of the row
-  if (VEC > 1 && !full)
-#pragma unroll
-    for (int i = 0; i < kDepth * NV; ++i)
-      if ((tid + i % NV * G) * VEC >= d) *reinterpret_cast<uint4*>(ring + i * 16 * kRowThreads) = make_uint4(0, 0, 0, 0);
+  Src::clear(smem, p.ring, tid, G, d);
   wait_for_previous();
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
   int64_t row = static_cast<int64_t>(blockIdx.x) * R + threadIdx.x / G;
@@ -258,7 +270,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) no
     if (VEC == 1) group_barrier(G);  // the whole row is there
     float x[kElems];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) Src::get(ring + stage * stage_bytes, src + row * p.s_x, i, tid, G, d, x + i * VEC);
+    for (int i = 0; i < NV; ++i) Src::get(ring + stage * stage_bytes, Src::offset(src + row * p.s_x), i, tid, G, d, x + i * VEC);
     float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < kElems; j += 2) s2 = fadd2(s2, make_float2(x[j], x[j + 1]));
@@ -278,10 +290,9 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) no
     }
     if (!full)
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if ((tid + i * G) * VEC >= d)
+      for (int i = Src::kSure; i < NV; ++i)
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) x[i * VEC + k] = 0.f;
+        for (int k = 0; k < VEC; ++k) x[i * VEC + k] = (tid + i * G) * VEC >= d ? 0.f : x[i * VEC + k];
 #pragma unroll
     for (int j = 0; j < kElems; j += 2) s2 = ffma2(make_float2(x[j], x[j + 1]), make_float2(x[j], x[j + 1]), s2);
     s[0] = s2.x + s2.y;
@@ -292,7 +303,6 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) no
     const float2 r2 = make_float2(rstd, rstd);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (!full && (tid + i * G) * VEC >= d) continue;
       float wv[VEC], bv[VEC];
       load_params<VEC>(w, tid + i * G, width, wv);
       load_params<VEC>(b, tid + i * G, width, bv);
@@ -307,7 +317,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) no
           wv[k + 1] = y.y;
         }
       }
-      store<T, VEC>(o + i * G * VEC, wv);
+      if (i < Src::kSure || full || (tid + i * G) * VEC < d) store<T, VEC>(o + i * G * VEC, wv);
     }
     if (tid == 0) {
       if (p.mean) p.mean[row] = mean;
@@ -330,10 +340,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) nor
   float* w = reinterpret_cast<float*>(smem + p.ring);
   const float inv_d = 1.f / static_cast<float>(d);
   const bool full = width == d;
-  if (VEC > 1 && !full)
-#pragma unroll
-    for (int i = 0; i < kDepth * 2 * NV; ++i)
-      if ((tid + i % NV * G) * VEC >= d) *reinterpret_cast<uint4*>(ring + i * 16 * kRowThreads) = make_uint4(0, 0, 0, 0);
+  Src::clear(smem, p.ring, tid, G, d);
   wait_for_previous();
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
   int64_t row = static_cast<int64_t>(blockIdx.x) * R + g;
@@ -359,6 +366,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) nor
     const int64_t after = row + step;
     const float next_mean = after < p.N ? p.mean[after] : 0.f, next_rstd = after < p.N ? p.rstd[after] : 0.f;
     const float2 m2 = make_float2(-mean, -mean), r2 = make_float2(rstd, rstd);
+    const int off_x = Src::offset(src_x + row * p.s_x), off_dy = Src::offset(src_dy + row * p.s_dy);
     // kPair elements at a time: a vector, or two loads of one element. Past d x, dy and w
     // are 0, and so is all that is added up.
     constexpr int kPair = VEC == 1 ? 2 : VEC;
@@ -367,8 +375,8 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) nor
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) {
         const int i = j / VEC + l;
-        Src::get(ring + stage * stage_bytes, src_x + row * p.s_x, i, tid, G, d, x + l);
-        Src::get(ring + stage * stage_bytes + stage_bytes / 2, src_dy + row * p.s_dy, i, tid, G, d, dy + l);
+        Src::get(ring + stage * stage_bytes, off_x, i, tid, G, d, x + l);
+        Src::get(ring + stage * stage_bytes + stage_bytes / 2, off_dy, i, tid, G, d, dy + l);
         load_params<VEC>(w, tid + i * G, width, wv + l);
       }
     };
@@ -412,7 +420,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) nor
 #pragma unroll
         for (int l = 0; l < kPair / VEC; ++l) {
           const int i = j / VEC + l;
-          if (full || (tid + i * G) * VEC < d) store<T, VEC>(o + i * G * VEC, x + l);
+          if (i < Src::kSure || full || (tid + i * G) * VEC < d) store<T, VEC>(o + i * G * VEC, x + l);
         }
       }
     }
@@ -578,17 +586,16 @@ __global__ void __launch_bounds__(kReduceThreads)
     static_cast<float*>(out)[c] = s;
 }
 
-// Threads a row and loads a thread. Many rows: a warp, or the fewest warps that hold the
-// row, so that few threads pay for each row; rows of few loads share a warp. Few rows:
-// more threads each, while half of them still find a place at once, for the chain of
-// loads and sums is what a call then waits for (512 x 2048 bf16: 6.8 us).
+// Threads a row and loads a thread. Many rows: as many loads as a thread holds, so that few
+// threads pay for each row, and several rows share a warp. Few rows: more threads each,
+// while half of them still find a place at once, for the chain of loads and sums is what a
+// call then waits for (512 x 2048 bf16: 3.6 us).
 struct Shape {
   int G, nv;
 };
 
 Shape shape_of(int64_t N, int64_t loads, int most_nv, int sms) {
   int G = 8, nv = 1;
-  while (G < 32 && G < loads) G *= 2;
   while (static_cast<int64_t>(G) * nv < loads) {
     if (nv < most_nv)
       nv *= 2;
@@ -613,7 +620,7 @@ cudaError_t launch_held(NormParams p, int sms, int* parts, cudaStream_t stream) 
   const auto kernel = kGradient ? norm_grad_kernel<T, VEC, NV> : norm_kernel<T, VEC, NV>;
   const int width = held_width(p.G, H::kElems), R = kRowThreads / p.G;
   p.ring = H::kDepth * (VEC > 1 ? H::kStage : R * row_room(p.d, sizeof(T)) * H::kTensors);
-  // The groups' column sums take the ring's place at the end, in stages of whole 16 bytes.
+  // The groups' columns' sums take the ring's place at the end.
   const int unit = H::kDepth * 32;
   if (kGradient && p.ring < R * width * 4) p.ring = (R * width * 4 + unit - 1) / unit * unit;
   const size_t smem = p.ring + static_cast<size_t>(width) * 4 * (kGradient ? 1 : 2);
