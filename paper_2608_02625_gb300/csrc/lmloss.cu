@@ -430,125 +430,144 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t base = tmem + lane_base + acc * kMaxBN;
         const int row = tl.m * kRows + rank * kBM + t_row;
         float ts = 0.f;  // stats: this tile's terms, relative to m
-        const int chunks = p.bn / 32;
-        if (2 * half >= chunks) release(acc);
+        const int groups = p.bn / 64;
+        if (half >= groups) release(acc);
+        // 64 columns at a time: two loads and one wait, and arithmetic enough without a
+        // dependence that two warps a scheduler keep it busy.
 #pragma unroll 1
-        for (int c = 2 * half; c < chunks; c += c & 1 ? 3 : 1) {
-          uint32_t v[32];
-          tmem_ld32(base + 32 * c, v);
-          tmem_wait_ld();
-          if ((c & 1) && c + 3 >= chunks) release(acc);
-          float x[32];
+        for (int g = half; g < groups; g += 2) {
+          float x[64];
+          {
+            uint32_t v0[32], v1[32];
+            tmem_ld32(base + 64 * g, v0);
+            tmem_ld32(base + 64 * g + 32, v1);
+            tmem_wait_ld(v0);
+            tmem_wait_ld(v1);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+            for (int e = 0; e < 32; ++e) {
+              x[e] = __uint_as_float(v0[e]);
+              x[32 + e] = __uint_as_float(v1[e]);
+            }
+          }
+          if (g + 2 >= groups) release(acc);
+          const int col0 = (kMode == kGrad ? p.v0 : 0) + tl.n * p.bn + 64 * g;
           if (kMode == kStats) {
-            const int col0 = tl.n * p.bn + 32 * c;
-            if (static_cast<unsigned>(target - col0) < 32u) {
+            if (static_cast<unsigned>(target - col0) < 64u) {
               float xt = x[0];
 #pragma unroll
-              for (int e = 1; e < 32; ++e)
+              for (int e = 1; e < 64; ++e)
                 if (target - col0 == e) xt = x[e];
               p.x_target[row] = xt;
             }
-            if (col0 + 32 > p.V) {
+            if (col0 + 64 > p.V) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
+              for (int e = 0; e < 64; ++e)
                 if (col0 + e >= p.V) x[e] = -INFINITY;
             }
-            float cm0 = fmaxf(x[0], x[1]), cm1 = fmaxf(x[2], x[3]);
+            float cm[4];
 #pragma unroll
-            for (int e = 4; e < 32; e += 4) {
-              cm0 = fmax3(cm0, x[e], x[e + 1]);
-              cm1 = fmax3(cm1, x[e + 2], x[e + 3]);
+            for (int k = 0; k < 4; ++k) {
+              cm[k] = fmax3(x[16 * k], x[16 * k + 1], x[16 * k + 2]);
+#pragma unroll
+              for (int e = 3; e < 15; e += 2) cm[k] = fmax3(cm[k], x[16 * k + e], x[16 * k + e + 1]);
+              cm[k] = fmaxf(cm[k], x[16 * k + 15]);
             }
-            const float cm = fmaxf(cm0, cm1);
-            if (cm > m) {
-              const float a = m == -INFINITY ? 1.f : ex2_approx((m - cm) * kLog2e);  // nothing, or a NaN, yet
+            const float top = fmaxf(fmax3(cm[0], cm[1], cm[2]), cm[3]);
+            if (top > m) {
+              const float a = m == -INFINITY ? 1.f : ex2_approx((m - top) * kLog2e);  // nothing, or a NaN, yet
               s *= a;
               ts *= a;
-              m = cm;
+              m = top;
             }
             const float ml = m == -INFINITY ? 0.f : m * kLog2e;
             const float2 k2 = make_float2(kLog2e, kLog2e), n2 = make_float2(-ml, -ml);
-            float2 sum = make_float2(0.f, 0.f);
+            float2 sum[4] = {};
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
+            for (int e = 0; e < 64; e += 2) {
               const float2 y = ffma2(make_float2(x[e], x[e + 1]), k2, n2);
-              sum = fadd2(sum, make_float2(ex2_approx(y.x), ex2_approx(y.y)));
+              sum[e / 2 % 4] = fadd2(sum[e / 2 % 4], make_float2(ex2_approx(y.x), ex2_approx(y.y)));
             }
-            ts += sum.x + sum.y;
+            const float2 both = fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3]));
+            ts += both.x + both.y;
           } else {
             if (kMode == kGrad) {
-              const int col0 = p.v0 + tl.n * p.bn + 32 * c;
               const float2 k2 = make_float2(kLog2e, kLog2e), n2 = make_float2(-lse2, -lse2);
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) {
+              for (int e = 0; e < 64; e += 2) {
                 const float2 y = ffma2(make_float2(x[e], x[e + 1]), k2, n2);
                 x[e] = ex2_approx(y.x);
                 x[e + 1] = ex2_approx(y.y);
               }
-              if (static_cast<unsigned>(target - col0) < 32u) {
+              if (static_cast<unsigned>(target - col0) < 64u) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if (target - col0 == e) x[e] -= 1.f;
+                for (int e = 0; e < 64; ++e) x[e] -= target - col0 == e ? 1.f : 0.f;
               }
-              if (col0 + 32 > p.V) {
-#pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if (col0 + e >= p.V) x[e] = 0.f;
-              }
-              // Rows behind the scored ones hold anything: their g is 0.
               const float2 d2 = make_float2(dloss, dloss);
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) {
+              for (int e = 0; e < 64; e += 2) {
                 const float2 y = fmul2(make_float2(x[e], x[e + 1]), d2);
-                x[e] = target >= 0 ? y.x : 0.f;
-                x[e + 1] = target >= 0 ? y.y : 0.f;
+                x[e] = y.x;
+                x[e + 1] = y.y;
+              }
+              if (col0 + 64 > p.V) {
+#pragma unroll
+                for (int e = 0; e < 64; ++e)
+                  if (col0 + e >= p.V) x[e] = 0.f;
+              }
+              if (target < 0) {  // rows behind the scored ones hold anything: their g is 0
+#pragma unroll
+                for (int e = 0; e < 64; ++e) x[e] = 0.f;
               }
             }
             if (kMode == kBack && tl.k1 == tl.k0) {  // no scored row: nothing was multiplied
 #pragma unroll
-              for (int e = 0; e < 32; ++e) x[e] = 0.f;
+              for (int e = 0; e < 64; ++e) x[e] = 0.f;
             }
-            // 128 bytes of a row a buffer: 32 columns of fp32, 64 of bf16 (two chunks).
-            const bool wide = kMode == kBack && !tl.dw;
-            const bool opens = wide || (c & 1) == 0, closes = wide || (c & 1) == 1;
-            if (opens) {
-              if (lane == 0) bulk_wait_read<0>();  // the store before has left the buffer
-              __syncwarp();
-            }
+            const int r0 = tl.m * kRows + rank * kBM + qw * 32;
             uint8_t* dst = buf + lane * 128;
-            if (wide) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                *reinterpret_cast<float4*>(dst + ((e ^ (lane & 7)) << 4)) =
-                    make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                *reinterpret_cast<uint4*>(dst + (((4 * (c & 1) + e) ^ (lane & 7)) << 4)) =
-                    make_uint4(pack_bf16x2(x[8 * e], x[8 * e + 1]), pack_bf16x2(x[8 * e + 2], x[8 * e + 3]),
-                               pack_bf16x2(x[8 * e + 4], x[8 * e + 5]), pack_bf16x2(x[8 * e + 6], x[8 * e + 7]));
-            }
-            if (closes) {
+            const auto filled = [&](auto store) {
               fence_proxy_async_smem();
               __syncwarp();
               if (lane == 0) {
-                const int r0 = tl.m * kRows + rank * kBM + qw * 32;
-                const int col = tl.n * p.bn + 32 * (wide ? c : c - 1);
-                if (kMode == kGrad) {
-                  tma_store_2d(&mo, buf, 0, col / 64 * p.n_pad + r0);
-                } else if (tl.dw) {
-                  if (p.v0 + r0 < p.dw_rows && col < p.dw_cols) tma_store_2d(&mdo, buf, col, p.v0 + r0);
-                } else if (col < p.dh_cols) {
-                  const int y = tl.split * work.row_blocks * kRows + r0;
-                  if (!p.add)
-                    tma_store_2d(&mo, buf, col, y);
-                  else if (tl.k1 > tl.k0)
-                    tma_add_2d(&mo, buf, col, y);
-                }
+                store();
                 bulk_commit();
               }
+            };
+            const auto free_again = [&] {  // the store before has left the buffer
+              if (lane == 0) bulk_wait_read<0>();
+              __syncwarp();
+            };
+            if (kMode == kBack && !tl.dw) {
+              // 32 columns of fp32 a buffer.
+              const int y = tl.split * work.row_blocks * kRows + r0;
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                free_again();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  *reinterpret_cast<float4*>(dst + ((e ^ (lane & 7)) << 4)) =
+                      make_float4(x[32 * c + 4 * e], x[32 * c + 4 * e + 1], x[32 * c + 4 * e + 2], x[32 * c + 4 * e + 3]);
+                filled([&] {
+                  if (col0 + 32 * c >= p.dh_cols) return;
+                  if (!p.add)
+                    tma_store_2d(&mo, buf, col0 + 32 * c, y);
+                  else if (tl.k1 > tl.k0)
+                    tma_add_2d(&mo, buf, col0 + 32 * c, y);
+                });
+              }
+            } else {
+              free_again();
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<uint4*>(dst + ((e ^ (lane & 7)) << 4)) =
+                    make_uint4(pack_bf16x2(x[8 * e], x[8 * e + 1]), pack_bf16x2(x[8 * e + 2], x[8 * e + 3]),
+                               pack_bf16x2(x[8 * e + 4], x[8 * e + 5]), pack_bf16x2(x[8 * e + 6], x[8 * e + 7]));
+              filled([&] {
+                if (kMode == kGrad)
+                  tma_store_2d(&mo, buf, 0, (col0 - p.v0) / 64 * p.n_pad + r0);
+                else if (p.v0 + r0 < p.dw_rows && col0 < p.dw_cols)
+                  tma_store_2d(&mdo, buf, col0, p.v0 + r0);
+              });
             }
           }
         }
