@@ -278,7 +278,7 @@ int dlm_refine_update_ranked(const dlm_tensor* tokens, const dlm_tensor* mask, c
  * product, whose time goes by the scored rows.
  *
  *   hidden      [N, d] or [B, L, d] BF16, rows evenly strided, any alignment; d a multiple
- *               of 8
+ *               of 8 up to 2^20, N up to 2^28, V up to 2^30
  *   weight      [V, d] BF16; base pointer and row stride multiples of 16 bytes
  *   targets     N I32, contiguous (any rank with N elements, like loss and lse)
  *   loss, lse   N F32, contiguous
@@ -327,8 +327,8 @@ size_t dlm_lmhead_loss_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t
  *   out[r, c] = (x[r, c] - mean[r]) * rstd[r] * weight[c] + bias[c]
  *
  *   x, out        [N, d] or [B, L, d], BF16 or F32 (both the same dtype); innermost
- *                 contiguous, rows evenly strided; any d >= 1, any alignment (16-byte
- *                 aligned rows are faster)
+ *                 contiguous, rows evenly strided; d from 1 to 2^24, any alignment
+ *                 (16-byte aligned rows are faster)
  *   weight, bias  d entries, BF16 or F32 (both the same dtype), contiguous; bias may be
  *                 NULL
  *   mean, rstd    N F32, contiguous: what dlm_layer_norm_grad reads; either may be NULL

@@ -13,8 +13,8 @@ extern "C" {
 #endif
 
 /*
- * Sets the budget of every bounded wait in the attention and fused
- * projection kernels launched afterwards by this library (default 2e9 ns;
+ * Sets the budget of every bounded wait in the attention, fused projection
+ * and projection loss kernels launched afterwards by this library (default 2e9 ns;
  * 100 .. 2e9 accepted, DLM_ERR_ARG otherwise). With a budget of a few hundred
  * ns the waits of a real pipeline run out: the kernel records
  * DLM_DEVERR_TIMEOUT, lets the copies and MMAs it issued land, frees its

@@ -227,8 +227,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 32 * kEpiWarp0) {  // parameters, not memory that another kernel writes
     prefetch_tmap(&ma);
     prefetch_tmap(&mb);
-    if (kMode != kStats) prefetch_tmap(&mo);
-    if (kMode == kBack) {
+    if (kMode == kGrad || (kMode == kBack && p.want_dh)) prefetch_tmap(&mo);
+    if (kMode == kBack && p.want_dw) {
       prefetch_tmap(&mda);
       prefetch_tmap(&mdb);
       prefetch_tmap(&mdo);
@@ -310,18 +310,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    // Teardown: every copy issued lands before the block exits (a pair's leader waits for
-    // both CTAs' copies, the other CTA for it).
-    if (lane == 0 && rank == 0) {
+    // Teardown: every copy issued lands before the block exits. A single CTA waits for its
+    // barriers; of a pair, whose copies complete on the leader's, each waits for the MMAs
+    // that read its stages, and where something has given up (the other CTA's copies, on
+    // which a barrier may wait, then need not come) gives the copies a millisecond.
+    if (kCtas == 2) {
+      bool landed = ok;
+      for (int s = 0; s < kStages; ++s) {
+        const int n_s = fill > s ? (fill - s + kStages - 1) / kStages : 0;
+        if (n_s && landed) landed = warp_wait(&sm.empty[s], (n_s - 1) & 1, abort, p.err, p.wait_ns);
+      }
+      if (!landed) {
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 1000000) {
+        }
+      }
+    } else if (lane == 0) {
       for (int s = 0; s < kStages; ++s) {
         const int n_s = fill > s ? (fill - s + kStages - 1) / kStages : 0;
         if (n_s) mbar_drain(&sm.full[s], (n_s - 1) & 1);
-      }
-    }
-    if (kCtas == 2 && !ok) {
-      // Given up: copies that no barrier accounts for any more get a millisecond to land.
-      const uint64_t t0 = global_timer_ns();
-      while (global_timer_ns() - t0 < 1000000) {
       }
     }
     __syncwarp();

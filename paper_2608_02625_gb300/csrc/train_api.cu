@@ -85,12 +85,14 @@ int require_error_word() {
   return DLM_OK;
 }
 
+constexpr int64_t kMostNormWidth = int64_t{1} << 24;
+
 bool aligned_rows(const dlm_tensor* t) {
   if (reinterpret_cast<uintptr_t>(t->data) % 16 != 0) return false;
   return t->shape[0] <= 1 || (t->stride[0] * elem_size(t->dtype)) % 16 == 0;
 }
 
-constexpr int64_t kMostRows = int64_t{1} << 30, kMostWidth = int64_t{1} << 20;
+constexpr int64_t kMostRows = int64_t{1} << 28, kMostVocab = int64_t{1} << 30, kMostWidth = int64_t{1} << 20;
 
 // The arguments that the loss and its gradients share.
 int prepare_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_tensor* targets, LossArgs* a) {
@@ -102,8 +104,8 @@ int prepare_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_t
   if (weight->shape[1] != a->d) return fail(DLM_ERR_SHAPE, "weight must be [V, d] with the d of hidden");
   if (a->d < 8 || a->d % 8 != 0) return fail(DLM_ERR_SHAPE, "d must be a positive multiple of 8 (got %lld)", (long long)a->d);
   if (a->V < 1) return fail(DLM_ERR_SHAPE, "V must be >= 1");
-  if (a->N > kMostRows || a->V > kMostRows || a->d > kMostWidth)
-    return fail(DLM_ERR_SHAPE, "at most 2^30 rows and tokens and a width of 2^20");
+  if (a->N > kMostRows || a->V > kMostVocab || a->d > kMostWidth)
+    return fail(DLM_ERR_SHAPE, "at most 2^28 rows, 2^30 tokens and a width of 2^20");
   if (a->V > 1 && weight->stride[0] < a->d) return fail(DLM_ERR_STRIDE, "weight rows overlap");
   if (!aligned_rows(weight)) return fail(DLM_ERR_ALIGN, "weight rows must start at multiples of 16 bytes");
   a->hidden = hidden->data;
@@ -143,7 +145,7 @@ int dlm_lmhead_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dl
 }
 
 size_t dlm_lmhead_loss_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int64_t piece) {
-  const bool fine = rows > 0 && rows <= kMostRows && vocab > 0 && vocab <= kMostRows && d > 0 && d <= kMostWidth && piece >= 0;
+  const bool fine = rows > 0 && rows <= kMostRows && vocab > 0 && vocab <= kMostVocab && d > 0 && d <= kMostWidth && piece >= 0;
   return fine ? loss_grad_workspace_bytes(rows, vocab, d, piece) : 0;
 }
 
@@ -202,7 +204,7 @@ int dlm_layer_norm(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tens
   if ((st = rows_of(x, "x", kMaskBF16F32, &a.N, &a.d, &a.s_x))) return st;
   if ((st = rows_of(out, "out", 1 << x->dtype, &N2, &d2, &a.s_out))) return st;
   if (!same_shape(x, out)) return fail(DLM_ERR_SHAPE, "out must have the shape of x");
-  if (a.d < 1) return fail(DLM_ERR_SHAPE, "rows must have at least one element");
+  if (a.d < 1 || a.d > kMostNormWidth) return fail(DLM_ERR_SHAPE, "rows must have between 1 and 2^24 elements");
   if ((st = check_vector(weight, "weight", kMaskBF16F32, a.d, false))) return st;
   if ((st = check_vector(bias, "bias", 1 << weight->dtype, a.d, true))) return st;
   if ((st = check_vector(mean, "mean", 1 << DLM_F32, a.N, true))) return st;
@@ -239,7 +241,7 @@ int dlm_layer_norm_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_t
   if ((st = rows_of(dout, "dout", 1 << x->dtype, &N2, &d2, &a.s_dout))) return st;
   if ((st = rows_of(dx, "dx", 1 << x->dtype, &N2, &d2, &a.s_dx))) return st;
   if (!same_shape(x, dout) || !same_shape(x, dx)) return fail(DLM_ERR_SHAPE, "dout and dx must have the shape of x");
-  if (a.d < 1) return fail(DLM_ERR_SHAPE, "rows must have at least one element");
+  if (a.d < 1 || a.d > kMostNormWidth) return fail(DLM_ERR_SHAPE, "rows must have between 1 and 2^24 elements");
   if ((st = check_vector(weight, "weight", kMaskBF16F32, a.d, false))) return st;
   if ((st = check_vector(mean, "mean", 1 << DLM_F32, a.N, false))) return st;
   if ((st = check_vector(rstd, "rstd", 1 << DLM_F32, a.N, false))) return st;

@@ -24,6 +24,7 @@ NORM = {
     "rank_1": (dict(x=T(BF16, [64], MB)), -3), "out_shape": (dict(out=T(BF16, [6, 63], 4 * MB)), -3),
     "weight_length": (dict(w=T(F32, [63], 2 * MB)), -3), "rstd_length": (dict(rstd=T(F32, [5], 6 * MB)), -3),
     "no_columns": (dict(x=T(BF16, [6, 0], MB), out=T(BF16, [6, 0], 4 * MB), w=T(F32, [0], 2 * MB)), -3),
+    "too_wide": (dict(x=T(BF16, [1, 2 ** 24 + 8], MB), out=T(BF16, [1, 2 ** 24 + 8], 4 * MB)), -3),
     "columns_apart": (dict(x=T(BF16, [6, 64], MB, [128, 2])), -4), "rows_overlap": (dict(x=T(BF16, [6, 64], MB, [32, 1])), -4),
     "uneven_rows": (dict(x=T(BF16, [2, 3, 64], MB, [1000, 64, 1]), out=T(BF16, [2, 3, 64], 4 * MB)), -4),
     "weight_apart": (dict(w=T(F32, [64], 2 * MB, [2])), -4), "mean_misaligned": (dict(mean=T(F32, [6], 5 * MB + 2)), -5),

@@ -18,7 +18,7 @@ pytestmark = pytest.mark.gpu
 
 BF, F32 = torch.bfloat16, torch.float32
 SIZES = [(1, 1), (3, 7), (5, 8), (1, 64), (700, 64), (33, 100), (2, 200), (70, 1001), (9, 2048), (640, 2048), (301, 513),
-         (5, 2501), (4, 4096), (3, 5001), (6, 8192), (2, 8200), (3, 16384), (2, 20001)]
+         (5, 2501), (4, 4096), (3, 5001), (6, 8192), (4, 8191), (2, 8200), (3, 16384), (2, 20001)]
 K = 64
 
 

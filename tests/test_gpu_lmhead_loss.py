@@ -96,7 +96,7 @@ def fp64_lse(h, w, t):
 
 SIZES = [(1, 1, 8), (3, 7, 8), (1, 300, 64), (128, 256, 64), (130, 1000, 72), (129, 257, 200), (300, 2049, 128), (64, 4099, 512),
          (257, 1024, 320), (5, 151, 2048), (1000, 513, 264), (90, 40000, 64), (520, 1000, 72), (2000, 300, 64), (769, 5000, 128),
-         (1025, 2600, 512)]
+         (1025, 2600, 512), (600, 1100, 1024), (513, 300, 2048)]
 
 
 @pytest.mark.parametrize("scored", ["all", "half", "none", "first", "last"])
@@ -127,7 +127,7 @@ def test_gradients(N, V, d, scored):
 
 
 @pytest.mark.parametrize("N,V,d,piece", [(300, 2049, 128, 256), (300, 2049, 128, 1024), (64, 4099, 512, 1024), (20, 1300, 72, 512),
-                                         (700, 900, 64, 256), (1500, 3000, 320, 1024)])
+                                         (700, 900, 64, 256), (1500, 3000, 320, 1024), (700, 2000, 512, 512)])
 def test_pieces_and_single_gradients(N, V, d, piece):
     """Several pieces of the vocabulary; d_hidden or d_weight alone (the sums of d_hidden
     may then be split otherwise)."""
@@ -258,9 +258,9 @@ def test_gradients_against_differences():
             assert abs(diff - float(dh[r, k])) <= 2.0 ** -7 * abs(diff) + curve + 2.0 ** -8 * 0.1 + 1e-4
 
 
-def test_same_bits_again_on_another_stream_and_replayed():
+@pytest.mark.parametrize("N,V,d", [(500, 3001, 192), (700, 3001, 1024)])
+def test_same_bits_again_on_another_stream_and_replayed(N, V, d):
     from paper_2608_02625_gb300 import binding as B
-    N, V, d = 500, 3001, 192
     h, w, t, dl = inputs(N, V, d, seed=5)
     new = lambda: [torch.empty(N, device=dev()), torch.empty(N, device=dev()), torch.empty_like(h), torch.empty_like(w)]  # noqa: E731
 
