@@ -4,7 +4,7 @@
 //   out  = x min(1, max_norm / (norm + 1e-6))
 //
 // Two launches over the same chunks of the tensors. The first sums squares: a
-// thread adds a chunk's in fp32 (up to 256, in eight sums) and the chunks' in fp64,
+// thread adds a chunk's in fp32 (up to 128, in eight sums) and the chunks' in fp64,
 // and each CTA leaves one fp64 sum in the caller's workspace. The second adds those
 // in a fixed order (every CTA for itself: a thousand numbers) and scales, walking the
 // chunks from the last to the first, so that what the first launch read last may still
