@@ -20,12 +20,14 @@
 // With many rows two CTAs share a tile of 256 rows (cta_group::2): each loads half of B,
 // which an MMA of one CTA's reads whole, and shared memory feeds the MMAs with fewer
 // pauses (4096 x 20000 x 2048: grad 203 -> 175 us, 90 % of the tensor pipe's cycles; dw
-// 247 -> 207, dh 250 -> 207).
+// 247 -> 207, dh 250 -> 207). What such an MMA reads most of, B, is K-major (with an
+// MN-major B both products keep the pipe 73 % busy): dw multiplies g^T by the hidden states
+// transposed once, dh is computed transposed, W^T g^T, and turned back with its rounding.
+// Single CTAs, with few rows or little width, take the operands as they lie.
 // g is rounded to bf16 because the tensor cores take it so: every term of d_hidden and
 // d_weight is off by at most 2^-8 relative, as the result is by its own rounding to bf16;
 // all sums are fp32. Warp 0 loads by TMA, warp 1 issues tcgen05.mma (both operands in
-// shared memory, K-major or MN-major as their matrix lies in memory, so nothing is
-// transposed), warps 4-11 read the fp32 accumulators (two, so a tile's epilogue runs
+// shared memory), warps 4-11 read the fp32 accumulators (two, so a tile's epilogue runs
 // under the next one's K loop) and write their tiles through shared memory by TMA.
 // Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, drains and exits.
 #include <cooperative_groups.h>
@@ -94,14 +96,15 @@ struct Params {
   int V;
   int kblocks;          // stats, grad: K steps (of d);  back: those of dh (of the piece)
   int bn;               // columns of a tile
-  int tiles;            // stats, grad: vocabulary tiles;  back: tiles of d
+  int tiles;            // stats, grad: vocabulary tiles;  back: dw's tiles of d
+  int dh_tiles;         // back: dh's tiles of d
   int parts;            // stats: parts of the vocabulary;  back: dw's tiles of the piece's rows
   int v0;               // first vocabulary column of the piece
   int n_pad;            // rows of a panel of g
   int a_rows;           // stats: rows of the hidden box
   int want_dw, want_dh;
   int add;              // dh: add to what the pieces before left
-  int dw_rows, dw_cols, dh_cols;  // extents of what is written
+  int dw_rows, dw_cols, dh_cols;  // extents of what is written (dh_cols: single CTAs)
   const int* target;    // of each scored row
   const float* lse2;    // lse log2(e)
   const float* dloss;
@@ -154,6 +157,10 @@ __device__ __forceinline__ float dw_cost(int steps) { return max(steps, 4) + 1.f
 template <int kMode, int kCtas>
 struct Work {
   static constexpr int kRows = kBM * kCtas;  // rows of a tile
+  // Columns of a tile: a pair's of dh are rows of g, 256 of them.
+  static __device__ __forceinline__ int bn(const Params& p, const Tile& t) {
+    return kMode == kBack && kCtas == 2 && !t.dw ? kMaxBN : p.bn;
+  }
   int items, row_blocks, k, splits;
   int k_dw, k_tail;               // back: dw's K steps, and the 16s of the last
   int dh, dw, left, meanwhile;    // back: tiles of each, dh's in its last round, dw's a worker meanwhile
@@ -167,7 +174,7 @@ struct Work {
     if (kMode != kBack) return;
     k_dw = (n + kBK - 1) / kBK;
     k_tail = (n - (k_dw - 1) * kBK + 15) / 16;
-    dh = p.want_dh ? splits * row_blocks * p.tiles : 0;
+    dh = p.want_dh ? splits * row_blocks * p.dh_tiles : 0;
     dw = p.want_dw ? p.parts * p.tiles : 0;
     left = dh % workers;
     meanwhile = left ? static_cast<int>(dh_cost(k / splits, row_blocks) / dw_cost(k_dw)) : 0;
@@ -202,8 +209,9 @@ struct Work {
     if (kMode == kStats) return {item % row_blocks, t, 0, k, 0, false};
     if (kMode == kGrad) return {item % row_blocks, item / row_blocks, 0, k, 0, false};
     if (item >= dh) return {(item - dh) / p.tiles, (item - dh) % p.tiles, 0, k_dw, 0, true};
-    const int per = row_blocks * p.tiles, split = item / per, rest = item % per;
-    return {rest / p.tiles, rest % p.tiles, static_cast<int>(static_cast<long long>(k) * split / splits),
+    const int per = row_blocks * p.dh_tiles, split = item / per, rest = item % per;
+    const int rows = rest / p.dh_tiles, cols = rest % p.dh_tiles;
+    return {kCtas == 2 ? cols : rows, kCtas == 2 ? rows : cols, static_cast<int>(static_cast<long long>(k) * split / splits),
             static_cast<int>(static_cast<long long>(k) * (split + 1) / splits), split, false};
   }
 };
@@ -267,19 +275,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* abort = &sm.abort;
   wait_for_previous();
   const Work<kMode, kCtas> work(p, workers);
-  const int bn_own = p.bn / kCtas;  // this CTA's columns of B
-  const int boxes = bn_own / 64;    // its MN-major boxes
-
   if (warp == 0) {
     // ================================================================ TMA producer
-    const uint32_t stage_bytes = kCtas * ((kMode == kStats && kCtas == 1 ? p.a_rows * 128 : kABytes) + bn_own * 128);
     int fill = 0;
     bool ok = true;
     for (int j = 0, item; ok && (item = work.item(worker, workers, j)) >= 0; ++j) {
       const int t1 = work.last(p, item);
       for (int t = work.first(p, item); ok && t < t1; ++t) {
         const Tile tl = work.tile(p, item, t);
-        const int m0 = tl.m * kRows + rank * kBM, n0 = tl.n * p.bn + rank * bn_own;
+        const int bn = work.bn(p, tl), bn_own = bn / kCtas;  // columns of B, and this CTA's
+        const int m0 = tl.m * kRows + rank * kBM, n0 = tl.n * bn + rank * bn_own;
+        const uint32_t stage_bytes = kCtas * ((kMode == kStats && kCtas == 1 ? p.a_rows * 128 : kABytes) + bn_own * 128);
         for (int kb = tl.k0; kb < tl.k1; ++kb, ++fill) {
           const int st = fill % kStages;
           if (fill >= kStages && !warp_wait(&sm.empty[st], ((fill / kStages) - 1) & 1, abort, p.err, p.wait_ns)) {
@@ -301,10 +307,16 @@ __global__ void __launch_bounds__(kThreads, 1)
               load(sm.b[st], &mb, kb * kBK, p.v0 + n0);
             } else if (tl.dw) {
               for (int i = 0; i < 2; ++i) load(sm.a[st] + i * kBoxBytes, &mda, 0, (m0 / 64 + i) * p.n_pad + kb * kBK);
-              for (int i = 0; i < boxes; ++i) load(sm.b[st] + i * kBoxBytes, &mdb, n0 + 64 * i, kb * kBK);
+              if (kCtas == 2)
+                load(sm.b[st], &mdb, kb * kBK, n0);
+              else
+                for (int i = 0; i < bn_own / 64; ++i) load(sm.b[st] + i * kBoxBytes, &mdb, n0 + 64 * i, kb * kBK);
+            } else if (kCtas == 2) {
+              for (int i = 0; i < 2; ++i) load(sm.a[st] + i * kBoxBytes, &ma, m0 + 64 * i, p.v0 + kb * kBK);
+              load(sm.b[st], &mb, 0, kb * p.n_pad + n0);
             } else {
               load(sm.a[st], &ma, 0, kb * p.n_pad + m0);
-              for (int i = 0; i < boxes; ++i) load(sm.b[st] + i * kBoxBytes, &mb, n0 + 64 * i, p.v0 + kb * kBK);
+              for (int i = 0; i < bn_own / 64; ++i) load(sm.b[st] + i * kBoxBytes, &mb, n0 + 64 * i, p.v0 + kb * kBK);
             }
           }
         }
@@ -341,8 +353,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         mma_commit_elect(bar);
     };
     // A step of 16 in K: 32 bytes of each row (K-major), or 16 rows of 128 bytes (MN-major:
-    // back's operands but for dh's A).
-    constexpr bool b_mn = kMode == kBack;
+    // single CTAs' B in back, g in dw, and a pair's weight in dh).
+    constexpr bool b_mn = kMode == kBack && kCtas == 1;
     constexpr uint32_t b_step = b_mn ? 128 : 2;
     const uint64_t b_desc0 = sdesc_sw128(smem_u32(sm.b[0]), b_mn ? kBoxBytes : 16, 1024);
     int fill = 0, tile = 0;
@@ -359,9 +371,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
         const uint32_t d_tmem = tmem + acc * kMaxBN;
-        const bool a_mn = kMode == kBack && tl.dw;
+        const bool a_mn = kMode == kBack && (kCtas == 2 || tl.dw);
         const uint32_t a_step = a_mn ? 128 : 2;
-        const uint32_t idesc = idesc_bf16_f32(kRows, p.bn, a_mn, b_mn);
+        const uint32_t idesc = idesc_bf16_f32(kRows, work.bn(p, tl), a_mn, b_mn);
         const uint64_t a_desc0 = sdesc_sw128(smem_u32(sm.a[0]), a_mn ? kBoxBytes : 16, 1024);
         for (int kb = tl.k0; kb < tl.k1; ++kb, ++fill) {
           const int st = fill % kStages;
@@ -437,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t base = tmem + lane_base + acc * kMaxBN;
         const int row = tl.m * kRows + rank * kBM + t_row;
         float ts = 0.f;  // stats: this tile's terms, relative to m
-        const int groups = p.bn / 64;
+        const int groups = work.bn(p, tl) / 64;
         if (half >= groups) release(acc);
         // 64 columns at a time: two loads and one wait, and arithmetic enough without a
         // dependence that two warps a scheduler keep it busy.
@@ -457,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           if (g + 2 >= groups) release(acc);
-          const int col0 = (kMode == kGrad ? p.v0 : 0) + tl.n * p.bn + 64 * g;
+          const int col0 = (kMode == kGrad ? p.v0 : 0) + tl.n * work.bn(p, tl) + 64 * g;
           if (kMode == kStats) {
             if (static_cast<unsigned>(target - col0) < 64u) {
               float xt = x[0];
@@ -545,8 +557,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               __syncwarp();
             };
             if (kMode == kBack && !tl.dw) {
-              // 32 columns of fp32 a buffer.
-              const int y = tl.split * work.row_blocks * kRows + r0;
+              // 32 columns of fp32 a buffer. The splits' sums lie behind each other: a pair's, whose
+              // tile is transposed, along the columns.
+              const int behind = tl.split * work.row_blocks * kRows;
+              const int x0 = col0 + (kCtas == 2 ? behind : 0), y = r0 + (kCtas == 2 ? 0 : behind);
 #pragma unroll
               for (int c = 0; c < 2; ++c) {
                 free_again();
@@ -555,11 +569,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                   *reinterpret_cast<float4*>(dst + ((e ^ (lane & 7)) << 4)) =
                       make_float4(x[32 * c + 4 * e], x[32 * c + 4 * e + 1], x[32 * c + 4 * e + 2], x[32 * c + 4 * e + 3]);
                 filled([&] {
-                  if (col0 + 32 * c >= p.dh_cols) return;
+                  if (kCtas == 1 && x0 + 32 * c >= p.dh_cols) return;
                   if (!p.add)
-                    tma_store_2d(&mo, buf, col0 + 32 * c, y);
+                    tma_store_2d(&mo, buf, x0 + 32 * c, y);
                   else if (tl.k1 > tl.k0)
-                    tma_add_2d(&mo, buf, col0 + 32 * c, y);
+                    tma_add_2d(&mo, buf, x0 + 32 * c, y);
                 });
               }
             } else {
@@ -617,6 +631,9 @@ struct GatherParams {
   float* to_lse2;
   float* to_dloss;
   uint4* to_hidden;     // [., d_pad]
+  int* origin;          // pairs' gradients: the row of each scored one
+  __nv_bfloat16* d_hidden;  // pairs' gradients: 0 for rows that are not scored (may be null)
+  int64_t s_dhidden;
   float* loss;          // loss only: 0 for rows that are not scored
   float* lse_out;
   int block_rows;       // rows of a tile
@@ -658,6 +675,20 @@ __device__ int choose_splits(const GatherParams& p, int n) {
   return splits;
 }
 
+__device__ __forceinline__ void store_bf16x8(__nv_bfloat16* dst, uint4 v, bool aligned) {
+  if (aligned) {
+    *reinterpret_cast<uint4*>(dst) = v;
+    return;
+  }
+  unsigned short* e = reinterpret_cast<unsigned short*>(dst);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    e[2 * k] = static_cast<unsigned short>(w[k] & 0xFFFFu);
+    e[2 * k + 1] = static_cast<unsigned short>(w[k] >> 16);
+  }
+}
+
 __device__ int block_count(int v, int* sums) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -674,7 +705,7 @@ __device__ int block_count(int v, int* sums) {
 // last one knows their number and what has to be behind them.
 __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const GatherParams p) {
   __shared__ int sums[kGatherThreads / 32];
-  __shared__ int source[kGatherThreads];
+  __shared__ int source[kGatherThreads], others[kGatherThreads];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   wait_for_previous();
   const int64_t r0 = static_cast<int64_t>(blockIdx.x) * p.rows_per_cta;
@@ -703,12 +734,14 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
     if (on) {
       source[at] = static_cast<int>(r - base);
       p.to_target[before + at] = t;
+      if (p.origin) p.origin[before + at] = static_cast<int>(r);
       if (p.to_lse2) {
         p.to_lse2[before + at] = p.lse[r] * kLog2e;
         p.to_dloss[before + at] = p.dloss[r];
       }
     }
     if (r < r1) {
+      if (!on) others[threadIdx.x - at] = static_cast<int>(threadIdx.x);
       p.place[r] = on ? before + at : -1;
       if (!on && p.loss) {
         p.loss[r] = 0.f;
@@ -740,6 +773,14 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
       for (int k = 0; k < kLoads; ++k)
         if (i0 + k * kGatherThreads < words) p.to_hidden[static_cast<int64_t>(before) * vecs + i0 + k * kGatherThreads] = v[k];
     }
+    if (p.d_hidden) {
+      const int rows = static_cast<int>(r1 - base < kGatherThreads ? r1 - base : kGatherThreads) - total;
+      const bool whole = ((reinterpret_cast<uintptr_t>(p.d_hidden) | static_cast<uintptr_t>(p.s_dhidden * 2)) & 15) == 0;
+      for (int64_t i = threadIdx.x; i < static_cast<int64_t>(rows) * full; i += kGatherThreads) {
+        const int row = static_cast<int>(i / full), col = static_cast<int>(i - static_cast<int64_t>(row) * full);
+        store_bf16x8(p.d_hidden + (base + others[row]) * p.s_dhidden + 8 * col, make_uint4(0, 0, 0, 0), whole);
+      }
+    }
     before += total;
   }
   if (blockIdx.x != gridDim.x - 1) return;
@@ -761,6 +802,35 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
 #pragma unroll 4
   for (int64_t i = static_cast<int64_t>(n) * vecs + threadIdx.x; i < rows_end * vecs; i += kGatherThreads)
     p.to_hidden[i] = make_uint4(0, 0, 0, 0);
+}
+
+// The hidden states of the scored rows transposed, [d_pad, n_pad], for a pair's dw: 64 x 64
+// a CTA (what lies behind the last 64 rows is left as it is).
+constexpr int kTransposeThreads = 256;
+__global__ void __launch_bounds__(kTransposeThreads)
+    loss_transpose_kernel(const Plan* plan, const uint4* hidden, int d_pad, int n_pad, uint4* out) {
+  __shared__ uint32_t tile[64][33];  // rows of 32 pairs of columns
+  wait_for_previous();
+  const int r0 = blockIdx.x * 64, d0 = blockIdx.y * 64, r = threadIdx.x >> 3, v = threadIdx.x & 7;
+  if (r0 >= plan->n) return;
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    const uint4 u = hidden[(static_cast<int64_t>(r0 + r + i) * d_pad + d0) / 8 + v];
+    tile[r + i][4 * v] = u.x;
+    tile[r + i][4 * v + 1] = u.y;
+    tile[r + i][4 * v + 2] = u.z;
+    tile[r + i][4 * v + 3] = u.w;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    const int c = r + i, shift = (c & 1) * 16;
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      w[k] = (tile[8 * v + 2 * k][c >> 1] >> shift & 0xFFFFu) | (tile[8 * v + 2 * k + 1][c >> 1] >> shift) << 16;
+    out[(static_cast<int64_t>(d0 + c) * n_pad + r0) / 8 + v] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
 }
 
 // ---------------------------------------------------------------- results
@@ -838,6 +908,35 @@ __global__ void __launch_bounds__(kFinishThreads)
   }
 }
 
+// The same from a pair's sums, [., columns] with a row for each column of d_hidden and the
+// splits behind each other, whole blocks of rows apart: 32 rows x 64 columns a CTA.
+constexpr int kTurnThreads = 256;
+__global__ void __launch_bounds__(kTurnThreads)
+    loss_dhidden_turn_kernel(const Plan* plan, const int* origin, const float* part, int block_rows, int d, int64_t columns,
+                             __nv_bfloat16* out, int64_t s_out, int aligned) {
+  __shared__ float tile[64][33];
+  wait_for_previous();
+  const int n = plan->n, splits = plan->splits, r0 = blockIdx.x * 32, d0 = blockIdx.y * 64;
+  if (r0 >= n) return;
+  const int64_t step = static_cast<int64_t>((n + block_rows - 1) / block_rows) * block_rows;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float a[8] = {};
+  for (int s = 0; s < splits; ++s) {
+    const float* src = part + (d0 + warp) * columns + s * step + r0 + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] += src[8 * i * columns];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) tile[warp + 8 * i][lane] = a[i];
+  __syncthreads();
+  const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+  if (r0 + r >= n || d0 + c >= d) return;
+  uint32_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = pack_bf16x2(tile[c + 2 * k][r], tile[c + 2 * k + 1][r]);
+  store_bf16x8(out + static_cast<int64_t>(origin[r0 + r]) * s_out + d0 + c, make_uint4(w[0], w[1], w[2], w[3]), aligned);
+}
+
 // ---------------------------------------------------------------- host side
 
 int sm_count() {
@@ -907,8 +1006,9 @@ Team team_for(int64_t N, int64_t d, int64_t least_d) {
 // Places of the workspace, from its start.
 struct Layout {
   int64_t n_pad, d_pad;
-  size_t plan, place, target, lse2, dloss, hidden, x_target, part, sums, g;  // byte offsets
-  size_t sums_rows;  // gradients: rows of fp32 sums
+  size_t plan, place, target, lse2, dloss, hidden, x_target, part, origin, turned, sums, g;  // byte offsets
+  int64_t sums_rows;  // gradients: rows of fp32 sums (pairs: columns, of d_rows rows)
+  int64_t d_rows;
 };
 
 size_t take(size_t* at, size_t bytes) {
@@ -932,12 +1032,16 @@ Layout layout_of(int64_t N, int64_t d, bool grad) {
   } else {
     l.lse2 = take(&at, l.n_pad * 4);
     l.dloss = take(&at, l.n_pad * 4);
+    if (N >= kPairRows && d >= kPairGradWidth) {
+      l.origin = take(&at, l.n_pad * 4);
+      l.turned = take(&at, l.n_pad * l.d_pad * 2);
+    }
     // Room for splits of dh: up to 32 of them, 192 MB, and one in any case.
-    const int64_t most = (int64_t{192} << 20) / (l.d_pad * 4) / (2 * kBM) * (2 * kBM);
-    int64_t rows = 32 * l.n_pad < most ? 32 * l.n_pad : most;
-    if (rows < l.n_pad) rows = l.n_pad;
-    l.sums_rows = static_cast<size_t>(rows);
-    l.sums = take(&at, l.sums_rows * l.d_pad * 4);
+    l.d_rows = (d + 2 * kBM - 1) / (2 * kBM) * (2 * kBM);
+    const int64_t most = (int64_t{192} << 20) / (l.d_rows * 4) / (2 * kBM) * (2 * kBM);
+    l.sums_rows = 32 * l.n_pad < most ? 32 * l.n_pad : most;
+    if (l.sums_rows < l.n_pad) l.sums_rows = l.n_pad;
+    l.sums = take(&at, static_cast<size_t>(l.sums_rows) * l.d_rows * 4);
   }
   l.g = at;
   return l;
@@ -1044,11 +1148,18 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   g.dloss = a.dloss;
   g.to_lse2 = reinterpret_cast<float*>(ws + l.lse2);
   g.to_dloss = reinterpret_cast<float*>(ws + l.dloss);
-  g.tiles = d_tiles;
+  const bool pairs = team.ctas == 2;
+  const int dh_tiles = pairs ? static_cast<int>(l.d_rows / (2 * kBM)) : d_tiles;
+  g.tiles = dh_tiles;
   g.kblocks = static_cast<int>((first + kBK - 1) / kBK);
   g.dw_tiles = a.d_weight ? static_cast<int>((first + block_rows - 1) / block_rows) * d_tiles : 0;
   g.workers = team.workers;
   g.max_rows = l.sums_rows > 0x7FFFFFFF ? 0x7FFFFFFF : static_cast<int>(l.sums_rows);
+  if (pairs) {
+    g.origin = reinterpret_cast<int*>(ws + l.origin);
+    g.d_hidden = static_cast<__nv_bfloat16*>(a.d_hidden);
+    g.s_dhidden = a.s_dhidden;
+  }
   int st;
   if ((st = launch_gather(a, l, g, stream)) != DLM_OK) return st;
 
@@ -1057,11 +1168,16 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   if ((st = make_matrix_map(&grad.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, kBM)) != DLM_OK) return st;
   if ((st = make_matrix_map(&grad.b, a.weight, true, a.V, a.d, a.s_weight, bn_v / team.ctas)) != DLM_OK) return st;
   if ((st = make_matrix_map(&grad.out, ws + l.g, true, panel_rows, 64, 64, 32)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&back.a, ws + l.g, true, panel_rows, 64, 64, kBM)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&back.b, a.weight, true, a.V, a.d, a.s_weight, 64)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&back.out, ws + l.sums, false, static_cast<int64_t>(l.sums_rows), l.d_pad, l.d_pad, 32)) != DLM_OK) return st;
+  // dh: g times the weight, or, a pair's, the weight transposed times g transposed.
+  if ((st = make_matrix_map(pairs ? &back.b : &back.a, ws + l.g, true, panel_rows, 64, 64, kBM)) != DLM_OK) return st;
+  if ((st = make_matrix_map(pairs ? &back.a : &back.b, a.weight, true, a.V, a.d, a.s_weight, 64)) != DLM_OK) return st;
+  st = pairs ? make_matrix_map(&back.out, ws + l.sums, false, l.d_rows, l.sums_rows, l.sums_rows, 32)
+             : make_matrix_map(&back.out, ws + l.sums, false, l.sums_rows, l.d_pad, l.d_pad, 32);
+  if (st != DLM_OK) return st;
   if ((st = make_matrix_map(&back.dw_a, ws + l.g, true, panel_rows, 64, 64, 64)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&back.dw_b, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, 64)) != DLM_OK) return st;
+  st = pairs ? make_matrix_map(&back.dw_b, ws + l.turned, true, l.d_pad, l.n_pad, l.n_pad, bn_d / 2)
+             : make_matrix_map(&back.dw_b, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, 64);
+  if (st != DLM_OK) return st;
   if (a.d_weight && (st = make_matrix_map(&back.dw_out, a.d_weight, true, a.V, a.d, a.s_dweight, 32)) != DLM_OK) return st;
 
   Params p = common_params(a, l);
@@ -1073,6 +1189,14 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   p.dw_rows = p.V;
   p.dw_cols = static_cast<int>(a.d);
   p.dh_cols = static_cast<int>(l.d_pad);
+  p.dh_tiles = dh_tiles;
+  if (pairs && a.d_weight) {
+    const cudaError_t e = launch_overlapped(
+        loss_transpose_kernel, dim3(static_cast<unsigned>(l.n_pad / 64), static_cast<unsigned>(l.d_pad / 64)), kTransposeThreads, 0,
+        stream, 1, true, p.plan, reinterpret_cast<const uint4*>(ws + l.hidden), static_cast<int>(l.d_pad), p.n_pad,
+        reinterpret_cast<uint4*>(ws + l.turned));
+    if (e != cudaSuccess) return fail(DLM_ERR_CUDA, "hidden states launch: %s", cudaGetErrorString(e));
+  }
   for (int64_t v0 = 0; v0 < a.V; v0 += cols) {
     const int64_t vc = a.V - v0 < cols ? a.V - v0 : cols;
     p.v0 = static_cast<int>(v0);
@@ -1088,6 +1212,14 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
     if ((st = launch_product<kBack>(team.ctas, back, p, team.workers, team.workers, stream)) != DLM_OK) return st;
   }
   if (!a.d_hidden) return DLM_OK;
+  if (pairs) {
+    const bool whole = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 15) == 0;
+    const cudaError_t e = launch_overlapped(
+        loss_dhidden_turn_kernel, dim3(static_cast<unsigned>((a.N + 31) / 32), static_cast<unsigned>((a.d + 63) / 64)), kTurnThreads, 0,
+        stream, 1, true, p.plan, g.origin, reinterpret_cast<const float*>(ws + l.sums), block_rows, static_cast<int>(a.d),
+        l.sums_rows, static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden, whole ? 1 : 0);
+    return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "hidden gradient launch: %s", cudaGetErrorString(e));
+  }
   const int64_t vecs = a.N * (a.d / 4);
   const int64_t want = (vecs + kFinishThreads - 1) / kFinishThreads, most = static_cast<int64_t>(sm_count()) * 16;
   const bool aligned = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 7) == 0;

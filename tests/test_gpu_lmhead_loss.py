@@ -96,7 +96,7 @@ def fp64_lse(h, w, t):
 
 SIZES = [(1, 1, 8), (3, 7, 8), (1, 300, 64), (128, 256, 64), (130, 1000, 72), (129, 257, 200), (300, 2049, 128), (64, 4099, 512),
          (257, 1024, 320), (5, 151, 2048), (1000, 513, 264), (90, 40000, 64), (520, 1000, 72), (2000, 300, 64), (769, 5000, 128),
-         (1025, 2600, 512), (600, 1100, 1024), (513, 300, 2048)]
+         (1025, 2600, 512), (600, 1100, 1024), (513, 300, 2048), (1300, 700, 520)]
 
 
 @pytest.mark.parametrize("scored", ["all", "half", "none", "first", "last"])
@@ -145,19 +145,20 @@ def test_pieces_and_single_gradients(N, V, d, piece):
     assert torch.equal(dw, dw1) and B.device_error() == 0
 
 
-@pytest.mark.parametrize("offset,row,wrow", [(0, 72, 72), (1, 64, 64), (3, 71, 80), (8, 80, 64)])
-def test_strides_and_alignment(offset, row, wrow):
+@pytest.mark.parametrize("L,d", [(35, 64), (100, 512)], ids=["single_ctas", "pairs"])
+@pytest.mark.parametrize("offset,gap,wgap", [(0, 8, 8), (1, 0, 0), (3, 7, 16), (8, 16, 0)])
+def test_strides_and_alignment(offset, gap, wgap, L, d):
     from paper_2608_02625_gb300 import binding as B
-    N, V, d = 6 * 35, 700, 64
+    N, V, row, wrow = 6 * L, 700, d + gap, d + wgap
     h, w, t, dl = inputs(N, V, d, seed=2)
     gd = Guarded()
-    hs, ws_, ts = gd.like(h.view(6, 35, d), offset=offset, row=row), gd.like(w, row=wrow), t.view(6, 35)
-    loss, lse = gd.empty(6, 35), gd.empty(6, 35)
+    hs, ws_, ts = gd.like(h.view(6, L, d), offset=offset, row=row), gd.like(w, row=wrow), t.view(6, L)
+    loss, lse = gd.empty(6, L), gd.empty(6, L)
     B.dlm_lmhead_loss(hs, ws_, ts, loss, lse, ws_loss(N, d))
     gd.check()
     check_loss(h, w, t, loss.view(-1), lse.view(-1))
-    dh, dw = gd.empty(6, 35, d, dtype=BF, offset=offset, row=row), gd.empty(V, d, dtype=BF, row=wrow)
-    B.dlm_lmhead_loss_grad(hs, ws_, ts, lse, dl.view(6, 35), dh, dw, ws_grad(N, V, d))
+    dh, dw = gd.empty(6, L, d, dtype=BF, offset=offset, row=row), gd.empty(V, d, dtype=BF, row=wrow)
+    B.dlm_lmhead_loss_grad(hs, ws_, ts, lse, dl.view(6, L), dh, dw, ws_grad(N, V, d))
     gd.check()
     check_grad(h, w, t, lse.view(-1), dl, dh.reshape(N, d), dw)
 
