@@ -56,10 +56,13 @@ constexpr int kBoxBytes = 64 * 128;          // an MN-major box: 64 K rows of 64
 constexpr uint32_t kTmemCols = 2 * kMaxBN;   // two accumulators
 constexpr float kLog2e = 1.4426950408889634f;
 // From how many rows, and which width, CTAs work in pairs. V = 151552, graph us, single and
-// pairs: loss 512 x 2048 225, 214; 4096 x 1024 778, 741; 4096 x 512 400, 419 (the epilogues
-// of both wait for the slower); gradients 256 x 2048 460, 574 (tiles of 256 rows leave too
-// few); 512 x 2048 779, 716; 4096 x 512 1452, 1383; 4096 x 64 661, 718.
-constexpr int64_t kPairRows = 512, kPairLossWidth = 1024, kPairGradWidth = 512;
+// pairs: loss 512 x 2048 225, 214; 384 x 2048 181, 206 (tiles of 256 rows leave too few, and
+// the second is half empty); 4096 x 1024 778, 741; 4096 x 512 400, 419 (the epilogues of both
+// wait for the slower); gradients 384 x 2048 626, 631; 512 x 2048 712, 684; 4096 x 512 1452,
+// 1300; 4096 x 256 857, 803; 2048 x 256 (V = 20000) 82, 83; 4096 x 64 661, 718.
+constexpr int64_t kPairRows = 512;
+bool pairs_for_loss(int64_t N, int64_t d) { return N >= kPairRows && d >= 1024; }
+bool pairs_for_gradients(int64_t N, int64_t d) { return N >= kPairRows && d >= (N >= 4096 ? 256 : 512); }
 
 enum Mode { kStats, kGrad, kBack };
 
@@ -990,9 +993,9 @@ struct Team {
   int ctas, workers;
 };
 
-Team team_for(int64_t N, int64_t d, int64_t least_d) {
+Team team_for(bool pairs) {
   const int sms = sm_count();
-  if (N >= kPairRows && d >= least_d) {
+  if (pairs) {
     const auto kernel = loss_product_kernel<kBack, 2>;  // the same shared memory in every mode
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<2>())) == cudaSuccess) {
       const int pairs = active_clusters(reinterpret_cast<const void*>(kernel), 2, kThreads, smem_bytes<2>());
@@ -1032,7 +1035,7 @@ Layout layout_of(int64_t N, int64_t d, bool grad) {
   } else {
     l.lse2 = take(&at, l.n_pad * 4);
     l.dloss = take(&at, l.n_pad * 4);
-    if (N >= kPairRows && d >= kPairGradWidth) {
+    if (pairs_for_gradients(N, d)) {
       l.origin = take(&at, l.n_pad * 4);
       l.turned = take(&at, l.n_pad * l.d_pad * 2);
     }
@@ -1096,7 +1099,7 @@ size_t loss_grad_workspace_bytes(int64_t N, int64_t V, int64_t d, int64_t piece)
 
 int launch_loss(const LossArgs& a, cudaStream_t stream) {
   const Layout l = layout_of(a.N, a.d, false);
-  const Team team = team_for(a.N, a.d, kPairLossWidth);
+  const Team team = team_for(pairs_for_loss(a.N, a.d));
   const int block_rows = kBM * team.ctas;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   GatherParams g = {};
@@ -1127,7 +1130,7 @@ int launch_loss(const LossArgs& a, cudaStream_t stream) {
 
 int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   const Layout l = layout_of(a.N, a.d, true);
-  const Team team = team_for(a.N, a.d, kPairGradWidth);
+  const Team team = team_for(pairs_for_gradients(a.N, a.d));
   const int block_rows = kBM * team.ctas;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   const int64_t all = (a.V + 255) / 256 * 256;

@@ -96,7 +96,7 @@ def fp64_lse(h, w, t):
 
 SIZES = [(1, 1, 8), (3, 7, 8), (1, 300, 64), (128, 256, 64), (130, 1000, 72), (129, 257, 200), (300, 2049, 128), (64, 4099, 512),
          (257, 1024, 320), (5, 151, 2048), (1000, 513, 264), (90, 40000, 64), (520, 1000, 72), (2000, 300, 64), (769, 5000, 128),
-         (1025, 2600, 512), (600, 1100, 1024), (513, 300, 2048), (1300, 700, 520)]
+         (1025, 2600, 512), (600, 1100, 1024), (513, 300, 2048), (1300, 700, 520), (4200, 600, 264)]
 
 
 @pytest.mark.parametrize("scored", ["all", "half", "none", "first", "last"])
