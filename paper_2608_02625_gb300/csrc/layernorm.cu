@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) no
   float* w = reinterpret_cast<float*>(smem + p.ring);
   float* b = w + width;
   const float inv_d = 1.f / static_cast<float>(d);
-  const bool full = width == d;  // every element held is one of the row
+  const bool full = VEC > 1 && width == d;  // every element held is one of the row
   Src::clear(smem, p.ring, tid, G, d);
   wait_for_previous();
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) nor
   uint8_t* ring = smem + (VEC > 1 ? 16 * threadIdx.x : g * row_room(d, sizeof(T)));  // x, and dy half a stage on
   float* w = reinterpret_cast<float*>(smem + p.ring);
   const float inv_d = 1.f / static_cast<float>(d);
-  const bool full = width == d;
+  const bool full = VEC > 1 && width == d;
   Src::clear(smem, p.ring, tid, G, d);
   wait_for_previous();
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
@@ -402,8 +402,9 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) nor
     float s[2] = {s0.x + s0.y, s1.x + s1.y};
     row_sums<2>(s, G, red[parity]);
     if (row < p.N) {
-      const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
-      const float2 n1 = make_float2(-c1, -c1), n2 = make_float2(-c2, -c2);
+      // dx = dout (w rstd) + ((x - mean) (-rstd^2 c2) - rstd c1)
+      const float c1 = -rstd * (s[0] * inv_d), c2 = -rstd * (rstd * (s[1] * inv_d));
+      const float2 n1 = make_float2(c1, c1), n2 = make_float2(c2, c2);
       T* o = static_cast<T*>(p.out) + row * p.s_out + tid * VEC;
 #pragma unroll
       for (int j = 0; j < kElems; j += kPair) {
@@ -411,9 +412,8 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) nor
         get(j, x, dy, wv);
 #pragma unroll
         for (int k = 0; k < kPair; k += 2) {
-          const float2 xhat = fmul2(fadd2(make_float2(x[k], x[k + 1]), m2), r2);
-          const float2 a = fmul2(make_float2(dy[k], dy[k + 1]), make_float2(wv[k], wv[k + 1]));
-          const float2 y = fmul2(r2, fadd2(a, ffma2(xhat, n2, n1)));
+          const float2 rest = ffma2(fadd2(make_float2(x[k], x[k + 1]), m2), n2, n1);
+          const float2 y = ffma2(make_float2(dy[k], dy[k + 1]), fmul2(make_float2(wv[k], wv[k + 1]), r2), rest);
           x[k] = y.x;
           x[k + 1] = y.y;
         }
