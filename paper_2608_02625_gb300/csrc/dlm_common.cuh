@@ -55,7 +55,9 @@ constexpr bool kCheckBounds = false;
 // as a running kernel's leave, are spread unevenly over the SMs (400 vocabulary
 // rows after 400 others: 30.8 us where each CTA let the next kernel start at once,
 // 21.7 us evenly spread). The update, short and of one CTA a sequence, does so as
-// soon as it may, bf16 attention once a CTA's last loads are issued.
+// soon as it may, bf16 attention and the loss's products once a CTA's last loads are
+// issued (gradients of 64 rows 361 -> 333 us; layer norm and clipping, which do it when
+// their CTAs end, lost 2 % so).
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Lets the next kernel of the stream take free places on the SMs once every
 // block of this one has got here or ended.

@@ -325,6 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
+    launch_dependents();
     // Teardown: every copy issued lands before the block exits. A single CTA waits for its
     // barriers; of a pair, whose copies complete on the leader's, each waits for the MMAs
     // that read its stages, and where something has given up (the other CTA's copies, on
@@ -711,6 +712,7 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
   __shared__ int source[kGatherThreads], others[kGatherThreads];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   wait_for_previous();
+  launch_dependents();
   const int64_t r0 = static_cast<int64_t>(blockIdx.x) * p.rows_per_cta;
   const int64_t r1 = r0 + p.rows_per_cta < p.N ? r0 + p.rows_per_cta : p.N;
   const auto scored = [&](int t) { return static_cast<unsigned>(t) < static_cast<unsigned>(p.V); };
@@ -814,6 +816,7 @@ __global__ void __launch_bounds__(kTransposeThreads)
     loss_transpose_kernel(const Plan* plan, const uint4* hidden, int d_pad, int n_pad, uint4* out) {
   __shared__ uint32_t tile[64][33];  // rows of 32 pairs of columns
   wait_for_previous();
+  launch_dependents();
   const int r0 = blockIdx.x * 64, d0 = blockIdx.y * 64, r = threadIdx.x >> 3, v = threadIdx.x & 7;
   if (r0 >= plan->n) return;
 #pragma unroll
