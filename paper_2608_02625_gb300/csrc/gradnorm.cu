@@ -16,8 +16,8 @@
 // as kernel parameters, so a captured call needs no copy of a table.
 //
 // HBM bounds it: two reads and a write of everything. 310 M bf16 elements (621 MB): the
-// squares 91 us, the scaling 190 (eight CTAs an SM; four: 98 and 199), of 274 at the
-// copy rate.
+// squares 91 us (eight CTAs an SM; four: 98), the scaling about 200 (three CTAs, whose
+// eight vectors a thread in flight take 80 registers), of 274 at the copy rate.
 #include <cuda_bf16.h>
 
 #include <cstdint>
@@ -30,6 +30,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnit = kThreads * 8;  // chunks are multiples of this many elements
+constexpr int kScaleCtas = 3 * 152;
 
 struct Tensor {
   const void* in;
@@ -249,11 +250,14 @@ int launch_phase(const GradArgs& a, bool scale_phase, cudaStream_t stream) {
     int ctas = tab.chunks < kGradParts ? tab.chunks : kGradParts;
     if (ctas < 1) ctas = 1;
     tab.part = a.workspace + written;
-    written += ctas;
+    written += ctas;  // (of the first phase)
     tab.parts = a.workspace;
     tab.n_parts = a.parts;
     tab.max_norm = a.max_norm;
     tab.norm = l == 0 ? a.norm : nullptr;
+    // As many CTAs as run at once: a second wave would wait for the first one's chunks (53 MB:
+    // 49 us with 1216, 34).
+    if (scale_phase && ctas > kScaleCtas) ctas = kScaleCtas;
     if (scale_phase && !a.scale) {
       tab.chunks = 0;
       ctas = 1;
