@@ -1094,7 +1094,7 @@ size_t loss_grad_workspace_bytes(int64_t N, int64_t V, int64_t d, int64_t piece)
   const Layout l = layout_of(N, d, true);
   const int64_t all = (V + 255) / 256 * 256;
   // 2 GB of g unless told otherwise, but not under 1024 columns: the fewer pieces, the fewer tails.
-  int64_t cols = piece > 0 ? (piece + 255) / 256 * 256 : (int64_t{1} << 31) / (l.n_pad * 2) / 256 * 256;
+  int64_t cols = piece > all ? all : piece > 0 ? (piece + 255) / 256 * 256 : (int64_t{1} << 31) / (l.n_pad * 2) / 256 * 256;
   if (piece <= 0 && cols < 1024) cols = 1024;
   if (cols > all) cols = all;
   return l.g + static_cast<size_t>(l.n_pad) * cols * 2;

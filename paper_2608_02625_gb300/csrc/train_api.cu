@@ -227,7 +227,7 @@ int dlm_layer_norm(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tens
 }
 
 size_t dlm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t d) {
-  return rows > 0 && d > 0 ? norm_grad_workspace_bytes(rows, d) : 0;
+  return rows > 0 && d > 0 && d <= kMostNormWidth ? norm_grad_workspace_bytes(rows, d) : 0;
 }
 
 int dlm_layer_norm_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* mean,

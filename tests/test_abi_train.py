@@ -111,6 +111,8 @@ def test_workspace_sizes():
     assert B.dlm_layer_norm_grad_workspace_bytes(0, 64) == 0
     assert B.dlm_layer_norm_grad_workspace_bytes(6, 64) == 6 * 2 * 64 * 4
     assert B.dlm_layer_norm_grad_workspace_bytes(10 ** 6, 64) == B.dlm_layer_norm_grad_workspace_bytes(10 ** 7, 64)
+    assert B.dlm_layer_norm_grad_workspace_bytes(10 ** 6, 2 ** 24) > 0
+    assert B.dlm_layer_norm_grad_workspace_bytes(6, 2 ** 24 + 1) == B.dlm_layer_norm_grad_workspace_bytes(6, 2 ** 62) == 0
     assert B.dlm_clip_grad_norm_workspace_bytes() > 0
 
 
@@ -176,3 +178,4 @@ def test_loss_workspace_sizes():
     assert size(128, 10 ** 5, 64, 257) == size(128, 10 ** 5, 64, 512)
     assert size(128, 300, 64, 10 ** 6) == size(128, 300, 64, 300)
     assert size(16384, 151552, 2048) < 3 * 2 ** 30
+    assert size(128, 300, 64, 2 ** 63 - 1) == size(128, 300, 64, 300)
