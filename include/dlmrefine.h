@@ -378,7 +378,8 @@ size_t dlm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t d);
  *                contents needed; calls sharing it must not overlap on the GPU.
  * The norm is exact to fp32 rounding over the whole range of the inputs (squares that
  * leave fp32's range are summed in fp64) and summed in a fixed order. A NaN makes norm
- * and every output NaN; an infinity makes norm infinite and finite elements 0.
+ * and every output NaN; an infinity makes norm infinite and finite elements 0 (with an
+ * infinite max_norm too, the factor is inf / inf: every output NaN).
  */
 int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t count, float max_norm, dlm_tensor* norm,
                        void* workspace, size_t workspace_bytes);

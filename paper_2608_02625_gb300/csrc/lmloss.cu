@@ -1066,9 +1066,9 @@ int launch_gather(const LossArgs& a, const Layout& l, GatherParams g, cudaStream
   g.place = reinterpret_cast<int*>(ws + l.place);
   g.to_target = reinterpret_cast<int*>(ws + l.target);
   g.to_hidden = reinterpret_cast<uint4*>(ws + l.hidden);
-  // As many CTAs as run at once, but 256 rows each at most: every CTA counts the rows before its own.
+  // No more CTAs than run at once: every CTA counts the rows before its own.
   int64_t rows = 1;
-  while (rows < kGatherThreads && a.N > rows * 1024) rows *= 2;
+  while (a.N > rows * 1024) rows *= 2;
   g.rows_per_cta = static_cast<int>(rows);
   const cudaError_t e = launch_overlapped(loss_gather_kernel, dim3(static_cast<unsigned>((a.N + rows - 1) / rows)), kGatherThreads, 0,
                                           stream, 1, true, g);

@@ -122,6 +122,15 @@ def test_not_finite():
             assert int(torch.isnan(outs[0]).sum()) == 1
 
 
+def test_an_infinity_under_an_infinite_limit():
+    from paper_2608_02625_gb300 import binding as B
+    grads = make([5000, 40], [BF, F32], seed=4)
+    grads[0][77] = float("inf")
+    outs, norm = [torch.empty_like(g) for g in grads], torch.empty(1, device=dev())
+    B.dlm_clip_grad_norm(grads, outs, float("inf"), norm, workspace())
+    assert float(norm) == float("inf") and all(bool(torch.isnan(o).all()) for o in outs)
+
+
 def test_no_tensors():
     from paper_2608_02625_gb300 import binding as B
     for outs in (None, []):

@@ -126,6 +126,23 @@ def test_gradients(N, V, d, scored):
     check_grad(h, w, t, lse, dl, dh, dw, f"{N}x{V}x{d} {scored}")
 
 
+@pytest.mark.parametrize("scored", ["half", "last"])
+def test_more_rows_than_the_gathering_ctas_take_at_once(scored):
+    from paper_2608_02625_gb300 import binding as B
+    N, V, d = 270_003, 40, 16
+    h, w, t, dl = inputs(N, V, d, seed=6, scored=scored)
+    gd = Guarded()
+    loss, lse, dh, dw = gd.empty(N), gd.empty(N), gd.empty(N, d, dtype=BF), gd.empty(V, d, dtype=BF)
+    B.dlm_lmhead_loss(h, w, t, loss, lse, ws_loss(N, d))
+    gd.check()
+    check_loss(h, w, t, loss, lse)
+    lse = fp64_lse(h, w, t)
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh, dw, ws_grad(N, V, d))
+    gd.check()
+    assert B.device_error() == 0
+    check_grad(h, w, t, lse, dl, dh, dw)
+
+
 @pytest.mark.parametrize("N,V,d,piece", [(300, 2049, 128, 256), (300, 2049, 128, 1024), (64, 4099, 512, 1024), (20, 1300, 72, 512),
                                          (700, 900, 64, 256), (1500, 3000, 320, 1024), (700, 2000, 512, 512)])
 def test_pieces_and_single_gradients(N, V, d, piece):
