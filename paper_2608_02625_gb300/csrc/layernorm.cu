@@ -205,8 +205,8 @@ __device__ __forceinline__ int param_place(int e, int width) {
 
 // VEC: elements per load (16 bytes, or one where a base, a stride or d is not a multiple
 // of that); NV: loads per thread, row and tensor. CTAs on an SM by the registers that the
-// elements a thread holds take; the ring's depth by the shared memory of each.
-template <int VEC, int NV, bool kGradient>
+// elements a thread holds take; the ring's depth by the shared memory of each, kShort: a row less.
+template <int VEC, int NV, bool kGradient, bool kShort>
 struct Held {
   static constexpr int kElems = VEC * NV;
   static constexpr int kTensors = kGradient ? 2 : 1;
@@ -215,7 +215,7 @@ struct Held {
   static constexpr int kCtas = VEC == 1 ? (kElems <= 8 ? 4 : 2)
                                : kElems <= 8 ? 4 : !kGradient && kStage <= 16384 ? 3 : kShared / 2 / kStage >= 2 ? 2 : 1;
   static constexpr int kRoom = kShared / kCtas / kStage;
-  static constexpr int kDepth = VEC == 1 ? (NV <= 4 ? 6 : NV <= 8 ? 4 : 3) : kRoom > 6 ? 6 : kRoom;
+  static constexpr int kDepth = VEC == 1 ? (NV <= 4 ? 6 : NV <= 8 ? 4 : 3) : kRoom > 6 ? 6 : kRoom - (kShort ? 1 : 0);
   static_assert(kDepth >= 2, "a ring of one row waits for every load");
 };
 
@@ -236,9 +236,9 @@ __device__ __forceinline__ void stage_params(const NormParams& p, float* w, floa
   __syncthreads();
 }
 
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) norm_kernel(const NormParams p) {
-  using H = Held<VEC, NV, false>;
+template <typename T, int VEC, int NV, bool kShort>
+__global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false, kShort>::kCtas)) norm_kernel(const NormParams p) {
+  using H = Held<VEC, NV, false, kShort>;
   using Src = Row<T, VEC, NV>;
   constexpr int kElems = H::kElems, kDepth = H::kDepth;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -327,9 +327,9 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, false>::kCtas)) no
   fetch_wait<0>();
 }
 
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true>::kCtas)) norm_grad_kernel(const NormParams p) {
-  using H = Held<VEC, NV, true>;
+template <typename T, int VEC, int NV, bool kShort>
+__global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true, kShort>::kCtas)) norm_grad_kernel(const NormParams p) {
+  using H = Held<VEC, NV, true, kShort>;
   using Src = Row<T, VEC, NV>;
   constexpr int kElems = H::kElems, kDepth = H::kDepth;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -613,23 +613,44 @@ bool by_vectors(const void* p, int64_t stride, int esz) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * esz % 16 == 0;
 }
 
-// One CTA for every place on the SMs, or fewer: each walks rows.
-template <typename T, int VEC, int NV, bool kGradient>
-cudaError_t launch_held(NormParams p, int sms, int* parts, cudaStream_t stream) {
-  using H = Held<VEC, NV, kGradient>;
-  const auto kernel = kGradient ? norm_grad_kernel<T, VEC, NV> : norm_kernel<T, VEC, NV>;
-  const int width = held_width(p.G, H::kElems), R = kRowThreads / p.G;
-  p.ring = H::kDepth * (VEC > 1 ? H::kStage : R * row_room(p.d, sizeof(T)) * H::kTensors);
+// Shared memory of a CTA: the ring, and the weights (and biases).
+template <typename H, int VEC>
+size_t held_bytes(bool grad, const NormParams& p, int esz) {
+  const int R = kRowThreads / p.G, width = held_width(p.G, H::kElems);
+  int ring = H::kDepth * (VEC > 1 ? H::kStage : R * row_room(p.d, esz) * H::kTensors);
   // The groups' columns' sums take the ring's place at the end.
   const int unit = H::kDepth * 32;
-  if (kGradient && p.ring < R * width * 4) p.ring = (R * width * 4 + unit - 1) / unit * unit;
-  const size_t smem = p.ring + static_cast<size_t>(width) * 4 * (kGradient ? 1 : 2);
+  if (grad && ring < R * width * 4) ring = (R * width * 4 + unit - 1) / unit * unit;
+  return ring + static_cast<size_t>(width) * 4 * (grad ? 1 : 2);
+}
+
+// CTAs that find room on an SM beside each other (each takes 1 KB for the system, and what
+// is declared in the kernel): the weights of wide rows leave it for fewer than the registers do.
+template <typename H>
+int held_ctas(size_t smem) {
+  const int fit = static_cast<int>(228 * 1024 / (smem + 1024 + 512));
+  return fit < 1 ? 1 : fit < H::kCtas ? fit : H::kCtas;
+}
+
+// One CTA for every place on the SMs, or fewer: each walks rows.
+template <typename T, int VEC, int NV, bool kGradient, bool kShort>
+cudaError_t launch_held(NormParams p, int sms, int* parts, cudaStream_t stream) {
+  using H = Held<VEC, NV, kGradient, kShort>;
+  const size_t smem = held_bytes<H, VEC>(kGradient, p, sizeof(T));
+  if constexpr (!kShort && VEC == 8 && NV > 2) {
+    // A row less in the ring where that leaves room for one more CTA (16384 x 2048 elements as
+    // rows of 8192: 46.4 -> 36.8 us, the gradients 61.6 -> 57.4; fp32 rows gain nothing).
+    using S = Held<VEC, NV, kGradient, true>;
+    if (held_ctas<S>(held_bytes<S, VEC>(kGradient, p, sizeof(T))) > held_ctas<H>(smem))
+      return launch_held<T, VEC, NV, kGradient, true>(p, sms, parts, stream);
+  }
+  const auto kernel = kGradient ? norm_grad_kernel<T, VEC, NV, kShort> : norm_kernel<T, VEC, NV, kShort>;
+  const int R = kRowThreads / p.G;
+  p.ring = static_cast<int>(smem) - held_width(p.G, H::kElems) * 4 * (kGradient ? 1 : 2);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  // The weights of wide rows leave room for fewer CTAs than the registers do.
-  const int fit = static_cast<int>(224 * 1024 / (smem + 1536));
   const int most = norm_max_parts(p.d);
-  int places = sms * (fit < 1 ? 1 : fit < H::kCtas ? fit : H::kCtas);
+  int places = sms * held_ctas<H>(smem);
   if (kGradient && places > most) places = most;
   const int64_t want = (p.N + R - 1) / R;
   *parts = static_cast<int>(want < places ? want : places);
@@ -638,7 +659,7 @@ cudaError_t launch_held(NormParams p, int sms, int* parts, cudaStream_t stream) 
 
 template <typename T, int VEC, int NV>
 cudaError_t launch_shape(bool grad, const NormParams& p, int sms, int* parts, cudaStream_t stream) {
-  return grad ? launch_held<T, VEC, NV, true>(p, sms, parts, stream) : launch_held<T, VEC, NV, false>(p, sms, parts, stream);
+  return grad ? launch_held<T, VEC, NV, true, false>(p, sms, parts, stream) : launch_held<T, VEC, NV, false, false>(p, sms, parts, stream);
 }
 
 template <typename T, int VEC>
@@ -666,11 +687,17 @@ int launch_typed(bool grad, NormParams p, int* parts, cudaStream_t stream) {
   if (p.d > kHeldWidth) {
     e = vec ? launch_wide<T, kVec>(grad, p, sms, parts, stream) : launch_wide<T, 1>(grad, p, sms, parts, stream);
   } else {
-    const Shape s = vec ? shape_of(p.N, p.d / kVec, 32 / kVec, sms) : shape_of(p.N, (p.d + 3) / 4 * 4, 32, sms);
+    Shape s = vec ? shape_of(p.N, p.d / kVec, 32 / kVec, sms) : shape_of(p.N, (p.d + 3) / 4 * 4, 32, sms);
+    // Three quarters of the loads where they hold the row (16384 x 2048 elements as rows of
+    // 2560 bf16: 37 -> 34 us, the gradients 59 -> 52; of 6144 42 -> 37, 59 -> 54), but not the
+    // gradients of narrow fp32 rows, where two CTAs with two rows each in their rings do worse
+    // than one with three (1536: 71 -> 76; 2560: 86 -> 76).
+    if (vec && s.nv == 32 / kVec && s.G * (24 / kVec) >= p.d / kVec && (!grad || kVec == 8 || p.d > 2048)) s.nv = 24 / kVec;
     p.G = s.G;
     if (vec)
       e = s.nv == 1   ? launch_shape<T, kVec, 1>(grad, p, sms, parts, stream)
           : s.nv == 2 ? launch_shape<T, kVec, 2>(grad, p, sms, parts, stream)
+          : s.nv == 24 / kVec ? launch_shape<T, kVec, 24 / kVec>(grad, p, sms, parts, stream)
           : s.nv == 4 ? launch_shape<T, kVec, 4>(grad, p, sms, parts, stream)
                       : launch_shape<T, kVec, 32 / kVec>(grad, p, sms, parts, stream);
     else

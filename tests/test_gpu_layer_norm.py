@@ -81,6 +81,13 @@ def test_norm_and_gradients(N, d, dt, wdt):
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("N", [9, 1500])
+@pytest.mark.parametrize("d", [768, 1280, 2560, 3080, 5120, 6144, 6152])
+def test_widths_between_powers_of_two(N, d, dt):
+    test_norm_and_gradients(N, d, dt, F32)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("d,row,offset", [(64, 80, 0), (64, 71, 0), (64, 64, 1), (2048, 2056, 8), (333, 400, 3), (8200, 8208, 8)])
 def test_strided_rows_and_any_alignment(dt, d, row, offset):
     """Rows apart, in two leading dimensions, off 16-byte boundaries; no saved
