@@ -310,8 +310,10 @@ size_t dlm_lmhead_loss_workspace_bytes(int64_t rows, int64_t d);
  *               pieces of `piece` columns, and of about 2 GB with piece = 0, which is
  *               as fast as it gets; the least is what piece = 256 needs. Calls sharing it
  *               must not overlap on the GPU.
- * g is rounded to bf16 for the tensor cores (at most 2^-8 relative in each term), all sums
- * are fp32, the results are rounded to bf16. The same inputs and workspace size give the
+ * g is rounded to bf16 for the tensor cores (at most 2^-8 relative in each term; the
+ * target's, most of a row's gradient, enters d_hidden unrounded, and d_weight as a multiple
+ * of 2^-8 of 1 - p where every row has the same dloss), all sums are fp32, the results are
+ * rounded to bf16. The same inputs and workspace size give the
  * same bits. No output may overlap another tensor.
  */
 int dlm_lmhead_loss_grad(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_tensor* targets, const dlm_tensor* lse,

@@ -26,7 +26,10 @@
 // Single CTAs, with few rows or little width, take the operands as they lie.
 // g is rounded to bf16 because the tensor cores take it so: every term of d_hidden and
 // d_weight is off by at most 2^-8 relative, as the result is by its own rounding to bf16;
-// all sums are fp32. Warp 0 loads by TMA, warp 1 issues tcgen05.mma (both operands in
+// all sums are fp32. The one large term, the target's, would stand out: of d_hidden its
+// rounding is made good at the end, with the target's row of the weight, and where every
+// row has the same dloss, the mean's, g is rounded without dloss's mantissa, which leaves
+// -(1 - p) nearly exact. Warp 0 loads by TMA, warp 1 issues tcgen05.mma (both operands in
 // shared memory), warps 4-11 read the fp32 accumulators (two, so a tile's epilogue runs
 // under the next one's K loop) and write their tiles through shared memory by TMA.
 // Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, drains and exits.
@@ -90,8 +93,9 @@ static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "s
 
 // What the first launch leaves for the others.
 struct Plan {
-  int n;       // scored rows
-  int splits;  // K splits of dh
+  int n;        // scored rows
+  int splits;   // K splits of dh
+  float scale;  // what g is divided by: the first scored row's dloss, its power of two taken out
 };
 
 struct Params {
@@ -111,6 +115,7 @@ struct Params {
   const int* target;    // of each scored row
   const float* lse2;    // lse log2(e)
   const float* dloss;
+  float* rest;          // grad: what the rounding of g took from the target's, of each scored row
   float2* part;         // stats: (maximum, sum) [half of the warps][part][row]
   float* x_target;      // stats: the target's logit
   int* err;
@@ -135,6 +140,11 @@ __device__ __forceinline__ void tma_add_2d(const void* tmap, const void* src, in
                    reinterpret_cast<uint64_t>(tmap)),
                "r"(smem_u32(src)), "r"(c0), "r"(c1)
                : "memory");
+}
+
+// *v = x where i == e. (Selects in C++ become an index into an array in local memory.)
+__device__ __forceinline__ void take_if(int i, int e, float x, float* v) {
+  asm("{\n.reg .pred q;\nsetp.eq.s32 q, %1, %2;\nselp.f32 %0, %3, %0, q;\n}" : "+f"(*v) : "r"(i), "r"(e), "f"(x));
 }
 
 // One output tile and its K steps [k0, k1). m, n: its row and column tiles; dw: of
@@ -427,6 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           mbar_arrive(&sm.acc_empty[acc]);
       }
     };
+    const float scale = kMode == kStats ? 1.f : p.plan->scale;
     int tile = 0;
     bool ok = true;
     for (int j = 0, item; ok && (item = work.item(worker, workers, j)) >= 0; ++j) {
@@ -439,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         target = p.target[row];
         if (kMode == kGrad) {
           lse2 = p.lse2[row];
-          dloss = p.dloss[row];
+          dloss = p.dloss[row] / scale;
         }
       }
       for (int t = work.first(p, item); t < t1; ++t, ++tile) {
@@ -524,6 +535,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (static_cast<unsigned>(target - col0) < 64u) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e) x[e] -= target - col0 == e ? 1.f : 0.f;
+                float gt = 0.f;
+#pragma unroll
+                for (int e = 0; e < 64; ++e) take_if(target - col0, e, x[e], &gt);
+                gt *= dloss;
+                const float rest = gt - __bfloat162float(__float2bfloat16_rn(gt));
+                p.rest[row] = fabsf(rest) < INFINITY ? rest : 0.f;
               }
               const float2 d2 = make_float2(dloss, dloss);
 #pragma unroll
@@ -540,6 +557,15 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (target < 0) {  // rows behind the scored ones hold anything: their g is 0
 #pragma unroll
                 for (int e = 0; e < 64; ++e) x[e] = 0.f;
+              }
+            }
+            if (kMode == kBack && tl.dw) {
+              const float2 s2 = make_float2(scale, scale);
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) {
+                const float2 y = fmul2(make_float2(x[e], x[e + 1]), s2);
+                x[e] = y.x;
+                x[e + 1] = y.y;
               }
             }
             if (kMode == kBack && tl.k1 == tl.k0) {  // no scored row: nothing was multiplied
@@ -741,8 +767,13 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
       p.to_target[before + at] = t;
       if (p.origin) p.origin[before + at] = static_cast<int>(r);
       if (p.to_lse2) {
+        const float dl = p.dloss[r];
         p.to_lse2[before + at] = p.lse[r] * kLog2e;
-        p.to_dloss[before + at] = p.dloss[r];
+        p.to_dloss[before + at] = dl;
+        if (before + at == 0) {  // 1 where there is no such number
+          const uint32_t bits = __float_as_uint(dl), exponent = bits >> 23 & 0xFFu;
+          p.plan->scale = exponent == 0 || exponent == 255 ? 1.f : __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u);
+        }
       }
     }
     if (r < r1) {
@@ -874,23 +905,34 @@ __global__ void __launch_bounds__(kCombineThreads)
   }
 }
 
+// What turns the sums of g weight into d_hidden: the rest of the target's g, and the scale.
+struct Finish {
+  const int* target;  // of each row (pairs: of each scored one)
+  const float* rest;  // of each scored row
+  const __nv_bfloat16* weight;
+  int64_t s_weight;
+};
+
 // d_hidden: the splits' sums of each scored row, zeros for the others; four columns a
 // thread, eight splits' loads in flight.
 constexpr int kFinishThreads = 128;
 __global__ void __launch_bounds__(kFinishThreads)
-    loss_dhidden_kernel(const Plan* plan, const int* place, const float* part, int N, int block_rows, int d, int d_pad,
-                        __nv_bfloat16* out, int64_t s_out, int aligned) {
+    loss_dhidden_kernel(const Plan* plan, const Finish f, const int* place, const float* part, int N, int block_rows, int d,
+                        int d_pad, __nv_bfloat16* out, int64_t s_out, int aligned) {
   wait_for_previous();
   const int vecs = d / 4, splits = plan->splits;
+  const float scale = plan->scale;
   const int64_t step = static_cast<int64_t>((plan->n + block_rows - 1) / block_rows) * block_rows * d_pad;
   const int64_t total = static_cast<int64_t>(N) * vecs;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x; i < total;
        i += static_cast<int64_t>(gridDim.x) * kFinishThreads) {
     const int64_t r = i / vecs;
-    const int col = static_cast<int>(i - r * vecs) * 4, c = place[r];
+    const int col = static_cast<int>(i - r * vecs) * 4, c = place[r], t = f.target[r];
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c >= 0) {
       const float* src = part + static_cast<int64_t>(c) * d_pad + col;
+      const uint2 w = *reinterpret_cast<const uint2*>(f.weight + t * f.s_weight + col);
+      const float rest = f.rest[c];
       for (int s = 0; s < splits; s += 8) {
         float4 v[8];
 #pragma unroll
@@ -899,6 +941,8 @@ __global__ void __launch_bounds__(kFinishThreads)
 #pragma unroll
         for (int k = 0; k < 8; ++k) a = make_float4(a.x + v[k].x, a.y + v[k].y, a.z + v[k].z, a.w + v[k].w);
       }
+      a = make_float4(fmaf(rest, __uint_as_float(w.x << 16), a.x) * scale, fmaf(rest, __uint_as_float(w.x & 0xFFFF0000u), a.y) * scale,
+                      fmaf(rest, __uint_as_float(w.y << 16), a.z) * scale, fmaf(rest, __uint_as_float(w.y & 0xFFFF0000u), a.w) * scale);
     }
     const uint2 o = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
     __nv_bfloat16* dst = out + r * s_out + col;
@@ -918,7 +962,7 @@ __global__ void __launch_bounds__(kFinishThreads)
 // splits behind each other, whole blocks of rows apart: 32 rows x 64 columns a CTA.
 constexpr int kTurnThreads = 256;
 __global__ void __launch_bounds__(kTurnThreads)
-    loss_dhidden_turn_kernel(const Plan* plan, const int* origin, const float* part, int block_rows, int d, int64_t columns,
+    loss_dhidden_turn_kernel(const Plan* plan, const Finish f, const int* origin, const float* part, int block_rows, int d, int64_t columns,
                              __nv_bfloat16* out, int64_t s_out, int aligned) {
   __shared__ float tile[64][33];
   wait_for_previous();
@@ -926,6 +970,14 @@ __global__ void __launch_bounds__(kTurnThreads)
   if (r0 >= n) return;
   const int64_t step = static_cast<int64_t>((n + block_rows - 1) / block_rows) * block_rows;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+  const bool on = r0 + r < n && d0 + c < d;
+  uint4 u = make_uint4(0, 0, 0, 0);
+  float rest = 0.f;
+  if (on) {
+    u = *reinterpret_cast<const uint4*>(f.weight + f.target[r0 + r] * f.s_weight + d0 + c);
+    rest = f.rest[r0 + r];
+  }
   float a[8] = {};
   for (int s = 0; s < splits; ++s) {
     const float* src = part + (d0 + warp) * columns + s * step + r0 + lane;
@@ -935,11 +987,13 @@ __global__ void __launch_bounds__(kTurnThreads)
 #pragma unroll
   for (int i = 0; i < 8; ++i) tile[warp + 8 * i][lane] = a[i];
   __syncthreads();
-  const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
-  if (r0 + r >= n || d0 + c >= d) return;
-  uint32_t w[4];
+  if (!on) return;
+  const float scale = plan->scale;
+  uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) w[k] = pack_bf16x2(tile[c + 2 * k][r], tile[c + 2 * k + 1][r]);
+  for (int k = 0; k < 4; ++k)
+    w[k] = pack_bf16x2(fmaf(rest, __uint_as_float(w[k] << 16), tile[c + 2 * k][r]) * scale,
+                       fmaf(rest, __uint_as_float(w[k] & 0xFFFF0000u), tile[c + 2 * k + 1][r]) * scale);
   store_bf16x8(out + static_cast<int64_t>(origin[r0 + r]) * s_out + d0 + c, make_uint4(w[0], w[1], w[2], w[3]), aligned);
 }
 
@@ -1012,7 +1066,7 @@ Team team_for(bool pairs) {
 // Places of the workspace, from its start.
 struct Layout {
   int64_t n_pad, d_pad;
-  size_t plan, place, target, lse2, dloss, hidden, x_target, part, origin, turned, sums, g;  // byte offsets
+  size_t plan, place, target, lse2, dloss, rest, hidden, x_target, part, origin, turned, sums, g;  // byte offsets
   int64_t sums_rows;  // gradients: rows of fp32 sums (pairs: columns, of d_rows rows)
   int64_t d_rows;
 };
@@ -1038,6 +1092,7 @@ Layout layout_of(int64_t N, int64_t d, bool grad) {
   } else {
     l.lse2 = take(&at, l.n_pad * 4);
     l.dloss = take(&at, l.n_pad * 4);
+    l.rest = take(&at, l.n_pad * 4);
     if (pairs_for_gradients(N, d)) {
       l.origin = take(&at, l.n_pad * 4);
       l.turned = take(&at, l.n_pad * l.d_pad * 2);
@@ -1190,6 +1245,7 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   p.n_pad = static_cast<int>(l.n_pad);
   p.lse2 = g.to_lse2;
   p.dloss = g.to_dloss;
+  p.rest = reinterpret_cast<float*>(ws + l.rest);
   p.want_dw = a.d_weight != nullptr;
   p.want_dh = a.d_hidden != nullptr;
   p.dw_rows = p.V;
@@ -1218,11 +1274,12 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
     if ((st = launch_product<kBack>(team.ctas, back, p, team.workers, team.workers, stream)) != DLM_OK) return st;
   }
   if (!a.d_hidden) return DLM_OK;
+  const Finish f = {pairs ? p.target : a.targets, p.rest, static_cast<const __nv_bfloat16*>(a.weight), a.s_weight};
   if (pairs) {
     const bool whole = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 15) == 0;
     const cudaError_t e = launch_overlapped(
         loss_dhidden_turn_kernel, dim3(static_cast<unsigned>((a.N + 31) / 32), static_cast<unsigned>((a.d + 63) / 64)), kTurnThreads, 0,
-        stream, 1, true, p.plan, g.origin, reinterpret_cast<const float*>(ws + l.sums), block_rows, static_cast<int>(a.d),
+        stream, 1, true, p.plan, f, g.origin, reinterpret_cast<const float*>(ws + l.sums), block_rows, static_cast<int>(a.d),
         l.sums_rows, static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden, whole ? 1 : 0);
     return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "hidden gradient launch: %s", cudaGetErrorString(e));
   }
@@ -1230,7 +1287,7 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   const int64_t want = (vecs + kFinishThreads - 1) / kFinishThreads, most = static_cast<int64_t>(sm_count()) * 16;
   const bool aligned = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 7) == 0;
   const cudaError_t e = launch_overlapped(
-      loss_dhidden_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), kFinishThreads, 0, stream, 1, true, p.plan,
+      loss_dhidden_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), kFinishThreads, 0, stream, 1, true, p.plan, f,
       reinterpret_cast<const int*>(ws + l.place), reinterpret_cast<const float*>(ws + l.sums), static_cast<int>(a.N), block_rows,
       static_cast<int>(a.d), static_cast<int>(l.d_pad), static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden, aligned ? 1 : 0);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "hidden gradient launch: %s", cudaGetErrorString(e));

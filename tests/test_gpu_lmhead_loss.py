@@ -126,6 +126,67 @@ def test_gradients(N, V, d, scored):
     check_grad(h, w, t, lse, dl, dh, dw, f"{N}x{V}x{d} {scored}")
 
 
+@pytest.mark.parametrize("weights", ["equal", "any"])
+@pytest.mark.parametrize("N,V,d,piece", [(200, 3001, 128, 0), (200, 3001, 128, 1024), (600, 2500, 512, 0), (1, 300, 64, 0)])
+def test_the_targets_terms_keep_their_precision(N, V, d, piece, weights):
+    """The bounds of check_grad but for the target's term, which is most of a row's
+    gradient. In d_hidden it is not rounded to bf16: two fp32 roundings instead of 2^-8.
+    With equal weights it is rounded as 2^k (1 - p) in d_weight, between 1/2 and 1 a number
+    of steps of 2^-8, 1 one of them: off by at most min(p, 2^-9). The equal weight is one
+    that bf16 misses by 0.9 of half a step."""
+    from paper_2608_02625_gb300 import binding as B
+    h, w, t, dl = inputs(N, V, d, seed=7, scored="all")
+    if weights == "equal":
+        dl.fill_(2.0 ** -6 * (1 + 0.9 * 2.0 ** -8))
+    lse = fp64_lse(h, w, t)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh, dw, ws_grad(N, V, d, piece))
+    H, W, T, rows, ex, x = bounds(h, w, t)
+    S, D = host(lse), host(dl)
+    rh, rw, g = oracle.lm_head_loss_grad(H, W, T, S, D)
+    x = np.maximum(x, np.abs(S))
+    at = np.arange(N), T
+    hot = np.zeros_like(g)
+    hot[at] = 1.0
+    p = np.abs(g + D[:, None] * hot)
+    dg = p * (ex + 8 * U32 * x + 2.0 ** -21)[:, None] + 4 * U32 * D[:, None]
+    mags = np.abs(g) * (1 + 2.0 ** -8) + dg
+    off = 2.0 ** -8 * np.abs(g)
+    off[at] = 2 * U32 * np.abs(g[at])
+    b = (dg + off) @ np.abs(W) + ((V / 16 + 4) * STEP + 80 * U32) * (mags @ np.abs(W))
+    within(host(dh), rh, b + HALF[BF] * (np.abs(rh) + b) + 1e-40, "d_hidden")
+    if weights == "equal":
+        off[at] = np.minimum(p[at], 2.0 ** -9 * D) + 2 * U32 * np.abs(g[at])
+        b = (dg + off).T @ np.abs(H) + (N / 16 + 8) * STEP * (mags.T @ np.abs(H))
+        within(host(dw), rw, b + HALF[BF] * (np.abs(rw) + b) + 1e-40, "d_weight")
+    assert B.device_error() == 0
+
+
+@pytest.mark.parametrize("bad", [0.0, float("inf"), float("nan"), -0.75, 1e-39])
+def test_any_weight_of_the_first_row(bad):
+    """Whatever the first scored row's weight is, the other rows' gradients are theirs."""
+    from paper_2608_02625_gb300 import binding as B
+    N, V, d = 60, 500, 64
+    h, w, t, dl = inputs(N, V, d, seed=8, scored="all")
+    lse = fp64_lse(h, w, t)
+    dl[0] = bad
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh, dw, ws_grad(N, V, d))
+    if np.isfinite(bad):
+        check_grad(h, w, t, lse, dl.abs(), dh * torch.where(dl < 0, -1, 1)[:, None].to(BF), None)
+        keep = dl.clone()
+        keep[0] = 0.0
+        dh1, dw1 = torch.empty_like(h), torch.empty_like(w)
+        B.dlm_lmhead_loss_grad(h, w, t, lse, keep, dh1, dw1, ws_grad(N, V, d))
+        if bad in (0.0, 1e-39):
+            assert torch.equal(dw, dw1)
+    else:
+        assert not bool(torch.isfinite(dh[0]).any())
+        keep = t.clone()
+        keep[0] = -1
+        check_grad(h, w, keep, lse, dl, torch.cat([torch.zeros_like(dh[:1]), dh[1:]]), None)
+
+
 @pytest.mark.parametrize("scored", ["half", "last"])
 def test_more_rows_than_the_gathering_ctas_take_at_once(scored):
     from paper_2608_02625_gb300 import binding as B
