@@ -162,6 +162,19 @@ def test_the_targets_terms_keep_their_precision(N, V, d, piece, weights):
     assert B.device_error() == 0
 
 
+@pytest.mark.parametrize("N,V", [(128, 300), (100, 1), (77, 5)])
+def test_many_rows_of_one_token(N, V):
+    from paper_2608_02625_gb300 import binding as B
+    d = 128
+    h, w, t, dl = inputs(N, V, d, seed=10, scored="all")
+    t.fill_(V - 1)
+    lse = fp64_lse(h, w, t)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh, dw, ws_grad(N, V, d))
+    assert B.device_error() == 0
+    check_grad(h, w, t, lse, dl, dh, dw)
+
+
 @pytest.mark.parametrize("bad", [0.0, float("inf"), float("nan"), -0.75, 1e-39])
 def test_any_weight_of_the_first_row(bad):
     """Whatever the first scored row's weight is, the other rows' gradients are theirs."""
