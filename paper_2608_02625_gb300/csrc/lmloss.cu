@@ -58,14 +58,17 @@ constexpr int kABytes = kBM * kBK * 2;
 constexpr int kBoxBytes = 64 * 128;          // an MN-major box: 64 K rows of 64 columns
 constexpr uint32_t kTmemCols = 2 * kMaxBN;   // two accumulators
 constexpr float kLog2e = 1.4426950408889634f;
-// From how many rows, and which width, CTAs work in pairs. V = 151552, graph us, single and
-// pairs: loss 512 x 2048 225, 214; 384 x 2048 181, 206 (tiles of 256 rows leave too few, and
-// the second is half empty); 4096 x 1024 778, 741; 4096 x 512 400, 419 (the epilogues of both
-// wait for the slower); gradients 384 x 2048 626, 631; 512 x 2048 712, 684; 4096 x 512 1452,
-// 1300; 4096 x 256 857, 803; 2048 x 256 (V = 20000) 82, 83; 4096 x 64 661, 718.
-constexpr int64_t kPairRows = 512;
-bool pairs_for_loss(int64_t N, int64_t d) { return N >= kPairRows && d >= 1024; }
-bool pairs_for_gradients(int64_t N, int64_t d) { return N >= kPairRows && d >= (N >= 4096 ? 256 : 512); }
+// Which calls may run in pairs of CTAs, by rows and width, and whether they do, by the number
+// of scored rows, which the GPU alone knows: both forms are launched, and one of them ends at
+// once (a gradient of 640 rows 893 -> 916 us, of 4096 no more; a quarter of 512 rows 513 ->
+// 328, of 1024 567 -> 467). V = 151552, d = 2048, graph us, single and pairs: loss 129 rows 134,
+// 121; 256 137, 127; 320 (of the pair's two tiles one is nearly empty) 184, 200; 448 232, 217;
+// gradients 256 460, 559; 320 601, 619; 448 771, 668; 512 712, 684. By width: loss 4096 x 1024
+// 778, 741; x 512 400, 419 (the epilogues of both wait for the slower); gradients 4096 x 512
+// 1452, 1300; x 256 857, 803; x 64 661, 718; 2048 x 256 (V = 20000) 82, 83.
+bool pairs_for_loss(int64_t N, int64_t d) { return N > kBM && d >= 1024; }
+bool pairs_for_gradients(int64_t N, int64_t d) { return N > 3 * kBM && d >= (N >= 4096 ? 256 : 512); }
+__device__ bool pairs_pay(int n, bool gradients) { return n > 3 * kBM || (!gradients && n > kBM && n <= 2 * kBM); }
 
 enum Mode { kStats, kGrad, kBack };
 
@@ -94,12 +97,14 @@ static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "s
 // What the first launch leaves for the others.
 struct Plan {
   int n;        // scored rows
+  int pairs;    // whether CTAs work in pairs
   int splits;   // K splits of dh
   float scale;  // what g is divided by: the first scored row's dloss, its power of two taken out
 };
 
 struct Params {
   const Plan* plan;
+  int either;           // both forms are launched: this one works if the plan says so
   int V;
   int kblocks;          // stats, grad: K steps (of d);  back: those of dh (of the piece)
   int bn;               // columns of a tile
@@ -245,6 +250,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int rank = kCtas == 2 ? static_cast<int>(blockIdx.x & 1) : 0;  // in the pair
   const int worker = static_cast<int>(blockIdx.x) / kCtas, workers = static_cast<int>(gridDim.x) / kCtas;
 
+  if (p.either) {
+    wait_for_previous();
+    if (p.plan->pairs != (kCtas == 2)) return;
+  }
   if (threadIdx.x == 32 * kEpiWarp0) {  // parameters, not memory that another kernel writes
     prefetch_tmap(&ma);
     prefetch_tmap(&mb);
@@ -666,8 +675,12 @@ struct GatherParams {
   int64_t s_dhidden;
   float* loss;          // loss only: 0 for rows that are not scored
   float* lse_out;
-  int block_rows;       // rows of a tile
-  int tiles, kblocks, workers, max_rows, dw_tiles;  // gradients: what the K splits of dh depend on
+  bool gradients, either;  // either: pairs, or not
+  struct Form {
+    int block_rows;     // rows of a tile
+    int tiles, workers, dw_tiles;  // gradients: what the K splits of dh depend on, with kblocks and max_rows
+  } form[2];            // single CTAs, pairs
+  int kblocks, max_rows;
 };
 
 constexpr int kGatherThreads = 256;
@@ -675,18 +688,18 @@ constexpr int kGatherThreads = 256;
 // The K splits of dh that end the launch first: no worker is done before its rounds of dh,
 // nor before its share of dh and dw. A lane of a warp looks at two numbers of splits (one
 // thread at all of them: 8 us).
-__device__ int choose_splits(const GatherParams& p, int n) {
-  const int lane = threadIdx.x & 31, blocks = (n + p.block_rows - 1) / p.block_rows;
+__device__ int choose_splits(const GatherParams& p, const GatherParams::Form& f, int n) {
+  const int lane = threadIdx.x & 31, blocks = (n + f.block_rows - 1) / f.block_rows;
   const float c_dw = dw_cost((n + kBK - 1) / kBK);
   float best = INFINITY;
   int splits = 1;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int s = lane + 32 * k + 1;
-    const bool fits = s == 1 || (s <= p.kblocks && blocks <= p.max_rows / p.block_rows / s);
-    const int dh = blocks * p.tiles * s, rounds = (dh + p.workers - 1) / p.workers;
+    const bool fits = s == 1 || (s <= p.kblocks && blocks <= p.max_rows / f.block_rows / s);
+    const int dh = blocks * f.tiles * s, rounds = (dh + f.workers - 1) / f.workers;
     const float c_dh = dh_cost((p.kblocks + s - 1) / s, max(blocks, 1));
-    const float share = (static_cast<float>(dh) * c_dh + static_cast<float>(p.dw_tiles) * c_dw) / static_cast<float>(p.workers);
+    const float share = (static_cast<float>(dh) * c_dh + static_cast<float>(f.dw_tiles) * c_dw) / static_cast<float>(f.workers);
     const float cost = fits ? fmaxf(static_cast<float>(rounds) * c_dh, share) : INFINITY;
     if (cost < best) {
       best = cost;
@@ -820,11 +833,13 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
     before += total;
   }
   if (blockIdx.x != gridDim.x - 1) return;
-  const int n = before, end = (n + p.block_rows - 1) / p.block_rows * p.block_rows;
+  const int n = before, end = (n + 2 * kBM - 1) / (2 * kBM) * (2 * kBM);
   if (warp == 0) {
-    const int splits = p.tiles ? choose_splits(p, n) : 1;
+    const int pairs = p.either && pairs_pay(n, p.gradients);
+    const int splits = p.gradients ? choose_splits(p, p.form[pairs], n) : 1;
     if (lane == 0) {
       p.plan->n = n;
+      p.plan->pairs = pairs;
       p.plan->splits = splits;
     }
   }
@@ -849,7 +864,7 @@ __global__ void __launch_bounds__(kTransposeThreads)
   wait_for_previous();
   launch_dependents();
   const int r0 = blockIdx.x * 64, d0 = blockIdx.y * 64, r = threadIdx.x >> 3, v = threadIdx.x & 7;
-  if (r0 >= plan->n) return;
+  if (!plan->pairs || r0 >= plan->n) return;
 #pragma unroll
   for (int i = 0; i < 64; i += 32) {
     const uint4 u = hidden[(static_cast<int64_t>(r0 + r + i) * d_pad + d0) / 8 + v];
@@ -875,14 +890,15 @@ __global__ void __launch_bounds__(kTransposeThreads)
 // Joins the parts of each scored row, a warp a row.
 constexpr int kCombineThreads = 256;
 __global__ void __launch_bounds__(kCombineThreads)
-    loss_combine_kernel(const Plan* plan, const int* place, const float2* part, const float* x_target, int N, int block_rows,
-                        int parts, float* loss, float* lse) {
+    loss_combine_kernel(const Plan* plan, const int* place, const float2* part, const float* x_target, int N, int parts_single,
+                        int parts_pairs, float* loss, float* lse) {
   wait_for_previous();
   const int64_t r = (static_cast<int64_t>(blockIdx.x) * kCombineThreads + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
   if (r >= N) return;
   const int c = place[r];
   if (c < 0) return;  // written by the first launch
+  const int block_rows = plan->pairs ? 2 * kBM : kBM, parts = plan->pairs ? parts_pairs : parts_single;
   const int64_t step = static_cast<int64_t>((plan->n + block_rows - 1) / block_rows) * block_rows;
   constexpr int kPer = (2 * kLossMaxParts + 31) / 32;
   float2 v[kPer];
@@ -917,12 +933,13 @@ struct Finish {
 // thread, eight splits' loads in flight.
 constexpr int kFinishThreads = 128;
 __global__ void __launch_bounds__(kFinishThreads)
-    loss_dhidden_kernel(const Plan* plan, const Finish f, const int* place, const float* part, int N, int block_rows, int d,
-                        int d_pad, __nv_bfloat16* out, int64_t s_out, int aligned) {
+    loss_dhidden_kernel(const Plan* plan, const Finish f, const int* place, const float* part, int N, int d, int d_pad,
+                        __nv_bfloat16* out, int64_t s_out, int aligned) {
   wait_for_previous();
+  if (plan->pairs) return;
   const int vecs = d / 4, splits = plan->splits;
   const float scale = plan->scale;
-  const int64_t step = static_cast<int64_t>((plan->n + block_rows - 1) / block_rows) * block_rows * d_pad;
+  const int64_t step = static_cast<int64_t>((plan->n + kBM - 1) / kBM) * kBM * d_pad;
   const int64_t total = static_cast<int64_t>(N) * vecs;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x; i < total;
        i += static_cast<int64_t>(gridDim.x) * kFinishThreads) {
@@ -962,13 +979,14 @@ __global__ void __launch_bounds__(kFinishThreads)
 // splits behind each other, whole blocks of rows apart: 32 rows x 64 columns a CTA.
 constexpr int kTurnThreads = 256;
 __global__ void __launch_bounds__(kTurnThreads)
-    loss_dhidden_turn_kernel(const Plan* plan, const Finish f, const int* origin, const float* part, int block_rows, int d, int64_t columns,
+    loss_dhidden_turn_kernel(const Plan* plan, const Finish f, const int* origin, const float* part, int d, int64_t columns,
                              __nv_bfloat16* out, int64_t s_out, int aligned) {
   __shared__ float tile[64][33];
   wait_for_previous();
+  if (!plan->pairs) return;
   const int n = plan->n, splits = plan->splits, r0 = blockIdx.x * 32, d0 = blockIdx.y * 64;
   if (r0 >= n) return;
-  const int64_t step = static_cast<int64_t>((n + block_rows - 1) / block_rows) * block_rows;
+  const int64_t step = static_cast<int64_t>((n + 2 * kBM - 1) / (2 * kBM)) * (2 * kBM);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
   const bool on = r0 + r < n && d0 + c < d;
@@ -1045,22 +1063,21 @@ int launch_product(int ctas, const Maps& m, const Params& p, int64_t items, int 
   return ctas == 2 ? launch_product<kMode, 2>(m, p, items, workers, stream) : launch_product<kMode, 1>(m, p, items, workers, stream);
 }
 
-// CTAs that share a tile, and how many such groups run at once.
+// CTAs that share a tile, and how many such groups run at once. Pairs: none where the device
+// has no place for them.
 struct Team {
   int ctas, workers;
 };
 
-Team team_for(bool pairs) {
+Team team_of(int ctas) {
   const int sms = sm_count();
-  if (pairs) {
-    const auto kernel = loss_product_kernel<kBack, 2>;  // the same shared memory in every mode
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<2>())) == cudaSuccess) {
-      const int pairs = active_clusters(reinterpret_cast<const void*>(kernel), 2, kThreads, smem_bytes<2>());
-      if (pairs > 0) return {2, pairs < sms / 2 ? pairs : sms / 2};
-    }
-    cudaGetLastError();
-  }
-  return {1, sms};
+  if (ctas == 1) return {1, sms};
+  const auto kernel = loss_product_kernel<kBack, 2>;  // the same shared memory in every mode
+  int pairs = 0;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<2>())) == cudaSuccess)
+    pairs = active_clusters(reinterpret_cast<const void*>(kernel), 2, kThreads, smem_bytes<2>());
+  if (pairs <= 0) cudaGetLastError();
+  return {2, pairs < sms / 2 ? pairs : sms / 2};
 }
 
 // Places of the workspace, from its start.
@@ -1157,39 +1174,42 @@ size_t loss_grad_workspace_bytes(int64_t N, int64_t V, int64_t d, int64_t piece)
 
 int launch_loss(const LossArgs& a, cudaStream_t stream) {
   const Layout l = layout_of(a.N, a.d, false);
-  const Team team = team_for(pairs_for_loss(a.N, a.d));
-  const int block_rows = kBM * team.ctas;
+  const Team teams[2] = {team_of(1), pairs_for_loss(a.N, a.d) ? team_of(2) : Team{2, 0}};
+  const bool either = teams[1].workers > 0;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   GatherParams g = {};
-  g.block_rows = block_rows;
+  g.either = either;
   g.loss = a.loss;
   g.lse_out = a.lse_out;
   int st;
   if ((st = launch_gather(a, l, g, stream)) != DLM_OK) return st;
   Params p = common_params(a, l);
-  const int64_t row_blocks = (a.N + block_rows - 1) / block_rows;
+  p.either = either;
   p.kblocks = static_cast<int>(l.d_pad / kBK);
-  p.bn = choose_bn(a.V, row_blocks, team.workers, team.ctas);
-  p.tiles = static_cast<int>((a.V + p.bn - 1) / p.bn);
-  p.parts = p.tiles < kLossMaxParts ? p.tiles : kLossMaxParts;
-  p.a_rows = team.ctas == 1 && a.N < kBM ? static_cast<int>((a.N + 7) / 8 * 8) : kBM;
   p.part = reinterpret_cast<float2*>(ws + l.part);
   p.x_target = reinterpret_cast<float*>(ws + l.x_target);
-  Maps m = {};
-  if ((st = make_matrix_map(&m.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, p.a_rows)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&m.b, a.weight, true, a.V, a.d, a.s_weight, p.bn / team.ctas)) != DLM_OK) return st;
-  if ((st = launch_product<kStats>(team.ctas, m, p, p.parts * row_blocks, team.workers, stream)) != DLM_OK) return st;
+  int parts[2] = {};
+  for (int i = 0; i <= (either ? 1 : 0); ++i) {
+    const Team& team = teams[i];
+    const int64_t block_rows = kBM * team.ctas, row_blocks = (a.N + block_rows - 1) / block_rows;
+    p.bn = choose_bn(a.V, row_blocks, team.workers, team.ctas);
+    p.tiles = static_cast<int>((a.V + p.bn - 1) / p.bn);
+    p.parts = parts[i] = p.tiles < kLossMaxParts ? p.tiles : kLossMaxParts;
+    p.a_rows = a.N < kBM ? static_cast<int>((a.N + 7) / 8 * 8) : kBM;
+    Maps m = {};
+    if ((st = make_matrix_map(&m.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, p.a_rows)) != DLM_OK) return st;
+    if ((st = make_matrix_map(&m.b, a.weight, true, a.V, a.d, a.s_weight, p.bn / team.ctas)) != DLM_OK) return st;
+    if ((st = launch_product<kStats>(team.ctas, m, p, p.parts * row_blocks, team.workers, stream)) != DLM_OK) return st;
+  }
   const cudaError_t e = launch_overlapped(
       loss_combine_kernel, dim3(static_cast<unsigned>((a.N * 32 + kCombineThreads - 1) / kCombineThreads)), kCombineThreads, 0, stream,
       1, true, p.plan, reinterpret_cast<const int*>(ws + l.place), static_cast<const float2*>(p.part),
-      static_cast<const float*>(p.x_target), static_cast<int>(a.N), block_rows, 2 * p.parts, a.loss, a.lse_out);
+      static_cast<const float*>(p.x_target), static_cast<int>(a.N), 2 * parts[0], 2 * parts[1], a.loss, a.lse_out);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "loss combine launch: %s", cudaGetErrorString(e));
 }
 
 int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   const Layout l = layout_of(a.N, a.d, true);
-  const Team team = team_for(pairs_for_gradients(a.N, a.d));
-  const int block_rows = kBM * team.ctas;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   const int64_t all = (a.V + 255) / 256 * 256;
   int64_t cols = static_cast<int64_t>((a.workspace_bytes - l.g) / (static_cast<size_t>(l.n_pad) * 2)) / 256 * 256;
@@ -1198,50 +1218,65 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   const int64_t most_cols = int64_t{0x7FFFFF00} / l.n_pad * 64 / 256 * 256;
   if (cols > most_cols) cols = most_cols;
   if (cols > all) cols = all;
-  const int64_t row_blocks = (a.N + block_rows - 1) / block_rows, first = cols < a.V ? cols : a.V;
-  const int bn_d = choose_bn(a.d, 1, 1, team.ctas);
-  const int bn_v = choose_bn(first, row_blocks, team.workers, team.ctas);
-  const int d_tiles = static_cast<int>((a.d + bn_d - 1) / bn_d);
+  const int64_t first = cols < a.V ? cols : a.V, panel_rows = l.n_pad * (cols / 64);
 
+  // Single CTAs, and pairs where they may work.
+  struct Form {
+    Team team;
+    int64_t row_blocks;
+    int bn_d, bn_v, d_tiles, dh_tiles;
+    Maps grad, back;
+  } forms[2] = {};
+  forms[0].team = team_of(1);
+  forms[1].team = pairs_for_gradients(a.N, a.d) ? team_of(2) : Team{2, 0};
+  const bool either = forms[1].team.workers > 0;
   GatherParams g = {};
-  g.block_rows = block_rows;
+  int st;
+  for (int i = 0; i <= (either ? 1 : 0); ++i) {
+    Form& f = forms[i];
+    const bool pairs = i == 1;
+    const int ctas = f.team.ctas, block_rows = kBM * ctas;
+    f.row_blocks = (a.N + block_rows - 1) / block_rows;
+    f.bn_d = choose_bn(a.d, 1, 1, ctas);
+    f.bn_v = choose_bn(first, f.row_blocks, f.team.workers, ctas);
+    f.d_tiles = static_cast<int>((a.d + f.bn_d - 1) / f.bn_d);
+    f.dh_tiles = pairs ? static_cast<int>(l.d_rows / (2 * kBM)) : f.d_tiles;
+    g.form[i] = {block_rows, f.dh_tiles, f.team.workers,
+                 a.d_weight ? static_cast<int>((first + block_rows - 1) / block_rows) * f.d_tiles : 0};
+    Maps &grad = f.grad, &back = f.back;
+    if ((st = make_matrix_map(&grad.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, kBM)) != DLM_OK) return st;
+    if ((st = make_matrix_map(&grad.b, a.weight, true, a.V, a.d, a.s_weight, f.bn_v / ctas)) != DLM_OK) return st;
+    if ((st = make_matrix_map(&grad.out, ws + l.g, true, panel_rows, 64, 64, 32)) != DLM_OK) return st;
+    // dh: g times the weight, or, a pair's, the weight transposed times g transposed.
+    if ((st = make_matrix_map(pairs ? &back.b : &back.a, ws + l.g, true, panel_rows, 64, 64, kBM)) != DLM_OK) return st;
+    if ((st = make_matrix_map(pairs ? &back.a : &back.b, a.weight, true, a.V, a.d, a.s_weight, 64)) != DLM_OK) return st;
+    st = pairs ? make_matrix_map(&back.out, ws + l.sums, false, l.d_rows, l.sums_rows, l.sums_rows, 32)
+               : make_matrix_map(&back.out, ws + l.sums, false, l.sums_rows, l.d_pad, l.d_pad, 32);
+    if (st != DLM_OK) return st;
+    if ((st = make_matrix_map(&back.dw_a, ws + l.g, true, panel_rows, 64, 64, 64)) != DLM_OK) return st;
+    st = pairs ? make_matrix_map(&back.dw_b, ws + l.turned, true, l.d_pad, l.n_pad, l.n_pad, f.bn_d / 2)
+               : make_matrix_map(&back.dw_b, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, 64);
+    if (st != DLM_OK) return st;
+    if (a.d_weight && (st = make_matrix_map(&back.dw_out, a.d_weight, true, a.V, a.d, a.s_dweight, 32)) != DLM_OK) return st;
+  }
+
+  g.gradients = true;
+  g.either = either;
   g.lse = a.lse;
   g.dloss = a.dloss;
   g.to_lse2 = reinterpret_cast<float*>(ws + l.lse2);
   g.to_dloss = reinterpret_cast<float*>(ws + l.dloss);
-  const bool pairs = team.ctas == 2;
-  const int dh_tiles = pairs ? static_cast<int>(l.d_rows / (2 * kBM)) : d_tiles;
-  g.tiles = dh_tiles;
   g.kblocks = static_cast<int>((first + kBK - 1) / kBK);
-  g.dw_tiles = a.d_weight ? static_cast<int>((first + block_rows - 1) / block_rows) * d_tiles : 0;
-  g.workers = team.workers;
   g.max_rows = l.sums_rows > 0x7FFFFFFF ? 0x7FFFFFFF : static_cast<int>(l.sums_rows);
-  if (pairs) {
+  if (either) {
     g.origin = reinterpret_cast<int*>(ws + l.origin);
     g.d_hidden = static_cast<__nv_bfloat16*>(a.d_hidden);
     g.s_dhidden = a.s_dhidden;
   }
-  int st;
   if ((st = launch_gather(a, l, g, stream)) != DLM_OK) return st;
 
-  Maps grad = {}, back = {};
-  const int64_t panel_rows = l.n_pad * (cols / 64);
-  if ((st = make_matrix_map(&grad.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, kBM)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&grad.b, a.weight, true, a.V, a.d, a.s_weight, bn_v / team.ctas)) != DLM_OK) return st;
-  if ((st = make_matrix_map(&grad.out, ws + l.g, true, panel_rows, 64, 64, 32)) != DLM_OK) return st;
-  // dh: g times the weight, or, a pair's, the weight transposed times g transposed.
-  if ((st = make_matrix_map(pairs ? &back.b : &back.a, ws + l.g, true, panel_rows, 64, 64, kBM)) != DLM_OK) return st;
-  if ((st = make_matrix_map(pairs ? &back.a : &back.b, a.weight, true, a.V, a.d, a.s_weight, 64)) != DLM_OK) return st;
-  st = pairs ? make_matrix_map(&back.out, ws + l.sums, false, l.d_rows, l.sums_rows, l.sums_rows, 32)
-             : make_matrix_map(&back.out, ws + l.sums, false, l.sums_rows, l.d_pad, l.d_pad, 32);
-  if (st != DLM_OK) return st;
-  if ((st = make_matrix_map(&back.dw_a, ws + l.g, true, panel_rows, 64, 64, 64)) != DLM_OK) return st;
-  st = pairs ? make_matrix_map(&back.dw_b, ws + l.turned, true, l.d_pad, l.n_pad, l.n_pad, bn_d / 2)
-             : make_matrix_map(&back.dw_b, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, 64);
-  if (st != DLM_OK) return st;
-  if (a.d_weight && (st = make_matrix_map(&back.dw_out, a.d_weight, true, a.V, a.d, a.s_dweight, 32)) != DLM_OK) return st;
-
   Params p = common_params(a, l);
+  p.either = either;
   p.n_pad = static_cast<int>(l.n_pad);
   p.lse2 = g.to_lse2;
   p.dloss = g.to_dloss;
@@ -1251,8 +1286,7 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   p.dw_rows = p.V;
   p.dw_cols = static_cast<int>(a.d);
   p.dh_cols = static_cast<int>(l.d_pad);
-  p.dh_tiles = dh_tiles;
-  if (pairs && a.d_weight) {
+  if (either && a.d_weight) {
     const cudaError_t e = launch_overlapped(
         loss_transpose_kernel, dim3(static_cast<unsigned>(l.n_pad / 64), static_cast<unsigned>(l.d_pad / 64)), kTransposeThreads, 0,
         stream, 1, true, p.plan, reinterpret_cast<const uint4*>(ws + l.hidden), static_cast<int>(l.d_pad), p.n_pad,
@@ -1262,34 +1296,42 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   for (int64_t v0 = 0; v0 < a.V; v0 += cols) {
     const int64_t vc = a.V - v0 < cols ? a.V - v0 : cols;
     p.v0 = static_cast<int>(v0);
-    p.kblocks = static_cast<int>(l.d_pad / kBK);
-    p.bn = bn_v;
-    p.tiles = static_cast<int>((vc + bn_v - 1) / bn_v);
-    if ((st = launch_product<kGrad>(team.ctas, grad, p, p.tiles * row_blocks, team.workers, stream)) != DLM_OK) return st;
-    p.bn = bn_d;
-    p.tiles = d_tiles;
-    p.parts = static_cast<int>((vc + block_rows - 1) / block_rows);
-    p.kblocks = static_cast<int>((vc + kBK - 1) / kBK);
     p.add = v0 > 0;
-    if ((st = launch_product<kBack>(team.ctas, back, p, team.workers, team.workers, stream)) != DLM_OK) return st;
+    for (int i = 0; i <= (either ? 1 : 0); ++i) {
+      const Form& f = forms[i];
+      p.kblocks = static_cast<int>(l.d_pad / kBK);
+      p.bn = f.bn_v;
+      p.tiles = static_cast<int>((vc + f.bn_v - 1) / f.bn_v);
+      if ((st = launch_product<kGrad>(f.team.ctas, f.grad, p, p.tiles * f.row_blocks, f.team.workers, stream)) != DLM_OK) return st;
+    }
+    for (int i = 0; i <= (either ? 1 : 0); ++i) {
+      const Form& f = forms[i];
+      const int block_rows = kBM * f.team.ctas;
+      p.bn = f.bn_d;
+      p.tiles = f.d_tiles;
+      p.dh_tiles = f.dh_tiles;
+      p.parts = static_cast<int>((vc + block_rows - 1) / block_rows);
+      p.kblocks = static_cast<int>((vc + kBK - 1) / kBK);
+      if ((st = launch_product<kBack>(f.team.ctas, f.back, p, f.team.workers, f.team.workers, stream)) != DLM_OK) return st;
+    }
   }
   if (!a.d_hidden) return DLM_OK;
-  const Finish f = {pairs ? p.target : a.targets, p.rest, static_cast<const __nv_bfloat16*>(a.weight), a.s_weight};
-  if (pairs) {
-    const bool whole = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 15) == 0;
-    const cudaError_t e = launch_overlapped(
-        loss_dhidden_turn_kernel, dim3(static_cast<unsigned>((a.N + 31) / 32), static_cast<unsigned>((a.d + 63) / 64)), kTurnThreads, 0,
-        stream, 1, true, p.plan, f, g.origin, reinterpret_cast<const float*>(ws + l.sums), block_rows, static_cast<int>(a.d),
-        l.sums_rows, static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden, whole ? 1 : 0);
-    return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "hidden gradient launch: %s", cudaGetErrorString(e));
-  }
+  Finish f = {a.targets, p.rest, static_cast<const __nv_bfloat16*>(a.weight), a.s_weight};
   const int64_t vecs = a.N * (a.d / 4);
   const int64_t want = (vecs + kFinishThreads - 1) / kFinishThreads, most = static_cast<int64_t>(sm_count()) * 16;
-  const bool aligned = ((reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2)) & 7) == 0;
-  const cudaError_t e = launch_overlapped(
+  const uintptr_t place = reinterpret_cast<uintptr_t>(a.d_hidden) | static_cast<uintptr_t>(a.s_dhidden * 2);
+  cudaError_t e = launch_overlapped(
       loss_dhidden_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), kFinishThreads, 0, stream, 1, true, p.plan, f,
-      reinterpret_cast<const int*>(ws + l.place), reinterpret_cast<const float*>(ws + l.sums), static_cast<int>(a.N), block_rows,
-      static_cast<int>(a.d), static_cast<int>(l.d_pad), static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden, aligned ? 1 : 0);
+      reinterpret_cast<const int*>(ws + l.place), reinterpret_cast<const float*>(ws + l.sums), static_cast<int>(a.N),
+      static_cast<int>(a.d), static_cast<int>(l.d_pad), static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden,
+      (place & 7) == 0 ? 1 : 0);
+  if (e == cudaSuccess && either) {
+    f.target = p.target;
+    e = launch_overlapped(
+        loss_dhidden_turn_kernel, dim3(static_cast<unsigned>((a.N + 31) / 32), static_cast<unsigned>((a.d + 63) / 64)), kTurnThreads, 0,
+        stream, 1, true, p.plan, f, g.origin, reinterpret_cast<const float*>(ws + l.sums), static_cast<int>(a.d), l.sums_rows,
+        static_cast<__nv_bfloat16*>(a.d_hidden), a.s_dhidden, (place & 15) == 0 ? 1 : 0);
+  }
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "hidden gradient launch: %s", cudaGetErrorString(e));
 }
 

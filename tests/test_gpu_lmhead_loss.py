@@ -162,6 +162,38 @@ def test_the_targets_terms_keep_their_precision(N, V, d, piece, weights):
     assert B.device_error() == 0
 
 
+@pytest.mark.parametrize("N,V,d", [(900, 1500, 1024), (300, 700, 1024), (4200, 300, 256)])
+def test_replayed_with_more_and_fewer_scored_rows(N, V, d):
+    """One captured pass over numbers of scored rows that take single CTAs and pairs."""
+    from paper_2608_02625_gb300 import binding as B
+    h, w, all_t, dl = inputs(N, V, d, seed=12, scored="all")
+    t = all_t.clone()
+    loss, lse, dh, dw = torch.empty(N, device=dev()), torch.empty(N, device=dev()), torch.empty_like(h), torch.empty_like(w)
+    a, b = ws_loss(N, d), ws_grad(N, V, d, 512)
+
+    def go():
+        B.dlm_lmhead_loss(h, w, t, loss, lse, a)
+        B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh, dw, b)
+
+    go()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        go()
+    order = torch.randperm(N, generator=torch.Generator().manual_seed(1))
+    for n in (N, 384, 385, 128, 129, 256, 257, 0, 1, N - 1):
+        if n > N:
+            continue
+        keep = torch.zeros(N, dtype=torch.bool)
+        keep[order[:n]] = True
+        t.copy_(torch.where(keep.to(dev()), all_t, -1))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_loss(h, w, t, loss, lse, f"{n} of {N}")
+        check_grad(h, w, t, lse, dl, dh, dw, f"{n} of {N}", -(-V // 512))
+    assert B.device_error() == 0
+
+
 @pytest.mark.parametrize("N,V", [(128, 300), (100, 1), (77, 5)])
 def test_many_rows_of_one_token(N, V):
     from paper_2608_02625_gb300 import binding as B
