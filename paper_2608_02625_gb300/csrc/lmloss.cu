@@ -65,10 +65,21 @@ constexpr float kLog2e = 1.4426950408889634f;
 // 121; 256 137, 127; 320 (of the pair's two tiles one is nearly empty) 184, 200; 448 232, 217;
 // gradients 256 460, 559; 320 601, 619; 448 771, 668; 512 712, 684. By width: loss 4096 x 1024
 // 778, 741; x 512 400, 419 (the epilogues of both wait for the slower); gradients 4096 x 512
-// 1452, 1300; x 256 857, 803; x 64 661, 718; 2048 x 256 (V = 20000) 82, 83.
-bool pairs_for_loss(int64_t N, int64_t d) { return N > kBM && d >= 1024; }
-bool pairs_for_gradients(int64_t N, int64_t d) { return N > 3 * kBM && d >= (N >= 4096 ? 256 : 512); }
-__device__ bool pairs_pay(int n, bool gradients) { return n > 3 * kBM || (!gradients && n > kBM && n <= 2 * kBM); }
+// 1452, 1300; x 256 857, 803; x 64 661, 718; 2048 x 256 (V = 20000) 82, 83. Of small products
+// pairs make too few tiles, each later done: gradients of 500 x 4000 x 512 31, 57;
+// 700 x 10000 x 1024 59, 65; 1024 x 10000 x 1024 80, 79; 1024 x 20000 x 1024 120, 109; loss
+// 1024 x 4000 x 2048 27, 29; 2048 x 4000 x 2048 41, 41; 1024 x 10000 x 2048 61, 60.
+constexpr double kPairLoss = 16e9, kPairGradients = 10e9;  // n V d
+bool pairs_have_room(int64_t N, int64_t d) { return N > 3 * kBM && d >= (N >= 4096 ? 256 : 512); }  // gradients' workspace
+// The scored rows from which pairs pay for themselves; 0: never, in a call of N rows.
+int pair_rows(int64_t N, int64_t V, int64_t d, bool gradients) {
+  if (gradients ? !pairs_have_room(N, d) : N <= kBM || d < 1024) return 0;
+  const double rows = ceil((gradients ? kPairGradients : kPairLoss) / (static_cast<double>(V) * static_cast<double>(d)));
+  return rows > static_cast<double>(N) ? 0 : rows < 1.0 ? 1 : static_cast<int>(rows);
+}
+__device__ bool pairs_pay(int n, int from, bool gradients) {
+  return n >= from && (n > 3 * kBM || (!gradients && n > kBM && n <= 2 * kBM));
+}
 
 enum Mode { kStats, kGrad, kBack };
 
@@ -675,7 +686,8 @@ struct GatherParams {
   int64_t s_dhidden;
   float* loss;          // loss only: 0 for rows that are not scored
   float* lse_out;
-  bool gradients, either;  // either: pairs, or not
+  bool gradients;
+  int pair_rows;        // the scored rows from which CTAs work in pairs, 0: never
   struct Form {
     int block_rows;     // rows of a tile
     int tiles, workers, dw_tiles;  // gradients: what the K splits of dh depend on, with kblocks and max_rows
@@ -835,7 +847,7 @@ __global__ void __launch_bounds__(kGatherThreads) loss_gather_kernel(const Gathe
   if (blockIdx.x != gridDim.x - 1) return;
   const int n = before, end = (n + 2 * kBM - 1) / (2 * kBM) * (2 * kBM);
   if (warp == 0) {
-    const int pairs = p.either && pairs_pay(n, p.gradients);
+    const int pairs = p.pair_rows && pairs_pay(n, p.pair_rows, p.gradients);
     const int splits = p.gradients ? choose_splits(p, p.form[pairs], n) : 1;
     if (lane == 0) {
       p.plan->n = n;
@@ -1110,7 +1122,7 @@ Layout layout_of(int64_t N, int64_t d, bool grad) {
     l.lse2 = take(&at, l.n_pad * 4);
     l.dloss = take(&at, l.n_pad * 4);
     l.rest = take(&at, l.n_pad * 4);
-    if (pairs_for_gradients(N, d)) {
+    if (pairs_have_room(N, d)) {
       l.origin = take(&at, l.n_pad * 4);
       l.turned = take(&at, l.n_pad * l.d_pad * 2);
     }
@@ -1174,11 +1186,12 @@ size_t loss_grad_workspace_bytes(int64_t N, int64_t V, int64_t d, int64_t piece)
 
 int launch_loss(const LossArgs& a, cudaStream_t stream) {
   const Layout l = layout_of(a.N, a.d, false);
-  const Team teams[2] = {team_of(1), pairs_for_loss(a.N, a.d) ? team_of(2) : Team{2, 0}};
+  const int from = pair_rows(a.N, a.V, a.d, false);
+  const Team teams[2] = {team_of(1), from ? team_of(2) : Team{2, 0}};
   const bool either = teams[1].workers > 0;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   GatherParams g = {};
-  g.either = either;
+  g.pair_rows = either ? from : 0;
   g.loss = a.loss;
   g.lse_out = a.lse_out;
   int st;
@@ -1228,7 +1241,8 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
     Maps grad, back;
   } forms[2] = {};
   forms[0].team = team_of(1);
-  forms[1].team = pairs_for_gradients(a.N, a.d) ? team_of(2) : Team{2, 0};
+  const int from = pair_rows(a.N, a.V, a.d, true);
+  forms[1].team = from ? team_of(2) : Team{2, 0};
   const bool either = forms[1].team.workers > 0;
   GatherParams g = {};
   int st;
@@ -1261,7 +1275,7 @@ int launch_loss_grad(const LossArgs& a, cudaStream_t stream) {
   }
 
   g.gradients = true;
-  g.either = either;
+  g.pair_rows = either ? from : 0;
   g.lse = a.lse;
   g.dloss = a.dloss;
   g.to_lse2 = reinterpret_cast<float*>(ws + l.lse2);

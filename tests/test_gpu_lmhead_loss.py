@@ -126,8 +126,95 @@ def test_gradients(N, V, d, scored):
     check_grad(h, w, t, lse, dl, dh, dw, f"{N}x{V}x{d} {scored}")
 
 
+# Products large enough for pairs of CTAs (with half of the rows scored, single ones).
+PAIRS = [(700, 11500, 2048), (1300, 12401, 1032), (200, 40001, 2048), (4200, 9301, 264)]
+
+
+@pytest.mark.parametrize("N,V,d,scored", [(*s, k) for s in PAIRS for k in ("all", "half")] + [(*PAIRS[0], "none"), (*PAIRS[0], "last")])
+def test_pairs(N, V, d, scored):
+    from paper_2608_02625_gb300 import binding as B
+    h, w, t, dl = inputs(N, V, d, seed=13, scored=scored)
+    gd = Guarded()
+    loss, lse, dh, dw = gd.empty(N), gd.empty(N), gd.empty(N, d, dtype=BF), gd.empty(V, d, dtype=BF)
+    B.dlm_lmhead_loss(h, w, t, loss, lse, ws_loss(N, d))
+    gd.check()
+    check_loss(h, w, t, loss, lse)
+    lse = fp64_lse(h, w, t)
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh, dw, ws_grad(N, V, d))
+    gd.check()
+    assert B.device_error() == 0
+    check_grad(h, w, t, lse, dl, dh, dw)
+
+
+def test_pairs_pieces_and_single_gradients():
+    from paper_2608_02625_gb300 import binding as B
+    N, V, d, piece = 900, 11300, 1024, 4096
+    h, w, t, dl = inputs(N, V, d, seed=14, scored="all")
+    t[::50] = -1
+    lse = fp64_lse(h, w, t)
+    ws = ws_grad(N, V, d, piece)
+    dh, dw, dh1, dw1 = (torch.full(s, 7.0, dtype=BF, device=dev()) for s in ((N, d), (V, d), (N, d), (V, d)))
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh, dw, ws)
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, dh1, None, ws)
+    B.dlm_lmhead_loss_grad(h, w, t, lse, dl, None, dw1, ws)
+    torch.cuda.synchronize()
+    check_grad(h, w, t, lse, dl, dh, dw, "both", 3)
+    check_grad(h, w, t, lse, dl, dh1, None, "d_hidden alone", 3)
+    assert torch.equal(dw, dw1) and B.device_error() == 0
+
+
+@pytest.mark.parametrize("offset,gap,wgap", [(1, 0, 0), (3, 7, 16), (8, 16, 8)])
+def test_pairs_strides_and_alignment(offset, gap, wgap):
+    from paper_2608_02625_gb300 import binding as B
+    L, V, d = 130, 20500, 1024
+    N, row, wrow = 6 * L, d + gap, d + wgap
+    h, w, t, dl = inputs(N, V, d, seed=15, scored="all")
+    t[5::90] = V
+    gd = Guarded()
+    hs, ws_, ts = gd.like(h.view(6, L, d), offset=offset, row=row), gd.like(w, row=wrow), t.view(6, L)
+    loss, lse = gd.empty(6, L), gd.empty(6, L)
+    B.dlm_lmhead_loss(hs, ws_, ts, loss, lse, ws_loss(N, d))
+    gd.check()
+    check_loss(h, w, t, loss.view(-1), lse.view(-1))
+    dh, dw = gd.empty(6, L, d, dtype=BF, offset=offset, row=row), gd.empty(V, d, dtype=BF, row=wrow)
+    B.dlm_lmhead_loss_grad(hs, ws_, ts, lse, dl.view(6, L), dh, dw, ws_grad(N, V, d))
+    gd.check()
+    check_grad(h, w, t, lse.view(-1), dl, dh.reshape(N, d), dw)
+
+
+def test_pairs_replayed_with_more_and_fewer_scored_rows():
+    """One captured pass over numbers of scored rows that take single CTAs and pairs; the
+    same number gives the same bits as without the graph."""
+    from paper_2608_02625_gb300 import binding as B
+    N, V, d = 900, 9000, 2048
+    h, w, all_t, dl = inputs(N, V, d, seed=16, scored="all")
+    t = all_t.clone()
+    new = lambda: [torch.empty(N, device=dev()), torch.empty(N, device=dev()), torch.empty_like(h), torch.empty_like(w)]  # noqa: E731
+    a, b, first, out = ws_loss(N, d), ws_grad(N, V, d), new(), new()
+
+    def go(o):
+        B.dlm_lmhead_loss(h, w, t, o[0], o[1], a)
+        B.dlm_lmhead_loss_grad(h, w, t, o[1], dl, o[2], o[3], b)
+
+    go(first)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        go(out)
+    for n in (100, N, 600, 0, N):
+        t.copy_(torch.where(torch.arange(N, device=dev()) % N < n, all_t, -1))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_loss(h, w, t, out[0], out[1], f"{n} of {N}")
+        check_grad(h, w, t, out[1], dl, out[2], out[3], f"{n} of {N}")
+    assert B.device_error() == 0
+    for x, y in zip(first, out):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("weights", ["equal", "any"])
-@pytest.mark.parametrize("N,V,d,piece", [(200, 3001, 128, 0), (200, 3001, 128, 1024), (600, 2500, 512, 0), (1, 300, 64, 0)])
+@pytest.mark.parametrize("N,V,d,piece", [(200, 3001, 128, 0), (200, 3001, 128, 1024), (600, 2500, 512, 0), (1, 300, 64, 0),
+                                         (800, 13000, 1024, 0)])
 def test_the_targets_terms_keep_their_precision(N, V, d, piece, weights):
     """The bounds of check_grad but for the target's term, which is most of a row's
     gradient. In d_hidden it is not rounded to bf16: two fp32 roundings instead of 2^-8.

@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
 
 
-@pytest.mark.parametrize("N,V,d", [(256, 4096, 2048), (1024, 4096, 2048)], ids=["single_ctas", "pairs"])
+@pytest.mark.parametrize("N,V,d", [(256, 4096, 2048), (1024, 4096, 2048), (2048, 5200, 2048)],
+                         ids=["single_ctas", "more_rows", "pairs"])
 def test_loss_pipelines_time_out_and_recover(tmp_path, N, V, d):
     from paper_2608_02625_gb300 import binding as Bn
     from paper_2608_02625_gb300 import build
