@@ -436,6 +436,15 @@ __device__ __forceinline__ void mma_commit_pair_elect(uint64_t* bar) {
       : "memory");
 }
 
+// The same on the issuing CTA's barrier alone.
+__device__ __forceinline__ void mma_commit_leader_elect(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+      : "memory");
+}
+
 // The address of a shared variable of CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t smem_of_rank(const void* p, uint32_t rank) {
   uint32_t a;

@@ -95,7 +95,7 @@ struct Smem {
   uint64_t empty[kStages];  // stage read by its MMAs  (MMA -> TMA)
   uint64_t acc_full[2];     // accumulator complete    (MMA -> epilogue)
   uint64_t acc_empty[2];    // accumulator read out    (epilogue -> MMA; a pair's: in the leader)
-  uint64_t done;            // every MMA completed     (teardown)
+  uint64_t done;            // every MMA completed     (teardown; a pair's: in the leader)
   uint32_t tmem_base;
   int abort;
 };
@@ -435,7 +435,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         commit(&sm.acc_full[acc]);
       }
     }
-    commit(&sm.done);
+    // In this CTA alone: the other one does not wait for it, and may be gone when it arrives.
+    if (kCtas == 2)
+      mma_commit_leader_elect(&sm.done);
+    else
+      mma_commit_elect(&sm.done);
     mbar_drain(&sm.done, 0);
     __syncwarp();
   } else if (warp >= kEpiWarp0) {
