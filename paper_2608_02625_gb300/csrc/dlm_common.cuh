@@ -452,6 +452,11 @@ __device__ __forceinline__ uint32_t smem_of_rank(const void* p, uint32_t rank) {
   return a;
 }
 
+// Written to a shared variable of another CTA of the cluster; seen behind a cluster barrier.
+__device__ __forceinline__ void store_at(uint32_t cluster_addr, int v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }

@@ -98,6 +98,9 @@ struct Smem {
   uint64_t done;            // every MMA completed     (teardown; a pair's: in the leader)
   uint32_t tmem_base;
   int abort;
+  // Of a pair, in both CTAs: what each has loaded, what the leader's MMAs have committed, and
+  // whether a role of either has given up.
+  int loads[2], mma_steps, mma_tiles, gave_up;
 };
 template <int kCtas>
 constexpr size_t smem_bytes() {
@@ -286,6 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(&sm.done, 1);
     sm.abort = 0;
+    sm.gave_up = 0;
     fence_mbar_init();
     fence_proxy_async_smem();
   }
@@ -308,6 +312,41 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* abort = &sm.abort;
   wait_for_previous();
   const Work<kMode, kCtas> work(p, workers);
+  // A role of a pair that ends early (a whole warp): see the end.
+  const auto give_up = [&] {
+    if (kCtas == 2 && lane < 2) store_at(smem_of_rank(&sm.gave_up, lane), 1);
+  };
+  // Step kb of a tile to stage st, by one thread.
+  const auto load_stage = [&](const Tile& tl, int kb, int st) {
+    const int bn = work.bn(p, tl), bn_own = bn / kCtas;  // columns of B, and this CTA's
+    const int m0 = tl.m * kRows + rank * kBM, n0 = tl.n * bn + rank * bn_own;
+    const uint32_t stage_bytes = kCtas * ((kMode == kStats && kCtas == 1 ? p.a_rows * 128 : kABytes) + bn_own * 128);
+    uint64_t* bar = &sm.full[st];
+    const uint32_t pair_bar = kCtas == 2 ? smem_of_rank(bar, 0) : 0;  // the leader's
+    const auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1) {
+      if (kCtas == 2)
+        tma_load_2d_pair(dst, map, pair_bar, c0, c1);
+      else
+        tma_load_2d(dst, map, bar, c0, c1);
+    };
+    if (rank == 0) mbar_arrive_expect_tx(bar, stage_bytes);
+    if (kMode == kStats || kMode == kGrad) {
+      load(sm.a[st], &ma, kb * kBK, m0);
+      load(sm.b[st], &mb, kb * kBK, p.v0 + n0);
+    } else if (tl.dw) {
+      for (int i = 0; i < 2; ++i) load(sm.a[st] + i * kBoxBytes, &mda, 0, (m0 / 64 + i) * p.n_pad + kb * kBK);
+      if (kCtas == 2)
+        load(sm.b[st], &mdb, kb * kBK, n0);
+      else
+        for (int i = 0; i < bn_own / 64; ++i) load(sm.b[st] + i * kBoxBytes, &mdb, n0 + 64 * i, kb * kBK);
+    } else if (kCtas == 2) {
+      for (int i = 0; i < 2; ++i) load(sm.a[st] + i * kBoxBytes, &ma, m0 + 64 * i, p.v0 + kb * kBK);
+      load(sm.b[st], &mb, 0, kb * p.n_pad + n0);
+    } else {
+      load(sm.a[st], &ma, 0, kb * p.n_pad + m0);
+      for (int i = 0; i < bn_own / 64; ++i) load(sm.b[st] + i * kBoxBytes, &mb, n0 + 64 * i, p.v0 + kb * kBK);
+    }
+  };
   if (warp == 0) {
     // ================================================================ TMA producer
     int fill = 0;
@@ -316,61 +355,29 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int t1 = work.last(p, item);
       for (int t = work.first(p, item); ok && t < t1; ++t) {
         const Tile tl = work.tile(p, item, t);
-        const int bn = work.bn(p, tl), bn_own = bn / kCtas;  // columns of B, and this CTA's
-        const int m0 = tl.m * kRows + rank * kBM, n0 = tl.n * bn + rank * bn_own;
-        const uint32_t stage_bytes = kCtas * ((kMode == kStats && kCtas == 1 ? p.a_rows * 128 : kABytes) + bn_own * 128);
         for (int kb = tl.k0; kb < tl.k1; ++kb, ++fill) {
           const int st = fill % kStages;
           if (fill >= kStages && !warp_wait(&sm.empty[st], ((fill / kStages) - 1) & 1, abort, p.err, p.wait_ns)) {
             ok = false;
             break;
           }
-          if (lane == 0) {
-            uint64_t* bar = &sm.full[st];
-            const uint32_t pair_bar = kCtas == 2 ? smem_of_rank(bar, 0) : 0;  // the leader's
-            const auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1) {
-              if (kCtas == 2)
-                tma_load_2d_pair(dst, map, pair_bar, c0, c1);
-              else
-                tma_load_2d(dst, map, bar, c0, c1);
-            };
-            if (rank == 0) mbar_arrive_expect_tx(bar, stage_bytes);
-            if (kMode == kStats || kMode == kGrad) {
-              load(sm.a[st], &ma, kb * kBK, m0);
-              load(sm.b[st], &mb, kb * kBK, p.v0 + n0);
-            } else if (tl.dw) {
-              for (int i = 0; i < 2; ++i) load(sm.a[st] + i * kBoxBytes, &mda, 0, (m0 / 64 + i) * p.n_pad + kb * kBK);
-              if (kCtas == 2)
-                load(sm.b[st], &mdb, kb * kBK, n0);
-              else
-                for (int i = 0; i < bn_own / 64; ++i) load(sm.b[st] + i * kBoxBytes, &mdb, n0 + 64 * i, kb * kBK);
-            } else if (kCtas == 2) {
-              for (int i = 0; i < 2; ++i) load(sm.a[st] + i * kBoxBytes, &ma, m0 + 64 * i, p.v0 + kb * kBK);
-              load(sm.b[st], &mb, 0, kb * p.n_pad + n0);
-            } else {
-              load(sm.a[st], &ma, 0, kb * p.n_pad + m0);
-              for (int i = 0; i < bn_own / 64; ++i) load(sm.b[st] + i * kBoxBytes, &mb, n0 + 64 * i, p.v0 + kb * kBK);
-            }
-          }
+          if (lane == 0) load_stage(tl, kb, st);
         }
       }
     }
     launch_dependents();
     // Teardown: every copy issued lands before the block exits. A single CTA waits for its
     // barriers; of a pair, whose copies complete on the leader's, each waits for the MMAs
-    // that read its stages, and where something has given up (the other CTA's copies, on
-    // which a barrier may wait, then need not come) gives the copies a millisecond.
+    // that read its stages, and where something has given up both settle their accounts
+    // behind the roles.
     if (kCtas == 2) {
       bool landed = ok;
       for (int s = 0; s < kStages; ++s) {
         const int n_s = fill > s ? (fill - s + kStages - 1) / kStages : 0;
         if (n_s && landed) landed = warp_wait(&sm.empty[s], (n_s - 1) & 1, abort, p.err, p.wait_ns);
       }
-      if (!landed) {
-        const uint64_t t0 = global_timer_ns();
-        while (global_timer_ns() - t0 < 1000000) {
-        }
-      }
+      if (lane < 2) store_at(smem_of_rank(&sm.loads[rank], lane), fill);  // here and in the other CTA
+      if (!landed) give_up();
     } else if (lane == 0) {
       for (int s = 0; s < kStages; ++s) {
         const int n_s = fill > s ? (fill - s + kStages - 1) / kStages : 0;
@@ -441,6 +448,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     else
       mma_commit_elect(&sm.done);
     mbar_drain(&sm.done, 0);
+    if (!ok) give_up();
+    if (kCtas == 2 && lane < 2) {
+      store_at(smem_of_rank(&sm.mma_steps, lane), fill);
+      store_at(smem_of_rank(&sm.mma_tiles, lane), tile);
+    }
     __syncwarp();
   } else if (warp >= kEpiWarp0) {
     // ================================================================ epilogue
@@ -648,7 +660,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         s += ts;
       }
-      if (!ok) break;
+      if (!ok) {
+        give_up();
+        break;
+      }
       if (kMode == kStats)
         p.part[(static_cast<int64_t>(item) + static_cast<int64_t>(half) * work.items) * kRows + rank * kBM + t_row] = make_float2(m, s);
     }
@@ -661,6 +676,42 @@ __global__ void __launch_bounds__(kThreads, 1)
     cg::this_cluster().sync();  // neither CTA's memory goes while the pair's copies and MMAs may use it
   else
     __syncthreads();
+  if (kCtas == 2 && sm.gave_up) {  // (the same in both)
+    if (threadIdx.x == 0) {
+      // The commits that arrive here, one of a barrier on its way at most: the next one needs
+      // what has waited for it.
+      const int steps = sm.mma_steps, tiles = sm.mma_tiles;
+      bool came = true;
+      for (int s = 0; s < kStages; ++s) {
+        const int n_s = steps > s ? (steps - s + kStages - 1) / kStages : 0;
+        if (n_s && came) came = mbar_drain(&sm.empty[s], (n_s - 1) & 1);
+      }
+      for (int i = 0; i < 2; ++i) {
+        const int n_i = tiles > i ? (tiles - i + 1) / 2 : 0;
+        if (n_i && came) came = mbar_drain(&sm.acc_full[i], (n_i - 1) & 1);
+      }
+      // The CTA behind loads what the other one has loaded (into stages that are free, or the
+      // other one's would not have been), so that every step's barrier in the leader gets
+      // all its bytes; there their number is waited for.
+      const int mine = sm.loads[rank], both = max(sm.loads[0], sm.loads[1]);
+      int at = 0;
+      for (int j = 0, item; at < both && (item = work.item(worker, workers, j)) >= 0; ++j) {
+        const int t1 = work.last(p, item);
+        for (int t = work.first(p, item); at < both && t < t1; ++t) {
+          const Tile tl = work.tile(p, item, t);
+          for (int kb = tl.k0; at < both && kb < tl.k1; ++kb, ++at)
+            if (at >= mine) load_stage(tl, kb, at % kStages);
+        }
+      }
+      if (rank == 0)
+        for (int s = 0; s < kStages; ++s) {
+          const int n_s = both > s ? (both - s + kStages - 1) / kStages : 0;
+          if (n_s && came) came = mbar_drain(&sm.full[s], (n_s - 1) & 1);
+        }
+    }
+    __syncwarp();
+    cg::this_cluster().sync();
+  }
   if (warp == 1) {
     tc_fence_after();
     if (kCtas == 2)
