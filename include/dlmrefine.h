@@ -378,8 +378,9 @@ size_t dlm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t d);
  *   norm         1 F32
  *   workspace    >= dlm_clip_grad_norm_workspace_bytes() bytes, 8-byte aligned, no initial
  *                contents needed; calls sharing it must not overlap on the GPU.
- * The norm is exact to fp32 rounding over the whole range of the inputs (squares that
- * leave fp32's range are summed in fp64) and summed in a fixed order. A NaN makes norm
+ * The norm is off by at most 12 roundings of fp32 (7.2e-7 relative) over the whole range of the
+ * inputs (a thread's squares, 128 of them in eight sums, are added in fp32, or in fp64 where
+ * they leave its range; all else in fp64) and summed in a fixed order. A NaN makes norm
  * and every output NaN; an infinity makes norm infinite and finite elements 0 (with an
  * infinite max_norm too, the factor is inf / inf: every output NaN).
  */

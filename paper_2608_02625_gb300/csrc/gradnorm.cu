@@ -94,15 +94,21 @@ __device__ double squares(const T* x, int64_t n, bool vectors) {
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
         const float f = f32_of(v[k].e[e]);
-        acc[e] = fmaf(f, f, acc[e]);
+        float& a = acc[(k * kPer + e) % 8];
+        a = fmaf(f, f, a);
         any |= bits_of(f);
       }
   }
-#pragma unroll 4
-  for (int i = whole + threadIdx.x; i < n; i += kThreads) {
-    const float f = f32_of(x[i]);
-    acc[0] = fmaf(f, f, acc[0]);
-    any |= bits_of(f);
+  for (int i = whole + threadIdx.x; i < n; i += kThreads * 8) {
+    float f[8] = {};
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i + k * kThreads < n) f[k] = f32_of(x[i + k * kThreads]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      acc[k] = fmaf(f[k], f[k], acc[k]);
+      any |= bits_of(f[k]);
+    }
   }
   const float s = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
   if (any == 0 || (s >= 0x1p-80f && s <= 0x1p120f)) return s;

@@ -160,3 +160,20 @@ def test_same_bits_again_on_another_stream_and_replayed():
     torch.cuda.synchronize()
     for a, b, c in zip(first, second, third):
         assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("dt,offset,big", [(F32, 0, 1024), (F32, 1, 256), (BF, 0, 2048), (BF, 1, 256)])
+def test_small_squares_behind_a_large_one(dt, offset, big):
+    """Chunks of 32768 elements (from 75 M in all), 128 a thread, of which each thread's first
+    ones are 4096 and the others 0.98: beside 2^24 a square below 1 is lost. In eight sums of
+    at most 17 squares, three levels of pairs and fp64 beyond them the sum of squares is off by
+    20 U relative at most, the norm by half of that and its own rounding; one sum of 128 loses
+    62 U of the norm here, four of 32 15 U."""
+    from paper_2608_02625_gb300 import binding as B
+    n = 80_000_003
+    x = torch.full((n + offset,), 0.98, dtype=dt, device=dev())[offset:]
+    x[torch.arange(n, device=dev()) % 32768 < big] = 4096.0
+    want = float(sum(p.double().square().sum() for p in x.split(10_000_000)) ** 0.5)
+    norm = torch.empty(1, device=dev())
+    B.dlm_clip_grad_norm([x], None, 1.0, norm, workspace())
+    assert abs(float(norm) - want) <= 12 * U32 * want
