@@ -402,8 +402,9 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true, kShort>::kCt
     float s[2] = {s0.x + s0.y, s1.x + s1.y};
     row_sums<2>(s, G, red[parity]);
     if (row < p.N) {
-      // dx = dout (w rstd) + ((x - mean) (-rstd^2 c2) - rstd c1)
-      const float c1 = -rstd * (s[0] * inv_d), c2 = -rstd * (rstd * (s[1] * inv_d));
+      // dx = rstd (dout w - ((x - mean) (rstd c2) + c1)): no square of rstd, which overflows where
+      // a row's deviations are below 1e-19.
+      const float c1 = -(s[0] * inv_d), c2 = -(rstd * (s[1] * inv_d));
       const float2 n1 = make_float2(c1, c1), n2 = make_float2(c2, c2);
       T* o = static_cast<T*>(p.out) + row * p.s_out + tid * VEC;
 #pragma unroll
@@ -413,7 +414,7 @@ __global__ void __launch_bounds__(kRowThreads, (Held<VEC, NV, true, kShort>::kCt
 #pragma unroll
         for (int k = 0; k < kPair; k += 2) {
           const float2 rest = ffma2(fadd2(make_float2(x[k], x[k + 1]), m2), n2, n1);
-          const float2 y = ffma2(make_float2(dy[k], dy[k + 1]), fmul2(make_float2(wv[k], wv[k + 1]), r2), rest);
+          const float2 y = fmul2(ffma2(make_float2(dy[k], dy[k + 1]), make_float2(wv[k], wv[k + 1]), rest), r2);
           x[k] = y.x;
           x[k + 1] = y.y;
         }

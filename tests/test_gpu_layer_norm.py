@@ -223,3 +223,18 @@ def test_same_bits_again_and_on_another_stream_and_replayed():
     torch.cuda.synchronize()
     for a, b_, c in zip(first, second, third):
         assert torch.equal(a, b_) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("d", [64, 1001, 2048, 5120, 8191, 8200])
+def test_gradients_of_rows_of_tiny_deviations(d, dt):
+    """eps = 0 and deviations of 1e-20: rstd is 1e20, whose square fp32 does not hold, the
+    gradients are of that size."""
+    _, w, _, dy = inputs(9, d, dt, F32, seed=9)
+    x = (torch.randn(9, d, generator=torch.Generator(device="cpu").manual_seed(d)) * 1e-20).to(dt).to(dev())
+    mean, rstd = (torch.from_numpy(v).float().to(dev()) for v in oracle.layer_norm(host(x), host(w), None, 0.0)[1:])
+    gd = Guarded()
+    dx, dw, db = gd.empty(9, d, dtype=dt), gd.empty(d), gd.empty(d)
+    run_grad(dy, x, w, mean, rstd, dx, dw, db)
+    gd.check()
+    check_grad(dy, x, w, mean, rstd, dx, dw, db, f"d={d}")
