@@ -42,7 +42,9 @@
  * - Calls are asynchronous on the stream set by dlm_set_stream for the calling
  *   thread (default: the legacy default stream). Outputs are valid once that
  *   stream has been synchronised. Arguments are validated on the host before
- *   any launch; a nonzero return means nothing was launched.
+ *   any launch; a nonzero return means nothing was launched (but for
+ *   DLM_ERR_CUDA where a launch itself failed: of a call of several launches
+ *   those before it may run).
  * - Values that live in device memory (sequence and prompt lengths) cannot be
  *   checked on the host: the kernels clamp them into range and record
  *   DLM_DEVERR_LENGTH in the device error word (dlm_get_device_error).
@@ -279,7 +281,8 @@ int dlm_refine_update_ranked(const dlm_tensor* tokens, const dlm_tensor* mask, c
  *
  *   hidden      [N, d] or [B, L, d] BF16, rows evenly strided, any alignment; d a multiple
  *               of 8 up to 2^20, N up to 2^28, V up to 2^30
- *   weight      [V, d] BF16; base pointer and row stride multiples of 16 bytes
+ *   weight      [V, d] BF16; base pointer and row stride multiples of 16 bytes, the stride below
+ *               2^40 bytes
  *   targets     N I32, contiguous (any rank with N elements, like loss and lse)
  *   loss, lse   N F32, contiguous
  *   workspace   >= dlm_lmhead_loss_workspace_bytes(N, d) bytes, 16-byte aligned, no initial
@@ -302,7 +305,7 @@ size_t dlm_lmhead_loss_workspace_bytes(int64_t rows, int64_t d);
  *   dloss       N F32, contiguous: the gradient of each row's loss (1 / n for a mean over n
  *               scored rows; a weight per row for a masked diffusion loss)
  *   d_hidden    the shape of hidden, BF16, rows evenly strided, any alignment; or NULL
- *   d_weight    [V, d] BF16; base pointer and row stride multiples of 16 bytes; or NULL
+ *   d_weight    [V, d] BF16; base pointer and row stride as weight's; or NULL
  *               (a frozen projection), not both
  *   workspace   16-byte aligned, no initial contents needed. The call works through the
  *               vocabulary in pieces, as large as the workspace allows (multiples of 256

@@ -1245,34 +1245,45 @@ int launch_loss(const LossArgs& a, cudaStream_t stream) {
   const Team teams[2] = {team_of(1), from ? team_of(2) : Team{2, 0}};
   const bool either = teams[1].workers > 0;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
-  GatherParams g = {};
-  g.pair_rows = either ? from : 0;
-  g.loss = a.loss;
-  g.lse_out = a.lse_out;
-  int st;
-  if ((st = launch_gather(a, l, g, stream)) != DLM_OK) return st;
   Params p = common_params(a, l);
   p.either = either;
   p.kblocks = static_cast<int>(l.d_pad / kBK);
   p.part = reinterpret_cast<float2*>(ws + l.part);
   p.x_target = reinterpret_cast<float*>(ws + l.x_target);
-  int parts[2] = {};
+  p.a_rows = a.N < kBM ? static_cast<int>((a.N + 7) / 8 * 8) : kBM;
+  // Single CTAs, and pairs where they may work; what can be refused, before the first launch.
+  struct Form {
+    int64_t row_blocks;
+    int bn, tiles, parts;
+    Maps maps;
+  } forms[2] = {};
+  int st;
   for (int i = 0; i <= (either ? 1 : 0); ++i) {
-    const Team& team = teams[i];
-    const int64_t block_rows = kBM * team.ctas, row_blocks = (a.N + block_rows - 1) / block_rows;
-    p.bn = choose_bn(a.V, row_blocks, team.workers, team.ctas);
-    p.tiles = static_cast<int>((a.V + p.bn - 1) / p.bn);
-    p.parts = parts[i] = p.tiles < kLossMaxParts ? p.tiles : kLossMaxParts;
-    p.a_rows = a.N < kBM ? static_cast<int>((a.N + 7) / 8 * 8) : kBM;
-    Maps m = {};
-    if ((st = make_matrix_map(&m.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, p.a_rows)) != DLM_OK) return st;
-    if ((st = make_matrix_map(&m.b, a.weight, true, a.V, a.d, a.s_weight, p.bn / team.ctas)) != DLM_OK) return st;
-    if ((st = launch_product<kStats>(team.ctas, m, p, p.parts * row_blocks, team.workers, stream)) != DLM_OK) return st;
+    Form& f = forms[i];
+    const int ctas = teams[i].ctas, block_rows = kBM * ctas;
+    f.row_blocks = (a.N + block_rows - 1) / block_rows;
+    f.bn = choose_bn(a.V, f.row_blocks, teams[i].workers, ctas);
+    f.tiles = static_cast<int>((a.V + f.bn - 1) / f.bn);
+    f.parts = f.tiles < kLossMaxParts ? f.tiles : kLossMaxParts;
+    if ((st = make_matrix_map(&f.maps.a, ws + l.hidden, true, l.n_pad, l.d_pad, l.d_pad, p.a_rows)) != DLM_OK) return st;
+    if ((st = make_matrix_map(&f.maps.b, a.weight, true, a.V, a.d, a.s_weight, f.bn / ctas)) != DLM_OK) return st;
+  }
+  GatherParams g = {};
+  g.pair_rows = either ? from : 0;
+  g.loss = a.loss;
+  g.lse_out = a.lse_out;
+  if ((st = launch_gather(a, l, g, stream)) != DLM_OK) return st;
+  for (int i = 0; i <= (either ? 1 : 0); ++i) {
+    const Form& f = forms[i];
+    p.bn = f.bn;
+    p.tiles = f.tiles;
+    p.parts = f.parts;
+    if ((st = launch_product<kStats>(teams[i].ctas, f.maps, p, f.parts * f.row_blocks, teams[i].workers, stream)) != DLM_OK) return st;
   }
   const cudaError_t e = launch_overlapped(
       loss_combine_kernel, dim3(static_cast<unsigned>((a.N * 32 + kCombineThreads - 1) / kCombineThreads)), kCombineThreads, 0, stream,
       1, true, p.plan, reinterpret_cast<const int*>(ws + l.place), static_cast<const float2*>(p.part),
-      static_cast<const float*>(p.x_target), static_cast<int>(a.N), 2 * parts[0], 2 * parts[1], a.loss, a.lse_out);
+      static_cast<const float*>(p.x_target), static_cast<int>(a.N), 2 * forms[0].parts, 2 * forms[1].parts, a.loss, a.lse_out);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "loss combine launch: %s", cudaGetErrorString(e));
 }
 

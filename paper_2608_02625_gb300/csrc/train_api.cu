@@ -1,6 +1,6 @@
 // libdlmrefine C ABI: the entry points of training the refiner's last layer
 // (argument validation, dispatch). The rules of the other entry points hold: a
-// nonzero status means that nothing was launched.
+// nonzero status means that nothing was launched, unless a launch itself failed.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -92,6 +92,15 @@ bool aligned_rows(const dlm_tensor* t) {
   return t->shape[0] <= 1 || (t->stride[0] * elem_size(t->dtype)) % 16 == 0;
 }
 
+// A matrix that TMA moves: even rows at multiples of 16 bytes, less than 2^40 bytes apart.
+int check_matrix(const dlm_tensor* t, const char* name, int64_t rows, int64_t width) {
+  if (rows > 1 && t->stride[0] < width) return fail(DLM_ERR_STRIDE, "%s rows overlap", name);
+  if (rows > 1 && t->stride[0] >= (int64_t{1} << 40) / elem_size(t->dtype))
+    return fail(DLM_ERR_STRIDE, "%s rows must lie less than 2^40 bytes apart", name);
+  if (!aligned_rows(t)) return fail(DLM_ERR_ALIGN, "%s rows must start at multiples of 16 bytes", name);
+  return DLM_OK;
+}
+
 constexpr int64_t kMostRows = int64_t{1} << 28, kMostVocab = int64_t{1} << 30, kMostWidth = int64_t{1} << 20;
 
 // The arguments that the loss and its gradients share.
@@ -106,8 +115,7 @@ int prepare_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_t
   if (a->V < 1) return fail(DLM_ERR_SHAPE, "V must be >= 1");
   if (a->N > kMostRows || a->V > kMostVocab || a->d > kMostWidth)
     return fail(DLM_ERR_SHAPE, "at most 2^28 rows, 2^30 tokens and a width of 2^20");
-  if (a->V > 1 && weight->stride[0] < a->d) return fail(DLM_ERR_STRIDE, "weight rows overlap");
-  if (!aligned_rows(weight)) return fail(DLM_ERR_ALIGN, "weight rows must start at multiples of 16 bytes");
+  if ((st = check_matrix(weight, "weight", a->V, a->d))) return st;
   a->hidden = hidden->data;
   a->weight = weight->data;
   a->targets = static_cast<const int32_t*>(targets->data);
@@ -168,8 +176,7 @@ int dlm_lmhead_loss_grad(const dlm_tensor* hidden, const dlm_tensor* weight, con
   if (d_weight) {
     if ((st = check_tensor(d_weight, "d_weight", 1 << DLM_BF16, 2, 2))) return st;
     if (!same_shape(weight, d_weight)) return fail(DLM_ERR_SHAPE, "d_weight must have the shape of weight");
-    if (a.V > 1 && d_weight->stride[0] < a.d) return fail(DLM_ERR_STRIDE, "d_weight rows overlap");
-    if (!aligned_rows(d_weight)) return fail(DLM_ERR_ALIGN, "d_weight rows must start at multiples of 16 bytes");
+    if ((st = check_matrix(d_weight, "d_weight", a.V, a.d))) return st;
     a.d_weight = d_weight->data;
     a.s_dweight = a.V > 1 ? d_weight->stride[0] : a.d;
   }

@@ -179,3 +179,15 @@ def test_loss_workspace_sizes():
     assert size(128, 300, 64, 10 ** 6) == size(128, 300, 64, 300)
     assert size(16384, 151552, 2048) < 3 * 2 ** 30
     assert size(128, 300, 64, 2 ** 63 - 1) == size(128, 300, 64, 300)
+
+
+@pytest.mark.parametrize("stride,status", [(2 ** 39, -4), (2 ** 60, -4), (2 ** 62 + 8, -4), (2 ** 39 - 8, None)])
+def test_rows_further_apart_than_a_copy_can_address(stride, status):
+    """2^40 bytes from row to row are refused before anything else of the device is asked for;
+    a stride below passes (to the check of the workspace, too small here)."""
+    far = lambda at: T(BF16, [2, 64], at, [stride, 1])  # noqa: E731
+    small = dict(ws=ctypes.c_void_p(16), nbytes=ctypes.c_size_t(16))
+    for name, args in (("dlm_lmhead_loss", {**loss_args(V=2), "w": far(20 * MB), **small}),
+                       ("dlm_lmhead_loss_grad", {**loss_grad_args(V=2), "w": far(20 * MB), **small}),
+                       ("dlm_lmhead_loss_grad", {**loss_grad_args(V=2), "dw": far(20 * MB), **small})):
+        assert call(name, *args.values()) == (-6 if status is None else status)

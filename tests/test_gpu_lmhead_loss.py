@@ -583,3 +583,30 @@ def test_a_training_step_of_the_last_layer():
     assert abs(float(norm) / float(total) - 1) <= 2.0 ** -5
     for got, want, s in ((dx, X.grad, 1.0), (dw, W.grad, scale), (dnw, NW.grad, scale), (dnb, NB.grad, scale)):
         assert float((got.double().cpu() - s * want).norm() / (s * want).norm()) <= 2.0 ** -5
+
+
+def test_a_refused_weight_leaves_the_outputs_alone():
+    """Rows of the weight 2^40 bytes apart (never read): nothing runs, not even for the rows
+    that are not scored."""
+    import ctypes
+
+    from paper_2608_02625_gb300 import binding as B
+    N, d = 40, 64
+    buf = torch.zeros(1 << 20, dtype=torch.uint8, device=dev())  # the weight behind the others
+    cut = lambda at, dtype, *s: buf[at:].view(dtype)[:int(np.prod(s))].view(*s)  # noqa: E731
+    h, loss, lse = cut(0, BF, N, d), cut(1 << 17, torch.float32, N), cut(2 << 17, torch.float32, N)
+    t, dh, dw = cut(3 << 17, torch.int32, N).fill_(-1), cut(4 << 17, BF, N, d), cut(5 << 17, BF, 2, d)
+    w = B.describe(cut(7 << 17, BF, 2, d))
+    w.stride[0] = 2 ** 39
+    for o in (loss, lse, dh, dw):
+        o.fill_(7.0)
+    dl = torch.ones(N, device=dev())
+    ws, wsg = ws_loss(N, d), ws_grad(N, 2, d)
+    refs = lambda *ts: [ctypes.byref(B.describe(x) if isinstance(x, torch.Tensor) else x) for x in ts]  # noqa: E731
+    torch.cuda.synchronize()
+    B._prepare(h, loss)
+    assert B.lib.dlm_lmhead_loss(*refs(h, w, t, loss, lse), *B._workspace(ws)) == -4
+    assert B.lib.dlm_lmhead_loss_grad(*refs(h, w, t, lse, dl, dh, dw), *B._workspace(wsg)) == -4
+    torch.cuda.synchronize()
+    for o in (loss, lse, dh, dw):
+        assert bool((o == 7.0).all())
