@@ -372,7 +372,8 @@ size_t dlm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t d);
  *   outs[i] = grads[i] * min(1, max_norm / (norm + 1e-6))
  *
  *   grads, outs  arrays of `count` descriptors (host memory, read during the call):
- *                contiguous tensors of any rank and size (empty ones too), BF16 or F32 each,
+ *                contiguous tensors of any rank (1 to 4) and size (empty ones, and up to 2^40
+ *                elements, in one extent if need be), BF16 or F32 each,
  *                outs[i] of the shape and dtype of grads[i]. outs[i] may be grads[i] itself
  *                (in place); no other overlap with an output is allowed, so a tensor listed
  *                twice is refused where it is written. outs NULL: the norm alone.

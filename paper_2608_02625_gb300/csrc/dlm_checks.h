@@ -25,8 +25,10 @@ inline int64_t numel(const dlm_tensor* t) {
 }
 
 // Checks pointer, dtype, rank, non-negative extents and a contiguous innermost
-// dimension. `name` appears in the error message.
-inline int check_tensor(const dlm_tensor* t, const char* name, int dtype_mask, int ndim_lo, int ndim_hi) {
+// dimension. `name` appears in the error message. most: the largest extent; the number of
+// elements fits 62 bits in any case.
+inline int check_tensor(const dlm_tensor* t, const char* name, int dtype_mask, int ndim_lo, int ndim_hi,
+                        int64_t most = 0x7FFFFFFF) {
   if (!t) return fail(DLM_ERR_NULL, "%s: descriptor is NULL", name);
   if (elem_size(t->dtype) == 0 || !((1 << t->dtype) & dtype_mask))
     return fail(DLM_ERR_DTYPE, "%s: unsupported dtype %d", name, t->dtype);
@@ -34,8 +36,11 @@ inline int check_tensor(const dlm_tensor* t, const char* name, int dtype_mask, i
     return fail(DLM_ERR_SHAPE, "%s: rank %d not in [%d, %d]", name, t->ndim, ndim_lo, ndim_hi);
   for (int i = 0; i < t->ndim; ++i) {
     if (t->shape[i] < 0) return fail(DLM_ERR_SHAPE, "%s: negative extent", name);
-    if (t->shape[i] > 0x7FFFFFFFLL) return fail(DLM_ERR_SHAPE, "%s: extent too large", name);
+    if (t->shape[i] > most) return fail(DLM_ERR_SHAPE, "%s: extent too large", name);
   }
+  double elements = 1;
+  for (int i = 0; i < t->ndim; ++i) elements *= static_cast<double>(t->shape[i] > 0 ? t->shape[i] : 1);
+  if (elements > 0x1p62) return fail(DLM_ERR_SHAPE, "%s: too many elements", name);
   if (numel(t) > 0) {
     if (!t->data) return fail(DLM_ERR_NULL, "%s: data pointer is NULL", name);
     if (t->shape[t->ndim - 1] > 1 && t->stride[t->ndim - 1] != 1)

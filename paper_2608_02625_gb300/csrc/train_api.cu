@@ -300,14 +300,13 @@ int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t 
     for (int i = 0; i < count; ++i) {
       const dlm_tensor* g = grads + i;
       const dlm_tensor* o = outs ? outs + i : g;
-      if ((st = check_tensor(g, "gradient", kMaskBF16F32, 1, 4))) return st;
+      constexpr int64_t kMost = int64_t{1} << 40;  // a flat buffer of all gradients is one extent
+      if ((st = check_tensor(g, "gradient", kMaskBF16F32, 1, 4, kMost))) return st;
       if (o != g) {
-        if ((st = check_tensor(o, "scaled gradient", 1 << g->dtype, 1, 4))) return st;
+        if ((st = check_tensor(o, "scaled gradient", 1 << g->dtype, 1, 4, kMost))) return st;
         if (!same_shape(g, o)) return fail(DLM_ERR_SHAPE, "tensor %d: the output must have the gradient's shape", i);
       }
-      double n = 1;
-      for (int k = 0; k < g->ndim; ++k) n *= static_cast<double>(g->shape[k]);
-      if (n > 0x1p40) return fail(DLM_ERR_SHAPE, "tensor %d: more than 2^40 elements", i);
+      if (numel(g) > kMost) return fail(DLM_ERR_SHAPE, "tensor %d: more than 2^40 elements", i);
       if (!is_dense(g) || !is_dense(o)) return fail(DLM_ERR_STRIDE, "tensor %d must be contiguous", i);
       const int64_t size = numel(g);
       if (size == 0) continue;

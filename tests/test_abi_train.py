@@ -191,3 +191,15 @@ def test_rows_further_apart_than_a_copy_can_address(stride, status):
                        ("dlm_lmhead_loss_grad", {**loss_grad_args(V=2), "w": far(20 * MB), **small}),
                        ("dlm_lmhead_loss_grad", {**loss_grad_args(V=2), "dw": far(20 * MB), **small})):
         assert call(name, *args.values()) == (-6 if status is None else status)
+
+
+def test_clip_takes_extents_past_32_bits():
+    """A flat buffer of 2^31 elements and more is taken (up to the check of overlaps, which
+    ends the call here); 2^40 elements are the most, in one extent or in several."""
+    big, out = T(BF16, [2 ** 31 + 5], MB), T(BF16, [2 ** 31 + 5], 3 * MB)
+    assert clip([big], [out]) == -6
+    assert clip([T(BF16, [2 ** 40], MB)], [T(BF16, [2 ** 40], 3 * MB)]) == -6
+    assert clip([T(BF16, [2 ** 40 + 1], MB)], None) == -3
+    assert clip([T(BF16, [2 ** 33, 2 ** 8], MB)], None) == -3
+    assert clip([T(BF16, [2 ** 40, 2 ** 40, 2 ** 40, 2 ** 8], MB)], None) == -3    # 2^128
+    assert clip([T(F32, [2 ** 31 + 5], MB)], [T(F32, [2 ** 31 + 4], 3 * MB)]) == -3

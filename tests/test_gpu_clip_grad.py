@@ -177,3 +177,19 @@ def test_small_squares_behind_a_large_one(dt, offset, big):
     norm = torch.empty(1, device=dev())
     B.dlm_clip_grad_norm([x], None, 1.0, norm, workspace())
     assert abs(float(norm) - want) <= 12 * U32 * want
+
+
+def test_offsets_past_32_bits():
+    """2.2e9 elements behind a small tensor, in place."""
+    from paper_2608_02625_gb300 import binding as B
+    n = 2_200_000_007
+    x = torch.full((n,), 2.0 ** -6, dtype=BF, device=dev())
+    x[-5:] = 3.0
+    small = torch.full((77,), 0.5, device=dev())
+    want = (n * 2.0 ** -12 + 5 * (9.0 - 2.0 ** -12) + 77 * 0.25) ** 0.5
+    norm = torch.empty(1, device=dev())
+    B.dlm_clip_grad_norm([small, x], [small, x], want / 2, norm, workspace())
+    assert abs(float(norm) - want) <= 12 * U32 * want
+    # the factor is 1/2 but for 1e-6 / norm and the norm's roundings, lost in bf16's
+    assert bool((x[:-5] == 2.0 ** -7).all()) and bool((x[-5:] == 1.5).all())
+    assert float((small - 0.25).abs().max()) <= 0.25 * (16 * U32 + 1e-6 / want)

@@ -238,3 +238,28 @@ def test_gradients_of_rows_of_tiny_deviations(d, dt):
     run_grad(dy, x, w, mean, rstd, dx, dw, db)
     gd.check()
     check_grad(dy, x, w, mean, rstd, dx, dw, db, f"d={d}")
+
+
+def test_offsets_past_32_bits():
+    """2.3e9 elements: the first and the last rows, and the sums over the columns, against
+    fp64 on the GPU. (Sums of ones times x: dbias is the number of rows exactly.)"""
+    from paper_2608_02625_gb300 import binding as B
+    N, d = 1_130_000, 2048
+    g = torch.Generator(device=dev()).manual_seed(4)
+    x = torch.empty(N, d, dtype=BF, device=dev()).normal_(generator=g)
+    w, b = 1 + 0.3 * torch.randn(d, device=dev(), generator=g), torch.randn(d, device=dev(), generator=g)
+    out, mean, rstd = torch.empty_like(x), torch.empty(N, device=dev()), torch.empty(N, device=dev())
+    B.dlm_layer_norm(x, w, b, 1e-5, out, mean, rstd)
+    dy, dx, dw, db = torch.ones_like(x), torch.empty_like(x), torch.empty(d, device=dev()), torch.empty(d, device=dev())
+    run_grad(dy, x, w, mean, rstd, dx, dw, db)
+    for r in (slice(0, 3), slice(2 ** 31 // d - 1, 2 ** 31 // d + 2), slice(N - 3, N)):
+        check_norm(x[r], w, b, out[r], mean[r], rstd[r], 1e-5)
+        check_grad(dy[r], x[r], w, mean[r], rstd[r], dx[r], None, None)
+    assert bool((db == N).all())
+    want, mags = torch.zeros(d, dtype=torch.float64, device=dev()), torch.zeros(d, dtype=torch.float64, device=dev())
+    for i in range(0, N, 50_000):
+        xhat = (x[i:i + 50_000].double() - mean[i:i + 50_000, None].double()) * rstd[i:i + 50_000, None].double()
+        want += xhat.sum(0)
+        mags += xhat.abs().sum(0)
+    # rows of one group one after another (N / 608 at most), then as in check_grad
+    assert bool(((dw.double() - want).abs() <= (N / 608 + 1 + 89) * U32 * mags).all())
