@@ -28,7 +28,7 @@
  * refiners as they are; these have no counterpart in it):
  *   dlm_lmhead_loss, dlm_lmhead_loss_grad  cross entropy of given tokens under the
  *                                          projection, logits never stored
- *   dlm_layer_norm, dlm_layer_norm_grad    the norm in front of the projection
+ *   dlm_layer_norm, dlm_layer_norm_grad    a layer norm in front of the projection
  *   dlm_clip_grad_norm                     the norm over all gradients, clipping
  *
  * Conventions shared by every call
@@ -325,21 +325,25 @@ int dlm_lmhead_loss_grad(const dlm_tensor* hidden, const dlm_tensor* weight, con
 size_t dlm_lmhead_loss_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int64_t piece);
 
 /*
- * Layer norm over the last dimension, the norm in front of an output
- * projection (dlm_lmhead_confidence):
+ * Layer norm over the last dimension, for models with such a norm in front of the output
+ * projection (dlm_lmhead_confidence); an RMS norm is another function:
  *   mean[r] = sum_c x[r, c] / d
  *   rstd[r] = 1 / sqrt(sum_c (x[r, c] - mean[r])^2 / d + eps)
  *   out[r, c] = (x[r, c] - mean[r]) * rstd[r] * weight[c] + bias[c]
  *
  *   x, out        [N, d] or [B, L, d], BF16 or F32 (both the same dtype); innermost
  *                 contiguous, rows evenly strided; d from 1 to 2^24, any alignment
- *                 (16-byte aligned rows are faster)
+ *                 (16-byte aligned rows are faster; of others the whole blocks of 16 bytes
+ *                 around a row are read, up to 15 bytes before and behind it, and dropped)
  *   weight, bias  d entries, BF16 or F32 (both the same dtype), contiguous; bias may be
  *                 NULL
  *   mean, rstd    N F32, contiguous: what dlm_layer_norm_grad reads; either may be NULL
  *   eps           finite, >= 0
  * Sums in fp32 over the centred values; one rounding to the output's dtype. out may
- * not overlap x. A row with a NaN or an infinity gives NaN.
+ * not overlap x. A row with a NaN or an infinity gives NaN. A row whose sum, or sum of
+ * centred squares, leaves fp32's range is outside of what this computes: deviations above
+ * about 1e19 / sqrt(d) (rstd is 0), and, where eps does not cover them, below 1e-19 (their
+ * squares lose digits, then vanish).
  */
 int dlm_layer_norm(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* bias, float eps, dlm_tensor* out,
                    dlm_tensor* mean, dlm_tensor* rstd);
@@ -351,7 +355,7 @@ int dlm_layer_norm(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tens
  *   dweight[c] = sum_r dout[r, c] xhat[r, c]
  *   dbias[c]   = sum_r dout[r, c]
  *
- *   dout, dx        the shape and dtype of x, rows evenly strided
+ *   dout, dx        the shape and dtype of x, rows evenly strided, any alignment (as above)
  *   mean, rstd      N F32, as dlm_layer_norm wrote them
  *   dweight, dbias  d entries of weight's dtype, contiguous; either may be NULL. With no
  *                   rows they are 0.

@@ -77,8 +77,9 @@ def _load():
     lib.dlm_refine_step_workspace_bytes.restype = ctypes.c_size_t
     for f in ("dlm_bidir_attn", "dlm_attn_masked", "dlm_vocab_confidence", "dlm_refine_update", "dlm_refine_step",
               "dlm_refine_step_static", "dlm_token_prob", "dlm_refine_update_ranked", "dlm_lmhead_confidence",
-              "dlm_lmhead_loss", "dlm_lmhead_loss_grad", "dlm_layer_norm", "dlm_layer_norm_grad", "dlm_clip_grad_norm", "dlm_set_stream", "dlm_set_attn_tiles_per_unit",
-              "dlm_version", "dlm_get_device_error"):
+              "dlm_lmhead_loss", "dlm_lmhead_loss_grad", "dlm_layer_norm", "dlm_layer_norm_grad",
+              "dlm_clip_grad_norm", "dlm_set_stream", "dlm_set_attn_tiles_per_unit", "dlm_version",
+              "dlm_get_device_error"):
         getattr(lib, f).restype = ctypes.c_int
     lib.dlm_loop_begin.argtypes = [ctypes.c_void_p]
     lib.dlm_loop_end.argtypes = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p)]

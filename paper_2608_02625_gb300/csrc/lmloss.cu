@@ -6,8 +6,9 @@
 //   d_hidden = g weight,   d_weight = g^T hidden
 //
 // Rows without a target (outside [0, V)) are not scored: the first launch copies the
-// hidden states of the others, in their order, to the workspace (n rows), so the products take time for scored rows alone -- of a
-// masked diffusion batch a quarter, say -- and their number stays on the GPU.
+// hidden states of the others, in their order, to the workspace (n rows), so the products
+// take time for scored rows alone -- of a masked diffusion batch a quarter, say -- and
+// their number stays on the GPU.
 //
 // The products run through one persistent kernel in three modes, 128 x bn output tiles a
 // CTA (bn up to 256), K steps of 64 through a ring of 192 KB:
@@ -32,7 +33,8 @@
 // -(1 - p) nearly exact. Warp 0 loads by TMA, warp 1 issues tcgen05.mma (both operands in
 // shared memory), warps 4-11 read the fp32 accumulators (two, so a tile's epilogue runs
 // under the next one's K loop) and write their tiles through shared memory by TMA.
-// Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, drains and exits.
+// Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, lets what it has on
+// its way land (a pair: in both CTAs) and exits.
 #include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
