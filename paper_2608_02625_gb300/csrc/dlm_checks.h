@@ -54,6 +54,7 @@ inline int check_tensor(const dlm_tensor* t, const char* name, int dtype_mask, i
 }
 
 inline bool is_dense(const dlm_tensor* t) {
+  if (numel(t) == 0) return true;
   int64_t expect = 1;
   for (int i = t->ndim - 1; i >= 0; --i) {
     if (t->shape[i] > 1 && t->stride[i] != expect) return false;

@@ -203,3 +203,15 @@ def test_clip_takes_extents_past_32_bits():
     assert clip([T(BF16, [2 ** 33, 2 ** 8], MB)], None) == -3
     assert clip([T(BF16, [2 ** 40, 2 ** 40, 2 ** 40, 2 ** 8], MB)], None) == -3    # 2^128
     assert clip([T(F32, [2 ** 31 + 5], MB)], [T(F32, [2 ** 31 + 4], 3 * MB)]) == -3
+
+
+def test_empty_tensors_of_several_dimensions():
+    """An empty tensor's strides say nothing (torch's of [5, 0] are 1, 1): taken as contiguous."""
+    empty = [T(BF16, [5, 0], 0, [1, 1]), T(F32, [0, 4, 3], 0, [12, 3, 1]), T(F32, [2, 0, 3], 0, [3, 3, 1])]
+    twice = [T(BF16, [100], 20 * MB)] * 2
+    assert clip(empty + twice, empty + twice) == -6    # (the overlap of the others)
+    none = dict(t=T(I32, [3, 0], 0, [1, 1]), lse=T(F32, [3, 0], 0, [1, 1]))
+    rows = T(BF16, [3, 0, 64], 0, [64, 64, 1])
+    assert call("dlm_lmhead_loss", *{**loss_args(), **none, "h": rows, "loss": T(F32, [0], 0)}.values()) == 0
+    assert call("dlm_lmhead_loss_grad", *{**loss_grad_args(), **none, "h": rows, "dloss": T(F32, [0], 0), "dh": rows,
+                                          "dw": None}.values()) == 0

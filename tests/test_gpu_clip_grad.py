@@ -193,3 +193,11 @@ def test_offsets_past_32_bits():
     # the factor is 1/2 but for 1e-6 / norm and the norm's roundings, lost in bf16's
     assert bool((x[:-5] == 2.0 ** -7).all()) and bool((x[-5:] == 1.5).all())
     assert float((small - 0.25).abs().max()) <= 0.25 * (16 * U32 + 1e-6 / want)
+
+
+def test_empty_gradients_of_several_dimensions():
+    from paper_2608_02625_gb300 import binding as B
+    grads = make([500], [F32], seed=9) + [torch.empty(s, dtype=BF, device=dev()) for s in ((5, 0), (0, 7), (2, 0, 3))]
+    outs, norm = [torch.empty_like(g) for g in grads], torch.empty(1, device=dev())
+    B.dlm_clip_grad_norm(grads, outs, 1e-3, norm, workspace())
+    check(grads[:1], outs[:1], norm, np.float64(np.float32(1e-3)))
