@@ -19,6 +19,8 @@ inline int64_t elem_size(int dtype) {
 }
 
 inline int64_t numel(const dlm_tensor* t) {
+  for (int i = 0; i < t->ndim; ++i)
+    if (t->shape[i] == 0) return 0;
   int64_t n = 1;
   for (int i = 0; i < t->ndim; ++i) n *= t->shape[i];
   return n;
@@ -39,7 +41,7 @@ inline int check_tensor(const dlm_tensor* t, const char* name, int dtype_mask, i
     if (t->shape[i] > most) return fail(DLM_ERR_SHAPE, "%s: extent too large", name);
   }
   double elements = 1;
-  for (int i = 0; i < t->ndim; ++i) elements *= static_cast<double>(t->shape[i] > 0 ? t->shape[i] : 1);
+  for (int i = 0; i < t->ndim; ++i) elements *= static_cast<double>(t->shape[i]);
   if (elements > 0x1p62) return fail(DLM_ERR_SHAPE, "%s: too many elements", name);
   if (numel(t) > 0) {
     if (!t->data) return fail(DLM_ERR_NULL, "%s: data pointer is NULL", name);

@@ -215,3 +215,12 @@ def test_empty_tensors_of_several_dimensions():
     assert call("dlm_lmhead_loss", *{**loss_args(), **none, "h": rows, "loss": T(F32, [0], 0)}.values()) == 0
     assert call("dlm_lmhead_loss_grad", *{**loss_grad_args(), **none, "h": rows, "dloss": T(F32, [0], 0), "dh": rows,
                                           "dw": None}.values()) == 0
+
+
+def test_an_empty_tensor_may_have_any_other_extents():
+    m = 2 ** 31 - 1
+    big = T(BF16, [100], 20 * MB)
+    for shape in ([0, m, m, m], [m, m, m, 0], [m, 0, m, m]):
+        empty = T(F32, shape, 0, [0, 0, 0, 1])
+        assert clip([empty, big, big], [empty, big, big]) == -6    # (the overlap of the others)
+    assert clip([T(F32, [m, m, m, 1], MB)], None) == -3
