@@ -187,3 +187,34 @@ def test_a_captured_call_over_the_numbers_of_scored_rows_where_the_form_changes(
             check(h, w, t, dl, *out)
         else:
             assert not any(bool(o.any()) for o in out)
+
+
+def test_two_host_threads_at_once():
+    """Each with its own stream, buffers and size; the library's calls run without the
+    interpreter's lock."""
+    import threading
+    sizes = [PAIRS, PIECES]
+    want = [waited(size, seed)[0] for size, seed in zip(sizes, (1, 2))]
+    steps = [Step(*size, seed) for size, seed in zip(sizes, (1, 2))]
+    got, failed = [None, None], []
+    torch.cuda.synchronize()
+
+    def work(k):
+        try:
+            stream = torch.cuda.Stream(dev())
+            with torch.cuda.device(dev()), torch.cuda.stream(stream):
+                got[k] = steps_of(steps[k])
+            stream.synchronize()
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    torch.cuda.synchronize()
+    assert steps[0].B.device_error(clear=True) == 0
+    for g, w in zip(got, want):
+        same(g, w)
