@@ -76,7 +76,10 @@ __device__ __forceinline__ const Tensor& find(const Tab& tab, int chunk) {
 
 __device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// This thread's share of the squares of x[0, n).
+// This thread's share of the squares of x[0, n): at most 17 in each of eight sums, whatever the
+// type and alignment. (Four sums of 32 for fp32: 155 M elements, norm and scaling, 300 instead of
+// 304 us, and up to 18 roundings of the norm instead of 11. Single elements in one sum: 68, and
+// 310 M of bf16 460 us instead of 300, the norm alone.)
 template <typename T>
 __device__ double squares(const T* x, int64_t n, bool vectors) {
   constexpr int kPer = 16 / sizeof(T), kLoads = 4;
