@@ -30,6 +30,7 @@
  *                                          projection, logits never stored
  *   dlm_layer_norm, dlm_layer_norm_grad    a layer norm in front of the projection
  *   dlm_clip_grad_norm                     the norm over all gradients, clipping
+ *   dlm_adamw                              the optimizer's step, clipping included
  *
  * Conventions shared by every call
  * --------------------------------
@@ -395,6 +396,59 @@ size_t dlm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t d);
 int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t count, float max_norm, dlm_tensor* norm,
                        void* workspace, size_t workspace_bytes);
 size_t dlm_clip_grad_norm_workspace_bytes(void);
+
+/*
+ * Parameters of an AdamW step.
+ *   beta1, beta2   in [0, 1);  eps, weight_decay  finite, >= 0
+ *   max_norm       >= 0 (infinity: no clipping); read only with a norm
+ *   lr             device float[1]: the learning rate
+ *   step           device int32[1]: the number t of this step, from 1 on; the caller counts.
+ *                  A value below 1 is taken as 1 and recorded as DLM_DEVERR_LENGTH.
+ *   norm           device float[1], the norm over all gradients (dlm_clip_grad_norm with outs
+ *                  NULL writes it): gradients are scaled by min(1, max_norm / (norm + 1e-6))
+ *                  on their way, and need not be written clipped before. NULL: not scaled.
+ * lr, step and norm are read when the step runs, so a captured step follows their changes.
+ */
+typedef struct dlm_adamw_params {
+  double beta1, beta2, eps, weight_decay, max_norm;
+  const float* lr;
+  const int32_t* step;
+  const float* norm;
+} dlm_adamw_params;
+
+/* Elements of a tensor that share a scale where states are held in 8 bits. */
+#define DLM_ADAMW_BLOCK 256
+
+/*
+ * One AdamW step (decoupled weight decay) over many tensors:
+ *   g = grads[i] min(1, max_norm / (norm + 1e-6))            (g = grads[i] without a norm)
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ *   params     arrays of `count` descriptors each (host memory, read during the call):
+ *   masters    contiguous tensors of any rank (1 to 4) and size (empty ones, and up to 2^40
+ *   grads      elements); the tensors at one place of the arrays have the same shape.
+ *   m, v       params BF16 or F32, updated in place; grads BF16 or F32, only read.
+ *              masters NULL, or F32 tensors that hold the weights: they are updated and
+ *              params, BF16, become their rounded copies (what params hold is not read).
+ *              m, v: F32, updated in place, zeros before the first step. Or U8: the e4m3
+ *              codes of m / scale and of sqrt(v) / scale, zeros before the first step.
+ *   m_scales,  NULL where m and v are F32. Where they are U8, F32 tensors with an entry for
+ *   v_scales   every DLM_ADAMW_BLOCK elements, the last ones' too: the block's largest
+ *              magnitude, of m or sqrt(v), over 448; zeros before the first step.
+ *   count      0 .. 15360
+ *   hyper      host memory, read during the call; of what it points to see above
+ * No tensor may overlap another one that is written, nor may lr, step and norm.
+ * Arithmetic in fp32. 8-bit states round to the nearest code (half a step: 2^-4 relative
+ * from 2^-6 of the scale up, 2^-10 of the scale below); a sqrt(v) above 0 is held as the
+ * smallest code at least, so that no weight is divided by eps alone on the next step. The
+ * step itself uses m and v before that rounding. A block whose scale is below fp32's normal
+ * range is held as zeros. A NaN or an infinity in a gradient makes its weight NaN, and
+ * where states are held in 8 bits those of its whole block.
+ */
+int dlm_adamw(const dlm_tensor* params, const dlm_tensor* masters, const dlm_tensor* grads, const dlm_tensor* m,
+              const dlm_tensor* v, const dlm_tensor* m_scales, const dlm_tensor* v_scales, int32_t count,
+              const dlm_adamw_params* hyper);
 
 /*
  * Steps A2 and A3 in one call (the per-position reduction of the confidences

@@ -37,6 +37,12 @@ class DlmRefineParams(ctypes.Structure):
                 ("prompt_lens", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p)]
 
 
+class DlmAdamwParams(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("max_norm", ctypes.c_double), ("lr", ctypes.c_void_p),
+                ("step", ctypes.c_void_p), ("norm", ctypes.c_void_p)]
+
+
 class DlmError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"libdlmrefine status {status}: {message}")
@@ -68,6 +74,7 @@ def _load():
     lib.dlm_layer_norm_grad_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64]
     lib.dlm_clip_grad_norm.argtypes = [P, P, ctypes.c_int32, ctypes.c_float, P, ctypes.c_void_p, ctypes.c_size_t]
     lib.dlm_clip_grad_norm_workspace_bytes.argtypes = []
+    lib.dlm_adamw.argtypes = [P] * 7 + [ctypes.c_int32, ctypes.POINTER(DlmAdamwParams)]
     for f in ("dlm_lmhead_loss_workspace_bytes", "dlm_lmhead_loss_grad_workspace_bytes",
               "dlm_layer_norm_grad_workspace_bytes", "dlm_clip_grad_norm_workspace_bytes"):
         getattr(lib, f).restype = ctypes.c_size_t
@@ -78,7 +85,7 @@ def _load():
     for f in ("dlm_bidir_attn", "dlm_attn_masked", "dlm_vocab_confidence", "dlm_refine_update", "dlm_refine_step",
               "dlm_refine_step_static", "dlm_token_prob", "dlm_refine_update_ranked", "dlm_lmhead_confidence",
               "dlm_lmhead_loss", "dlm_lmhead_loss_grad", "dlm_layer_norm", "dlm_layer_norm_grad",
-              "dlm_clip_grad_norm", "dlm_set_stream", "dlm_set_attn_tiles_per_unit", "dlm_version",
+              "dlm_clip_grad_norm", "dlm_adamw", "dlm_set_stream", "dlm_set_attn_tiles_per_unit", "dlm_version",
               "dlm_get_device_error"):
         getattr(lib, f).restype = ctypes.c_int
     lib.dlm_loop_begin.argtypes = [ctypes.c_void_p]
@@ -350,6 +357,49 @@ def dlm_clip_grad_norm(grads, outs, max_norm: float, norm, workspace):
     dn = describe(norm)
     _check(lib.dlm_clip_grad_norm(dg, do, n, float(max_norm), _ref(dn), *_workspace(workspace)))
     return outs, norm
+
+
+@dataclasses.dataclass
+class AdamwParams:
+    lr: torch.Tensor           # float32 [1] on the device
+    step: torch.Tensor         # int32 [1] on the device: the number of the step, from 1 on
+    beta1: float = 0.9
+    beta2: float = 0.999
+    eps: float = 1e-8
+    weight_decay: float = 0.0
+    norm: torch.Tensor | None = None  # float32 [1] on the device: gradients are clipped by it
+    max_norm: float = float("inf")
+
+    def to_c(self) -> DlmAdamwParams:
+        for t, dtype in ((self.lr, torch.float32), (self.step, torch.int32), (self.norm, torch.float32)):
+            if t is not None and (t.dtype != dtype or not t.is_cuda or t.numel() != 1):
+                raise ValueError("lr, step and norm must be one-element CUDA tensors (float32, int32, float32)")
+        return DlmAdamwParams(float(self.beta1), float(self.beta2), float(self.eps), float(self.weight_decay),
+                              float(self.max_norm), self.lr.data_ptr(), self.step.data_ptr(),
+                              None if self.norm is None else self.norm.data_ptr())
+
+
+_marshal.set_adamw_type(AdamwParams)
+
+ADAMW_BLOCK = 256  # elements that share a scale where states are held in 8 bits
+
+
+def dlm_adamw(params, masters, grads, m, v, m_scales, v_scales, hyper: AdamwParams):
+    """One AdamW step over lists of tensors, in place: params (with masters, float32 tensors
+    that hold the weights, their bfloat16 copies), m and v. m_scales and v_scales None: m and
+    v are float32; else uint8 codes (e4m3, of sqrt(v) for v) with a float32 scale for every
+    ADAMW_BLOCK elements. All states are zeros before the first step."""
+    if _done(_marshal.adamw(params, masters, grads, m, v, m_scales, v_scales, hyper)):
+        return params
+    lists = [params, masters, grads, m, v, m_scales, v_scales]
+    if any(x is not None and len(x) != len(params) for x in lists):
+        raise ValueError("every list must have one tensor per parameter")
+    _prepare(hyper.lr, hyper.step, hyper.norm, *[t for x in lists if x is not None for t in x])
+    n = len(params)
+    ds = [None if x is None else (DlmTensor * max(1, n))(*[describe(t) for t in x]) for x in lists]
+    cp = hyper.to_c()
+    _check(lib.dlm_adamw(*ds, n, ctypes.byref(cp)))
+    return params
 
 
 def dlm_token_prob(logits, tokens, lse, prob):

@@ -33,7 +33,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 LIBS = {
     "libdlmrefine.so": ["dlm_api.cu", "attn_tc.cu", "attn_f32.cu", "vocab.cu", "update.cu", "loop.cu", "lmhead.cu",
                         "selftest.cu", "train_api.cu", "lmloss.cu", "layernorm.cu",
-                        "gradnorm.cu"],
+                        "gradnorm.cu", "adamw.cu"],
     "libdlmsynth.so": ["synth.cu"],
 }
 # The Python binding's marshalling: host code against torch's headers, beside the library it calls.

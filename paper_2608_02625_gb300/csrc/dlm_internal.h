@@ -259,4 +259,29 @@ constexpr int kMaxGradTensors = 16 * kGradTable;
 inline size_t clip_grad_norm_workspace_bytes() { return sizeof(double) * kGradParts * (kMaxGradTensors / kGradTable); }
 int launch_clip_grad_norm(const GradArgs& a, cudaStream_t stream);
 
+// One AdamW step over many tensors.
+struct AdamwTensor {
+  void* p;         // weights, F32 or BF16 (with a master: its BF16 copy)
+  float* master;   // may be null
+  const void* g;
+  void* m;         // F32, or codes
+  void* v;
+  float* ms;       // scales of the codes
+  float* vs;
+  int64_t n;       // > 0
+  bool p_bf16, g_bf16;
+};
+struct AdamwArgs {
+  const AdamwTensor* tensors;
+  int count;
+  bool eight;      // states in 8 bits
+  double beta1, beta2, eps, weight_decay, max_norm;
+  const float* lr;
+  const int32_t* step;
+  const float* norm;  // may be null
+};
+constexpr int kAdamwBlock = 256;  // elements that share a scale
+constexpr int kAdamwTable = 384;  // tensors a launch
+int launch_adamw(const AdamwArgs& a, cudaStream_t stream);
+
 }  // namespace dlm

@@ -27,7 +27,9 @@ namespace {
 constexpr int kMaxTensors = 12;
 
 PyObject* g_params_type = nullptr;  // RefineParams
+PyObject* g_adamw_type = nullptr;   // AdamwParams
 PyObject *s_threshold, *s_k, *s_frac, *s_mask_id, *s_prompt, *s_seq;
+PyObject *s_beta1, *s_beta2, *s_eps, *s_decay, *s_max_norm, *s_lr, *s_step, *s_norm;
 
 // The tensors of one call. Every method returns false where the general path
 // has to decide.
@@ -68,6 +70,19 @@ class Call {
     p->remask_k = static_cast<int32_t>(k);
     p->mask_id = static_cast<int32_t>(mask_id);
     return lengths(o, s_prompt, &p->prompt_lens) && lengths(o, s_seq, &p->seq_lens);
+  }
+
+  bool adamw(PyObject* o, dlm_adamw_params* p) {
+    if (reinterpret_cast<PyObject*>(Py_TYPE(o)) != g_adamw_type) return false;
+    const void *lr, *step, *norm;
+    if (!number(o, s_beta1, &p->beta1) || !number(o, s_beta2, &p->beta2) || !number(o, s_eps, &p->eps) ||
+        !number(o, s_decay, &p->weight_decay) || !number(o, s_max_norm, &p->max_norm) || !scalar(o, s_lr, at::kFloat, false, &lr) ||
+        !scalar(o, s_step, at::kInt, false, &step) || !scalar(o, s_norm, at::kFloat, true, &norm))
+      return false;
+    p->lr = static_cast<const float*>(lr);
+    p->step = static_cast<const int32_t*>(step);
+    p->norm = static_cast<const float*>(norm);
+    return true;
   }
 
   // The current stream of the tensors' device, for the library.
@@ -146,6 +161,21 @@ class Call {
     const bool ok = plain(x, &t) && t->scalar_type() == at::kInt && t->is_contiguous();
     if (ok) *v = static_cast<const int32_t*>(t->data_ptr());
     Py_DECREF(x);  // the RefineParams keeps it
+    return ok;
+  }
+
+  // The address of a one-element tensor (null for None where `optional`).
+  bool scalar(PyObject* o, PyObject* name, at::ScalarType type, bool optional, const void** v) {
+    PyObject* x = PyObject_GetAttr(o, name);
+    if (!x) return false;
+    at::Tensor* t = nullptr;
+    bool ok = optional && x == Py_None;
+    *v = nullptr;
+    if (!ok && plain(x, &t) && t->scalar_type() == type && t->numel() == 1) {
+      *v = t->data_ptr();
+      ok = true;
+    }
+    Py_DECREF(x);  // the AdamwParams keeps it
     return ok;
   }
 
@@ -364,6 +394,26 @@ PyObject* clip_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// params, masters (or None), grads, m, v, m_scales, v_scales (None: states in 32 bits), hyper
+PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 8, [&](Call& c, int* st) {
+    std::vector<dlm_tensor> t[7];
+    dlm_tensor none;
+    dlm_tensor* p[7];
+    dlm_adamw_params hyper;
+    for (int i = 0; i < 7; ++i) {
+      const bool optional = i == 1 || i >= 5;
+      p[i] = nullptr;
+      if (optional && a[i] == Py_None) continue;
+      if (!c.list(a[i], &t[i]) || t[i].size() != t[0].size() || t[i].size() > INT32_MAX) return false;
+      p[i] = t[i].empty() ? &none : t[i].data();
+    }
+    if (!c.adamw(a[7], &hyper) || !c.stream()) return false;
+    *st = unlocked([&] { return dlm_adamw(p[0], p[1], p[2], p[3], p[4], p[5], p[6], static_cast<int32_t>(t[0].size()), &hyper); });
+    return true;
+  });
+}
+
 // handle (a non-zero int), device index
 PyObject* loop_launch(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(n, 2, [&](Call&, int* st) {
@@ -384,6 +434,12 @@ PyObject* set_params_type(PyObject*, PyObject* type) {
   Py_RETURN_NONE;
 }
 
+PyObject* set_adamw_type(PyObject*, PyObject* type) {
+  Py_XDECREF(g_adamw_type);
+  g_adamw_type = Py_NewRef(type);
+  Py_RETURN_NONE;
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bidir_attn),
                          FAST(attn_masked),
@@ -399,8 +455,10 @@ PyMethodDef methods[] = {FAST(bidir_attn),
                          FAST(layer_norm),
                          FAST(layer_norm_grad),
                          FAST(clip_grad_norm),
+                         FAST(adamw),
                          FAST(loop_launch),
                          {"set_params_type", set_params_type, METH_O, nullptr},
+                         {"set_adamw_type", set_adamw_type, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -414,5 +472,13 @@ PyMODINIT_FUNC PyInit__marshal(void) {
   s_mask_id = PyUnicode_InternFromString("mask_id");
   s_prompt = PyUnicode_InternFromString("prompt_lens");
   s_seq = PyUnicode_InternFromString("seq_lens");
+  s_beta1 = PyUnicode_InternFromString("beta1");
+  s_beta2 = PyUnicode_InternFromString("beta2");
+  s_eps = PyUnicode_InternFromString("eps");
+  s_decay = PyUnicode_InternFromString("weight_decay");
+  s_max_norm = PyUnicode_InternFromString("max_norm");
+  s_lr = PyUnicode_InternFromString("lr");
+  s_step = PyUnicode_InternFromString("step");
+  s_norm = PyUnicode_InternFromString("norm");
   return PyModule_Create(&module);
 }

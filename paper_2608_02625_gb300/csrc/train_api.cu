@@ -79,6 +79,40 @@ int check_workspace(const void* workspace, size_t bytes, size_t need, uintptr_t 
   return DLM_OK;
 }
 
+struct Span {
+  uintptr_t lo, hi;
+};
+
+// Whether no written range overlaps another range: both lists walked together in the order of
+// their addresses (which tensors allocated one after another often have already).
+bool written_apart(std::vector<Span>* read, std::vector<Span>* written) {
+  const auto before = [](const Span& p, const Span& q) { return p.lo < q.lo; };
+  for (std::vector<Span>* v : {read, written})
+    if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
+  uintptr_t end = 0, written_end = 0;  // the furthest end so far, of any and of a written range
+  for (size_t i = 0, j = 0; i < read->size() || j < written->size();) {
+    const bool write = i == read->size() || (j < written->size() && (*written)[j].lo < (*read)[i].lo);
+    const Span& p = write ? (*written)[j++] : (*read)[i++];
+    if (p.lo < (write ? end : written_end)) return false;
+    end = std::max(end, p.hi);
+    if (write) written_end = std::max(written_end, p.hi);
+  }
+  return true;
+}
+
+constexpr int64_t kMostElements = int64_t{1} << 40;  // of a tensor in a list (a flat buffer is one extent)
+
+// A contiguous tensor of a list, and the bytes that it takes (none where it is empty).
+int list_tensor(const dlm_tensor* t, const char* name, int dtype_mask, int i, Span* span) {
+  int st;
+  if ((st = check_tensor(t, name, dtype_mask, 1, 4, kMostElements))) return st;
+  if (numel(t) > kMostElements) return fail(DLM_ERR_SHAPE, "%s %d: more than 2^40 elements", name, i);
+  if (!is_dense(t)) return fail(DLM_ERR_STRIDE, "%s %d must be contiguous", name, i);
+  span->lo = reinterpret_cast<uintptr_t>(t->data);
+  span->hi = span->lo + static_cast<uintptr_t>(numel(t)) * elem_size(t->dtype);
+  return DLM_OK;
+}
+
 // Every kernel records device-side failures in the error word; refuse to launch without it.
 int require_error_word() {
   if (!device_error_word()) return fail(DLM_ERR_CUDA, "device error word unavailable on this device");
@@ -287,9 +321,6 @@ int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t 
   if (!(max_norm >= 0.f)) return fail(DLM_ERR_ARG, "max_norm must not be negative or NaN");
   if ((st = check_vector(norm, "norm", 1 << DLM_F32, 1, false))) return st;
   if ((st = check_workspace(workspace, workspace_bytes, clip_grad_norm_workspace_bytes(), 8, nullptr, 0))) return st;
-  struct Span {
-    uintptr_t lo, hi;
-  };
   // Nothing thrown leaves a C entry point: the only throwing calls are these vectors'.
   try {
     std::vector<GradTensor> list;
@@ -322,20 +353,8 @@ int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t 
     const uintptr_t norm_at = reinterpret_cast<uintptr_t>(norm->data), ws_at = reinterpret_cast<uintptr_t>(workspace);
     written.push_back({norm_at, norm_at + sizeof(float)});
     written.push_back({ws_at, ws_at + clip_grad_norm_workspace_bytes()});
-    // A written range may overlap no other: both lists walked together in the order of their
-    // addresses (which tensors allocated one after another often have already).
-    const auto before = [](const Span& p, const Span& q) { return p.lo < q.lo; };
-    for (std::vector<Span>* v : {&read, &written})
-      if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
-    uintptr_t end = 0, written_end = 0;  // the furthest end so far, of any and of a written range
-    for (size_t i = 0, j = 0; i < read.size() || j < written.size();) {
-      const bool write = i == read.size() || (j < written.size() && written[j].lo < read[i].lo);
-      const Span& p = write ? written[j++] : read[i++];
-      if (p.lo < (write ? end : written_end))
-        return fail(DLM_ERR_ARG, "an output overlaps a gradient, another output, norm or the workspace");
-      end = std::max(end, p.hi);
-      if (write) written_end = std::max(written_end, p.hi);
-    }
+    if (!written_apart(&read, &written))
+      return fail(DLM_ERR_ARG, "an output overlaps a gradient, another output, norm or the workspace");
     GradArgs a = {};
     a.grads = list.data();
     a.count = static_cast<int>(list.size());
@@ -346,6 +365,87 @@ int dlm_clip_grad_norm(const dlm_tensor* grads, const dlm_tensor* outs, int32_t 
     return launch_clip_grad_norm(a, current_stream());
   } catch (const std::bad_alloc&) {
     return fail(DLM_ERR_ARG, "out of host memory for the list of gradients");
+  }
+}
+
+int dlm_adamw(const dlm_tensor* params, const dlm_tensor* masters, const dlm_tensor* grads, const dlm_tensor* m,
+              const dlm_tensor* v, const dlm_tensor* m_scales, const dlm_tensor* v_scales, int32_t count,
+              const dlm_adamw_params* hyper) {
+  clear_error();
+  int st;
+  if (count < 0 || count > kMaxGradTensors) return fail(DLM_ERR_ARG, "count must be in [0, %d]", kMaxGradTensors);
+  if (count > 0 && (!params || !grads || !m || !v)) return fail(DLM_ERR_NULL, "params, grads, m or v is NULL");
+  if ((m_scales == nullptr) != (v_scales == nullptr)) return fail(DLM_ERR_NULL, "m_scales and v_scales must both be given or both be NULL");
+  if (!hyper || !hyper->lr || !hyper->step) return fail(DLM_ERR_NULL, "hyper, its lr or its step is NULL");
+  const auto in_unit = [](double b) { return b >= 0.0 && b < 1.0; };
+  const auto rate = [](double x) { return x >= 0.0 && !std::isinf(x); };
+  if (!in_unit(hyper->beta1) || !in_unit(hyper->beta2)) return fail(DLM_ERR_ARG, "beta1 and beta2 must be in [0, 1)");
+  if (!rate(hyper->eps) || !rate(hyper->weight_decay)) return fail(DLM_ERR_ARG, "eps and weight_decay must be finite and not negative");
+  if (hyper->norm && !(hyper->max_norm >= 0.0)) return fail(DLM_ERR_ARG, "max_norm must not be negative or NaN");
+  const uintptr_t scalars[3] = {reinterpret_cast<uintptr_t>(hyper->lr), reinterpret_cast<uintptr_t>(hyper->step),
+                                reinterpret_cast<uintptr_t>(hyper->norm)};
+  for (const uintptr_t at : scalars)
+    if (at % 4 != 0) return fail(DLM_ERR_ALIGN, "lr, step and norm must be 4-byte aligned");
+  AdamwArgs a = {};
+  a.eight = m_scales != nullptr;
+  const int state = a.eight ? 1 << DLM_U8 : 1 << DLM_F32;
+  // Nothing thrown leaves a C entry point: the only throwing calls are these vectors'.
+  try {
+    std::vector<AdamwTensor> list;
+    std::vector<Span> read, written;
+    list.reserve(count);
+    read.reserve(static_cast<size_t>(count) + 3);
+    written.reserve(6 * static_cast<size_t>(count));
+    for (const uintptr_t at : scalars)
+      if (at) read.push_back({at, at + 4});
+    for (int i = 0; i < count; ++i) {
+      struct Entry {
+        const dlm_tensor* t;
+        const char* name;
+        int mask;
+        bool scales;
+      };
+      const Entry entries[7] = {{grads + i, "gradient", kMaskBF16F32, false},
+                                {params + i, "params", masters ? 1 << DLM_BF16 : kMaskBF16F32, false},
+                                {masters ? masters + i : nullptr, "masters", 1 << DLM_F32, false},
+                                {m + i, "m", state, false},
+                                {v + i, "v", state, false},
+                                {a.eight ? m_scales + i : nullptr, "m_scales", 1 << DLM_F32, true},
+                                {a.eight ? v_scales + i : nullptr, "v_scales", 1 << DLM_F32, true}};
+      void* data[7] = {};
+      int64_t n = 0;
+      for (int k = 0; k < 7; ++k) {
+        const Entry& e = entries[k];
+        if (!e.t) continue;
+        Span span;
+        if ((st = list_tensor(e.t, e.name, e.mask, i, &span))) return st;
+        if (k == 0) n = numel(e.t);
+        if (e.scales ? numel(e.t) != (n + kAdamwBlock - 1) / kAdamwBlock : !same_shape(e.t, grads + i))
+          return fail(DLM_ERR_SHAPE, e.scales ? "%s %d: an entry for every 256 elements expected" : "%s %d must have the gradient's shape",
+                      e.name, i);
+        data[k] = e.t->data;
+        if (n > 0) (k == 0 ? read : written).push_back(span);
+      }
+      if (n == 0) continue;
+      list.push_back({data[1], static_cast<float*>(data[2]), data[0], data[3], data[4], static_cast<float*>(data[5]),
+                      static_cast<float*>(data[6]), n, params[i].dtype == DLM_BF16, grads[i].dtype == DLM_BF16});
+    }
+    if (!written_apart(&read, &written)) return fail(DLM_ERR_ARG, "a tensor that is written overlaps another one");
+    if (list.empty()) return DLM_OK;
+    if ((st = require_error_word())) return st;
+    a.tensors = list.data();
+    a.count = static_cast<int>(list.size());
+    a.beta1 = hyper->beta1;
+    a.beta2 = hyper->beta2;
+    a.eps = hyper->eps;
+    a.weight_decay = hyper->weight_decay;
+    a.max_norm = hyper->max_norm;
+    a.lr = hyper->lr;
+    a.step = hyper->step;
+    a.norm = hyper->norm;
+    return launch_adamw(a, current_stream());
+  } catch (const std::bad_alloc&) {
+    return fail(DLM_ERR_ARG, "out of host memory for the list of tensors");
   }
 }
 
