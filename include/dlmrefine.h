@@ -24,6 +24,12 @@
  *   dlm_loop_*               repeat a recorded pass on the GPU until no
  *                            confident edit remains (one graph launch)
  *
+ * A feed-forward block, for serving and training it:
+ *   dlm_gated_linear, dlm_gated_linear_grad  both projections of a gated block, the activation
+ *                                          and the product in one kernel; its gradients
+ *   dlm_linear, dlm_linear_grad            a projection with bias, activation and residual in
+ *                                          its epilogue; its gradients
+ *
  * Training and scoring the refiner's last layer (the paper takes trained
  * refiners as they are; these have no counterpart in it):
  *   dlm_lmhead_loss, dlm_lmhead_loss_grad  cross entropy of given tokens under the
@@ -269,6 +275,94 @@ int dlm_refine_update_ranked(const dlm_tensor* tokens, const dlm_tensor* mask, c
                              const dlm_tensor* conf, const dlm_tensor* tok_prob,
                              const dlm_refine_params* params, dlm_tensor* new_tokens,
                              dlm_tensor* new_mask, dlm_tensor* n_edits);
+
+/* Activations of dlm_gated_linear and dlm_linear. */
+#define DLM_ACT_NONE 0
+#define DLM_ACT_SILU 1 /* z / (1 + exp(-z)) */
+#define DLM_ACT_GELU 2 /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+
+/*
+ * The first half of a gated feed-forward block (the paper leaves the refiner's layers open; the
+ * other half is dlm_linear with the block's input as residual):
+ *   gate = x w_gate^T,   up = x w_up^T,   out = act(gate) * up
+ *
+ *   x             [N, d] or [B, L, d] BF16, rows evenly strided
+ *   w_gate, w_up  [f, d] BF16
+ *   act           DLM_ACT_*
+ *   out           [N, f] or [B, L, f] BF16
+ *   gate, up      the shape of out, BF16: what dlm_gated_linear_grad reads; or both NULL
+ * d and f are multiples of 8 up to 2^20, N up to 2^28, N d and N f up to 2^40. Every base pointer
+ * and row stride is a multiple of 16 bytes, strides below 2^40 bytes. No output may overlap
+ * another tensor. bf16 products, fp32 sums; out is computed from the sums and rounded once,
+ * gate and up are rounded on their own.
+ */
+int dlm_gated_linear(const dlm_tensor* x, const dlm_tensor* w_gate, const dlm_tensor* w_up, int32_t act, dlm_tensor* out,
+                     dlm_tensor* gate, dlm_tensor* up);
+
+/*
+ * Gradients of dlm_gated_linear given dout, the gradient of out:
+ *   dgate = dout * up * act'(gate),   dup = dout * act(gate)
+ *   dx = dgate w_gate + dup w_up + add,   dw_gate = dgate^T x,   dw_up = dup^T x
+ *
+ *   dout, gate, up  [N, f] or [B, L, f] BF16; gate and up as dlm_gated_linear wrote them
+ *   add             the shape of x, BF16, rows evenly strided, any alignment: what else goes to
+ *                   x's gradient (the part that passes around the block); may be dx itself; or NULL
+ *   dx              the shape of x, BF16, rows evenly strided, any alignment; or NULL
+ *   dw_gate, dw_up  [f, d] BF16; or both NULL (frozen weights), if dx is not
+ *   workspace       >= dlm_gated_linear_grad_workspace_bytes(N, f, d) bytes, 16-byte aligned, no
+ *                   initial contents needed; calls sharing it must not overlap on the GPU.
+ * Sizes, alignment and overlaps as above. dgate and dup are rounded to bf16 for the tensor
+ * cores (at most 2^-8 relative in each term), all sums are fp32, the results are rounded to bf16.
+ * The same inputs give the same bits.
+ */
+int dlm_gated_linear_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tensor* w_gate, const dlm_tensor* w_up,
+                          const dlm_tensor* gate, const dlm_tensor* up, int32_t act, const dlm_tensor* add, dlm_tensor* dx,
+                          dlm_tensor* dw_gate, dlm_tensor* dw_up, void* workspace, size_t workspace_bytes);
+size_t dlm_gated_linear_grad_workspace_bytes(int64_t rows, int64_t f, int64_t d);
+
+/*
+ * A projection with its epilogue:
+ *   z = x weight^T + bias,   out = act(z) + residual
+ *
+ *   x          [N, k] or [B, L, k] BF16, rows evenly strided
+ *   weight     [m, k] BF16
+ *   bias       m entries, BF16 or F32, contiguous; or NULL
+ *   act        DLM_ACT_*
+ *   residual   [N, m] or [B, L, m] BF16, rows evenly strided, any alignment; may be out itself; or NULL
+ *   out        [N, m] or [B, L, m] BF16, rows evenly strided, any alignment
+ *   pre        z, in the shape of out, BF16, rows evenly strided, any alignment (dlm_linear_grad reads
+ *              it, aligned); or NULL
+ *   workspace  >= dlm_linear_workspace_bytes(N, m, k) bytes, 16-byte aligned, no initial contents
+ *              needed; not used where that is 0. Calls sharing it must not overlap on the GPU.
+ * k and m are multiples of 8 up to 2^20, N up to 2^28, N k and N m up to 2^40. The base pointers
+ * and row strides of x and weight are multiples of 16 bytes, strides below 2^40 bytes. No output
+ * may overlap another tensor but as said. bf16 products, fp32 sums, one rounding of each output.
+ */
+int dlm_linear(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* bias, int32_t act, const dlm_tensor* residual,
+               dlm_tensor* out, dlm_tensor* pre, void* workspace, size_t workspace_bytes);
+size_t dlm_linear_workspace_bytes(int64_t rows, int64_t m, int64_t k);
+
+/*
+ * Gradients of dlm_linear given dout, the gradient of out (and so that of residual):
+ *   dz = dout * act'(pre),   dx = dz weight + add,   dweight = dz^T x,   dbias[c] = sum_r dz[r, c]
+ *
+ *   dout       [N, m] or [B, L, m] BF16;  pre  the same, as dlm_linear wrote it; NULL with
+ *              DLM_ACT_NONE, and only there
+ *   add        the shape of x, BF16, rows evenly strided, any alignment; may be dx itself; or NULL
+ *   dx         the shape of x, BF16, rows evenly strided, any alignment; or NULL
+ *   dweight    [m, k] BF16; or NULL
+ *   dbias      m entries, BF16 or F32, contiguous; or NULL; not all three NULL
+ *   workspace  >= dlm_linear_grad_workspace_bytes(N, m, k) bytes, 16-byte aligned, no initial
+ *              contents needed; calls sharing it must not overlap on the GPU.
+ * Sizes as above; the base pointers and row strides of dout, x, weight, pre and dweight are
+ * multiples of 16 bytes. With an activation dz is rounded to bf16 for the tensor cores (at most
+ * 2^-8 relative in each term; dbias sums it unrounded), all sums are fp32. The same inputs give
+ * the same bits.
+ */
+int dlm_linear_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* pre, int32_t act,
+                    const dlm_tensor* add, dlm_tensor* dx, dlm_tensor* dweight, dlm_tensor* dbias, void* workspace,
+                    size_t workspace_bytes);
+size_t dlm_linear_grad_workspace_bytes(int64_t rows, int64_t m, int64_t k);
 
 /*
  * Cross entropy of given tokens under the vocabulary projection, without writing

@@ -33,7 +33,7 @@ the fused projection + reduction kernel.
 
 ``train`` states the training and scoring of the refiner's last layer: layer
 norm, the cross entropy under the projection, their gradients, and clipping;
-``block`` the optimizer's step.
+``block`` a feed-forward block, its gradients, and the optimizer's step.
 
 Floating point is fp64 unless a comparison is defined in fp32 (edit threshold,
 remask order), where the fp32 values are compared exactly.
@@ -49,4 +49,5 @@ from .lmhead import lm_head_confidence, lm_head_logits  # noqa: F401
 from .loop import refine_passes  # noqa: F401
 from .train import (clip_grad_norm, layer_norm, layer_norm_grad, lm_head_loss, lm_head_loss_grad,  # noqa: F401
                     scored_rows)
-from .block import adamw, block_scales, e4m3_values, held  # noqa: F401
+from .block import (activation, adamw, block_scales, e4m3_values, gated_linear, gated_linear_grad, held, linear,  # noqa: F401
+                    linear_grad, sigmoid_of)

@@ -6,6 +6,9 @@ Plain numpy statements in fp64 of the textbook operations:
             p = p (1 - lr wd) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
             with g scaled by min(1, max_norm / (norm + 1e-6)) where a norm is given
 
+    gated   out = act(x Wg^T) (x Wu^T);  linear  out = act(x W^T + b) + residual;
+            their gradients from the chain rule, with act SiLU, GELU (tanh) or none
+
 8-bit states are e4m3 codes with a scale for each block of 256 elements, the block's
 largest magnitude over 448; the second moment's codes are of its square root.
 """
@@ -47,3 +50,52 @@ def adamw(p, g, m, v, t, lr, beta1, beta2, eps, weight_decay, norm=None, max_nor
     v = beta2 * v + (1.0 - beta2) * g * g
     change = (m / (1.0 - beta1 ** t)) / (np.sqrt(v / (1.0 - beta2 ** t)) + eps)
     return p - lr * weight_decay * p - lr * change, m, v
+
+
+def sigmoid_of(act, z):
+    """(s, ds/dz) with act(z) = z sigmoid(s): SiLU, or GELU in its tanh form."""
+    z = np.asarray(z, dtype=np.float64)
+    if act == "silu":
+        return z, np.ones_like(z)
+    c = 2.0 * np.sqrt(2.0 / np.pi)
+    return c * (z + 0.044715 * z ** 3), c * (1.0 + 3.0 * 0.044715 * z ** 2)
+
+
+def activation(act, z):
+    """(act(z), act'(z)) in fp64."""
+    z = np.asarray(z, dtype=np.float64)
+    if act == "none":
+        return z, np.ones_like(z)
+    s, ds = sigmoid_of(act, z)
+    with np.errstate(over="ignore"):
+        p = 1.0 / (1.0 + np.exp(-s))
+        q = 1.0 / (1.0 + np.exp(s))  # 1 - p
+    return z * p, p + z * p * q * ds
+
+
+def gated_linear(x, w_gate, w_up, act):
+    """(out, gate, up) in fp64."""
+    x, wg, wu = (np.asarray(t, dtype=np.float64) for t in (x, w_gate, w_up))
+    gate, up = x @ wg.T, x @ wu.T
+    return activation(act, gate)[0] * up, gate, up
+
+
+def gated_linear_grad(dout, x, w_gate, w_up, gate, up, act, add=0.0):
+    """(dx, dw_gate, dw_up, dgate, dup) in fp64, from the saved gate and up."""
+    dout, x, wg, wu, gate, up = (np.asarray(t, dtype=np.float64) for t in (dout, x, w_gate, w_up, gate, up))
+    value, slope = activation(act, gate)
+    dgate, dup = dout * up * slope, dout * value
+    return dgate @ wg + dup @ wu + add, dgate.T @ x, dup.T @ x, dgate, dup
+
+
+def linear(x, weight, bias, act, residual=0.0):
+    """(out, z) in fp64; bias and residual may be 0."""
+    z = np.asarray(x, dtype=np.float64) @ np.asarray(weight, dtype=np.float64).T + bias
+    return activation(act, z)[0] + residual, z
+
+
+def linear_grad(dout, x, weight, pre, act, add=0.0):
+    """(dx, dweight, dbias, dz) in fp64, from the saved z (any with act "none")."""
+    dout, x, w = (np.asarray(t, dtype=np.float64) for t in (dout, x, weight))
+    dz = dout if act == "none" else dout * activation(act, pre)[1]
+    return dz @ w + add, dz.T @ x, dz.sum(axis=0), dz

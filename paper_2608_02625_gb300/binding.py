@@ -74,6 +74,13 @@ def _load():
     lib.dlm_layer_norm_grad_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64]
     lib.dlm_clip_grad_norm.argtypes = [P, P, ctypes.c_int32, ctypes.c_float, P, ctypes.c_void_p, ctypes.c_size_t]
     lib.dlm_clip_grad_norm_workspace_bytes.argtypes = []
+    lib.dlm_gated_linear.argtypes = [P] * 3 + [ctypes.c_int32] + [P] * 3
+    lib.dlm_gated_linear_grad.argtypes = [P] * 6 + [ctypes.c_int32] + [P] * 4 + [ctypes.c_void_p, ctypes.c_size_t]
+    lib.dlm_linear.argtypes = [P] * 3 + [ctypes.c_int32] + [P] * 3 + [ctypes.c_void_p, ctypes.c_size_t]
+    lib.dlm_linear_grad.argtypes = [P] * 4 + [ctypes.c_int32] + [P] * 4 + [ctypes.c_void_p, ctypes.c_size_t]
+    for f in ("dlm_gated_linear_grad_workspace_bytes", "dlm_linear_workspace_bytes", "dlm_linear_grad_workspace_bytes"):
+        getattr(lib, f).argtypes = [ctypes.c_int64] * 3
+        getattr(lib, f).restype = ctypes.c_size_t
     lib.dlm_adamw.argtypes = [P] * 7 + [ctypes.c_int32, ctypes.POINTER(DlmAdamwParams)]
     for f in ("dlm_lmhead_loss_workspace_bytes", "dlm_lmhead_loss_grad_workspace_bytes",
               "dlm_layer_norm_grad_workspace_bytes", "dlm_clip_grad_norm_workspace_bytes"):
@@ -85,7 +92,8 @@ def _load():
     for f in ("dlm_bidir_attn", "dlm_attn_masked", "dlm_vocab_confidence", "dlm_refine_update", "dlm_refine_step",
               "dlm_refine_step_static", "dlm_token_prob", "dlm_refine_update_ranked", "dlm_lmhead_confidence",
               "dlm_lmhead_loss", "dlm_lmhead_loss_grad", "dlm_layer_norm", "dlm_layer_norm_grad",
-              "dlm_clip_grad_norm", "dlm_adamw", "dlm_set_stream", "dlm_set_attn_tiles_per_unit", "dlm_version",
+              "dlm_clip_grad_norm", "dlm_gated_linear", "dlm_gated_linear_grad", "dlm_linear", "dlm_linear_grad",
+              "dlm_adamw", "dlm_set_stream", "dlm_set_attn_tiles_per_unit", "dlm_version",
               "dlm_get_device_error"):
         getattr(lib, f).restype = ctypes.c_int
     lib.dlm_loop_begin.argtypes = [ctypes.c_void_p]
@@ -357,6 +365,66 @@ def dlm_clip_grad_norm(grads, outs, max_norm: float, norm, workspace):
     dn = describe(norm)
     _check(lib.dlm_clip_grad_norm(dg, do, n, float(max_norm), _ref(dn), *_workspace(workspace)))
     return outs, norm
+
+
+ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2  # GELU in its tanh form
+
+
+def dlm_gated_linear(x, w_gate, w_up, act: int, out, gate, up):
+    """out = act(x @ w_gate^T) * (x @ w_up^T), the first half of a gated feed-forward block.
+    gate and up (the two products, which dlm_gated_linear_grad reads) may both be None."""
+    if _done(_marshal.gated_linear(x, w_gate, w_up, act, out, gate, up)):
+        return out, gate, up
+    _prepare(x, w_gate, w_up, out, gate, up)
+    ds = [describe(t) for t in (x, w_gate, w_up, out, gate, up)]
+    _check(lib.dlm_gated_linear(*[_ref(d) for d in ds[:3]], int(act), *[_ref(d) for d in ds[3:]]))
+    return out, gate, up
+
+
+def dlm_gated_linear_grad_workspace_bytes(rows: int, f: int, d: int) -> int:
+    return lib.dlm_gated_linear_grad_workspace_bytes(int(rows), int(f), int(d))
+
+
+def dlm_gated_linear_grad(dout, x, w_gate, w_up, gate, up, act: int, add, dx, dw_gate, dw_up, workspace):
+    """Gradients of dlm_gated_linear. add (what else goes to dx; may be dx itself), dx, and
+    dw_gate with dw_up may be None."""
+    if _done(_marshal.gated_linear_grad(dout, x, w_gate, w_up, gate, up, act, add, dx, dw_gate, dw_up, workspace)):
+        return dx, dw_gate, dw_up
+    _prepare(dout, x, w_gate, w_up, gate, up, add, dx, dw_gate, dw_up, workspace)
+    ds = [describe(t) for t in (dout, x, w_gate, w_up, gate, up, add, dx, dw_gate, dw_up)]
+    _check(lib.dlm_gated_linear_grad(*[_ref(d) for d in ds[:6]], int(act), *[_ref(d) for d in ds[6:]], *_workspace(workspace)))
+    return dx, dw_gate, dw_up
+
+
+def dlm_linear_workspace_bytes(rows: int, m: int, k: int) -> int:
+    return lib.dlm_linear_workspace_bytes(int(rows), int(m), int(k))
+
+
+def dlm_linear(x, weight, bias, act: int, residual, out, pre, workspace):
+    """out = act(x @ weight^T + bias) + residual. bias, residual (may be out itself), pre (the
+    activation's argument, which dlm_linear_grad reads) may be None; the workspace too where
+    dlm_linear_workspace_bytes is 0."""
+    if _done(_marshal.linear(x, weight, bias, act, residual, out, pre, workspace)):
+        return out, pre
+    _prepare(x, weight, bias, residual, out, pre, workspace)
+    ds = [describe(t) for t in (x, weight, bias, residual, out, pre)]
+    _check(lib.dlm_linear(*[_ref(d) for d in ds[:3]], int(act), *[_ref(d) for d in ds[3:]], *_workspace(workspace)))
+    return out, pre
+
+
+def dlm_linear_grad_workspace_bytes(rows: int, m: int, k: int) -> int:
+    return lib.dlm_linear_grad_workspace_bytes(int(rows), int(m), int(k))
+
+
+def dlm_linear_grad(dout, x, weight, pre, act: int, add, dx, dweight, dbias, workspace):
+    """Gradients of dlm_linear. pre is None with ACT_NONE; add (what else goes to dx; may be dx
+    itself), dx, dweight and dbias may be None."""
+    if _done(_marshal.linear_grad(dout, x, weight, pre, act, add, dx, dweight, dbias, workspace)):
+        return dx, dweight, dbias
+    _prepare(dout, x, weight, pre, add, dx, dweight, dbias, workspace)
+    ds = [describe(t) for t in (dout, x, weight, pre, add, dx, dweight, dbias)]
+    _check(lib.dlm_linear_grad(*[_ref(d) for d in ds[:4]], int(act), *[_ref(d) for d in ds[4:]], *_workspace(workspace)))
+    return dx, dweight, dbias
 
 
 @dataclasses.dataclass

@@ -1,0 +1,44 @@
+// Activations of a feed-forward block, x sigmoid(s):
+//   SiLU         s = x
+//   GELU (tanh)  s = 2 sqrt(2 / pi) (x + 0.044715 x^3)   (x (1 + tanh(s / 2)) / 2)
+// sigmoid(s) = 1 / (1 + 2^(-s log2 e)) with the approximate exponential and reciprocal: off
+// by some 2^-21 relative for |s| up to 20, far below the rounding to bf16 behind it.
+#pragma once
+
+#include "dlm_common.cuh"
+
+namespace dlm {
+
+constexpr float kGelu = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+constexpr float kGeluCube = 0.044715f;
+
+__device__ __forceinline__ float sigmoid_approx(float s) {
+  float r;  // 1 / inf = 0
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2_approx(s * -1.4426950408889634f)));
+  return r;
+}
+
+// `act` is DLM_ACT_*, the same in every thread.
+__device__ __forceinline__ float activate(int act, float x) {
+  if (act == DLM_ACT_NONE) return x;
+  return x * sigmoid_approx(act == DLM_ACT_SILU ? x : kGelu * x * fmaf(kGeluCube, x * x, 1.f));
+}
+
+// Value and derivative at x: sigmoid (1 + x (1 - sigmoid) ds/dx). Past |x| = 100 the derivative
+// is 0 or 1 and is taken there, where nothing overflows (a NaN stays one).
+__device__ __forceinline__ void activate_grad(int act, float x, float* value, float* slope) {
+  if (act == DLM_ACT_NONE) {
+    *value = x;
+    *slope = 1.f;
+    return;
+  }
+  float c;
+  asm("{\n.reg .f32 t;\nmin.NaN.f32 t, %1, 0f42C80000;\nmax.NaN.f32 %0, t, 0fC2C80000;\n}" : "=f"(c) : "f"(x));
+  const bool silu = act == DLM_ACT_SILU;
+  const float p = sigmoid_approx(silu ? c : kGelu * c * fmaf(kGeluCube, c * c, 1.f));
+  const float ds = silu ? 1.f : kGelu * fmaf(3.f * kGeluCube, c * c, 1.f);
+  *value = x * p;
+  *slope = p * fmaf(c * (1.f - p), ds, 1.f);
+}
+
+}  // namespace dlm

@@ -259,6 +259,52 @@ constexpr int kMaxGradTensors = 16 * kGradTable;
 inline size_t clip_grad_norm_workspace_bytes() { return sizeof(double) * kGradParts * (kMaxGradTensors / kGradTable); }
 int launch_clip_grad_norm(const GradArgs& a, cudaStream_t stream);
 
+// Products of a feed-forward block. Matrices are bf16; those that TMA moves have rows at
+// multiples of 16 bytes.
+struct Matrix {
+  void* data;
+  int64_t rows, cols, stride;
+};
+// What happens to a product on its way out: act(z + bias) + residual. Any alignment.
+struct Epilogue {
+  int act;               // DLM_ACT_*
+  const void* bias;      // may be null
+  int bias_bf16;
+  const void* residual;  // may be null
+  void* out;
+  void* pre;             // z + bias; may be null
+  int64_t s_residual, s_out, s_pre;
+};
+
+struct GatedArgs {
+  Matrix x, w_gate, w_up;
+  int act;
+  Matrix out;            // the block only
+  Matrix gate, up;       // the block: written, may be null;  gradients: read
+  Matrix dout;           // gradients only, from here on
+  const void* add;       // may be null; any alignment, like dx
+  void* dx;              // may be null
+  int64_t s_add, s_dx;
+  Matrix dw_gate, dw_up; // may both be null
+  void* workspace;       // gated_grad_workspace_bytes
+};
+size_t gated_grad_workspace_bytes(int64_t N, int64_t f, int64_t d);
+int launch_gated(const GatedArgs& a, cudaStream_t stream);
+int launch_gated_grad(const GatedArgs& a, cudaStream_t stream);
+
+struct LinearArgs {
+  Matrix x, w;
+  Epilogue ep;           // gradients: act, bias_bf16 (of dbias), residual (added to dx), out (dx, may be null)
+  Matrix dout, pre;      // gradients only, from here on; pre null without an activation
+  Matrix dw;             // may be null
+  void* dbias;           // may be null
+  void* workspace;       // linear_workspace_bytes or linear_grad_workspace_bytes
+};
+size_t linear_workspace_bytes(int64_t N, int64_t m, int64_t k);
+size_t linear_grad_workspace_bytes(int64_t N, int64_t m, int64_t k);
+int launch_linear(const LinearArgs& a, cudaStream_t stream);
+int launch_linear_grad(const LinearArgs& a, cudaStream_t stream);
+
 // One AdamW step over many tensors.
 struct AdamwTensor {
   void* p;         // weights, F32 or BF16 (with a master: its BF16 copy)

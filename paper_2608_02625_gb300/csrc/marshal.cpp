@@ -394,6 +394,61 @@ PyObject* clip_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// x, w_gate, w_up, act, out, gate, up
+PyObject* gated_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 7, [&](Call& c, int* st) {
+    int32_t act;
+    if (!add_all(c, a, 0, 3) || !as_int32(a[3], &act) || !c.add(a[4]) || !c.add(a[5], true) || !c.add(a[6], true) || !c.stream())
+      return false;
+    *st = unlocked([&] { return dlm_gated_linear(c[0], c[1], c[2], act, c[3], c[4], c[5]); });
+    return true;
+  });
+}
+
+// dout, x, w_gate, w_up, gate, up, act, add, dx, dw_gate, dw_up, workspace
+PyObject* gated_linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 12, [&](Call& c, int* st) {
+    int32_t act;
+    void* ws;
+    size_t bytes;
+    if (!add_all(c, a, 0, 6) || !as_int32(a[6], &act)) return false;
+    for (int i = 7; i < 11; ++i)
+      if (!c.add(a[i], true)) return false;
+    if (!c.workspace(a[11], &ws, &bytes) || !c.stream()) return false;
+    *st = unlocked([&] { return dlm_gated_linear_grad(c[0], c[1], c[2], c[3], c[4], c[5], act, c[6], c[7], c[8], c[9], ws, bytes); });
+    return true;
+  });
+}
+
+// x, weight, bias, act, residual, out, pre, workspace (None where nothing needs it)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 8, [&](Call& c, int* st) {
+    int32_t act;
+    void* ws = nullptr;
+    size_t bytes = 0;
+    if (!add_all(c, a, 0, 2) || !c.add(a[2], true) || !as_int32(a[3], &act) || !c.add(a[4], true) || !c.add(a[5]) ||
+        !c.add(a[6], true) || (a[7] != Py_None && !c.workspace(a[7], &ws, &bytes)) || !c.stream())
+      return false;
+    *st = unlocked([&] { return dlm_linear(c[0], c[1], c[2], act, c[3], c[4], c[5], ws, bytes); });
+    return true;
+  });
+}
+
+// dout, x, weight, pre, act, add, dx, dweight, dbias, workspace
+PyObject* linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(n, 10, [&](Call& c, int* st) {
+    int32_t act;
+    void* ws;
+    size_t bytes;
+    if (!add_all(c, a, 0, 3) || !c.add(a[3], true) || !as_int32(a[4], &act)) return false;
+    for (int i = 5; i < 9; ++i)
+      if (!c.add(a[i], true)) return false;
+    if (!c.workspace(a[9], &ws, &bytes) || !c.stream()) return false;
+    *st = unlocked([&] { return dlm_linear_grad(c[0], c[1], c[2], c[3], act, c[4], c[5], c[6], c[7], ws, bytes); });
+    return true;
+  });
+}
+
 // params, masters (or None), grads, m, v, m_scales, v_scales (None: states in 32 bits), hyper
 PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(n, 8, [&](Call& c, int* st) {
@@ -455,6 +510,10 @@ PyMethodDef methods[] = {FAST(bidir_attn),
                          FAST(layer_norm),
                          FAST(layer_norm_grad),
                          FAST(clip_grad_norm),
+                         FAST(gated_linear),
+                         FAST(gated_linear_grad),
+                         FAST(linear),
+                         FAST(linear_grad),
                          FAST(adamw),
                          FAST(loop_launch),
                          {"set_params_type", set_params_type, METH_O, nullptr},

@@ -157,9 +157,230 @@ int prepare_loss(const dlm_tensor* hidden, const dlm_tensor* weight, const dlm_t
   return DLM_OK;
 }
 
+// A [N, width] or [B, L, width] tensor of bf16 rows (null allowed where `optional`: `to` is
+// left empty). aligned: as TMA and 16-byte loads take it.
+int block_rows(const dlm_tensor* t, const char* name, bool optional, bool aligned, Matrix* to) {
+  if (!t && optional) return DLM_OK;
+  int st;
+  int64_t N, width, stride;
+  if ((st = rows_of(t, name, 1 << DLM_BF16, &N, &width, &stride))) return st;
+  if (N > kMostRows || width > kMostWidth) return fail(DLM_ERR_SHAPE, "%s: at most 2^28 rows and a width of 2^20", name);
+  if (N * width > kMostElements) return fail(DLM_ERR_SHAPE, "%s: more than 2^40 elements", name);
+  if (width < 8 || width % 8 != 0) return fail(DLM_ERR_SHAPE, "%s: the width must be a positive multiple of 8 (got %lld)", name, (long long)width);
+  if (stride >= (int64_t{1} << 39)) return fail(DLM_ERR_STRIDE, "%s rows must lie less than 2^40 bytes apart", name);
+  if (aligned && N > 0 && (reinterpret_cast<uintptr_t>(t->data) % 16 != 0 || stride % 8 != 0))
+    return fail(DLM_ERR_ALIGN, "%s rows must start at multiples of 16 bytes", name);
+  *to = {t->data, N, width, stride};
+  return DLM_OK;
+}
+
+// A [rows, width] weight, or its gradient.
+int block_weight(const dlm_tensor* t, const char* name, int64_t width, bool optional, Matrix* to) {
+  if (!t && optional) return DLM_OK;
+  int st;
+  if ((st = check_tensor(t, name, 1 << DLM_BF16, 2, 2))) return st;
+  const int64_t rows = t->shape[0];
+  if (t->shape[1] != width) return fail(DLM_ERR_SHAPE, "%s must have the width of x", name);
+  if (rows < 8 || rows % 8 != 0 || rows > kMostWidth)
+    return fail(DLM_ERR_SHAPE, "%s: a multiple of 8 rows up to 2^20 expected (got %lld)", name, (long long)rows);
+  if ((st = check_matrix(t, name, rows, width))) return st;
+  *to = {t->data, rows, width, t->stride[0]};
+  return DLM_OK;
+}
+
+int check_act(int32_t act) {
+  if (act < DLM_ACT_NONE || act > DLM_ACT_GELU) return fail(DLM_ERR_ARG, "unknown activation %d", act);
+  return DLM_OK;
+}
+
+// Rows of the leading shape of x and a width of their own.
+int check_like(const Matrix& t, const dlm_tensor* desc, const char* name, const dlm_tensor* x, int64_t width) {
+  if (!desc) return DLM_OK;
+  bool same = desc->ndim == x->ndim && t.cols == width;
+  for (int i = 0; same && i < x->ndim - 1; ++i) same = desc->shape[i] == x->shape[i];
+  if (!same) return fail(DLM_ERR_SHAPE, "%s must have the rows of x and a width of %lld", name, (long long)width);
+  return DLM_OK;
+}
+
+// The gradient of no rows.
+int zero_matrix(const Matrix& t) {
+  if (!t.data) return DLM_OK;
+  const cudaError_t e = cudaMemset2DAsync(t.data, static_cast<size_t>(t.stride) * 2, 0, static_cast<size_t>(t.cols) * 2,
+                                          static_cast<size_t>(t.rows), current_stream());
+  return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "gradient of no rows: %s", cudaGetErrorString(e));
+}
+
+bool block_sizes(int64_t rows, int64_t a, int64_t b) {
+  const auto width = [](int64_t w) { return w >= 8 && w % 8 == 0 && w <= kMostWidth; };
+  return rows > 0 && rows <= kMostRows && width(a) && width(b) && rows * a <= kMostElements && rows * b <= kMostElements;
+}
+
 }  // namespace
 
 extern "C" {
+
+int dlm_gated_linear(const dlm_tensor* x, const dlm_tensor* w_gate, const dlm_tensor* w_up, int32_t act, dlm_tensor* out,
+                     dlm_tensor* gate, dlm_tensor* up) {
+  clear_error();
+  GatedArgs a = {};
+  int st;
+  if ((st = block_rows(x, "x", false, true, &a.x))) return st;
+  if ((st = block_weight(w_gate, "w_gate", a.x.cols, false, &a.w_gate))) return st;
+  if ((st = block_weight(w_up, "w_up", a.x.cols, false, &a.w_up))) return st;
+  if (!same_shape(w_gate, w_up)) return fail(DLM_ERR_SHAPE, "w_up must have the shape of w_gate");
+  if ((st = check_act(act))) return st;
+  if ((st = block_rows(out, "out", false, true, &a.out))) return st;
+  if ((gate == nullptr) != (up == nullptr)) return fail(DLM_ERR_NULL, "gate and up must both be given or both be NULL");
+  if ((st = block_rows(gate, "gate", true, true, &a.gate))) return st;
+  if ((st = block_rows(up, "up", true, true, &a.up))) return st;
+  if ((st = check_like(a.out, out, "out", x, a.w_gate.rows))) return st;
+  if ((st = check_like(a.gate, gate, "gate", x, a.w_gate.rows))) return st;
+  if ((st = check_like(a.up, up, "up", x, a.w_gate.rows))) return st;
+  const dlm_tensor* outs[3] = {out, gate, up};
+  const dlm_tensor* ins[3] = {x, w_gate, w_up};
+  if ((st = check_disjoint(outs, 3, ins, 3))) return st;
+  if (a.x.rows == 0) return DLM_OK;
+  if ((st = require_error_word())) return st;
+  a.act = act;
+  return launch_gated(a, current_stream());
+}
+
+size_t dlm_gated_linear_grad_workspace_bytes(int64_t rows, int64_t f, int64_t d) {
+  return block_sizes(rows, f, d) ? gated_grad_workspace_bytes(rows, f, d) : 0;
+}
+
+int dlm_gated_linear_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tensor* w_gate, const dlm_tensor* w_up,
+                          const dlm_tensor* gate, const dlm_tensor* up, int32_t act, const dlm_tensor* add, dlm_tensor* dx,
+                          dlm_tensor* dw_gate, dlm_tensor* dw_up, void* workspace, size_t workspace_bytes) {
+  clear_error();
+  GatedArgs a = {};
+  Matrix m_add = {}, m_dx = {};
+  int st;
+  if ((st = block_rows(x, "x", false, true, &a.x))) return st;
+  if ((st = block_weight(w_gate, "w_gate", a.x.cols, false, &a.w_gate))) return st;
+  if ((st = block_weight(w_up, "w_up", a.x.cols, false, &a.w_up))) return st;
+  if (!same_shape(w_gate, w_up)) return fail(DLM_ERR_SHAPE, "w_up must have the shape of w_gate");
+  if ((st = check_act(act))) return st;
+  if ((st = block_rows(dout, "dout", false, true, &a.dout))) return st;
+  if ((st = block_rows(gate, "gate", false, true, &a.gate))) return st;
+  if ((st = block_rows(up, "up", false, true, &a.up))) return st;
+  if ((st = check_like(a.dout, dout, "dout", x, a.w_gate.rows))) return st;
+  if ((st = check_like(a.gate, gate, "gate", x, a.w_gate.rows))) return st;
+  if ((st = check_like(a.up, up, "up", x, a.w_gate.rows))) return st;
+  if (add && !dx) return fail(DLM_ERR_NULL, "add is given, dx is NULL");
+  if ((st = block_rows(add, "add", true, false, &m_add))) return st;
+  if ((st = block_rows(dx, "dx", true, false, &m_dx))) return st;
+  if ((st = check_like(m_add, add, "add", x, a.x.cols))) return st;
+  if ((st = check_like(m_dx, dx, "dx", x, a.x.cols))) return st;
+  if ((dw_gate == nullptr) != (dw_up == nullptr)) return fail(DLM_ERR_NULL, "dw_gate and dw_up must both be given or both be NULL");
+  if (!dx && !dw_gate) return fail(DLM_ERR_NULL, "dx, dw_gate and dw_up are all NULL");
+  if ((st = block_weight(dw_gate, "dw_gate", a.x.cols, true, &a.dw_gate))) return st;
+  if ((st = block_weight(dw_up, "dw_up", a.x.cols, true, &a.dw_up))) return st;
+  if (dw_gate && (!same_shape(w_gate, dw_gate) || !same_shape(w_gate, dw_up)))
+    return fail(DLM_ERR_SHAPE, "dw_gate and dw_up must have the shape of w_gate");
+  const dlm_tensor* outs[3] = {dx, dw_gate, dw_up};
+  const dlm_tensor* ins[7] = {dout, x, w_gate, w_up, gate, up, add && dx && same_view(add, dx) ? nullptr : add};
+  if ((st = check_disjoint(outs, 3, ins, 7))) return st;
+  if (a.x.rows == 0) return (st = zero_matrix(a.dw_gate)) ? st : zero_matrix(a.dw_up);
+  const dlm_tensor* all[10] = {dout, x, w_gate, w_up, gate, up, add, dx, dw_gate, dw_up};
+  const size_t need = gated_grad_workspace_bytes(a.x.rows, a.w_gate.rows, a.x.cols);
+  if ((st = check_workspace(workspace, workspace_bytes, need, 16, all, 10))) return st;
+  if ((st = require_error_word())) return st;
+  a.act = act;
+  a.add = m_add.data;
+  a.s_add = m_add.stride;
+  a.dx = m_dx.data;
+  a.s_dx = m_dx.stride;
+  a.workspace = workspace;
+  return launch_gated_grad(a, current_stream());
+}
+
+size_t dlm_linear_workspace_bytes(int64_t rows, int64_t m, int64_t k) {
+  return block_sizes(rows, m, k) ? linear_workspace_bytes(rows, m, k) : 0;
+}
+
+int dlm_linear(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* bias, int32_t act, const dlm_tensor* residual,
+               dlm_tensor* out, dlm_tensor* pre, void* workspace, size_t workspace_bytes) {
+  clear_error();
+  LinearArgs a = {};
+  Matrix m_out = {}, m_residual = {}, m_pre = {};
+  int st;
+  if ((st = block_rows(x, "x", false, true, &a.x))) return st;
+  if ((st = block_weight(weight, "weight", a.x.cols, false, &a.w))) return st;
+  if ((st = check_vector(bias, "bias", kMaskBF16F32, a.w.rows, true))) return st;
+  if ((st = check_act(act))) return st;
+  if ((st = block_rows(residual, "residual", true, false, &m_residual))) return st;
+  if ((st = block_rows(out, "out", false, false, &m_out))) return st;
+  if ((st = block_rows(pre, "pre", true, false, &m_pre))) return st;
+  if ((st = check_like(m_residual, residual, "residual", x, a.w.rows))) return st;
+  if ((st = check_like(m_out, out, "out", x, a.w.rows))) return st;
+  if ((st = check_like(m_pre, pre, "pre", x, a.w.rows))) return st;
+  const dlm_tensor* outs[2] = {out, pre};
+  const dlm_tensor* ins[4] = {x, weight, bias, nullptr};
+  if ((st = check_disjoint(outs, 2, ins, 4))) return st;
+  if (residual && ((!same_view(residual, out) && overlaps(residual, out)) || (pre && overlaps(residual, pre))))
+    return fail(DLM_ERR_ARG, "an output overlaps an input");
+  if (a.x.rows == 0) return DLM_OK;
+  const dlm_tensor* all[6] = {x, weight, bias, residual, out, pre};
+  if ((st = check_workspace(workspace, workspace_bytes, linear_workspace_bytes(a.x.rows, a.w.rows, a.x.cols), 16, all, 6))) return st;
+  if ((st = require_error_word())) return st;
+  a.ep = {act, bias ? bias->data : nullptr, bias && bias->dtype == DLM_BF16, m_residual.data, m_out.data, m_pre.data,
+          m_residual.stride, m_out.stride, m_pre.stride};
+  a.workspace = workspace;
+  return launch_linear(a, current_stream());
+}
+
+size_t dlm_linear_grad_workspace_bytes(int64_t rows, int64_t m, int64_t k) {
+  return block_sizes(rows, m, k) ? linear_grad_workspace_bytes(rows, m, k) : 0;
+}
+
+int dlm_linear_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* pre, int32_t act,
+                    const dlm_tensor* add, dlm_tensor* dx, dlm_tensor* dweight, dlm_tensor* dbias, void* workspace,
+                    size_t workspace_bytes) {
+  clear_error();
+  LinearArgs a = {};
+  Matrix m_add = {}, m_dx = {};
+  int st;
+  if ((st = block_rows(x, "x", false, true, &a.x))) return st;
+  if ((st = block_weight(weight, "weight", a.x.cols, false, &a.w))) return st;
+  if ((st = check_act(act))) return st;
+  if ((st = block_rows(dout, "dout", false, true, &a.dout))) return st;
+  if ((act == DLM_ACT_NONE) != (pre == nullptr))
+    return fail(pre ? DLM_ERR_ARG : DLM_ERR_NULL, "pre belongs to an activation, and is needed with one");
+  if ((st = block_rows(pre, "pre", true, true, &a.pre))) return st;
+  if ((st = check_like(a.dout, dout, "dout", x, a.w.rows))) return st;
+  if ((st = check_like(a.pre, pre, "pre", x, a.w.rows))) return st;
+  if (add && !dx) return fail(DLM_ERR_NULL, "add is given, dx is NULL");
+  if ((st = block_rows(add, "add", true, false, &m_add))) return st;
+  if ((st = block_rows(dx, "dx", true, false, &m_dx))) return st;
+  if ((st = check_like(m_add, add, "add", x, a.x.cols))) return st;
+  if ((st = check_like(m_dx, dx, "dx", x, a.x.cols))) return st;
+  if (!dx && !dweight && !dbias) return fail(DLM_ERR_NULL, "dx, dweight and dbias are all NULL");
+  if ((st = block_weight(dweight, "dweight", a.x.cols, true, &a.dw))) return st;
+  if (dweight && !same_shape(weight, dweight)) return fail(DLM_ERR_SHAPE, "dweight must have the shape of weight");
+  if ((st = check_vector(dbias, "dbias", kMaskBF16F32, a.w.rows, true))) return st;
+  const dlm_tensor* outs[3] = {dx, dweight, dbias};
+  const dlm_tensor* ins[5] = {dout, x, weight, pre, add && dx && same_view(add, dx) ? nullptr : add};
+  if ((st = check_disjoint(outs, 3, ins, 5))) return st;
+  if (a.x.rows == 0) {
+    if ((st = zero_matrix(a.dw)) || !dbias) return st;
+    const cudaError_t e = cudaMemsetAsync(dbias->data, 0, static_cast<size_t>(a.w.rows * elem_size(dbias->dtype)), current_stream());
+    return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "gradient of no rows: %s", cudaGetErrorString(e));
+  }
+  const dlm_tensor* all[8] = {dout, x, weight, pre, add, dx, dweight, dbias};
+  const size_t need = linear_grad_workspace_bytes(a.x.rows, a.w.rows, a.x.cols);
+  if ((st = check_workspace(workspace, workspace_bytes, need, 16, all, 8))) return st;
+  if ((st = require_error_word())) return st;
+  a.ep.act = act;
+  a.ep.bias_bf16 = dbias && dbias->dtype == DLM_BF16;
+  a.ep.residual = m_add.data;
+  a.ep.s_residual = m_add.stride;
+  a.ep.out = m_dx.data;
+  a.ep.s_out = m_dx.stride;
+  a.dbias = dbias ? dbias->data : nullptr;
+  a.workspace = workspace;
+  return launch_linear_grad(a, current_stream());
+}
 
 size_t dlm_lmhead_loss_workspace_bytes(int64_t rows, int64_t d) {
   return rows > 0 && rows <= kMostRows && d > 0 && d <= kMostWidth ? loss_workspace_bytes(rows, d) : 0;

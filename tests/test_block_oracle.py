@@ -45,3 +45,41 @@ def test_blocks():
     codes = np.zeros(600, dtype=np.uint8)
     codes[[3, 300, 599]] = [0xFE, 0x7E, 0x7E]
     np.testing.assert_allclose(oracle.held(codes, [0.01, 0.1, 0.001]), x, rtol=1e-15)
+
+
+def act_of(name, z):
+    return {"none": lambda v: v, "silu": torch.nn.functional.silu,
+            "gelu": lambda v: torch.nn.functional.gelu(v, approximate="tanh")}[name](z)
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+def test_activations_are_torchs(act):
+    z = torch.linspace(-30, 30, 2001, dtype=torch.float64, requires_grad=True)
+    y = act_of(act, z)
+    y.sum().backward()
+    value, slope = oracle.activation(act, z.detach().numpy())
+    np.testing.assert_allclose(value, y.detach().numpy(), rtol=1e-9, atol=1e-13)
+    np.testing.assert_allclose(slope, z.grad.numpy(), rtol=1e-9, atol=1e-12)
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+def test_block_and_gradients_are_autograds(act):
+    rng = np.random.default_rng(1)
+    t = {n: torch.from_numpy(rng.standard_normal(s)).requires_grad_() for n, s in
+         (("x", (7, 16)), ("wg", (24, 16)), ("wu", (24, 16)), ("wd", (16, 24)), ("b", (16,)))}
+    gate, up = t["x"] @ t["wg"].T, t["x"] @ t["wu"].T
+    h = act_of(act, gate) * up
+    h.retain_grad()
+    z = h @ t["wd"].T + t["b"]
+    y = act_of(act, z) + t["x"]
+    dy = rng.standard_normal((7, 16))
+    y.backward(torch.from_numpy(dy))
+    n = {k: v.detach().numpy() for k, v in t.items()}
+    o_h, o_gate, o_up = oracle.gated_linear(n["x"], n["wg"], n["wu"], act)
+    o_y, o_z = oracle.linear(o_h, n["wd"], n["b"], act, n["x"])
+    np.testing.assert_allclose(o_y, y.detach().numpy(), rtol=1e-11, atol=1e-11)
+    dh, dwd, db, _ = oracle.linear_grad(dy, o_h, n["wd"], o_z, act)
+    dx, dwg, dwu, _, _ = oracle.gated_linear_grad(dh, n["x"], n["wg"], n["wu"], o_gate, o_up, act, add=dy)
+    for got, want in ((dh, h.grad), (dwd, t["wd"].grad), (db, t["b"].grad), (dx, t["x"].grad), (dwg, t["wg"].grad),
+                      (dwu, t["wu"].grad)):
+        np.testing.assert_allclose(got, want.numpy(), rtol=1e-9, atol=1e-9)
