@@ -28,6 +28,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kPerSm = 4;            // CTAs an SM (64 registers a thread)
 constexpr int kBlock = kAdamwBlock;  // elements of a warp's turn, and of a scale
 constexpr int kPer = kBlock / 32;    // elements a lane
 constexpr float kTop = 448.f;        // the largest e4m3 value
@@ -294,7 +295,7 @@ __device__ void chunk_step(const Tensor& t, int64_t at, int64_t end, const Step&
 }
 
 template <int kTensors, bool kEight>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<kTensors> tab) {
+__global__ void __launch_bounds__(kThreads, kPerSm) adamw_kernel(const __grid_constant__ Table<kTensors> tab) {
   __shared__ Step shared;
   wait_for_previous();
   if (threadIdx.x == 0) shared = step_of(tab);
@@ -361,11 +362,9 @@ void fill(const AdamwArgs& a, int first, Table<kTensors>* tab) {
 template <int kTensors, bool kEight>
 int launch_tables(const AdamwArgs& a, cudaStream_t stream) {
   const auto kernel = adamw_kernel<kTensors, kEight>;
-  int dev = 0, sms = 0, per_sm = 0;
+  int dev = 0, sms = 0;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, 0);
-  if (e != cudaSuccess) return fail(DLM_ERR_CUDA, "adamw launch: %s", cudaGetErrorString(e));
   Table<kTensors> tab;
   tab.beta1 = static_cast<float>(a.beta1);
   tab.rest1 = static_cast<float>(1.0 - a.beta1);
@@ -382,9 +381,9 @@ int launch_tables(const AdamwArgs& a, cudaStream_t stream) {
   tab.err = device_error_word();
   for (int first = 0; first < a.count; first += kTensors) {
     fill(a, first, &tab);
-    const int64_t most = static_cast<int64_t>(sms) * per_sm;
+    const int64_t most = static_cast<int64_t>(sms) * kPerSm;
     const int ctas = static_cast<int>(tab.chunks < most ? tab.chunks : most);
-    e = launch_overlapped(kernel, dim3(static_cast<unsigned>(ctas)), kThreads, 0, stream, 1, true, tab);
+    const cudaError_t e = launch_overlapped(kernel, dim3(static_cast<unsigned>(ctas)), kThreads, 0, stream, 1, true, tab);
     if (e != cudaSuccess) return fail(DLM_ERR_CUDA, "adamw launch: %s", cudaGetErrorString(e));
   }
   return DLM_OK;

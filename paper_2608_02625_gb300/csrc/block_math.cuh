@@ -5,6 +5,8 @@
 // by some 2^-21 relative for |s| up to 20, far below the rounding to bf16 behind it.
 #pragma once
 
+#include <cuda_bf16.h>
+
 #include "dlm_common.cuh"
 
 namespace dlm {
@@ -39,6 +41,31 @@ __device__ __forceinline__ void activate_grad(int act, float x, float* value, fl
   const float ds = silu ? 1.f : kGelu * fmaf(3.f * kGeluCube, c * c, 1.f);
   *value = x * p;
   *slope = p * fmaf(c * (1.f - p), ds, 1.f);
+}
+
+// Eight neighbouring columns of a row; wide: 16-byte aligned.
+__device__ __forceinline__ void load8(const __nv_bfloat16* src, bool wide, float (&x)[8]) {
+  if (wide) {
+    const uint4 u = *reinterpret_cast<const uint4*>(src);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[2 * k] = __uint_as_float(w[k] << 16);
+      x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = __bfloat162float(src[k]);
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* dst, bool wide, const float (&x)[8]) {
+  if (wide) {
+    *reinterpret_cast<uint4*>(dst) =
+        make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dst[k] = __float2bfloat16_rn(x[k]);
+  }
 }
 
 }  // namespace dlm

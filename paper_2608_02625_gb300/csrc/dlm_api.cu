@@ -72,6 +72,18 @@ int* device_error_word() {
   return g_err_addr[dev];
 }
 
+cudaError_t allow_smem(const void* kernel, int bytes) {
+  static ClusterTable table;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess)
+    table.get({kernel, dev, 1, 0, static_cast<size_t>(bytes)}, [&] {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+      return e == cudaSuccess ? 0 : -1;
+    });
+  return e;
+}
+
 int active_clusters(const void* kernel, int csize, int threads, size_t smem) {
   static ClusterTable table;
   int dev = 0;

@@ -69,6 +69,10 @@ class ClusterTable {
 // if none can; asked of the runtime once per device, kernel and sizes.
 int active_clusters(const void* kernel, int csize, int threads, size_t smem);
 
+// Lets a kernel take `bytes` of dynamic shared memory on the current device; the runtime is asked
+// once per device and kernel.
+cudaError_t allow_smem(const void* kernel, int bytes);
+
 // Launches a kernel that may start while the one before it in the stream still
 // runs (every kernel launched so calls wait_for_previous), in clusters
 // of `csize` CTAs; an ordinary launch where !overlap. carveout: how much of an SM's

@@ -30,6 +30,7 @@
 #include "dlm_common.cuh"
 #include "dlm_internal.h"
 #include "dlm_tmap.h"
+#include "products.h"
 
 namespace cg = cooperative_groups;
 
@@ -43,19 +44,18 @@ constexpr int kMaxBN = 256;
 constexpr int kThreads = 384;     // warp 0 TMA, warp 1 MMA, warps 4-11 epilogue
 constexpr int kEpiWarp0 = 4, kEpiWarps = 8;
 constexpr int kABytes = kBM * kBK * 2;
-constexpr int kBBytes = kMaxBN / 2 * kBK * 2;  // this CTA's half
 constexpr int kBoxBytes = 64 * 128;            // an MN-major box: 64 K rows of 64 columns
-constexpr int kStages = 6;                     // 192 KB
+constexpr int kRing = 192 * 1024;              // 6 stages with B's half of 128 rows, 8 with one of 64
+constexpr int kMaxStages = 8;
 constexpr uint32_t kTmemCols = 2 * kMaxBN;     // two accumulators
 
 enum Form { kGated, kCols, kColsTurned, kRowsForm };
 
 struct Smem {
-  alignas(1024) uint8_t a[kStages][kABytes];
-  alignas(1024) uint8_t b[kStages][kBBytes];
+  alignas(1024) uint8_t ring[kRing];               // stages: this CTA's A and B
   alignas(1024) uint8_t out[kEpiWarps][32 * 128];  // per epilogue warp, 32 rows x 128 bytes
-  uint64_t full[kStages];   // stage loaded            (TMA -> MMA; in the leader)
-  uint64_t empty[kStages];  // stage read by its MMAs  (MMA -> TMA)
+  uint64_t full[kMaxStages];   // stage loaded            (TMA -> MMA; in the leader)
+  uint64_t empty[kMaxStages];  // stage read by its MMAs  (MMA -> TMA)
   uint64_t acc_full[2];     // accumulator complete    (MMA -> epilogue)
   uint64_t acc_empty[2];    // accumulator read out    (epilogue -> MMA; in the leader)
   uint64_t done;            // every MMA completed     (teardown; in the leader)
@@ -78,9 +78,10 @@ struct Params {
   int kblocks, first_kblocks;             // K steps; those of the first run
   int bn;
   int act;
-  int n, cols;          // extents of the result as cols stores it: rows and columns;  gated, rows: of what TMA stores
+  int n, cols;          // extents of a result: rows and columns
   int keep;             // gated: gate and up too
-  const void* bias;     // cols, from here on; may be null
+  int wide;             // cols, from here on: rows of out, residual and pre are 16-byte aligned
+  const void* bias;     // may be null
   int bias_bf16;
   const __nv_bfloat16* residual;  // may be null
   __nv_bfloat16* out;
@@ -95,12 +96,30 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xffffffffu, ok);
 }
 
+// A wait that asked before (`ready`, of the same phase): to look at a barrier takes some 170
+// cycles, under which the step before is issued.
+__device__ __forceinline__ bool warp_wait_if(bool ready, uint64_t* bar, uint32_t parity, volatile int* abort, int* err, uint64_t budget_ns) {
+  if (!kCheckBounds && __all_sync(0xffffffffu, ready)) return true;
+  return warp_wait(bar, parity, abort, err, budget_ns);
+}
+
 __device__ __forceinline__ void tma_store_2d(const void* tmap, const void* src, int c0, int c1) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
                    reinterpret_cast<uint64_t>(tmap)),
                "r"(smem_u32(src)), "r"(c0), "r"(c1)
                : "memory");
 }
+
+// The stages in turn (their number goes by the tile's columns: no divisions in the loops).
+struct Ring {
+  int stage = 0, round = 0;  // round: the parity of this pass over the stages
+  __device__ __forceinline__ void next(int stages) {
+    if (++stage == stages) {
+      stage = 0;
+      round ^= 1;
+    }
+  }
+};
 
 // The t-th output tile. Tiles that run at the same time are about as many rows as columns, so
 // that both operands are shared in L2: eight row tiles at a time, all column tiles of those.
@@ -124,6 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
   const int worker = static_cast<int>(blockIdx.x >> 1), workers = static_cast<int>(gridDim.x >> 1);
   const int tiles = p.row_tiles * p.col_tiles;
   constexpr bool a_mn = kForm == kColsTurned || kForm == kRowsForm;
+  const int stage_bytes = kABytes + p.bn * 64, stages = kRing / stage_bytes;
 
   if (threadIdx.x == 32 * kEpiWarp0) {  // parameters, not memory that another kernel writes
     prefetch_tmap(&maps.a[0]);
@@ -131,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     if (kForm == kGated || kForm == kRowsForm) prefetch_tmap(&maps.out[0]);
   }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       mbar_init(&sm.full[s], 1);
       mbar_init(&sm.empty[s], 1);
     }
@@ -164,35 +184,39 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const int bn_own = p.bn / 2;
     const int m0 = tl.m * kRows + rank * kBM, n0 = tl.n * p.bn + rank * bn_own;
     const uint32_t bar = smem_of_rank(&sm.full[st], 0);
-    if (rank == 0) mbar_arrive_expect_tx(&sm.full[st], 2 * (kABytes + bn_own * 128));
+    uint8_t *a = sm.ring + st * stage_bytes, *b = a + kABytes;
+    if (rank == 0) mbar_arrive_expect_tx(&sm.full[st], 2 * stage_bytes);
     if (kForm == kGated) {
-      tma_load_2d_pair(sm.a[st], &maps.a[0], bar, kb * kBK, m0);
-      tma_load_2d_pair(sm.b[st], &maps.b[rank], bar, kb * kBK, tl.n * bn_own);
+      tma_load_2d_pair(a, &maps.a[0], bar, kb * kBK, m0);
+      tma_load_2d_pair(b, &maps.b[rank], bar, kb * kBK, tl.n * bn_own);
     } else if (kForm == kCols) {
-      tma_load_2d_pair(sm.a[st], &maps.a[0], bar, kb * kBK, m0);
-      tma_load_2d_pair(sm.b[st], &maps.b[0], bar, kb * kBK, n0);
+      tma_load_2d_pair(a, &maps.a[0], bar, kb * kBK, m0);
+      tma_load_2d_pair(b, &maps.b[0], bar, kb * kBK, n0);
     } else if (kForm == kColsTurned) {
       const int run = kb >= p.first_kblocks, k0 = (kb - run * p.first_kblocks) * kBK;
-      for (int i = 0; i < 2; ++i) tma_load_2d_pair(sm.a[st] + i * kBoxBytes, &maps.a[run], bar, m0 + 64 * i, k0);
-      tma_load_2d_pair(sm.b[st], &maps.b[run], bar, k0, n0);
+      for (int i = 0; i < 2; ++i) tma_load_2d_pair(a + i * kBoxBytes, &maps.a[run], bar, m0 + 64 * i, k0);
+      tma_load_2d_pair(b, &maps.b[run], bar, k0, n0);
     } else {
       const int second = tl.m >= p.first_tiles, r0 = m0 - second * p.first_tiles * kRows;
-      for (int i = 0; i < 2; ++i) tma_load_2d_pair(sm.a[st] + i * kBoxBytes, &maps.a[second], bar, r0 + 64 * i, kb * kBK);
-      tma_load_2d_pair(sm.b[st], &maps.b[0], bar, kb * kBK, n0);
+      for (int i = 0; i < 2; ++i) tma_load_2d_pair(a + i * kBoxBytes, &maps.a[second], bar, r0 + 64 * i, kb * kBK);
+      tma_load_2d_pair(b, &maps.b[0], bar, kb * kBK, n0);
     }
   };
   if (warp == 0) {
     // ================================================================ TMA producer
+    Ring ring;
     int fill = 0;
-    bool ok = true;
+    bool ok = true, ready = true;
     for (int t = worker; ok && t < tiles; t += workers) {
       const Tile tl = tile_of(p, t);
       for (int kb = 0; kb < p.kblocks; ++kb, ++fill) {
-        const int st = fill % kStages;
-        if (fill >= kStages && !warp_wait(&sm.empty[st], ((fill / kStages) - 1) & 1, abort, p.err, p.wait_ns)) {
+        const int st = ring.stage;
+        if (!warp_wait_if(ready, &sm.empty[st], ring.round ^ 1, abort, p.err, p.wait_ns)) {
           ok = false;
           break;
         }
+        ring.next(stages);
+        ready = fill + 1 < stages || mbar_test(&sm.empty[ring.stage], ring.round ^ 1);
         if (lane == 0) load_stage(tl, kb, st);
       }
     }
@@ -201,8 +225,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     // leader's barriers, so each CTA waits for the MMAs that read its stages, and where
     // something has given up both settle their accounts behind the roles.
     bool landed = ok;
-    for (int s = 0; s < kStages; ++s) {
-      const int n_s = fill > s ? (fill - s + kStages - 1) / kStages : 0;
+    for (int s = 0; s < stages; ++s) {
+      const int n_s = fill > s ? (fill - s + stages - 1) / stages : 0;
       if (n_s && landed) landed = warp_wait(&sm.empty[s], (n_s - 1) & 1, abort, p.err, p.wait_ns);
     }
     if (lane < 2) store_at(smem_of_rank(&sm.loads[rank], lane), fill);  // here and in the other CTA
@@ -213,10 +237,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     // A step of 16 in K: 32 bytes of each row (K-major), or 16 rows of 128 bytes (MN-major).
     constexpr uint32_t a_step = a_mn ? 128 : 2, b_step = 2;
     const uint32_t idesc = idesc_bf16_f32(kRows, p.bn, a_mn, false);
-    const uint64_t a_desc0 = sdesc_sw128(smem_u32(sm.a[0]), a_mn ? kBoxBytes : 16, 1024);
-    const uint64_t b_desc0 = sdesc_sw128(smem_u32(sm.b[0]), 16, 1024);
+    const uint64_t a_desc0 = sdesc_sw128(smem_u32(sm.ring), a_mn ? kBoxBytes : 16, 1024);
+    const uint64_t b_desc0 = sdesc_sw128(smem_u32(sm.ring + kABytes), 16, 1024);
+    Ring ring;
     int fill = 0, tile = 0;
-    bool ok = true;
+    bool ok = true, ready = false;
     for (int t = worker; ok && t < tiles; t += workers, ++tile) {
       const int acc = tile & 1;
       // The accumulator's previous tile (tile - 2) must have been read out.
@@ -227,14 +252,16 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       tc_fence_after();
       const uint32_t d_tmem = tmem + acc * kMaxBN;
       for (int kb = 0; kb < p.kblocks; ++kb, ++fill) {
-        const int st = fill % kStages;
-        if (!warp_wait(&sm.full[st], (fill / kStages) & 1, abort, p.err, p.wait_ns)) {
+        const int st = ring.stage;
+        if (!warp_wait_if(ready, &sm.full[st], ring.round, abort, p.err, p.wait_ns)) {
           ok = false;
           break;
         }
+        ring.next(stages);
+        ready = mbar_test(&sm.full[ring.stage], ring.round);
         tc_fence_after();
-        const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(st) * (kABytes >> 4);
-        const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(st) * (kBBytes >> 4);
+        const uint32_t at = static_cast<uint32_t>(st) * (stage_bytes >> 4);
+        const uint64_t a_desc = a_desc0 + at, b_desc = b_desc0 + at;
 #pragma unroll
         for (int kk = 0; kk < kBK / 16; ++kk)
           mma_ss_pair_elect(d_tmem, a_desc + kk * a_step, b_desc + kk * b_step, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
@@ -349,41 +376,50 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             put(e, f(8 * e), f(8 * e + 1), f(8 * e + 2), f(8 * e + 3), f(8 * e + 4), f(8 * e + 5), f(8 * e + 6), f(8 * e + 7));
           send(&maps.out[second], tl.n * p.bn + 64 * g, r0);
         } else {
-          // 32 rows of the result at a time, this lane's column of them.
-          const int col = m0 + lane;
-          const bool on = col < p.cols;
-          float bias = 0.f;
-          if (p.bias && on)
-            bias = p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[col]) : static_cast<const float*>(p.bias)[col];
+          // 32 rows of the result at a time, of which the lanes hold a column each, turned in shared
+          // memory: eight columns a lane of every eighth row (16-byte pieces swapped by the row, so
+          // that neither side meets a bank twice).
+          const int col = m0 + 8 * (lane & 3);
+          const bool on = col < p.cols;  // (a multiple of 8)
+          float bias[8] = {};
+          if (kForm == kCols && p.bias && on) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              bias[k] = p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[col + k])
+                                    : static_cast<const float*>(p.bias)[col + k];
+          }
 #pragma unroll 1
           for (int c = 0; c < 2; ++c) {
-            const int row0 = tl.n * p.bn + 64 * g + 32 * c, rows = min(32, p.n - row0);
-            __nv_bfloat16 add[32];
-            if (p.residual && on) {
-              const __nv_bfloat16* src = p.residual + row0 * p.s_residual + col;
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (e < rows) add[e] = src[e * p.s_residual];
-            }
+            const int row0 = tl.n * p.bn + 64 * g + 32 * c;
             uint32_t x[32];
             tmem_ld32(base + 64 * g + 32 * c, x);
             tmem_wait_ld(x);
             if (last && c == 1) release(acc);
-            if (on) {
-              if (p.pre) {
-                __nv_bfloat16* dst = p.pre + row0 * p.s_pre + col;
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if (e < rows) dst[e * p.s_pre] = __float2bfloat16_rn(__uint_as_float(x[e]) + bias);
-              }
-              __nv_bfloat16* dst = p.out + row0 * p.s_out + col;
+            for (int e = 0; e < 32; ++e) *reinterpret_cast<uint32_t*>(buf + e * 128 + ((lane * 4) ^ ((e & 7) << 4))) = x[e];
+            __syncwarp();
+#pragma unroll 1
+            for (int pass = 0; pass < 4; ++pass) {
+              const int e = 8 * pass + (lane >> 2);
+              const int64_t row = row0 + e;
+              if (row >= p.n || !on) continue;
+              const int piece = 2 * (lane & 3), swap = e & 7;
+              const float4 lo = *reinterpret_cast<const float4*>(buf + e * 128 + ((piece ^ swap) << 4));
+              const float4 hi = *reinterpret_cast<const float4*>(buf + e * 128 + (((piece + 1) ^ swap) << 4));
+              float z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, add[8] = {};
+              if (p.residual) load8(p.residual + row * p.s_residual + col, p.wide, add);
+              if (kForm == kCols) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                if (e >= rows) continue;
-                float y = activate(p.act, __uint_as_float(x[e]) + bias);
-                if (p.residual) y += __bfloat162float(add[e]);
-                dst[e * p.s_out] = __float2bfloat16_rn(y);
+                for (int k = 0; k < 8; ++k) z[k] += bias[k];
+                if (p.pre) store8(p.pre + row * p.s_pre + col, p.wide, z);
+                if (p.act != DLM_ACT_NONE) {
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) z[k] = activate(p.act, z[k]);
+                }
               }
+#pragma unroll
+              for (int k = 0; k < 8; ++k) z[k] += add[k];
+              store8(p.out + row * p.s_out + col, p.wide, z);
             }
             __syncwarp();
           }
@@ -403,8 +439,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       // what has waited for it.
       const int steps = sm.mma_steps, done = sm.mma_tiles;
       bool came = true;
-      for (int s = 0; s < kStages; ++s) {
-        const int n_s = steps > s ? (steps - s + kStages - 1) / kStages : 0;
+      for (int s = 0; s < stages; ++s) {
+        const int n_s = steps > s ? (steps - s + stages - 1) / stages : 0;
         if (n_s && came) came = mbar_drain(&sm.empty[s], (n_s - 1) & 1);
       }
       for (int i = 0; i < 2; ++i) {
@@ -419,11 +455,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       for (int t = worker; at < both && t < tiles; t += workers) {
         const Tile tl = tile_of(p, t);
         for (int kb = 0; at < both && kb < p.kblocks; ++kb, ++at)
-          if (at >= mine) load_stage(tl, kb, at % kStages);
+          if (at >= mine) load_stage(tl, kb, at % stages);
       }
       if (rank == 0)
-        for (int s = 0; s < kStages; ++s) {
-          const int n_s = both > s ? (both - s + kStages - 1) / kStages : 0;
+        for (int s = 0; s < stages; ++s) {
+          const int n_s = both > s ? (both - s + stages - 1) / stages : 0;
           if (n_s && came) came = mbar_drain(&sm.full[s], (n_s - 1) & 1);
         }
     }
@@ -454,73 +490,102 @@ __device__ __forceinline__ uint4 row8(const __nv_bfloat16* base, int64_t row, in
 }
 
 // dg = dout u act'(g), du = dout act(g), rounded to bf16 for the tensor cores: each term of the
-// gradients is off by at most 2^-8 relative, as the results are by their own rounding.
+// gradients is off by at most 2^-8 relative, as the results are by their own rounding. Two
+// vectors a thread in flight.
 constexpr int kPartThreads = 256;
 __global__ void __launch_bounds__(kPartThreads)
     gated_parts_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* gate, const __nv_bfloat16* up, int64_t s_dout, int64_t s_gate,
                        int64_t s_up, int act, int64_t rows, int vecs, uint4* dgate, uint4* dup) {
+  constexpr int kLoads = 2;
   wait_for_previous();
-  const int64_t total = rows * vecs;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPartThreads + threadIdx.x; i < total;
-       i += static_cast<int64_t>(gridDim.x) * kPartThreads) {
-    const int64_t r = i / vecs, c = i - r * vecs;
-    float d[8], g[8], u[8];
-    unpack8(row8(dout, r, s_dout, c), d);
-    unpack8(row8(gate, r, s_gate, c), g);
-    unpack8(row8(up, r, s_up, c), u);
+  const int64_t total = rows * vecs, step = static_cast<int64_t>(gridDim.x) * kPartThreads;
+  for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kPartThreads + threadIdx.x; i0 < total; i0 += kLoads * step) {
+    uint4 v[kLoads][3] = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float value, slope;
-      activate_grad(act, g[e], &value, &slope);
-      g[e] = d[e] * u[e] * slope;
-      u[e] = d[e] * value;
+    for (int k = 0; k < kLoads; ++k) {
+      const int64_t i = i0 + k * step, r = i / vecs, c = i - r * vecs;
+      if (i >= total) continue;
+      v[k][0] = row8(dout, r, s_dout, c);
+      v[k][1] = row8(gate, r, s_gate, c);
+      v[k][2] = row8(up, r, s_up, c);
     }
-    dgate[i] = pack8(g);
-    dup[i] = pack8(u);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int64_t i = i0 + k * step;
+      if (i >= total) continue;
+      float d[8], g[8], u[8];
+      unpack8(v[k][0], d);
+      unpack8(v[k][1], g);
+      unpack8(v[k][2], u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float value, slope;
+        activate_grad(act, g[e], &value, &slope);
+        g[e] = d[e] * u[e] * slope;
+        u[e] = d[e] * value;
+      }
+      dgate[i] = pack8(g);
+      dup[i] = pack8(u);
+    }
   }
 }
 
-// dz = dout act'(pre) (not written without an activation), and sums of its columns over runs
-// of rows: a warp 256 columns, eight warps every eighth row of the CTA's run.
+// dz = dout act'(pre) (not written without an activation), and sums of its columns over a run of
+// rows (to `sums`, or, where there is one run, to `dbias`): 64 columns a CTA, 32 rows at a time,
+// four of them a thread in flight.
 __global__ void __launch_bounds__(kPartThreads)
     linear_parts_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* pre, int64_t s_dout, int64_t s_pre, int act, int64_t rows,
-                        int64_t rows_per_part, int vecs, uint4* dz, float* sums) {
-  __shared__ float part[kPartThreads / 32][256 + 8];
+                        int64_t rows_per_part, int vecs, uint4* dz, float* sums, void* dbias, int bias_bf16) {
+  constexpr int kLoads = 4, kLanes = kPartThreads / 8;  // rows at a time
+  __shared__ float part[kLanes][64 + 1];
   wait_for_previous();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+  const int lane = threadIdx.x & 7, row = threadIdx.x >> 3;
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * 8 + lane;
   const int64_t r0 = blockIdx.y * rows_per_part, r1 = r0 + rows_per_part < rows ? r0 + rows_per_part : rows;
   float sum[8] = {};
-  if (c < vecs) {
-#pragma unroll 4
-    for (int64_t r = r0 + warp; r < r1; r += kPartThreads / 32) {
+  for (int64_t r = r0 + row; r < r1 && c < vecs; r += kLoads * kLanes) {
+    uint4 d4[kLoads] = {}, z4[kLoads] = {};
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      if (r + k * kLanes < r1) {
+        d4[k] = row8(dout, r + k * kLanes, s_dout, c);
+        if (pre) z4[k] = row8(pre, r + k * kLanes, s_pre, c);
+      }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      if (r + k * kLanes >= r1) continue;
       float d[8];
-      unpack8(row8(dout, r, s_dout, c), d);
+      unpack8(d4[k], d);
       if (pre) {
         float z[8];
-        unpack8(row8(pre, r, s_pre, c), z);
+        unpack8(z4[k], z);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float value, slope;
           activate_grad(act, z[e], &value, &slope);
           d[e] *= slope;
         }
-        dz[r * vecs + c] = pack8(d);
+        dz[(r + k * kLanes) * vecs + c] = pack8(d);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += d[e];
     }
   }
-  if (!sums) return;
+  if (!sums && !dbias) return;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) part[warp][8 * lane + e] = sum[e];
+  for (int e = 0; e < 8; ++e) part[row][8 * lane + e] = sum[e];
   __syncthreads();
-  const int64_t col = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, cols = static_cast<int64_t>(vecs) * 8;
-  if (col >= cols) return;
+  const int64_t cols = static_cast<int64_t>(vecs) * 8, col = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x;
+  if (threadIdx.x >= 64 || col >= cols) return;
   float s = 0.f;
 #pragma unroll
-  for (int w = 0; w < kPartThreads / 32; ++w) s += part[w][threadIdx.x];
-  sums[blockIdx.y * cols + col] = s;
+  for (int i = 0; i < kLanes; ++i) s += part[i][threadIdx.x];
+  if (sums)
+    sums[blockIdx.y * cols + col] = s;
+  else if (bias_bf16)
+    static_cast<__nv_bfloat16*>(dbias)[col] = __float2bfloat16_rn(s);
+  else
+    static_cast<float*>(dbias)[col] = s;
 }
 
 // The sums of all runs, a thread a column.
@@ -578,26 +643,30 @@ int sm_count() {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Columns of a tile: 256, or 128 where those leave pairs without a tile or much of the last one
-// empty (a narrow tile reads its other operand twice as often: a column counts 1.12 times).
-int choose_bn(int64_t cols, int64_t row_tiles, int workers) {
-  int best = 256;
-  double best_cost = 1e300;
-  for (int bn = 256; bn >= 128; bn /= 2) {
-    const int64_t rounds = ceil_div(ceil_div(cols, bn) * row_tiles, workers);
-    const double cost = static_cast<double>(rounds) * (bn / 256.0 * 0.88 + 0.12);
-    if (cost < best_cost - 1e-9) {
-      best_cost = cost;
-      best = bn;
-    }
+// Columns of a tile and the time as fitted to measurements (us): 256, or 128 where those leave pairs
+// without a tile or much of the last one empty. A K step takes 0.27 to 0.29 us, 0.205 of 128 columns
+// (0.245 with an MN-major A), a tile no less than its epilogue, which the last one adds.
+struct PairPlan {
+  int bn;
+  double us;
+};
+PairPlan plan_pairs(int64_t cols, int64_t row_tiles, int64_t kblocks, int workers, bool a_mn) {
+  PairPlan best = {256, 1e300};
+  for (int bn = 256; bn >= 128 && workers > 0; bn /= 2) {
+    const double rounds = static_cast<double>(ceil_div(ceil_div(cols, bn) * row_tiles, workers));
+    const double step = bn == 256 ? 0.28 : a_mn ? 0.245 : 0.205, epilogue = bn == 256 ? 2.4 : 1.5, k = static_cast<double>(kblocks) * step;
+    const double us = 3.2 + rounds * (k > epilogue ? k : epilogue) + epilogue;
+    if (us < best.us - 1e-9) best = {bn, us};
   }
   return best;
 }
 
+bool aligned(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
+
 template <int kForm>
 int pairs_of() {
   const auto kernel = product_kernel<kForm>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes)) != cudaSuccess) return 0;
+  if (allow_smem(reinterpret_cast<const void*>(kernel), static_cast<int>(kSmemBytes)) != cudaSuccess) return 0;
   return active_clusters(reinterpret_cast<const void*>(kernel), 2, kThreads, kSmemBytes);
 }
 
@@ -625,10 +694,14 @@ int operand_map(CUtensorMap* map, const Matrix& x, int box_rows) {
 // out = act(x w^T + bias) + residual (turned: w's columns instead of its rows; two runs of K).
 int launch_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const Epilogue& ep, cudaStream_t stream) {
   const int64_t N = x[0].rows, M = turned ? w[0].cols : w[0].rows;
+  const int64_t kblocks = ceil_div(x[0].cols, kBK);
   const int workers = turned ? pairs_of<kColsTurned>() : pairs_of<kCols>();
+  const PairPlan plan = plan_pairs(N, ceil_div(M, kRows), runs * kblocks, workers, turned);
+  const FewPlan few = plan_few(N, ceil_div(M, kBM), runs * kblocks, 1, false);
+  if (few.us < plan.us) return launch_few_cols(x, w, runs, turned, ep, few, stream);
   Params p = {};
   p.row_tiles = static_cast<int>(ceil_div(M, kRows));
-  p.bn = choose_bn(N, p.row_tiles, workers > 0 ? workers : 1);
+  p.bn = plan.bn;
   p.col_tiles = static_cast<int>(ceil_div(N, p.bn));
   Maps m = {};
   int st;
@@ -636,7 +709,7 @@ int launch_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const E
     if ((st = operand_map(&m.a[i], w[i], turned ? 64 : kBM)) != DLM_OK) return st;
     if ((st = operand_map(&m.b[i], x[i], p.bn / 2)) != DLM_OK) return st;
   }
-  p.first_kblocks = static_cast<int>(ceil_div(x[0].cols, kBK));
+  p.first_kblocks = static_cast<int>(kblocks);
   p.kblocks = runs * p.first_kblocks;
   p.act = ep.act;
   p.n = static_cast<int>(N);
@@ -649,28 +722,8 @@ int launch_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const E
   p.s_residual = ep.s_residual;
   p.s_out = ep.s_out;
   p.s_pre = ep.s_pre;
+  p.wide = aligned(ep.out, ep.s_out) && (!ep.residual || aligned(ep.residual, ep.s_residual)) && (!ep.pre || aligned(ep.pre, ep.s_pre));
   return turned ? launch_product<kColsTurned>(m, p, workers, stream) : launch_product<kCols>(m, p, workers, stream);
-}
-
-// out[i] = z[i]^T x, x given transposed; `count` matrices z of the same shape.
-int launch_rows(const Matrix* z, const Matrix& xt, const Matrix* out, int count, cudaStream_t stream) {
-  const int workers = pairs_of<kRowsForm>();
-  Params p = {};
-  p.first_tiles = static_cast<int>(ceil_div(z[0].cols, kRows));
-  p.row_tiles = count * p.first_tiles;
-  p.bn = choose_bn(xt.rows, p.row_tiles, workers > 0 ? workers : 1);
-  p.col_tiles = static_cast<int>(ceil_div(xt.rows, p.bn));
-  p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(z[0].rows, kBK));
-  p.n = static_cast<int>(z[0].cols);
-  p.cols = static_cast<int>(xt.rows);
-  Maps m = {};
-  int st;
-  for (int i = 0; i < count; ++i) {
-    if ((st = operand_map(&m.a[i], z[i], 64)) != DLM_OK) return st;
-    if ((st = operand_map(&m.out[i], out[i], 32)) != DLM_OK) return st;
-  }
-  if ((st = operand_map(&m.b[0], xt, p.bn / 2)) != DLM_OK) return st;
-  return launch_product<kRowsForm>(m, p, workers, stream);
 }
 
 size_t take(size_t* at, size_t bytes) {
@@ -681,9 +734,10 @@ size_t take(size_t* at, size_t bytes) {
 
 int64_t pad_rows(int64_t n) { return ceil_div(n, 64) * 64; }
 
-// Runs of rows whose sums of columns are kept: enough CTAs for every SM, of 64 rows at least.
+// Runs of rows whose sums of columns are kept: eight CTAs an SM, of 1024 rows at least (one run needs
+// no second launch).
 int64_t bias_parts(int64_t N, int64_t m) {
-  const int64_t want = ceil_div(4 * 152, ceil_div(m, 256)), most = ceil_div(N, 64);
+  const int64_t want = ceil_div(8 * 152, ceil_div(m, 64)), most = ceil_div(N, 1024);
   return want < most ? want : most;
 }
 
@@ -707,15 +761,46 @@ int launch_transpose(const Matrix& x, void* out, Matrix* turned, cudaStream_t st
                   "transposition");
 }
 
+// out[i] = z[i]^T x for `count` matrices z of the same shape; turned: room for x transposed.
+int launch_rows(const Matrix* z, const Matrix& x, void* turned, const Matrix* out, int count, cudaStream_t stream) {
+  const int workers = pairs_of<kRowsForm>();
+  const int64_t row_tiles = count * ceil_div(z[0].cols, kRows), kblocks = ceil_div(x.rows, kBK);
+  const PairPlan plan = plan_pairs(x.cols, row_tiles, kblocks, workers, true);
+  const FewPlan few = plan_few(z[0].cols, ceil_div(x.cols, kBM), kblocks, count, true);
+  if (few.us < plan.us + 1.5) return launch_few_outer(z, x, out, count, few, stream);  // 1.5: the transposition's launch
+  Matrix xt;
+  int st;
+  if ((st = launch_transpose(x, turned, &xt, stream)) != DLM_OK) return st;
+  Params p = {};
+  p.first_tiles = static_cast<int>(ceil_div(z[0].cols, kRows));
+  p.row_tiles = static_cast<int>(row_tiles);
+  p.bn = plan.bn;
+  p.col_tiles = static_cast<int>(ceil_div(xt.rows, p.bn));
+  p.kblocks = p.first_kblocks = static_cast<int>(kblocks);
+  p.n = static_cast<int>(z[0].cols);
+  p.cols = static_cast<int>(xt.rows);
+  Maps m = {};
+  for (int i = 0; i < count; ++i) {
+    if ((st = operand_map(&m.a[i], z[i], 64)) != DLM_OK) return st;
+    if ((st = operand_map(&m.out[i], out[i], 32)) != DLM_OK) return st;
+  }
+  if ((st = operand_map(&m.b[0], xt, p.bn / 2)) != DLM_OK) return st;
+  return launch_product<kRowsForm>(m, p, workers, stream);
+}
+
 }  // namespace
 
 int launch_gated(const GatedArgs& a, cudaStream_t stream) {
+  const int64_t f = a.w_gate.rows, row_tiles = ceil_div(a.x.rows, kRows), kblocks = ceil_div(a.x.cols, kBK);
   const int workers = pairs_of<kGated>();
+  const PairPlan plan = plan_pairs(2 * f, row_tiles, kblocks, workers, false);
+  const FewPlan few = plan_few(a.x.rows, ceil_div(f, 64), kblocks, 1, false);
+  if (few.us < plan.us) return launch_few_gated(a, few, stream);
   Params p = {};
-  p.row_tiles = static_cast<int>(ceil_div(a.x.rows, kRows));
-  p.bn = choose_bn(2 * a.w_gate.rows, p.row_tiles, workers > 0 ? workers : 1);
-  p.col_tiles = static_cast<int>(ceil_div(a.w_gate.rows, p.bn / 2));
-  p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(a.x.cols, kBK));
+  p.row_tiles = static_cast<int>(row_tiles);
+  p.bn = plan.bn;
+  p.col_tiles = static_cast<int>(ceil_div(f, p.bn / 2));
+  p.kblocks = p.first_kblocks = static_cast<int>(kblocks);
   p.act = a.act;
   p.n = static_cast<int>(a.x.rows);
   p.cols = static_cast<int>(a.w_gate.rows);
@@ -756,9 +841,7 @@ int launch_gated_grad(const GatedArgs& a, cudaStream_t stream) {
     if ((st = launch_cols(dz, w, 2, true, ep, stream)) != DLM_OK) return st;
   }
   if (!dw[0].data) return DLM_OK;
-  Matrix xt;
-  if ((st = launch_transpose(a.x, ws + l.turned, &xt, stream)) != DLM_OK) return st;
-  return launch_rows(dz, xt, dw, 2, stream);
+  return launch_rows(dz, a.x, ws + l.turned, dw, 2, stream);
 }
 
 size_t linear_workspace_bytes(int64_t N, int64_t m, int64_t k) {
@@ -779,17 +862,18 @@ int launch_linear_grad(const LinearArgs& a, cudaStream_t stream) {
   Matrix dz = a.dout;
   int st;
   if (a.pre.data || a.dbias) {
-    const int64_t parts = bias_parts(N, m), rows = ceil_div(N, parts);
-    float* sums = a.dbias ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
+    // Without a bias there are no sums, and the runs may be short.
+    const int64_t parts = a.dbias ? bias_parts(N, m) : ceil_div(N, 128), rows = ceil_div(N, parts);
+    float* sums = a.dbias && parts > 1 ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
     if (a.pre.data) dz = {ws + l.dz, N, m, m};
-    const dim3 grid(static_cast<unsigned>(ceil_div(m, 256)), static_cast<unsigned>(parts));
+    const dim3 grid(static_cast<unsigned>(ceil_div(m, 64)), static_cast<unsigned>(parts));
     st = launched(launch_overlapped(linear_parts_kernel, grid, kPartThreads, 0, stream, 1, true,
                                     static_cast<const __nv_bfloat16*>(a.dout.data), static_cast<const __nv_bfloat16*>(a.pre.data),
                                     a.dout.stride, a.pre.stride, a.ep.act, N, rows, static_cast<int>(m / 8),
-                                    reinterpret_cast<uint4*>(ws + l.dz), sums),
+                                    reinterpret_cast<uint4*>(ws + l.dz), sums, a.dbias, a.ep.bias_bf16),
                   "gradient parts");
     if (st != DLM_OK) return st;
-    if (a.dbias) {
+    if (sums) {
       st = launched(launch_overlapped(bias_sum_kernel, dim3(static_cast<unsigned>(ceil_div(m, kPartThreads))), kPartThreads, 0, stream, 1,
                                       true, static_cast<const float*>(sums), static_cast<int>(parts), static_cast<int>(m), a.dbias,
                                       a.ep.bias_bf16),
@@ -804,9 +888,7 @@ int launch_linear_grad(const LinearArgs& a, cudaStream_t stream) {
     if ((st = launch_cols(&dz, &a.w, 1, true, ep, stream)) != DLM_OK) return st;
   }
   if (!a.dw.data) return DLM_OK;
-  Matrix xt;
-  if ((st = launch_transpose(a.x, ws + l.turned, &xt, stream)) != DLM_OK) return st;
-  return launch_rows(&dz, xt, &a.dw, 1, stream);
+  return launch_rows(&dz, a.x, ws + l.turned, &a.dw, 1, stream);
 }
 
 }  // namespace dlm

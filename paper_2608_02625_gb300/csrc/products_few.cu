@@ -1,0 +1,434 @@
+// The products of a feed-forward block (products.cu) where they are small: few rows, as in
+// serving, or too few output tiles for pairs of CTAs.
+//
+// The result is computed transposed, in tiles of 128 of its columns (TMEM lanes) and n of its
+// rows, 16 to 128, so that few rows waste little of an MMA and the weights, which bound it,
+// stream through at 16 KB a K step. K is split over the CTAs of a cluster, up to 8 of them, for
+// enough CTAs to keep HBM busy: each leaves its fp32 sums in its shared memory, and each reads
+// its share of the rows from all of them (distributed shared memory, in the order of the ranks: the
+// same bits every time) for the epilogue. No partial sums go through memory, and no second launch.
+//   gated   A is 64 gate rows and the same 64 up rows; the epilogue has both in shared memory
+//   cols    A the weight's rows (K-major), B the rows of x
+//   turned  A the weight's columns (MN-major), B the rows of dz; K in up to two runs
+//   outer   dW = dz^T x: A the columns of x, B those of dz (both MN-major, as they lie)
+// Two CTAs an SM. Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, lets what
+// it has on its way land and goes on to the cluster's barriers with whatever it has.
+#include <cooperative_groups.h>
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <cstdint>
+
+#include "block_math.cuh"
+#include "dlm_common.cuh"
+#include "dlm_internal.h"
+#include "dlm_tmap.h"
+#include "products.h"
+
+namespace cg = cooperative_groups;
+
+namespace dlm {
+namespace {
+
+constexpr int kBM = 128;               // lanes: columns of the result (gated: 64, twice)
+constexpr int kBK = 64;                // K of a stage: 128 bytes of bf16
+constexpr int kThreads = 256;          // warp 0 TMA, warp 1 MMA; all of them the epilogue
+constexpr int kABytes = kBM * kBK * 2;
+constexpr int kBoxBytes = 64 * 128;    // an MN-major box: 64 K rows of 64 columns
+constexpr int kMaxStages = 6;
+constexpr int kStageRoom = 108 * 1024;  // of a CTA, so that two fit on an SM
+
+enum Form { kGated, kCols, kTurned, kOuter };
+
+struct Bars {
+  uint64_t full[kMaxStages];   // stage loaded           (TMA -> MMA)
+  uint64_t empty[kMaxStages];  // stage read by its MMAs (MMA -> TMA)
+  uint64_t done;               // every MMA completed
+  uint32_t tmem_base;
+  int abort;
+};
+
+struct Maps {
+  CUtensorMap a[2], b[2];  // [1]: up (gated), the second run of K (turned), the second matrix (outer: b)
+};
+
+// out[0]: the result; gated: gate and up behind it (may be null); outer: the second matrix's.
+struct Params {
+  int col_tiles, first_tiles;  // tiles of n rows of the result; outer: those of the first matrix
+  int n;                       // rows of a tile
+  int kblocks, first_kblocks;  // K steps; those of the first run
+  int splits, stages;
+  int rows, cols;              // extents of the result
+  int act, bias_bf16;
+  int wide;                    // rows of out, pre and residual are 16-byte aligned
+  const void* bias;
+  const __nv_bfloat16* residual;
+  __nv_bfloat16* out[3];
+  __nv_bfloat16* pre;
+  int64_t s_residual, s_out[3], s_pre;
+  uint32_t tmem_cols;
+  int* err;
+  uint64_t wait_ns;
+};
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* err, uint64_t budget_ns) {
+  const bool ok = mbar_wait_for(bar, parity, abort, err, budget_ns);
+  return __all_sync(0xffffffffu, ok);
+}
+
+// The stages in turn. (With fill % stages and fill / stages a step took 600 cycles, whatever it
+// loaded: two divisions in a warp of its own.)
+struct Ring {
+  int stage = 0, round = 0;  // round: the parity of this pass over the stages
+  __device__ __forceinline__ void next(int stages) {
+    if (++stage == stages) {
+      stage = 0;
+      round ^= 1;
+    }
+  }
+};
+
+// A wait that asked before (`ready`, of the same phase): to look at a barrier takes some 170
+// cycles, under which the step before is issued.
+__device__ __forceinline__ bool warp_wait_if(bool ready, uint64_t* bar, uint32_t parity, volatile int* abort, int* err, uint64_t budget_ns) {
+  if (!kCheckBounds && __all_sync(0xffffffffu, ready)) return true;
+  return warp_wait(bar, parity, abort, err, budget_ns);
+}
+
+__device__ __forceinline__ uint32_t smem_at_rank(uint32_t addr, uint32_t rank) {
+  uint32_t there;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  return there;
+}
+
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int kForm>
+__global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant__ Maps maps, const Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Bars bars;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  constexpr bool a_mn = kForm == kTurned || kForm == kOuter, b_mn = kForm == kOuter;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(blockIdx.x) % p.splits, tile = static_cast<int>(blockIdx.x) / p.splits;
+  const int row_tile = tile / p.col_tiles, col_tile = tile % p.col_tiles;
+  const int second = kForm == kOuter && col_tile >= p.first_tiles;
+  const int m0 = row_tile * (kForm == kGated ? 64 : kBM);          // first column of the result
+  const int n0 = (col_tile - second * p.first_tiles) * p.n;        // first row
+  const int k0 = static_cast<int>(static_cast<int64_t>(p.kblocks) * rank / p.splits);
+  const int k1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.splits);
+  const int b_bytes = p.n * 128, stage_bytes = kABytes + b_bytes;
+
+  if (threadIdx.x == 32) {
+    prefetch_tmap(&maps.a[0]);
+    prefetch_tmap(&maps.b[second]);
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&bars.full[s], 1);
+      mbar_init(&bars.empty[s], 1);
+    }
+    mbar_init(&bars.done, 1);
+    bars.abort = 0;
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 1) {
+    tmem_alloc(&bars.tmem_base, p.tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars.tmem_base;
+  volatile int* abort = &bars.abort;
+  wait_for_previous();
+
+  if (warp == 0) {
+    // ================================================================ TMA producer
+    Ring ring;
+    int fill = 0;
+    bool ready = true;
+    for (int kb = k0; kb < k1; ++kb, ++fill) {
+      const int st = ring.stage;
+      if (!warp_wait_if(ready, &bars.empty[st], ring.round ^ 1, abort, p.err, p.wait_ns)) break;
+      ring.next(p.stages);
+      ready = fill + 1 < p.stages || mbar_test(&bars.empty[ring.stage], ring.round ^ 1);
+      if (lane == 0) {
+        uint8_t *a = smem + st * stage_bytes, *b = a + kABytes;
+        uint64_t* bar = &bars.full[st];
+        mbar_arrive_expect_tx(bar, stage_bytes);
+        if (kForm == kGated) {
+          tma_load_2d(a, &maps.a[0], bar, kb * kBK, m0);
+          tma_load_2d(a + kABytes / 2, &maps.a[1], bar, kb * kBK, m0);
+          tma_load_2d(b, &maps.b[0], bar, kb * kBK, n0);
+        } else if (kForm == kCols) {
+          tma_load_2d(a, &maps.a[0], bar, kb * kBK, m0);
+          tma_load_2d(b, &maps.b[0], bar, kb * kBK, n0);
+        } else if (kForm == kTurned) {
+          const int run = kb >= p.first_kblocks, k = (kb - run * p.first_kblocks) * kBK;
+          for (int i = 0; i < 2; ++i) tma_load_2d(a + i * kBoxBytes, &maps.a[run], bar, m0 + 64 * i, k);
+          tma_load_2d(b, &maps.b[run], bar, k, n0);
+        } else {
+          for (int i = 0; i < 2; ++i) tma_load_2d(a + i * kBoxBytes, &maps.a[0], bar, m0 + 64 * i, kb * kBK);
+          for (int i = 0; i < p.n / 64; ++i) tma_load_2d(b + i * kBoxBytes, &maps.b[second], bar, n0 + 64 * i, kb * kBK);
+        }
+      }
+    }
+    launch_dependents();
+    if (lane == 0)  // every copy issued lands, whoever has given up
+      for (int s = 0; s < p.stages; ++s) {
+        const int n_s = fill > s ? (fill - s + p.stages - 1) / p.stages : 0;
+        if (n_s) mbar_drain(&bars.full[s], (n_s - 1) & 1);
+      }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ================================================================ MMA issuer
+    constexpr uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
+    const uint32_t idesc = idesc_bf16_f32(kBM, p.n, a_mn, b_mn);
+    const uint64_t a_desc0 = sdesc_sw128(smem_u32(smem), a_mn ? kBoxBytes : 16, 1024);
+    const uint64_t b_desc0 = sdesc_sw128(smem_u32(smem + kABytes), b_mn ? kBoxBytes : 16, 1024);
+    Ring ring;
+    int fill = 0;
+    bool ready = false;
+    for (int kb = k0; kb < k1; ++kb, ++fill) {
+      const int st = ring.stage;
+      if (!warp_wait_if(ready, &bars.full[st], ring.round, abort, p.err, p.wait_ns)) break;
+      ring.next(p.stages);
+      ready = mbar_test(&bars.full[ring.stage], ring.round);
+      tc_fence_after();
+      const uint32_t at = static_cast<uint32_t>(st) * (stage_bytes >> 4);
+#pragma unroll
+      for (int kk = 0; kk < kBK / 16; ++kk)
+        mma_ss_elect(tmem, a_desc0 + at + kk * a_step, b_desc0 + at + kk * b_step, idesc, (fill > 0 || kk > 0) ? 1u : 0u);
+      mma_commit_elect(&bars.empty[st]);
+    }
+    mma_commit_elect(&bars.done);
+    mbar_drain(&bars.done, 0);
+    __syncwarp();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+
+  // ================================================================ sums to shared memory
+  // [row of the tile][lane], over the stages, which nothing uses any more. (Rows are as many as
+  // fill a load; what is behind the valid ones is not read.)
+  const uint32_t sums = smem_u32(smem);
+  const int valid = min(p.n, p.rows - n0);  // rows of the result in this tile
+  for (int c = (warp >> 2) * 32; c < valid; c += 64) {
+    uint32_t x[32];
+    tmem_ld32(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + c, x);
+    tmem_wait_ld(x);
+    float* dst = reinterpret_cast<float*>(smem) + c * kBM + (warp & 3) * 32 + lane;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) dst[e * kBM] = __uint_as_float(x[e]);
+  }
+  tc_fence_before();
+  if (p.splits > 1)
+    cg::this_cluster().sync();
+  else
+    __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+
+  // ================================================================ epilogue: this CTA's rows
+  // Eight columns a thread. (Two: 69 instructions for them, and 10000 cycles for 128 rows.)
+  const int c0 = static_cast<int>(static_cast<int64_t>(valid) * rank / p.splits);
+  const int c1 = static_cast<int>(static_cast<int64_t>(valid) * (rank + 1) / p.splits);
+  const auto joined = [&](uint32_t at, float (&z)[8]) {  // lanes i .. i + 7 of a row, over all ranks
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int r0 = 0; r0 < p.splits; r0 += 4) {
+        float4 v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (r0 + r < p.splits) v[r] = load_cluster(smem_at_rank(at + 16 * h, r0 + r));
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (r0 + r < p.splits) s = make_float4(s.x + v[r].x, s.y + v[r].y, s.z + v[r].z, s.w + v[r].w);
+      }
+      z[4 * h] = s.x;
+      z[4 * h + 1] = s.y;
+      z[4 * h + 2] = s.z;
+      z[4 * h + 3] = s.w;
+    }
+  };
+  constexpr int kGroups = kForm == kGated ? 8 : 16;  // of eight columns
+  const int i = 8 * (threadIdx.x % kGroups), col = m0 + i;
+  if (col < p.cols) {  // (a multiple of 8)
+    const bool wide = p.wide;
+    float bias[8] = {};
+    if (kForm == kCols && p.bias) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        bias[k] = p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[col + k])
+                              : static_cast<const float*>(p.bias)[col + k];
+    }
+#pragma unroll 1
+    for (int c = c0 + threadIdx.x / kGroups; c < c1; c += kThreads / kGroups) {
+      const int64_t row = static_cast<int64_t>(n0) + c;
+      float add[8] = {};
+      if ((kForm == kCols || kForm == kTurned) && p.residual) load8(p.residual + row * p.s_residual + col, wide, add);
+      float z[8];
+      joined(sums + (c * kBM + i) * 4, z);
+      if (kForm == kGated) {
+        float u[8];
+        joined(sums + (c * kBM + 64 + i) * 4, u);
+        if (p.out[1]) {
+          store8(p.out[1] + row * p.s_out[1] + col, true, z);
+          store8(p.out[2] + row * p.s_out[2] + col, true, u);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z[k] = activate(p.act, z[k]) * u[k];
+      } else if (kForm == kCols) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z[k] += bias[k];
+        if (p.pre) store8(p.pre + row * p.s_pre + col, wide, z);
+        if (p.act != DLM_ACT_NONE) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) z[k] = activate(p.act, z[k]);
+        }
+      }
+      if (kForm == kCols || kForm == kTurned) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z[k] += add[k];
+      }
+      const int o = kForm == kOuter ? second : 0;
+      store8(p.out[o] + row * p.s_out[o] + col, wide, z);
+    }
+  }
+  if (p.splits > 1) cg::this_cluster().sync();  // nobody's sums go while others read them
+}
+
+// ---------------------------------------------------------------- host side
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+bool aligned(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
+
+template <int kForm>
+int launch_few(const Maps& m, Params p, int64_t row_tiles, const FewPlan& plan, cudaStream_t stream) {
+  p.splits = plan.splits;
+  const int stage = kABytes + p.n * 128;
+  const int64_t ctas = row_tiles * p.col_tiles * p.splits;
+  p.stages = kStageRoom / stage < kMaxStages ? kStageRoom / stage : kMaxStages;
+  p.tmem_cols = p.n <= 32 ? 32 : p.n <= 64 ? 64 : 128;
+  p.err = device_error_word();
+  p.wait_ns = wait_budget_ns();
+  const size_t smem = static_cast<size_t>(p.stages) * stage + 1024;
+  const auto kernel = few_kernel<kForm>;
+  cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel), kStageRoom + 1024);
+  if (e == cudaSuccess)
+    e = launch_overlapped(kernel, dim3(static_cast<unsigned>(ctas)), kThreads, smem, stream, p.splits, true,
+                          m, p);
+  return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
+}
+
+int operand_map(CUtensorMap* map, const Matrix& x, int box_rows) {
+  return make_matrix_map(map, x.data, true, x.rows, x.cols, x.stride, box_rows);
+}
+
+}  // namespace
+
+// Fitted to measured times (us): a launch, then for every round of two CTAs an SM the K steps
+// (more each where two CTAs share an SM) and the rows of the epilogue; later rounds start with what
+// the first one has done under the launch before. With splits one round only: clusters that
+// wait for places leave many empty (gated 64 x 2048 x 8192 in 512 CTAs of 2: 24 us, 256: 15).
+FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices, bool outer) {
+  constexpr int kPlaces = 2 * 152;
+  constexpr double kStep[4] = {0.22, 0.225, 0.27, 0.35}, kShared[4] = {0.34, 0.36, 0.40, 0.50};  // n = 16, 32, 64, 128
+  FewPlan best = {128, 1, 1e300};
+  for (int i = outer ? 2 : 0; i < 4; ++i) {
+    const int n = 16 << i;
+    if (n > 16 && n / 2 >= rows && !(outer && n == 64)) break;
+    for (int s = 1; s <= 8 && s <= kblocks; s *= 2) {
+      const int64_t ctas = row_tiles * matrices * ceil_div(rows, n) * s;
+      if (s > 1 && ctas > kPlaces) break;
+      const double rounds = static_cast<double>(ceil_div(ctas, kPlaces)), steps = static_cast<double>(ceil_div(kblocks, s));
+      const double us = 3.0 + rounds * (steps * (ctas > 152 ? kShared : kStep)[i] + 0.02 * n / s) + 1.8 * (rounds - 1) + (s > 1 ? 0.5 : 0.0);
+      if (us < best.us - 1e-9) best = {n, s, us};
+    }
+  }
+  return best;
+}
+
+int launch_few_gated(const GatedArgs& a, const FewPlan& plan, cudaStream_t stream) {
+  Params p = {};
+  p.rows = static_cast<int>(a.x.rows);
+  p.cols = static_cast<int>(a.w_gate.rows);
+  p.n = plan.n;
+  p.col_tiles = p.first_tiles = static_cast<int>(ceil_div(p.rows, p.n));
+  p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(a.x.cols, kBK));
+  p.act = a.act;
+  p.wide = 1;
+  const Matrix* outs[3] = {&a.out, &a.gate, &a.up};
+  for (int i = 0; i < 3; ++i) {
+    p.out[i] = static_cast<__nv_bfloat16*>(outs[i]->data);
+    p.s_out[i] = outs[i]->stride;
+  }
+  Maps m = {};
+  int st;
+  if ((st = operand_map(&m.a[0], a.w_gate, 64)) != DLM_OK) return st;
+  if ((st = operand_map(&m.a[1], a.w_up, 64)) != DLM_OK) return st;
+  if ((st = operand_map(&m.b[0], a.x, p.n)) != DLM_OK) return st;
+  return launch_few<kGated>(m, p, ceil_div(p.cols, 64), plan, stream);
+}
+
+int launch_few_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const Epilogue& ep, const FewPlan& plan,
+                    cudaStream_t stream) {
+  Params p = {};
+  p.rows = static_cast<int>(x[0].rows);
+  p.cols = static_cast<int>(turned ? w[0].cols : w[0].rows);
+  p.n = plan.n;
+  p.col_tiles = p.first_tiles = static_cast<int>(ceil_div(p.rows, p.n));
+  p.first_kblocks = static_cast<int>(ceil_div(x[0].cols, kBK));
+  p.kblocks = runs * p.first_kblocks;
+  p.act = ep.act;
+  p.bias = ep.bias;
+  p.bias_bf16 = ep.bias_bf16;
+  p.residual = static_cast<const __nv_bfloat16*>(ep.residual);
+  p.out[0] = static_cast<__nv_bfloat16*>(ep.out);
+  p.pre = static_cast<__nv_bfloat16*>(ep.pre);
+  p.s_residual = ep.s_residual;
+  p.s_out[0] = ep.s_out;
+  p.s_pre = ep.s_pre;
+  p.wide = aligned(p.out[0], p.s_out[0]) && (!p.residual || aligned(p.residual, p.s_residual)) && (!p.pre || aligned(p.pre, p.s_pre));
+  Maps m = {};
+  int st;
+  for (int i = 0; i < runs; ++i) {
+    if ((st = operand_map(&m.a[i], w[i], turned ? 64 : kBM)) != DLM_OK) return st;
+    if ((st = operand_map(&m.b[i], x[i], p.n)) != DLM_OK) return st;
+  }
+  const int64_t row_tiles = ceil_div(p.cols, kBM);
+  return turned ? launch_few<kTurned>(m, p, row_tiles, plan, stream) : launch_few<kCols>(m, p, row_tiles, plan, stream);
+}
+
+int launch_few_outer(const Matrix* z, const Matrix& x, const Matrix* out, int count, const FewPlan& plan, cudaStream_t stream) {
+  Params p = {};
+  p.rows = static_cast<int>(z[0].cols);
+  p.cols = static_cast<int>(x.cols);
+  p.n = plan.n;
+  p.first_tiles = static_cast<int>(ceil_div(p.rows, p.n));
+  p.col_tiles = count * p.first_tiles;
+  p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(x.rows, kBK));
+  p.wide = 1;
+  Maps m = {};
+  int st;
+  for (int i = 0; i < count; ++i) {
+    p.out[i] = static_cast<__nv_bfloat16*>(out[i].data);
+    p.s_out[i] = out[i].stride;
+    if ((st = operand_map(&m.b[i], z[i], 64)) != DLM_OK) return st;
+  }
+  if ((st = operand_map(&m.a[0], x, 64)) != DLM_OK) return st;
+  return launch_few<kOuter>(m, p, ceil_div(p.cols, kBM), plan, stream);
+}
+
+}  // namespace dlm
