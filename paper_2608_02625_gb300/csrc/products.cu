@@ -530,18 +530,19 @@ __global__ void __launch_bounds__(kPartThreads)
   }
 }
 
-// dz = dout act'(pre) (not written without an activation), and sums of its columns over a run of
-// rows (to `sums`, or, where there is one run, to `dbias`): 64 columns a CTA, 32 rows at a time,
-// four of them a thread in flight.
+// dz = dout act'(pre) (not written without an activation), and sums of its columns: 64 columns a
+// CTA, 32 rows at a time, four of them a thread in flight. The CTAs of a cluster share a run of rows,
+// whose sums its first one adds up in their order: to `sums`, or, where there is one run, to `dbias`.
 __global__ void __launch_bounds__(kPartThreads)
     linear_parts_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* pre, int64_t s_dout, int64_t s_pre, int act, int64_t rows,
-                        int64_t rows_per_part, int vecs, uint4* dz, float* sums, void* dbias, int bias_bf16) {
+                        int64_t rows_per_cta, int vecs, uint4* dz, float* sums, void* dbias, int bias_bf16) {
   constexpr int kLoads = 4, kLanes = kPartThreads / 8;  // rows at a time
-  __shared__ float part[kLanes][64 + 1];
+  __shared__ float part[kLanes][64 + 1], total[64];
   wait_for_previous();
   const int lane = threadIdx.x & 7, row = threadIdx.x >> 3;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 8 + lane;
-  const int64_t r0 = blockIdx.y * rows_per_part, r1 = r0 + rows_per_part < rows ? r0 + rows_per_part : rows;
+  const int ranks = static_cast<int>(cg::this_cluster().num_blocks()), rank = static_cast<int>(cg::this_cluster().block_rank());
+  const int64_t strip = blockIdx.x / ranks, c = strip * 8 + lane, run = static_cast<int64_t>(blockIdx.y) * ranks + rank;
+  const int64_t r0 = run * rows_per_cta, r1 = r0 + rows_per_cta < rows ? r0 + rows_per_cta : rows;
   float sum[8] = {};
   for (int64_t r = r0 + row; r < r1 && c < vecs; r += kLoads * kLanes) {
     uint4 d4[kLoads] = {}, z4[kLoads] = {};
@@ -575,17 +576,25 @@ __global__ void __launch_bounds__(kPartThreads)
 #pragma unroll
   for (int e = 0; e < 8; ++e) part[row][8 * lane + e] = sum[e];
   __syncthreads();
-  const int64_t cols = static_cast<int64_t>(vecs) * 8, col = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x;
-  if (threadIdx.x >= 64 || col >= cols) return;
-  float s = 0.f;
+  if (threadIdx.x < 64) {
+    float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < kLanes; ++i) s += part[i][threadIdx.x];
-  if (sums)
-    sums[blockIdx.y * cols + col] = s;
-  else if (bias_bf16)
-    static_cast<__nv_bfloat16*>(dbias)[col] = __float2bfloat16_rn(s);
-  else
-    static_cast<float*>(dbias)[col] = s;
+    for (int i = 0; i < kLanes; ++i) s += part[i][threadIdx.x];
+    total[threadIdx.x] = s;
+  }
+  cg::this_cluster().sync();
+  const int64_t cols = static_cast<int64_t>(vecs) * 8, col = strip * 64 + threadIdx.x;
+  if (rank == 0 && threadIdx.x < 64 && col < cols) {
+    float s = 0.f;
+    for (int i = 0; i < ranks; ++i) s += *cg::this_cluster().map_shared_rank(total + threadIdx.x, i);
+    if (sums)
+      sums[blockIdx.y * cols + col] = s;
+    else if (bias_bf16)
+      static_cast<__nv_bfloat16*>(dbias)[col] = __float2bfloat16_rn(s);
+    else
+      static_cast<float*>(dbias)[col] = s;
+  }
+  cg::this_cluster().sync();  // nobody's sums go while the first one reads them
 }
 
 // The sums of all runs, a thread a column.
@@ -650,6 +659,8 @@ struct PairPlan {
   int bn;
   double us;
 };
+constexpr double kTurnUs = 1.5;     // the launch that transposes x for the weights' gradients
+constexpr double kOverlapUs = 3.0;  // what one launch for two products saves
 PairPlan plan_pairs(int64_t cols, int64_t row_tiles, int64_t kblocks, int workers, bool a_mn) {
   PairPlan best = {256, 1e300};
   for (int bn = 256; bn >= 128 && workers > 0; bn /= 2) {
@@ -734,11 +745,17 @@ size_t take(size_t* at, size_t bytes) {
 
 int64_t pad_rows(int64_t n) { return ceil_div(n, 64) * 64; }
 
-// Runs of rows whose sums of columns are kept: eight CTAs an SM, of 1024 rows at least (one run needs
-// no second launch).
-int64_t bias_parts(int64_t N, int64_t m) {
-  const int64_t want = ceil_div(8 * 152, ceil_div(m, 64)), most = ceil_div(N, 1024);
-  return want < most ? want : most;
+// How the rows are split for the sums of dz's columns: CTAs of a cluster, of 64 rows each or more,
+// and runs, whose sums are kept (one run needs no second launch): eight CTAs an SM in all.
+struct BiasSplit {
+  int64_t runs;
+  int ranks;
+};
+BiasSplit bias_split(int64_t N, int64_t m) {
+  const int64_t want = ceil_div(8 * 152, ceil_div(m, 64)), most = ceil_div(N, 64), all = want < most ? want : most;
+  int ranks = 1;
+  while (ranks < 8 && ranks * 2 <= all) ranks *= 2;
+  return {all > 64 ? ceil_div(all, ranks) : 1, ranks};
 }
 
 struct GradLayout {
@@ -749,7 +766,7 @@ GradLayout grad_layout(int64_t N, int64_t m, int64_t d, int matrices) {
   l.dz = take(&l.bytes, static_cast<size_t>(N) * m * 2);
   if (matrices == 2) l.second = take(&l.bytes, static_cast<size_t>(N) * m * 2);
   l.turned = take(&l.bytes, static_cast<size_t>(d) * pad_rows(N) * 2);
-  if (matrices == 1) l.sums = take(&l.bytes, static_cast<size_t>(bias_parts(N, m)) * m * 4);
+  if (matrices == 1) l.sums = take(&l.bytes, static_cast<size_t>(bias_split(N, m).runs) * m * 4);
   return l;
 }
 
@@ -767,7 +784,7 @@ int launch_rows(const Matrix* z, const Matrix& x, void* turned, const Matrix* ou
   const int64_t row_tiles = count * ceil_div(z[0].cols, kRows), kblocks = ceil_div(x.rows, kBK);
   const PairPlan plan = plan_pairs(x.cols, row_tiles, kblocks, workers, true);
   const FewPlan few = plan_few(z[0].cols, ceil_div(x.cols, kBM), kblocks, count, true);
-  if (few.us < plan.us + 1.5) return launch_few_outer(z, x, out, count, few, stream);  // 1.5: the transposition's launch
+  if (few.us < plan.us + kTurnUs) return launch_few_outer(z, x, out, count, few, stream);
   Matrix xt;
   int st;
   if ((st = launch_transpose(x, turned, &xt, stream)) != DLM_OK) return st;
@@ -786,6 +803,33 @@ int launch_rows(const Matrix* z, const Matrix& x, void* turned, const Matrix* ou
   }
   if ((st = operand_map(&m.b[0], xt, p.bn / 2)) != DLM_OK) return st;
   return launch_product<kRowsForm>(m, p, workers, stream);
+}
+
+// dx = sum z[i] w[i] + what ep adds (none without ep.out), dw[i] = z[i]^T x (none without data).
+int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue& ep, const Matrix& x, void* turned, const Matrix* dw,
+                     cudaStream_t stream) {
+  const int64_t x_tiles = ceil_div(x.cols, kBM), x_kblocks = count * ceil_div(z[0].cols, kBK), w_kblocks = ceil_div(x.rows, kBK);
+  // In one launch, or apart, where each runs as it is fastest: by the sizes alone, so that each has
+  // the same bits without the other.
+  FewPlan fx = {}, fw = {};
+  double both = 1e300;
+  for (int s = 1; s <= 8; s *= 2) {
+    const FewPlan a = plan_few(x.rows, x_tiles, x_kblocks, 1, false, s), b = plan_few(z[0].cols, x_tiles, w_kblocks, count, true, s, true);
+    if (a.us + b.us >= both) continue;
+    both = a.us + b.us;
+    fx = a;
+    fw = b;
+  }
+  const double pairs_x = plan_pairs(x.rows, ceil_div(x.cols, kRows), x_kblocks, pairs_of<kColsTurned>(), true).us;
+  const double pairs_w = plan_pairs(x.cols, count * ceil_div(z[0].cols, kRows), w_kblocks, pairs_of<kRowsForm>(), true).us + kTurnUs;
+  const double few_x = plan_few(x.rows, x_tiles, x_kblocks, 1, false).us, few_w = plan_few(z[0].cols, x_tiles, w_kblocks, count, true).us;
+  if (both - kOverlapUs < (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w)) {
+    if (ep.out && dw[0].data) return launch_few_gradients(z, w, count, ep, fx, x, dw, fw, stream);
+    return ep.out ? launch_few_cols(z, w, count, true, ep, fx, stream) : dw[0].data ? launch_few_outer(z, x, dw, count, fw, stream) : DLM_OK;
+  }
+  int st;
+  if (ep.out && (st = launch_cols(z, w, count, true, ep, stream)) != DLM_OK) return st;
+  return dw[0].data ? launch_rows(z, x, turned, dw, count, stream) : DLM_OK;
 }
 
 }  // namespace
@@ -832,16 +876,12 @@ int launch_gated_grad(const GatedArgs& a, cudaStream_t stream) {
                                       static_cast<uint4*>(dz[0].data), static_cast<uint4*>(dz[1].data)),
                     "gradient parts");
   if (st != DLM_OK) return st;
-  if (a.dx) {
-    Epilogue ep = {};
-    ep.residual = a.add;
-    ep.s_residual = a.s_add;
-    ep.out = a.dx;
-    ep.s_out = a.s_dx;
-    if ((st = launch_cols(dz, w, 2, true, ep, stream)) != DLM_OK) return st;
-  }
-  if (!dw[0].data) return DLM_OK;
-  return launch_rows(dz, a.x, ws + l.turned, dw, 2, stream);
+  Epilogue ep = {};
+  ep.residual = a.add;
+  ep.s_residual = a.s_add;
+  ep.out = a.dx;
+  ep.s_out = a.s_dx;
+  return launch_gradients(dz, w, 2, ep, a.x, ws + l.turned, dw, stream);
 }
 
 size_t linear_workspace_bytes(int64_t N, int64_t m, int64_t k) {
@@ -862,12 +902,12 @@ int launch_linear_grad(const LinearArgs& a, cudaStream_t stream) {
   Matrix dz = a.dout;
   int st;
   if (a.pre.data || a.dbias) {
-    // Without a bias there are no sums, and the runs may be short.
-    const int64_t parts = a.dbias ? bias_parts(N, m) : ceil_div(N, 128), rows = ceil_div(N, parts);
-    float* sums = a.dbias && parts > 1 ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
+    const BiasSplit split = a.dbias ? bias_split(N, m) : BiasSplit{N < (int64_t{1} << 22) ? ceil_div(N, 128) : 1 << 15, 1};
+    const int64_t rows = ceil_div(N, split.runs * split.ranks);
+    float* sums = a.dbias && split.runs > 1 ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
     if (a.pre.data) dz = {ws + l.dz, N, m, m};
-    const dim3 grid(static_cast<unsigned>(ceil_div(m, 64)), static_cast<unsigned>(parts));
-    st = launched(launch_overlapped(linear_parts_kernel, grid, kPartThreads, 0, stream, 1, true,
+    const dim3 grid(static_cast<unsigned>(ceil_div(m, 64) * split.ranks), static_cast<unsigned>(split.runs));
+    st = launched(launch_overlapped(linear_parts_kernel, grid, kPartThreads, 0, stream, split.ranks, true,
                                     static_cast<const __nv_bfloat16*>(a.dout.data), static_cast<const __nv_bfloat16*>(a.pre.data),
                                     a.dout.stride, a.pre.stride, a.ep.act, N, rows, static_cast<int>(m / 8),
                                     reinterpret_cast<uint4*>(ws + l.dz), sums, a.dbias, a.ep.bias_bf16),
@@ -875,20 +915,16 @@ int launch_linear_grad(const LinearArgs& a, cudaStream_t stream) {
     if (st != DLM_OK) return st;
     if (sums) {
       st = launched(launch_overlapped(bias_sum_kernel, dim3(static_cast<unsigned>(ceil_div(m, kPartThreads))), kPartThreads, 0, stream, 1,
-                                      true, static_cast<const float*>(sums), static_cast<int>(parts), static_cast<int>(m), a.dbias,
+                                      true, static_cast<const float*>(sums), static_cast<int>(split.runs), static_cast<int>(m), a.dbias,
                                       a.ep.bias_bf16),
                     "bias gradient");
       if (st != DLM_OK) return st;
     }
   }
-  if (a.ep.out) {  // d x
-    Epilogue ep = a.ep;
-    ep.act = DLM_ACT_NONE;
-    ep.bias = nullptr;
-    if ((st = launch_cols(&dz, &a.w, 1, true, ep, stream)) != DLM_OK) return st;
-  }
-  if (!a.dw.data) return DLM_OK;
-  return launch_rows(&dz, a.x, ws + l.turned, &a.dw, 1, stream);
+  Epilogue ep = a.ep;  // of d x
+  ep.act = DLM_ACT_NONE;
+  ep.bias = nullptr;
+  return launch_gradients(&dz, &a.w, 1, ep, a.x, ws + l.turned, &a.dw, stream);
 }
 
 }  // namespace dlm

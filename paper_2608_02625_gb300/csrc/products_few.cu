@@ -107,14 +107,20 @@ __device__ __forceinline__ float4 load_cluster(uint32_t addr) {
   return v;
 }
 
+__device__ __forceinline__ float4 load_own(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 template <int kForm>
-__global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant__ Maps maps, const Params p) {
+__device__ __forceinline__ void few_product(const Maps& maps, const Params& p, int block) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ Bars bars;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   constexpr bool a_mn = kForm == kTurned || kForm == kOuter, b_mn = kForm == kOuter;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(blockIdx.x) % p.splits, tile = static_cast<int>(blockIdx.x) / p.splits;
+  const int rank = block % p.splits, tile = block / p.splits;
   const int row_tile = tile / p.col_tiles, col_tile = tile % p.col_tiles;
   const int second = kForm == kOuter && col_tile >= p.first_tiles;
   const int m0 = row_tile * (kForm == kGated ? 64 : kBM);          // first column of the result
@@ -228,32 +234,39 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant_
 #pragma unroll
     for (int e = 0; e < 32; ++e) dst[e * kBM] = __uint_as_float(x[e]);
   }
+  // Tensor memory is given back before the wait for the cluster's other CTAs: whoever waits for
+  // some of it, a CTA that this one would wait for among them, waits for this CTA's own work alone.
   tc_fence_before();
-  if (p.splits > 1)
-    cg::this_cluster().sync();
-  else
-    __syncthreads();
+  __syncthreads();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, p.tmem_cols);
   }
+  if (p.splits > 1) cg::this_cluster().sync();
 
   // ================================================================ epilogue: this CTA's rows
   // Eight columns a thread. (Two: 69 instructions for them, and 10000 cycles for 128 rows.)
   const int c0 = static_cast<int>(static_cast<int64_t>(valid) * rank / p.splits);
   const int c1 = static_cast<int>(static_cast<int64_t>(valid) * (rank + 1) / p.splits);
+  // The cluster's rank of the first CTA of this tile (the cluster is larger than the splits where one
+  // launch computes both gradients).
+  const uint32_t first_rank = cg::this_cluster().block_rank() - static_cast<uint32_t>(rank);
   const auto joined = [&](uint32_t at, float (&z)[8]) {  // lanes i .. i + 7 of a row, over all ranks
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int r0 = 0; r0 < p.splits; r0 += 4) {
-        float4 v[4];
+      if (p.splits == 1) {
+        s = load_own(at + 16 * h);
+      } else {
+        for (int r0 = 0; r0 < p.splits; r0 += 4) {
+          float4 v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (r0 + r < p.splits) v[r] = load_cluster(smem_at_rank(at + 16 * h, r0 + r));
+          for (int r = 0; r < 4; ++r)
+            if (r0 + r < p.splits) v[r] = load_cluster(smem_at_rank(at + 16 * h, first_rank + r0 + r));
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (r0 + r < p.splits) s = make_float4(s.x + v[r].x, s.y + v[r].y, s.z + v[r].z, s.w + v[r].w);
+          for (int r = 0; r < 4; ++r)
+            if (r0 + r < p.splits) s = make_float4(s.x + v[r].x, s.y + v[r].y, s.z + v[r].z, s.w + v[r].w);
+        }
       }
       z[4 * h] = s.x;
       z[4 * h + 1] = s.y;
@@ -305,7 +318,25 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant_
       store8(p.out[o] + row * p.s_out[o] + col, wide, z);
     }
   }
+  __syncwarp();
   if (p.splits > 1) cg::this_cluster().sync();  // nobody's sums go while others read them
+}
+
+template <int kForm>
+__global__ void __launch_bounds__(kThreads, 3) few_kernel(const __grid_constant__ Maps maps, const Params p) {
+  few_product<kForm>(maps, p, static_cast<int>(blockIdx.x));
+}
+
+// Both gradients of a projection from dz: the first CTAs compute d x, those behind them dW. One
+// reads the weights, the other writes as much: at the same time they use HBM both ways.
+__global__ void __launch_bounds__(kThreads, 3)
+    few_gradients_kernel(const __grid_constant__ Maps x_maps, const Params x, const __grid_constant__ Maps w_maps, const Params w, int x_ctas,
+                         int w_ctas) {
+  const int block = static_cast<int>(blockIdx.x);
+  if (block < x_ctas)
+    few_product<kTurned>(x_maps, x, block);
+  else if (block - x_ctas < w_ctas)  // (whole clusters are launched)
+    few_product<kOuter>(w_maps, w, block - x_ctas);
 }
 
 // ---------------------------------------------------------------- host side
@@ -314,21 +345,32 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 bool aligned(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
 
-template <int kForm>
-int launch_few(const Maps& m, Params p, int64_t row_tiles, const FewPlan& plan, cudaStream_t stream) {
+// What the plan leaves to fill in; the CTAs and their shared memory.
+struct Launch {
+  int64_t ctas;
+  size_t smem;
+};
+Launch complete(Params* to, int64_t row_tiles, const FewPlan& plan) {
+  Params& p = *to;
   p.splits = plan.splits;
-  const int stage = kABytes + p.n * 128;
-  const int64_t ctas = row_tiles * p.col_tiles * p.splits;
+  // No more stages than steps, but room for the sums: where K is short, three CTAs fit on an SM.
+  const int stage = kABytes + p.n * 128, steps = static_cast<int>(ceil_div(p.kblocks, p.splits));
   p.stages = kStageRoom / stage < kMaxStages ? kStageRoom / stage : kMaxStages;
+  if (p.stages > steps) p.stages = steps;
   p.tmem_cols = p.n <= 32 ? 32 : p.n <= 64 ? 64 : 128;
   p.err = device_error_word();
   p.wait_ns = wait_budget_ns();
-  const size_t smem = static_cast<size_t>(p.stages) * stage + 1024;
+  const int sums = static_cast<int>(ceil_div(p.n, 32) * 32) * kBM * 4;
+  return {row_tiles * p.col_tiles * p.splits, static_cast<size_t>(p.stages * stage > sums ? p.stages * stage : sums) + 1024};
+}
+
+template <int kForm>
+int launch_few(const Maps& m, Params p, int64_t row_tiles, const FewPlan& plan, cudaStream_t stream) {
+  const Launch l = complete(&p, row_tiles, plan);
   const auto kernel = few_kernel<kForm>;
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel), kStageRoom + 1024);
   if (e == cudaSuccess)
-    e = launch_overlapped(kernel, dim3(static_cast<unsigned>(ctas)), kThreads, smem, stream, p.splits, true,
-                          m, p);
+    e = launch_overlapped(kernel, dim3(static_cast<unsigned>(l.ctas)), kThreads, l.smem, stream, p.splits, true, m, p);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
 }
 
@@ -339,21 +381,24 @@ int operand_map(CUtensorMap* map, const Matrix& x, int box_rows) {
 }  // namespace
 
 // Fitted to measured times (us): a launch, then for every round of two CTAs an SM the K steps
-// (more each where two CTAs share an SM) and the rows of the epilogue; later rounds start with what
-// the first one has done under the launch before. With splits one round only: clusters that
-// wait for places leave many empty (gated 64 x 2048 x 8192 in 512 CTAs of 2: 24 us, 256: 15).
-FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices, bool outer) {
-  constexpr int kPlaces = 2 * 152;
+// (more each where two CTAs share an SM) and the rows of the epilogue, which cost more where other
+// CTAs' sums are read (some 20 bytes a ns an SM from their shared memory); later rounds start with
+// what the first one has done under the launch before. With splits one round only.
+FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices, bool outer, int splits, bool or_one) {
+  constexpr int kSms = 152;
   constexpr double kStep[4] = {0.22, 0.225, 0.27, 0.35}, kShared[4] = {0.34, 0.36, 0.40, 0.50};  // n = 16, 32, 64, 128
   FewPlan best = {128, 1, 1e300};
   for (int i = outer ? 2 : 0; i < 4; ++i) {
     const int n = 16 << i;
     if (n > 16 && n / 2 >= rows && !(outer && n == 64)) break;
     for (int s = 1; s <= 8 && s <= kblocks; s *= 2) {
+      if (splits && s != splits && !(or_one && s == 1)) continue;
       const int64_t ctas = row_tiles * matrices * ceil_div(rows, n) * s;
-      if (s > 1 && ctas > kPlaces) break;
-      const double rounds = static_cast<double>(ceil_div(ctas, kPlaces)), steps = static_cast<double>(ceil_div(kblocks, s));
-      const double us = 3.0 + rounds * (steps * (ctas > 152 ? kShared : kStep)[i] + 0.02 * n / s) + 1.8 * (rounds - 1) + (s > 1 ? 0.5 : 0.0);
+      if (s > 1 && ctas > 2 * kSms) break;
+      const bool shared = ctas > kSms;
+      const double rounds = static_cast<double>(ceil_div(ctas, 2 * kSms)), steps = static_cast<double>(ceil_div(kblocks, s));
+      const double epilogue = s == 1 ? 0.012 * n : 0.5 + 0.03 * n * (shared ? 2 : 1);
+      const double us = 3.0 + rounds * (steps * (shared ? kShared : kStep)[i] + epilogue) + 1.8 * (rounds - 1);
       if (us < best.us - 1e-9) best = {n, s, us};
     }
   }
@@ -382,9 +427,10 @@ int launch_few_gated(const GatedArgs& a, const FewPlan& plan, cudaStream_t strea
   return launch_few<kGated>(m, p, ceil_div(p.cols, 64), plan, stream);
 }
 
-int launch_few_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const Epilogue& ep, const FewPlan& plan,
-                    cudaStream_t stream) {
-  Params p = {};
+namespace {
+
+int set_up_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const Epilogue& ep, const FewPlan& plan, Maps* maps, Params* to) {
+  Params& p = *to;
   p.rows = static_cast<int>(x[0].rows);
   p.cols = static_cast<int>(turned ? w[0].cols : w[0].rows);
   p.n = plan.n;
@@ -401,18 +447,16 @@ int launch_few_cols(const Matrix* x, const Matrix* w, int runs, bool turned, con
   p.s_out[0] = ep.s_out;
   p.s_pre = ep.s_pre;
   p.wide = aligned(p.out[0], p.s_out[0]) && (!p.residual || aligned(p.residual, p.s_residual)) && (!p.pre || aligned(p.pre, p.s_pre));
-  Maps m = {};
   int st;
   for (int i = 0; i < runs; ++i) {
-    if ((st = operand_map(&m.a[i], w[i], turned ? 64 : kBM)) != DLM_OK) return st;
-    if ((st = operand_map(&m.b[i], x[i], p.n)) != DLM_OK) return st;
+    if ((st = operand_map(&maps->a[i], w[i], turned ? 64 : kBM)) != DLM_OK) return st;
+    if ((st = operand_map(&maps->b[i], x[i], p.n)) != DLM_OK) return st;
   }
-  const int64_t row_tiles = ceil_div(p.cols, kBM);
-  return turned ? launch_few<kTurned>(m, p, row_tiles, plan, stream) : launch_few<kCols>(m, p, row_tiles, plan, stream);
+  return DLM_OK;
 }
 
-int launch_few_outer(const Matrix* z, const Matrix& x, const Matrix* out, int count, const FewPlan& plan, cudaStream_t stream) {
-  Params p = {};
+int set_up_outer(const Matrix* z, const Matrix& x, const Matrix* out, int count, const FewPlan& plan, Maps* maps, Params* to) {
+  Params& p = *to;
   p.rows = static_cast<int>(z[0].cols);
   p.cols = static_cast<int>(x.cols);
   p.n = plan.n;
@@ -420,15 +464,48 @@ int launch_few_outer(const Matrix* z, const Matrix& x, const Matrix* out, int co
   p.col_tiles = count * p.first_tiles;
   p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(x.rows, kBK));
   p.wide = 1;
-  Maps m = {};
   int st;
   for (int i = 0; i < count; ++i) {
     p.out[i] = static_cast<__nv_bfloat16*>(out[i].data);
     p.s_out[i] = out[i].stride;
-    if ((st = operand_map(&m.b[i], z[i], 64)) != DLM_OK) return st;
+    if ((st = operand_map(&maps->b[i], z[i], 64)) != DLM_OK) return st;
   }
-  if ((st = operand_map(&m.a[0], x, 64)) != DLM_OK) return st;
-  return launch_few<kOuter>(m, p, ceil_div(p.cols, kBM), plan, stream);
+  return operand_map(&maps->a[0], x, 64);
+}
+
+}  // namespace
+
+int launch_few_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const Epilogue& ep, const FewPlan& plan,
+                    cudaStream_t stream) {
+  Maps m = {};
+  Params p = {};
+  const int st = set_up_cols(x, w, runs, turned, ep, plan, &m, &p);
+  if (st != DLM_OK) return st;
+  const int64_t row_tiles = ceil_div(p.cols, kBM);
+  return turned ? launch_few<kTurned>(m, p, row_tiles, plan, stream) : launch_few<kCols>(m, p, row_tiles, plan, stream);
+}
+
+int launch_few_outer(const Matrix* z, const Matrix& x, const Matrix* out, int count, const FewPlan& plan, cudaStream_t stream) {
+  Maps m = {};
+  Params p = {};
+  const int st = set_up_outer(z, x, out, count, plan, &m, &p);
+  return st != DLM_OK ? st : launch_few<kOuter>(m, p, ceil_div(p.cols, kBM), plan, stream);
+}
+
+int launch_few_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue& ep, const FewPlan& x_plan, const Matrix& x,
+                         const Matrix* dw, const FewPlan& w_plan, cudaStream_t stream) {
+  Maps xm = {}, wm = {};
+  Params xp = {}, wp = {};
+  int st;
+  if ((st = set_up_cols(z, w, count, true, ep, x_plan, &xm, &xp)) != DLM_OK) return st;
+  if ((st = set_up_outer(z, x, dw, count, w_plan, &wm, &wp)) != DLM_OK) return st;
+  const Launch xl = complete(&xp, ceil_div(xp.cols, kBM), x_plan), wl = complete(&wp, ceil_div(wp.cols, kBM), w_plan);
+  cudaError_t e = allow_smem(reinterpret_cast<const void*>(few_gradients_kernel), kStageRoom + 1024);
+  const int64_t s = xp.splits, ctas = xl.ctas + ceil_div(wl.ctas, s) * s;
+  if (e == cudaSuccess)
+    e = launch_overlapped(few_gradients_kernel, dim3(static_cast<unsigned>(ctas)), kThreads, xl.smem > wl.smem ? xl.smem : wl.smem, stream,
+                          xp.splits, true, xm, xp, wm, wp, static_cast<int>(xl.ctas), static_cast<int>(wl.ctas));
+  return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "gradients launch: %s", cudaGetErrorString(e));
 }
 
 }  // namespace dlm
