@@ -536,8 +536,8 @@ typedef struct dlm_adamw_params {
  * Arithmetic in fp32. 8-bit states round to the nearest code (half a step: 2^-4 relative
  * from 2^-6 of the scale up, 2^-10 of the scale below); a sqrt(v) above 0 is held as the
  * smallest code at least, so that no weight is divided by eps alone on the next step. The
- * step itself uses m and v before that rounding. A block whose scale is below fp32's normal
- * range is held as zeros. A NaN or an infinity in a gradient makes its weight NaN, and
+ * step itself uses m and v before that rounding. With 8-bit states a v below fp32's normal range
+ * counts as 0, and a block whose scale is below it is held as zeros. A NaN or an infinity in a gradient makes its weight NaN, and
  * where states are held in 8 bits those of its whole block.
  */
 int dlm_adamw(const dlm_tensor* params, const dlm_tensor* masters, const dlm_tensor* grads, const dlm_tensor* m,

@@ -3,7 +3,7 @@
 Tolerances, in roundings of fp32 (U = 2^-24). A coefficient and the clipping factor are
 rounded once each, so with M = |beta1 m| + |(1 - beta1) g| the new m is off by at most 6 U M
 (two coefficients, two products, the factor, the sum) and the new v, all of whose terms are
-positive, by 8 U v; sqrt(v) then by 5 U. The step's size, lr / (1 - beta1^t) m / (sqrt(v) /
+positive, by 8 U v; sqrt(v) then by 6 U (half of that, and an approximation good to 2 U). The step's size, lr / (1 - beta1^t) m / (sqrt(v) /
 sqrt(1 - beta2^t) + eps): the two corrections by 5 U each (the rounded t ln beta, expm1f of one
 ulp, a division or a square root and its reciprocal), the quotient by another 5 (its
 approximation is good to 2 ulp); so by 32 U lr / (1 - beta1^t) M / (sqrt(v / (1 - beta2^t)) +
@@ -101,7 +101,7 @@ class Case:
                 within(host(self.v[i]), v, 8 * U32 * v, w + " v")
                 continue
             for codes, scales, x, err, least in ((self.m, self.ms, m, 6 * U32 * M, 2.0 ** -10),
-                                                 (self.v, self.vs, np.sqrt(v), 5 * U32 * np.sqrt(v), 2.0 ** -9)):
+                                                 (self.v, self.vs, np.sqrt(v), 6 * U32 * np.sqrt(v), 2.0 ** -9)):
                 s = oracle.block_scales(x)
                 top = np.maximum.reduceat(err, np.arange(0, len(err), 256)) if len(err) else err
                 within(host(scales[i]), s, (top + 448 * 2 * U32 * s) / 448, w + " scale")
