@@ -660,7 +660,10 @@ struct PairPlan {
   double us;
 };
 constexpr double kTurnUs = 1.5;     // the launch that transposes x for the weights' gradients
-constexpr double kOverlapUs = 3.0;  // what one launch for two products saves
+// What one launch for two products saves, with weights up to this size: 64 x 1024 x 4096 13.9 -> 9.5 us, but
+// 64 x 8192 x 2048 (33 MB) 24.5 -> 35.8.
+constexpr double kOverlapUs = 3.0;
+constexpr int64_t kBothBytes = 20 << 20;
 PairPlan plan_pairs(int64_t cols, int64_t row_tiles, int64_t kblocks, int workers, bool a_mn) {
   PairPlan best = {256, 1e300};
   for (int bn = 256; bn >= 128 && workers > 0; bn /= 2) {
@@ -823,7 +826,8 @@ int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue
   const double pairs_x = plan_pairs(x.rows, ceil_div(x.cols, kRows), x_kblocks, pairs_of<kColsTurned>(), true).us;
   const double pairs_w = plan_pairs(x.cols, count * ceil_div(z[0].cols, kRows), w_kblocks, pairs_of<kRowsForm>(), true).us + kTurnUs;
   const double few_x = plan_few(x.rows, x_tiles, x_kblocks, 1, false).us, few_w = plan_few(z[0].cols, x_tiles, w_kblocks, count, true).us;
-  if (both - kOverlapUs < (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w)) {
+  const bool small = count * z[0].cols * x.cols * 2 <= kBothBytes;
+  if (small && both - kOverlapUs < (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w)) {
     if (ep.out && dw[0].data) return launch_few_gradients(z, w, count, ep, fx, x, dw, fw, stream);
     return ep.out ? launch_few_cols(z, w, count, true, ep, fx, stream) : dw[0].data ? launch_few_outer(z, x, dw, count, fw, stream) : DLM_OK;
   }

@@ -11,7 +11,9 @@
 //   cols    A the weight's rows (K-major), B the rows of x
 //   turned  A the weight's columns (MN-major), B the rows of dz; K in up to two runs
 //   outer   dW = dz^T x: A the columns of x, B those of dz (both MN-major, as they lie)
-// Two CTAs an SM. Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, lets what
+// Two CTAs an SM, more where K is short. Where dW's K is not split (few_weights), CTAs take one tile
+// after another and write it while the next one is computed: with a CTA for each tile 64 x 2048 x 8192
+// took 14 us for what is written in 8. Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, lets what
 // it has on its way land and goes on to the cluster's barriers with whatever it has.
 #include <cooperative_groups.h>
 #include <cuda.h>
@@ -37,6 +39,7 @@ constexpr int kABytes = kBM * kBK * 2;
 constexpr int kBoxBytes = 64 * 128;    // an MN-major box: 64 K rows of 64 columns
 constexpr int kMaxStages = 6;
 constexpr int kStageRoom = 108 * 1024;  // of a CTA, so that two fit on an SM
+constexpr int kSharedRoom = 74 * 1024;  // three, where one launch computes both gradients in many CTAs
 
 enum Form { kGated, kCols, kTurned, kOuter };
 
@@ -44,6 +47,8 @@ struct Bars {
   uint64_t full[kMaxStages];   // stage loaded           (TMA -> MMA)
   uint64_t empty[kMaxStages];  // stage read by its MMAs (MMA -> TMA)
   uint64_t done;               // every MMA completed
+  uint64_t acc_full[2];        // few_weights: accumulator complete (MMA -> epilogue)
+  uint64_t acc_empty[2];       // accumulator read out              (epilogue -> MMA)
   uint32_t tmem_base;
   int abort;
 };
@@ -55,6 +60,7 @@ struct Maps {
 // out[0]: the result; gated: gate and up behind it (may be null); outer: the second matrix's.
 struct Params {
   int col_tiles, first_tiles;  // tiles of n rows of the result; outer: those of the first matrix
+  int tiles;                   // few_weights: all
   int n;                       // rows of a tile
   int kblocks, first_kblocks;  // K steps; those of the first run
   int splits, stages;
@@ -322,6 +328,154 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
   if (p.splits > 1) cg::this_cluster().sync();  // nobody's sums go while others read them
 }
 
+// dW = dz^T x, 128 x 128 a tile, by `workers` CTAs. Not transposed: A is dz's columns, B those of x
+// (both MN-major), and the sums go from tensor memory to the result, a row of it a lane, under the next
+// tile's loads and MMAs (two accumulators).
+constexpr int kEpiWarp0 = 4;  // warps 4-7
+__device__ __forceinline__ void few_weights(const Maps& maps, const Params& p, int worker, int workers) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Bars bars;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  constexpr int kStageBytes = 2 * kABytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&bars.full[s], 1);
+      mbar_init(&bars.empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.acc_full[i], 1);
+      mbar_init(&bars.acc_empty[i], 4);
+    }
+    mbar_init(&bars.done, 1);
+    bars.abort = 0;
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 1) {
+    tmem_alloc(&bars.tmem_base, 256);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars.tmem_base;
+  volatile int* abort = &bars.abort;
+  wait_for_previous();
+  struct Tile {
+    int second, row, col;
+  };
+  const auto tile_of = [&](int t) {
+    const int strip = t % p.col_tiles, second = strip >= p.first_tiles;
+    return Tile{second, (strip - second * p.first_tiles) * kBM, t / p.col_tiles * kBM};
+  };
+  if (warp == 0) {
+    Ring ring;
+    int fill = 0;
+    bool ok = true, ready = true;
+    for (int t = worker; ok && t < p.tiles; t += workers) {
+      const Tile tl = tile_of(t);
+      for (int kb = 0; kb < p.kblocks; ++kb, ++fill) {
+        const int st = ring.stage;
+        if (!warp_wait_if(ready, &bars.empty[st], ring.round ^ 1, abort, p.err, p.wait_ns)) {
+          ok = false;
+          break;
+        }
+        ring.next(p.stages);
+        ready = fill + 1 < p.stages || mbar_test(&bars.empty[ring.stage], ring.round ^ 1);
+        if (lane == 0) {
+          uint8_t *a = smem + st * kStageBytes, *b = a + kABytes;
+          uint64_t* bar = &bars.full[st];
+          mbar_arrive_expect_tx(bar, kStageBytes);
+          for (int i = 0; i < 2; ++i) tma_load_2d(a + i * kBoxBytes, &maps.b[tl.second], bar, tl.row + 64 * i, kb * kBK);
+          for (int i = 0; i < 2; ++i) tma_load_2d(b + i * kBoxBytes, &maps.a[0], bar, tl.col + 64 * i, kb * kBK);
+        }
+      }
+    }
+    launch_dependents();
+    if (lane == 0)  // every copy issued lands, whoever has given up
+      for (int s = 0; s < p.stages; ++s) {
+        const int n_s = fill > s ? (fill - s + p.stages - 1) / p.stages : 0;
+        if (n_s) mbar_drain(&bars.full[s], (n_s - 1) & 1);
+      }
+    __syncwarp();
+  } else if (warp == 1) {
+    const uint32_t idesc = idesc_bf16_f32(kBM, kBM, true, true);
+    const uint64_t a_desc0 = sdesc_sw128(smem_u32(smem), kBoxBytes, 1024), b_desc0 = sdesc_sw128(smem_u32(smem + kABytes), kBoxBytes, 1024);
+    Ring ring;
+    int tile = 0;
+    bool ok = true, ready = false;
+    for (int t = worker; ok && t < p.tiles; t += workers, ++tile) {
+      const int acc = tile & 1;
+      if (tile >= 2 && !warp_wait(&bars.acc_empty[acc], ((tile >> 1) - 1) & 1, abort, p.err, p.wait_ns)) break;
+      tc_fence_after();
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        const int st = ring.stage;
+        if (!warp_wait_if(ready, &bars.full[st], ring.round, abort, p.err, p.wait_ns)) {
+          ok = false;
+          break;
+        }
+        ring.next(p.stages);
+        ready = mbar_test(&bars.full[ring.stage], ring.round);
+        tc_fence_after();
+        const uint32_t at = static_cast<uint32_t>(st) * (kStageBytes >> 4);
+#pragma unroll
+        for (int kk = 0; kk < kBK / 16; ++kk)
+          mma_ss_elect(tmem + acc * kBM, a_desc0 + at + kk * 128, b_desc0 + at + kk * 128, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+        mma_commit_elect(&bars.empty[st]);
+      }
+      if (!ok) break;
+      mma_commit_elect(&bars.acc_full[acc]);
+    }
+    mma_commit_elect(&bars.done);
+    mbar_drain(&bars.done, 0);
+    __syncwarp();
+  } else if (warp >= kEpiWarp0) {
+    const int qw = warp & 3;
+    int tile = 0;
+    for (int t = worker; t < p.tiles; t += workers, ++tile) {
+      const Tile tl = tile_of(t);
+      const int acc = tile & 1;
+      if (!warp_wait(&bars.acc_full[acc], (tile >> 1) & 1, abort, p.err, p.wait_ns)) break;
+      tc_fence_after();
+      const int64_t row = tl.row + qw * 32 + lane;
+#pragma unroll 1
+      for (int c = 0; c < kBM; c += 32) {
+        uint32_t x[32];
+        tmem_ld32(tmem + (static_cast<uint32_t>(qw * 32) << 16) + acc * kBM + c, x);
+        tmem_wait_ld(x);
+        if (c + 32 == kBM) {  // every column has been read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars.acc_empty[acc]);
+        }
+        const int n = min(32, p.cols - tl.col - c);  // (a multiple of 8)
+        if (row < p.rows && n > 0) {
+          __nv_bfloat16* dst = p.out[tl.second] + row * p.s_out[tl.second] + tl.col + c;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (8 * k < n) {
+              const auto f = [&](int e) { return __uint_as_float(x[8 * k + e]); };
+              *reinterpret_cast<uint4*>(dst + 8 * k) =
+                  make_uint4(pack_bf16x2(f(0), f(1)), pack_bf16x2(f(2), f(3)), pack_bf16x2(f(4), f(5)), pack_bf16x2(f(6), f(7)));
+            }
+        }
+        __syncwarp();
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 256);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 2) few_weights_kernel(const __grid_constant__ Maps maps, const Params p) {
+  few_weights(maps, p, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+}
+
 template <int kForm>
 __global__ void __launch_bounds__(kThreads, 3) few_kernel(const __grid_constant__ Maps maps, const Params p) {
   few_product<kForm>(maps, p, static_cast<int>(blockIdx.x));
@@ -335,8 +489,12 @@ __global__ void __launch_bounds__(kThreads, 3)
   const int block = static_cast<int>(blockIdx.x);
   if (block < x_ctas)
     few_product<kTurned>(x_maps, x, block);
-  else if (block - x_ctas < w_ctas)  // (whole clusters are launched)
+  else if (block - x_ctas >= w_ctas)
+    return;  // whole clusters are launched
+  else if (w.splits > 1)
     few_product<kOuter>(w_maps, w, block - x_ctas);
+  else
+    few_weights(w_maps, w, block - x_ctas, w_ctas);
 }
 
 // ---------------------------------------------------------------- host side
@@ -350,12 +508,12 @@ struct Launch {
   int64_t ctas;
   size_t smem;
 };
-Launch complete(Params* to, int64_t row_tiles, const FewPlan& plan) {
+Launch complete(Params* to, int64_t row_tiles, const FewPlan& plan, int room) {
   Params& p = *to;
   p.splits = plan.splits;
   // No more stages than steps, but room for the sums: where K is short, three CTAs fit on an SM.
   const int stage = kABytes + p.n * 128, steps = static_cast<int>(ceil_div(p.kblocks, p.splits));
-  p.stages = kStageRoom / stage < kMaxStages ? kStageRoom / stage : kMaxStages;
+  p.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
   if (p.stages > steps) p.stages = steps;
   p.tmem_cols = p.n <= 32 ? 32 : p.n <= 64 ? 64 : 128;
   p.err = device_error_word();
@@ -364,9 +522,20 @@ Launch complete(Params* to, int64_t row_tiles, const FewPlan& plan) {
   return {row_tiles * p.col_tiles * p.splits, static_cast<size_t>(p.stages * stage > sums ? p.stages * stage : sums) + 1024};
 }
 
+// few_weights: as many CTAs as have tiles, up to `most`.
+Launch complete_weights(Params* to, int room, int most) {
+  Params& p = *to;
+  p.splits = 1;
+  p.tiles = static_cast<int>(ceil_div(p.cols, kBM)) * p.col_tiles;
+  p.stages = room / (2 * kABytes);
+  p.err = device_error_word();
+  p.wait_ns = wait_budget_ns();
+  return {p.tiles < most ? p.tiles : most, static_cast<size_t>(p.stages) * 2 * kABytes + 1024};
+}
+
 template <int kForm>
 int launch_few(const Maps& m, Params p, int64_t row_tiles, const FewPlan& plan, cudaStream_t stream) {
-  const Launch l = complete(&p, row_tiles, plan);
+  const Launch l = complete(&p, row_tiles, plan, kStageRoom);
   const auto kernel = few_kernel<kForm>;
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel), kStageRoom + 1024);
   if (e == cudaSuccess)
@@ -390,9 +559,17 @@ FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices,
   FewPlan best = {128, 1, 1e300};
   for (int i = outer ? 2 : 0; i < 4; ++i) {
     const int n = 16 << i;
-    if (n > 16 && n / 2 >= rows && !(outer && n == 64)) break;
+    if (n > 16 && n / 2 >= rows && !outer) break;
     for (int s = 1; s <= 8 && s <= kblocks; s *= 2) {
       if (splits && s != splits && !(or_one && s == 1)) continue;
+      if (outer && s == 1) {  // few_weights: a tile's steps, or its 32 KB written
+        if (n < 128) continue;
+        const double tiles = static_cast<double>(ceil_div(row_tiles * matrices * ceil_div(rows, n), kSms));
+        const double step = (tiles > 1 || splits ? 0.42 : 0.35) * static_cast<double>(kblocks);
+        const double us = 4.5 + tiles * (step > 1.2 ? step : 1.2);
+        if (us < best.us - 1e-9) best = {n, s, us};
+        continue;
+      }
       const int64_t ctas = row_tiles * matrices * ceil_div(rows, n) * s;
       if (s > 1 && ctas > 2 * kSms) break;
       const bool shared = ctas > kSms;
@@ -459,7 +636,7 @@ int set_up_outer(const Matrix* z, const Matrix& x, const Matrix* out, int count,
   Params& p = *to;
   p.rows = static_cast<int>(z[0].cols);
   p.cols = static_cast<int>(x.cols);
-  p.n = plan.n;
+  p.n = plan.splits > 1 ? plan.n : kBM;
   p.first_tiles = static_cast<int>(ceil_div(p.rows, p.n));
   p.col_tiles = count * p.first_tiles;
   p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(x.rows, kBK));
@@ -489,7 +666,15 @@ int launch_few_outer(const Matrix* z, const Matrix& x, const Matrix* out, int co
   Maps m = {};
   Params p = {};
   const int st = set_up_outer(z, x, out, count, plan, &m, &p);
-  return st != DLM_OK ? st : launch_few<kOuter>(m, p, ceil_div(p.cols, kBM), plan, stream);
+  if (st != DLM_OK) return st;
+  if (plan.splits > 1) return launch_few<kOuter>(m, p, ceil_div(p.cols, kBM), plan, stream);
+  // Six stages where a CTA has an SM to itself, three where two share one.
+  const bool alone = ceil_div(p.cols, kBM) * p.col_tiles <= 152;
+  const Launch l = complete_weights(&p, alone ? 6 * 2 * kABytes : kStageRoom, 2 * 152);
+  cudaError_t e = allow_smem(reinterpret_cast<const void*>(few_weights_kernel), 6 * 2 * kABytes + 1024);
+  if (e == cudaSuccess)
+    e = launch_overlapped(few_weights_kernel, dim3(static_cast<unsigned>(l.ctas)), kThreads, l.smem, stream, 1, true, m, p);
+  return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
 }
 
 int launch_few_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue& ep, const FewPlan& x_plan, const Matrix& x,
@@ -499,7 +684,12 @@ int launch_few_gradients(const Matrix* z, const Matrix* w, int count, const Epil
   int st;
   if ((st = set_up_cols(z, w, count, true, ep, x_plan, &xm, &xp)) != DLM_OK) return st;
   if ((st = set_up_outer(z, x, dw, count, w_plan, &wm, &wp)) != DLM_OK) return st;
-  const Launch xl = complete(&xp, ceil_div(xp.cols, kBM), x_plan), wl = complete(&wp, ceil_div(wp.cols, kBM), w_plan);
+  const int64_t x_tiles = ceil_div(xp.cols, kBM), w_tiles = ceil_div(wp.cols, kBM);
+  const int64_t all = x_tiles * xp.col_tiles * x_plan.splits +
+                      (w_plan.splits > 1 || w_tiles * wp.col_tiles < 152 ? w_tiles * wp.col_tiles * w_plan.splits : 152);
+  const int room = all <= 2 * 152 ? kStageRoom : kSharedRoom;
+  const Launch xl = complete(&xp, x_tiles, x_plan, room);
+  const Launch wl = w_plan.splits > 1 ? complete(&wp, w_tiles, w_plan, room) : complete_weights(&wp, room, 152);
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(few_gradients_kernel), kStageRoom + 1024);
   const int64_t s = xp.splits, ctas = xl.ctas + ceil_div(wl.ctas, s) * s;
   if (e == cudaSuccess)
