@@ -761,6 +761,14 @@ BiasSplit bias_split(int64_t N, int64_t m) {
   return {all > 64 ? ceil_div(all, ranks) : 1, ranks};
 }
 
+// Runs of rows where there are no sums: 128 rows a CTA, fewer where that leaves SMs empty.
+int64_t part_runs(int64_t N, int64_t m) {
+  int64_t rows = 128;
+  while (rows > 32 && ceil_div(N, rows) * ceil_div(m, 64) < 4 * 152) rows /= 2;
+  const int64_t runs = ceil_div(N, rows);
+  return runs < 1 << 15 ? runs : 1 << 15;
+}
+
 struct GradLayout {
   size_t dz, second, turned, sums, bytes;
 };
@@ -906,7 +914,7 @@ int launch_linear_grad(const LinearArgs& a, cudaStream_t stream) {
   Matrix dz = a.dout;
   int st;
   if (a.pre.data || a.dbias) {
-    const BiasSplit split = a.dbias ? bias_split(N, m) : BiasSplit{N < (int64_t{1} << 22) ? ceil_div(N, 128) : 1 << 15, 1};
+    const BiasSplit split = a.dbias ? bias_split(N, m) : BiasSplit{part_runs(N, m), 1};
     const int64_t rows = ceil_div(N, split.runs * split.ranks);
     float* sums = a.dbias && split.runs > 1 ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
     if (a.pre.data) dz = {ws + l.dz, N, m, m};
