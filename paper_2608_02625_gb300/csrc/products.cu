@@ -498,6 +498,7 @@ __global__ void __launch_bounds__(kPartThreads)
                        int64_t s_up, int act, int64_t rows, int vecs, uint4* dgate, uint4* dup) {
   constexpr int kLoads = 2;
   wait_for_previous();
+  launch_dependents();
   const int64_t total = rows * vecs, step = static_cast<int64_t>(gridDim.x) * kPartThreads;
   for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kPartThreads + threadIdx.x; i0 < total; i0 += kLoads * step) {
     uint4 v[kLoads][3] = {};
@@ -539,6 +540,7 @@ __global__ void __launch_bounds__(kPartThreads)
   constexpr int kLoads = 4, kLanes = kPartThreads / 8;  // rows at a time
   __shared__ float part[kLanes][64 + 1], total[64];
   wait_for_previous();
+  launch_dependents();
   const int lane = threadIdx.x & 7, row = threadIdx.x >> 3;
   const int ranks = static_cast<int>(cg::this_cluster().num_blocks()), rank = static_cast<int>(cg::this_cluster().block_rank());
   const int64_t strip = blockIdx.x / ranks, c = strip * 8 + lane, run = static_cast<int64_t>(blockIdx.y) * ranks + rank;
@@ -600,6 +602,7 @@ __global__ void __launch_bounds__(kPartThreads)
 // The sums of all runs, a thread a column.
 __global__ void __launch_bounds__(kPartThreads) bias_sum_kernel(const float* sums, int parts, int cols, void* out, int bf16) {
   wait_for_previous();
+  launch_dependents();
   const int col = blockIdx.x * kPartThreads + threadIdx.x;
   if (col >= cols) return;
   float s = 0.f;
@@ -617,6 +620,7 @@ __global__ void __launch_bounds__(kPartThreads)
     transpose_kernel(const __nv_bfloat16* x, int64_t stride, int64_t rows, int cols, int64_t pad, uint4* out) {
   __shared__ uint32_t tile[64][33];  // rows of 32 pairs of columns
   wait_for_previous();
+  launch_dependents();
   const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64;
   const int d0 = blockIdx.y * 64, r = threadIdx.x >> 3, v = threadIdx.x & 7;
 #pragma unroll
@@ -659,11 +663,7 @@ struct PairPlan {
   int bn;
   double us;
 };
-constexpr double kTurnUs = 1.5;     // the launch that transposes x for the weights' gradients
-// What one launch for two products saves, with weights up to this size: 64 x 1024 x 4096 13.9 -> 9.5 us, but
-// 64 x 8192 x 2048 (33 MB) 24.5 -> 35.8.
-constexpr double kOverlapUs = 3.0;
-constexpr int64_t kBothBytes = 20 << 20;
+constexpr double kTurnUs = 3.0;  // the launch that transposes x for the weights' gradients
 PairPlan plan_pairs(int64_t cols, int64_t row_tiles, int64_t kblocks, int workers, bool a_mn) {
   PairPlan best = {256, 1e300};
   for (int bn = 256; bn >= 128 && workers > 0; bn /= 2) {
@@ -820,22 +820,26 @@ int launch_rows(const Matrix* z, const Matrix& x, void* turned, const Matrix* ou
 int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue& ep, const Matrix& x, void* turned, const Matrix* dw,
                      cudaStream_t stream) {
   const int64_t x_tiles = ceil_div(x.cols, kBM), x_kblocks = count * ceil_div(z[0].cols, kBK), w_kblocks = ceil_div(x.rows, kBK);
-  // In one launch, or apart, where each runs as it is fastest: by the sizes alone, so that each has
-  // the same bits without the other.
+  // In one launch, or apart, whichever is fitted as faster, by the sizes alone, so that each has the
+  // same bits without the other. In one launch the longer one takes its time and the shorter one a
+  // quarter of its own; with weights up to 20 MB only (64 x 1024 x 4096: 13.9 -> 9.5 us, but
+  // 64 x 8192 x 2048, 33 MB: 24.5 -> 35.8, as the weights of dx then share the SMs with the stores of dw).
+  constexpr int64_t kMostBytes = 20 << 20;
   FewPlan fx = {}, fw = {};
   double both = 1e300;
   for (int s = 1; s <= 8; s *= 2) {
     const FewPlan a = plan_few(x.rows, x_tiles, x_kblocks, 1, false, s), b = plan_few(z[0].cols, x_tiles, w_kblocks, count, true, s, true);
-    if (a.us + b.us >= both) continue;
-    both = a.us + b.us;
+    const double us = a.us > b.us ? a.us + 0.25 * b.us : b.us + 0.25 * a.us;
+    if (us >= both) continue;
+    both = us;
     fx = a;
     fw = b;
   }
   const double pairs_x = plan_pairs(x.rows, ceil_div(x.cols, kRows), x_kblocks, pairs_of<kColsTurned>(), true).us;
   const double pairs_w = plan_pairs(x.cols, count * ceil_div(z[0].cols, kRows), w_kblocks, pairs_of<kRowsForm>(), true).us + kTurnUs;
   const double few_x = plan_few(x.rows, x_tiles, x_kblocks, 1, false).us, few_w = plan_few(z[0].cols, x_tiles, w_kblocks, count, true).us;
-  const bool small = count * z[0].cols * x.cols * 2 <= kBothBytes;
-  if (small && both - kOverlapUs < (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w)) {
+  const double apart = (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w) + 1.5;
+  if (count * z[0].cols * x.cols * 2 <= kMostBytes && both < apart) {
     if (ep.out && dw[0].data) return launch_few_gradients(z, w, count, ep, fx, x, dw, fw, stream);
     return ep.out ? launch_few_cols(z, w, count, true, ep, fx, stream) : dw[0].data ? launch_few_outer(z, x, dw, count, fw, stream) : DLM_OK;
   }

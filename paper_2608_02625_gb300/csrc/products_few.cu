@@ -564,9 +564,10 @@ FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices,
       if (splits && s != splits && !(or_one && s == 1)) continue;
       if (outer && s == 1) {  // few_weights: a tile's steps, or its 32 KB written
         if (n < 128) continue;
-        const double tiles = static_cast<double>(ceil_div(row_tiles * matrices * ceil_div(rows, n), kSms));
-        const double step = (tiles > 1 || splits ? 0.42 : 0.35) * static_cast<double>(kblocks);
-        const double us = 4.5 + tiles * (step > 1.2 ? step : 1.2);
+        const double tiles = static_cast<double>(ceil_div(row_tiles * matrices * ceil_div(rows, n), kSms)), k = static_cast<double>(kblocks);
+        // (six stages where a CTA has an SM to itself, three where it has not, two where both
+        // gradients share a launch)
+        const double steps = splits ? 0.7 * k : tiles > 1 ? 0.4 + 0.85 * k : 0.35 * k, us = 4.5 + tiles * (steps > 1.45 ? steps : 1.45);
         if (us < best.us - 1e-9) best = {n, s, us};
         continue;
       }
