@@ -72,6 +72,11 @@ int* device_error_word() {
   return g_err_addr[dev];
 }
 
+bool bind_context() {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess;
+}
+
 cudaError_t allow_smem(const void* kernel, int bytes) {
   static ClusterTable table;
   int dev = 0;

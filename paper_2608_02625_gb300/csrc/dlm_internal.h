@@ -14,6 +14,10 @@ namespace dlm {
 // Device address of the error word of the current device (set up once per device).
 int* device_error_word();
 
+// Makes the current device's context the calling host thread's. The runtime does so by itself with
+// a launch, but the driver's own calls (tensor maps) fail in a thread that has made none yet.
+bool bind_context();
+
 // Budget of each bounded wait in the pipelined kernels (ns): 2 s, which no
 // legitimate wait inside one launch approaches. Only DLM_CHECK_BOUNDS builds
 // can change it (dlm_checked_set_wait_budget), to make waits run out in tests.

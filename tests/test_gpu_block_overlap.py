@@ -1,5 +1,7 @@
 """The feed-forward block in a training step: chains of calls without waits between them, two
-streams, captured graphs that share a workspace, and the whole step against fp64 autograd."""
+streams, two threads, captured graphs that share a workspace, and the whole step against fp64 autograd."""
+import threading
+
 import pytest
 import torch
 
@@ -106,6 +108,35 @@ def test_two_streams_at_once(size):
     for g, w in zip(got, want):
         for a, b in zip(g, w):
             assert torch.equal(a, b)
+
+
+def test_two_threads_at_once():
+    """Each thread its own stream, its own step."""
+    size = SIZES[2]
+    want = [run(size, True, seed) for seed in (1, 2)]
+    steps = [Step(*size, seed) for seed in (1, 2)]
+    torch.cuda.synchronize()
+    got, wrong = [[], []], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream(dev())):
+                for _ in range(3):
+                    for call in steps[i].calls():
+                        call()
+                    got[i] += steps[i].seen()
+        except Exception as e:  # noqa: BLE001
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong and steps[0].B.device_error(clear=True) == 0
+    for g, w in zip(got, want):
+        assert len(g) == len(w) and all(torch.equal(a, b) for a, b in zip(g, w))
 
 
 def test_two_graphs_with_one_workspace():
