@@ -293,7 +293,7 @@ int dlm_refine_update_ranked(const dlm_tensor* tokens, const dlm_tensor* mask, c
  *   gate, up      the shape of out, BF16: what dlm_gated_linear_grad reads; or both NULL
  * d and f are multiples of 8 up to 2^20, N up to 2^28, N d and N f up to 2^40. Every base pointer
  * and row stride is a multiple of 16 bytes, strides below 2^40 bytes. No output may overlap
- * another tensor. bf16 products, fp32 sums; out is computed from the sums and rounded once,
+ * another tensor (column ranges of one buffer do not). bf16 products, fp32 sums; out is computed from the sums and rounded once,
  * gate and up are rounded on their own.
  */
 int dlm_gated_linear(const dlm_tensor* x, const dlm_tensor* w_gate, const dlm_tensor* w_up, int32_t act, dlm_tensor* out,

@@ -50,14 +50,33 @@ int check_vector(const dlm_tensor* t, const char* name, int dtype_mask, int64_t 
   return DLM_OK;
 }
 
+// Bytes between the rows of a tensor whose rows are evenly strided; 0 for a vector or a single row.
+int64_t row_pitch(const dlm_tensor* t) {
+  if (t->ndim < 2 || numel(t) <= t->shape[t->ndim - 1]) return 0;
+  return (t->ndim == 3 && t->shape[1] == 1 ? t->stride[0] : t->stride[t->ndim - 2]) * elem_size(t->dtype);
+}
+
+// As overlaps(), of tensors with evenly strided rows, but the rows of one may lie between those of
+// the other (column ranges of one buffer).
+bool rows_overlap(const dlm_tensor* a, const dlm_tensor* b) {
+  if (!overlaps(a, b)) return false;
+  const int64_t pitch = row_pitch(a);
+  if (pitch == 0 || pitch != row_pitch(b)) return true;
+  const auto width = [](const dlm_tensor* t) { return t->shape[t->ndim - 1] * elem_size(t->dtype); };
+  const intptr_t apart = static_cast<intptr_t>(reinterpret_cast<uintptr_t>(b->data) - reinterpret_cast<uintptr_t>(a->data));
+  const int64_t at = (apart % pitch + pitch) % pitch;  // where b's rows start in a's pitch
+  return at < width(a) || at + width(b) > pitch;
+}
+
 // No output may overlap an input or another output. Null descriptors are skipped.
-int check_disjoint(const dlm_tensor* const* outs, int n_outs, const dlm_tensor* const* ins, int n_ins) {
+int check_disjoint(const dlm_tensor* const* outs, int n_outs, const dlm_tensor* const* ins, int n_ins,
+                   bool (*overlap)(const dlm_tensor*, const dlm_tensor*) = overlaps) {
   for (int i = 0; i < n_outs; ++i) {
     if (!outs[i]) continue;
     for (int j = 0; j < n_ins; ++j)
-      if (ins[j] && overlaps(outs[i], ins[j])) return fail(DLM_ERR_ARG, "an output overlaps an input");
+      if (ins[j] && overlap(outs[i], ins[j])) return fail(DLM_ERR_ARG, "an output overlaps an input");
     for (int j = 0; j < i; ++j)
-      if (outs[j] && overlaps(outs[i], outs[j])) return fail(DLM_ERR_ARG, "outputs overlap each other");
+      if (outs[j] && overlap(outs[i], outs[j])) return fail(DLM_ERR_ARG, "outputs overlap each other");
   }
   return DLM_OK;
 }
@@ -238,7 +257,7 @@ int dlm_gated_linear(const dlm_tensor* x, const dlm_tensor* w_gate, const dlm_te
   if ((st = check_like(a.up, up, "up", x, a.w_gate.rows))) return st;
   const dlm_tensor* outs[3] = {out, gate, up};
   const dlm_tensor* ins[3] = {x, w_gate, w_up};
-  if ((st = check_disjoint(outs, 3, ins, 3))) return st;
+  if ((st = check_disjoint(outs, 3, ins, 3, rows_overlap))) return st;
   if (a.x.rows == 0) return DLM_OK;
   if ((st = require_error_word())) return st;
   a.act = act;
@@ -280,7 +299,7 @@ int dlm_gated_linear_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm
     return fail(DLM_ERR_SHAPE, "dw_gate and dw_up must have the shape of w_gate");
   const dlm_tensor* outs[3] = {dx, dw_gate, dw_up};
   const dlm_tensor* ins[7] = {dout, x, w_gate, w_up, gate, up, add && dx && same_view(add, dx) ? nullptr : add};
-  if ((st = check_disjoint(outs, 3, ins, 7))) return st;
+  if ((st = check_disjoint(outs, 3, ins, 7, rows_overlap))) return st;
   if (a.x.rows == 0) return (st = zero_matrix(a.dw_gate)) ? st : zero_matrix(a.dw_up);
   const dlm_tensor* all[10] = {dout, x, w_gate, w_up, gate, up, add, dx, dw_gate, dw_up};
   const size_t need = gated_grad_workspace_bytes(a.x.rows, a.w_gate.rows, a.x.cols);
@@ -317,8 +336,8 @@ int dlm_linear(const dlm_tensor* x, const dlm_tensor* weight, const dlm_tensor* 
   if ((st = check_like(m_pre, pre, "pre", x, a.w.rows))) return st;
   const dlm_tensor* outs[2] = {out, pre};
   const dlm_tensor* ins[4] = {x, weight, bias, nullptr};
-  if ((st = check_disjoint(outs, 2, ins, 4))) return st;
-  if (residual && ((!same_view(residual, out) && overlaps(residual, out)) || (pre && overlaps(residual, pre))))
+  if ((st = check_disjoint(outs, 2, ins, 4, rows_overlap))) return st;
+  if (residual && ((!same_view(residual, out) && rows_overlap(residual, out)) || (pre && rows_overlap(residual, pre))))
     return fail(DLM_ERR_ARG, "an output overlaps an input");
   if (a.x.rows == 0) return DLM_OK;
   const dlm_tensor* all[6] = {x, weight, bias, residual, out, pre};
@@ -361,7 +380,7 @@ int dlm_linear_grad(const dlm_tensor* dout, const dlm_tensor* x, const dlm_tenso
   if ((st = check_vector(dbias, "dbias", kMaskBF16F32, a.w.rows, true))) return st;
   const dlm_tensor* outs[3] = {dx, dweight, dbias};
   const dlm_tensor* ins[5] = {dout, x, weight, pre, add && dx && same_view(add, dx) ? nullptr : add};
-  if ((st = check_disjoint(outs, 3, ins, 5))) return st;
+  if ((st = check_disjoint(outs, 3, ins, 5, rows_overlap))) return st;
   if (a.x.rows == 0) {
     if ((st = zero_matrix(a.dw)) || !dbias) return st;
     const cudaError_t e = cudaMemsetAsync(dbias->data, 0, static_cast<size_t>(a.w.rows * elem_size(dbias->dtype)), current_stream());

@@ -36,6 +36,10 @@ GATED = {
     "up_misaligned": (dict(up=T(BF16, [6, 40], 6 * MB + 2)), -5),
     "act_unknown": (dict(act=3), -6), "act_negative": (dict(act=-1), -6), "out_on_x": (dict(out=b([6, 40], 1)), -6),
     "gate_on_out": (dict(gate=T(BF16, [6, 40], 4 * MB + 16)), -6), "up_on_wu": (dict(up=b([6, 40], 3)), -6),
+    "up_between_rows_too_wide": (dict(gate=b([6, 40], 5, [72, 1]), up=T(BF16, [6, 40], 5 * MB + 80, [72, 1])), -6),
+    "up_on_gates_ends": (dict(gate=b([6, 40], 5, [80, 1]), up=T(BF16, [6, 40], 5 * MB + 64, [80, 1])), -6),
+    "up_before_gate": (dict(gate=T(BF16, [6, 40], 5 * MB + 64, [80, 1]), up=b([6, 40], 5, [80, 1])), -6),
+    "other_pitch": (dict(gate=b([6, 40], 5, [96, 1]), up=T(BF16, [6, 40], 5 * MB + 80, [88, 1])), -6),
 }
 
 

@@ -165,6 +165,43 @@ def test_batches_and_strided_rows(L):
     assert not y[..., 0].any() and not y[..., 65:].any()
 
 
+@pytest.mark.parametrize("N", [1, 20, 300])
+def test_column_ranges_of_one_buffer(N):
+    """Tensors whose rows lie between each other's: the same bits as apart, and nothing else written."""
+    from paper_2608_02625_gb300 import binding as B
+    d, f = 136, 264
+    x, wg, wu = block(N, d, f)
+    e = lambda *s: torch.full(s, 7.0, dtype=BF, device=dev())  # noqa: E731
+    wide, apart = e(N, 3 * f + 16), [e(N, f) for _ in range(3)]
+    parts = [wide[:, i * (f + 8):i * (f + 8) + f] for i in range(3)]
+    for out, gate, up in (parts, apart):
+        B.dlm_gated_linear(x, wg, wu, 1, out, gate, up)
+    assert all(torch.equal(a, b) for a, b in zip(parts, apart))
+    assert bool((wide[:, f:f + 8] == 7).all()) and bool((wide[:, 2 * f + 8:2 * f + 16] == 7).all())
+    # weights beside their gradients, dx beside x
+    w = e(f, 4 * d)
+    ws, dws = (w[:, :d], w[:, d:2 * d]), (w[:, 2 * d:3 * d], w[:, 3 * d:])
+    for to, t in zip(ws, (wg, wu)):
+        to.copy_(t)
+    xs = e(N, 2 * d)
+    xs[:, :d].copy_(x)
+    dout = rand(N, f, seed=3)
+    dx, dw = e(N, d), [e(f, d) for _ in range(2)]
+    B.dlm_gated_linear_grad(dout, x, wg, wu, apart[1], apart[2], 1, x, dx, *dw, grad_ws(N, f, d))
+    B.dlm_gated_linear_grad(dout, xs[:, :d], *ws, parts[1], parts[2], 1, xs[:, :d], xs[:, d:], *dws, grad_ws(N, f, d))
+    assert torch.equal(xs[:, d:], dx) and torch.equal(xs[:, :d], x) and all(torch.equal(a, b) for a, b in zip(dws, dw))
+    assert torch.equal(ws[0], wg) and torch.equal(ws[1], wu)
+    # a projection's result and its pre beside the residual
+    for r in (parts, apart):
+        r[2].copy_(dout)
+        B.dlm_linear(x, wg, None, 2, r[2], r[0], r[1], linear_ws(N, f, d))
+    assert all(torch.equal(a, b) for a, b in zip(parts, apart)) and torch.equal(parts[2], dout)
+    B.dlm_linear_grad(dout, x, wg, apart[1], 2, None, dx, dw[0], None, linear_grad_ws(N, f, d))
+    B.dlm_linear_grad(dout, xs[:, :d], ws[0], parts[1], 2, None, xs[:, d:], dws[0], None, linear_grad_ws(N, f, d))
+    assert torch.equal(xs[:, d:], dx) and torch.equal(dws[0], dw[0]) and torch.equal(xs[:, :d], x)
+    no_error()
+
+
 @pytest.mark.parametrize("N", [5, 100, 400])
 def test_what_is_not_part_of_a_tensor_is_not_read(N):
     """NaN around every input: behind the last row and between rows."""
