@@ -439,8 +439,11 @@ class AdamwParams:
     max_norm: float = float("inf")
 
     def to_c(self) -> DlmAdamwParams:
-        for t, dtype in ((self.lr, torch.float32), (self.step, torch.int32), (self.norm, torch.float32)):
-            if t is not None and (t.dtype != dtype or not t.is_cuda or t.numel() != 1):
+        for name, dtype in (("lr", torch.float32), ("step", torch.int32), ("norm", torch.float32)):
+            t = getattr(self, name)
+            if t is None and name == "norm":
+                continue
+            if t is None or t.dtype != dtype or not t.is_cuda or t.numel() != 1:
                 raise ValueError("lr, step and norm must be one-element CUDA tensors (float32, int32, float32)")
         return DlmAdamwParams(float(self.beta1), float(self.beta2), float(self.eps), float(self.weight_decay),
                               float(self.max_norm), self.lr.data_ptr(), self.step.data_ptr(),

@@ -108,6 +108,15 @@ def test_the_binding_refuses_lists_of_other_lengths():
         B.dlm_adamw([1], None, [], [], [], None, None, B.AdamwParams(None, None))
 
 
+def test_the_binding_refuses_scalars_that_are_missing_or_on_the_host():
+    import torch
+
+    from paper_2608_02625_gb300 import binding as B
+    for lr, step in ((None, None), (torch.ones(1), None), (torch.ones(1), torch.ones(1, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            B.AdamwParams(lr, step).to_c()
+
+
 SRC = r"""
 #include <stddef.h>
 #include <stdio.h>
