@@ -822,14 +822,16 @@ int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue
   const int64_t x_tiles = ceil_div(x.cols, kBM), x_kblocks = count * ceil_div(z[0].cols, kBK), w_kblocks = ceil_div(x.rows, kBK);
   // In one launch, or apart, whichever is fitted as faster, by the sizes alone, so that each has the
   // same bits without the other. In one launch the longer one takes its time and the shorter one a
-  // quarter of its own; with weights up to 20 MB only (64 x 1024 x 4096: 13.9 -> 9.5 us, but
-  // 64 x 8192 x 2048, 33 MB: 24.5 -> 35.8, as the weights of dx then share the SMs with the stores of dw).
-  constexpr int64_t kMostBytes = 20 << 20;
+  // tenth of its own, where all CTAs run at once, two an SM (64 x 2048 x 8192 with a gate: 43.2 -> 35.5 us
+  // with 128 CTAs for dx; 256 x 2048 x 8192: 64.7 -> 48.1 with 128, 65.5 with 256), and few CTAs that read
+  // leave HBM to those that write (1 x 2048 x 8192: 34.3 us with 64 for dx, 40.0 with 128).
   FewPlan fx = {}, fw = {};
   double both = 1e300;
   for (int s = 1; s <= 8; s *= 2) {
     const FewPlan a = plan_few(x.rows, x_tiles, x_kblocks, 1, false, s), b = plan_few(z[0].cols, x_tiles, w_kblocks, count, true, s, true);
-    const double us = a.us > b.us ? a.us + 0.25 * b.us : b.us + 0.25 * a.us;
+    const int64_t x_ctas = x_tiles * ceil_div(x.rows, a.n) * s;
+    if (x_ctas + few_outer_ctas(z[0].cols, x_tiles, count, b) > 2 * 152) continue;
+    const double us = (a.us > b.us ? a.us + 0.1 * b.us : b.us + 0.1 * a.us) + 0.015 * static_cast<double>(x_ctas);
     if (us >= both) continue;
     both = us;
     fx = a;
@@ -838,8 +840,8 @@ int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue
   const double pairs_x = plan_pairs(x.rows, ceil_div(x.cols, kRows), x_kblocks, pairs_of<kColsTurned>(), true).us;
   const double pairs_w = plan_pairs(x.cols, count * ceil_div(z[0].cols, kRows), w_kblocks, pairs_of<kRowsForm>(), true).us + kTurnUs;
   const double few_x = plan_few(x.rows, x_tiles, x_kblocks, 1, false).us, few_w = plan_few(z[0].cols, x_tiles, w_kblocks, count, true).us;
-  const double apart = (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w) + 1.5;
-  if (count * z[0].cols * x.cols * 2 <= kMostBytes && both < apart) {
+  const double apart = (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w) + 3.0;
+  if (both < apart) {
     if (ep.out && dw[0].data) return launch_few_gradients(z, w, count, ep, fx, x, dw, fw, stream);
     return ep.out ? launch_few_cols(z, w, count, true, ep, fx, stream) : dw[0].data ? launch_few_outer(z, x, dw, count, fw, stream) : DLM_OK;
   }

@@ -16,6 +16,8 @@ struct FewPlan {
 // row_tiles: tiles across it; outer: both operands MN-major, tiles of whole 64s of rows. splits:
 // these alone (0: any), or one where that is allowed too.
 FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices, bool outer, int splits = 0, bool or_one = false);
+// The CTAs of launch_few_outer, those of the whole GPU at most where K is not split.
+int64_t few_outer_ctas(int64_t rows, int64_t row_tiles, int matrices, const FewPlan& plan);
 
 int launch_few_gated(const GatedArgs& a, const FewPlan& plan, cudaStream_t stream);
 // out = act(x w^T + bias) + residual (turned: w's columns instead of its rows; up to two runs of K).

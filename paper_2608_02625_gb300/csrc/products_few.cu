@@ -12,9 +12,11 @@
 //   turned  A the weight's columns (MN-major), B the rows of dz; K in up to two runs
 //   outer   dW = dz^T x: A the columns of x, B those of dz (both MN-major, as they lie)
 // Two CTAs an SM, more where K is short. Where dW's K is not split (few_weights), CTAs take one tile
-// after another and write it while the next one is computed: with a CTA for each tile 64 x 2048 x 8192
-// took 14 us for what is written in 8. Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, lets what
-// it has on its way land and goes on to the cluster's barriers with whatever it has.
+// after another and write it while the next one is computed.
+// HBM bounds it, behind some 3 us of launch, first loads and joins: one row against 33 MB of weights
+// (2048 x 8192) takes 8.9 us, 67 MB with a gate 14.8, where 4.9 and 9.9 are what reading them takes.
+// Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, lets what it has on its way
+// land and goes on to the cluster's barriers with whatever it has.
 #include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -37,9 +39,9 @@ constexpr int kBK = 64;                // K of a stage: 128 bytes of bf16
 constexpr int kThreads = 256;          // warp 0 TMA, warp 1 MMA; all of them the epilogue
 constexpr int kABytes = kBM * kBK * 2;
 constexpr int kBoxBytes = 64 * 128;    // an MN-major box: 64 K rows of 64 columns
+constexpr int kSms = 152;
 constexpr int kMaxStages = 6;
 constexpr int kStageRoom = 108 * 1024;  // of a CTA, so that two fit on an SM
-constexpr int kSharedRoom = 74 * 1024;  // three, where one launch computes both gradients in many CTAs
 
 enum Form { kGated, kCols, kTurned, kOuter };
 
@@ -66,7 +68,7 @@ struct Params {
   int splits, stages;
   int rows, cols;              // extents of the result
   int act, bias_bf16;
-  int wide;                    // rows of out, pre and residual are 16-byte aligned
+  int wide;                    // rows of out, pre and residual are 16-byte aligned; 2 (outer): of out 32-byte
   const void* bias;
   const __nv_bfloat16* residual;
   __nv_bfloat16* out[3];
@@ -330,7 +332,8 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
 
 // dW = dz^T x, 128 x 128 a tile, by `workers` CTAs. Not transposed: A is dz's columns, B those of x
 // (both MN-major), and the sums go from tensor memory to the result, a row of it a lane, under the next
-// tile's loads and MMAs (two accumulators).
+// tile's loads and MMAs (two accumulators). Stores of 32 bytes, whole sectors: 64 x 2048 x 8192 takes
+// 10.9 us (33 MB at 4.07 TB/s, the rate of plain writes: 8.2), with stores of 16 bytes 14.6.
 constexpr int kEpiWarp0 = 4;  // warps 4-7
 __device__ __forceinline__ void few_weights(const Maps& maps, const Params& p, int worker, int workers) {
   extern __shared__ uint8_t smem_raw[];
@@ -452,13 +455,20 @@ __device__ __forceinline__ void few_weights(const Maps& maps, const Params& p, i
         const int n = min(32, p.cols - tl.col - c);  // (a multiple of 8)
         if (row < p.rows && n > 0) {
           __nv_bfloat16* dst = p.out[tl.second] + row * p.s_out[tl.second] + tl.col + c;
+          uint32_t w[16];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (8 * k < n) {
-              const auto f = [&](int e) { return __uint_as_float(x[8 * k + e]); };
-              *reinterpret_cast<uint4*>(dst + 8 * k) =
-                  make_uint4(pack_bf16x2(f(0), f(1)), pack_bf16x2(f(2), f(3)), pack_bf16x2(f(4), f(5)), pack_bf16x2(f(6), f(7)));
-            }
+          for (int k = 0; k < 16; ++k) w[k] = pack_bf16x2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
+          if (p.wide == 2 && n == 32) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 16 * k), "r"(w[8 * k]), "r"(w[8 * k + 1]),
+                           "r"(w[8 * k + 2]), "r"(w[8 * k + 3]), "r"(w[8 * k + 4]), "r"(w[8 * k + 5]), "r"(w[8 * k + 6]), "r"(w[8 * k + 7])
+                           : "memory");
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (8 * k < n) *reinterpret_cast<uint4*>(dst + 8 * k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+          }
         }
         __syncwarp();
       }
@@ -482,8 +492,9 @@ __global__ void __launch_bounds__(kThreads, 3) few_kernel(const __grid_constant_
 }
 
 // Both gradients of a projection from dz: the first CTAs compute d x, those behind them dW. One
-// reads the weights, the other writes as much: at the same time they use HBM both ways.
-__global__ void __launch_bounds__(kThreads, 3)
+// reads the weights, the other writes as much: at the same time they use HBM both ways. 64 rows, 2048
+// x 8192 with a gate: 35.5 us (134 MB, 3.8 TB/s with the element-wise part's launch), 43.2 in two launches.
+__global__ void __launch_bounds__(kThreads, 2)
     few_gradients_kernel(const __grid_constant__ Maps x_maps, const Params x, const __grid_constant__ Maps w_maps, const Params w, int x_ctas,
                          int w_ctas) {
   const int block = static_cast<int>(blockIdx.x);
@@ -508,12 +519,12 @@ struct Launch {
   int64_t ctas;
   size_t smem;
 };
-Launch complete(Params* to, int64_t row_tiles, const FewPlan& plan, int room) {
+Launch complete(Params* to, int64_t row_tiles, const FewPlan& plan, int room, int most = kMaxStages) {
   Params& p = *to;
   p.splits = plan.splits;
   // No more stages than steps, but room for the sums: where K is short, three CTAs fit on an SM.
   const int stage = kABytes + p.n * 128, steps = static_cast<int>(ceil_div(p.kblocks, p.splits));
-  p.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
+  p.stages = room / stage < most ? room / stage : most;
   if (p.stages > steps) p.stages = steps;
   p.tmem_cols = p.n <= 32 ? 32 : p.n <= 64 ? 64 : 128;
   p.err = device_error_word();
@@ -549,12 +560,16 @@ int operand_map(CUtensorMap* map, const Matrix& x, int box_rows) {
 
 }  // namespace
 
+int64_t few_outer_ctas(int64_t rows, int64_t row_tiles, int matrices, const FewPlan& plan) {
+  const int64_t tiles = row_tiles * matrices * ceil_div(rows, plan.splits > 1 ? plan.n : kBM);
+  return plan.splits > 1 ? tiles * plan.splits : tiles < kSms ? tiles : kSms;
+}
+
 // Fitted to measured times (us): a launch, then for every round of two CTAs an SM the K steps
 // (more each where two CTAs share an SM) and the rows of the epilogue, which cost more where other
 // CTAs' sums are read (some 20 bytes a ns an SM from their shared memory); later rounds start with
 // what the first one has done under the launch before. With splits one round only.
 FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices, bool outer, int splits, bool or_one) {
-  constexpr int kSms = 152;
   constexpr double kStep[4] = {0.22, 0.225, 0.27, 0.35}, kShared[4] = {0.34, 0.36, 0.40, 0.50};  // n = 16, 32, 64, 128
   FewPlan best = {128, 1, 1e300};
   for (int i = outer ? 2 : 0; i < 4; ++i) {
@@ -562,12 +577,13 @@ FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices,
     if (n > 16 && n / 2 >= rows && !outer) break;
     for (int s = 1; s <= 8 && s <= kblocks; s *= 2) {
       if (splits && s != splits && !(or_one && s == 1)) continue;
-      if (outer && s == 1) {  // few_weights: a tile's steps, or its 32 KB written
+      if (outer && s == 1) {  // few_weights
         if (n < 128) continue;
-        const double tiles = static_cast<double>(ceil_div(row_tiles * matrices * ceil_div(rows, n), kSms)), k = static_cast<double>(kblocks);
-        // (six stages where a CTA has an SM to itself, three where it has not, two where both
-        // gradients share a launch)
-        const double steps = splits ? 0.7 * k : tiles > 1 ? 0.4 + 0.85 * k : 0.35 * k, us = 4.5 + tiles * (steps > 1.45 ? steps : 1.45);
+        const int64_t all = row_tiles * matrices * ceil_div(rows, n);
+        const double tiles = static_cast<double>(all), k = static_cast<double>(kblocks), round = 0.5 * k > 0.92 ? 0.5 * k : 0.92;
+        double us = 3.6 + 0.35 * k;                                        // an SM for each tile, six stages
+        if (all > kSms) us = 3.0 + (tiles > 304 ? tiles / 304 : 1) * (k > 2 ? 1.3 + 0.38 * k : 2.2);  // two CTAs an SM, three stages
+        if (splits) us = 4.5 + static_cast<double>(ceil_div(all, kSms)) * round;  // one an SM beside those of dx
         if (us < best.us - 1e-9) best = {n, s, us};
         continue;
       }
@@ -641,13 +657,15 @@ int set_up_outer(const Matrix* z, const Matrix& x, const Matrix* out, int count,
   p.first_tiles = static_cast<int>(ceil_div(p.rows, p.n));
   p.col_tiles = count * p.first_tiles;
   p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(x.rows, kBK));
-  p.wide = 1;
+  bool sectors = true;
   int st;
   for (int i = 0; i < count; ++i) {
     p.out[i] = static_cast<__nv_bfloat16*>(out[i].data);
     p.s_out[i] = out[i].stride;
+    sectors = sectors && reinterpret_cast<uintptr_t>(out[i].data) % 32 == 0 && out[i].stride % 16 == 0;
     if ((st = operand_map(&maps->b[i], z[i], 64)) != DLM_OK) return st;
   }
+  p.wide = sectors ? 2 : 1;
   return operand_map(&maps->a[0], x, 64);
 }
 
@@ -670,8 +688,8 @@ int launch_few_outer(const Matrix* z, const Matrix& x, const Matrix* out, int co
   if (st != DLM_OK) return st;
   if (plan.splits > 1) return launch_few<kOuter>(m, p, ceil_div(p.cols, kBM), plan, stream);
   // Six stages where a CTA has an SM to itself, three where two share one.
-  const bool alone = ceil_div(p.cols, kBM) * p.col_tiles <= 152;
-  const Launch l = complete_weights(&p, alone ? 6 * 2 * kABytes : kStageRoom, 2 * 152);
+  const bool alone = ceil_div(p.cols, kBM) * p.col_tiles <= kSms;
+  const Launch l = complete_weights(&p, alone ? 6 * 2 * kABytes : kStageRoom, 2 * kSms);
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(few_weights_kernel), 6 * 2 * kABytes + 1024);
   if (e == cudaSuccess)
     e = launch_overlapped(few_weights_kernel, dim3(static_cast<unsigned>(l.ctas)), kThreads, l.smem, stream, 1, true, m, p);
@@ -686,11 +704,9 @@ int launch_few_gradients(const Matrix* z, const Matrix* w, int count, const Epil
   if ((st = set_up_cols(z, w, count, true, ep, x_plan, &xm, &xp)) != DLM_OK) return st;
   if ((st = set_up_outer(z, x, dw, count, w_plan, &wm, &wp)) != DLM_OK) return st;
   const int64_t x_tiles = ceil_div(xp.cols, kBM), w_tiles = ceil_div(wp.cols, kBM);
-  const int64_t all = x_tiles * xp.col_tiles * x_plan.splits +
-                      (w_plan.splits > 1 || w_tiles * wp.col_tiles < 152 ? w_tiles * wp.col_tiles * w_plan.splits : 152);
-  const int room = all <= 2 * 152 ? kStageRoom : kSharedRoom;
-  const Launch xl = complete(&xp, x_tiles, x_plan, room);
-  const Launch wl = w_plan.splits > 1 ? complete(&wp, w_tiles, w_plan, room) : complete_weights(&wp, room, 152);
+  // (Four stages: with six of 16 rows what is read crowds out what is written: 40.2 us, not 37.7.)
+  const Launch xl = complete(&xp, x_tiles, x_plan, kStageRoom, 4);
+  const Launch wl = w_plan.splits > 1 ? complete(&wp, w_tiles, w_plan, kStageRoom) : complete_weights(&wp, kStageRoom, kSms);
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(few_gradients_kernel), kStageRoom + 1024);
   const int64_t s = xp.splits, ctas = xl.ctas + ceil_div(wl.ctas, s) * s;
   if (e == cudaSuccess)
