@@ -489,26 +489,39 @@ __device__ __forceinline__ uint4 row8(const __nv_bfloat16* base, int64_t row, in
   return *reinterpret_cast<const uint4*>(base + row * stride + 8 * vec);
 }
 
-// dg = dout u act'(g), du = dout act(g), rounded to bf16 for the tensor cores: each term of the
-// gradients is off by at most 2^-8 relative, as the results are by their own rounding. Two
-// vectors a thread in flight.
+// kGate: dg = dout u act'(g), du = dout act(g); else dg = dout act'(g). Rounded to bf16 for the tensor
+// cores: each term of the gradients is off by at most 2^-8 relative, as the results are by their own
+// rounding. Two vectors a thread in flight. HBM bounds it: 16384 x 8192 with a gate 207 us (1.34 GB,
+// 6.5 TB/s, 95 % of a copy), without one 123 (805 MB).
 constexpr int kPartThreads = 256;
+template <bool kGate>
 __global__ void __launch_bounds__(kPartThreads)
-    gated_parts_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* gate, const __nv_bfloat16* up, int64_t s_dout, int64_t s_gate,
-                       int64_t s_up, int act, int64_t rows, int vecs, uint4* dgate, uint4* dup) {
-  constexpr int kLoads = 2;
+    parts_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* gate, const __nv_bfloat16* up, int64_t s_dout, int64_t s_gate,
+                 int64_t s_up, int act, int64_t rows, int vecs, uint4* dgate, uint4* dup) {
+  constexpr int kLoads = kGate ? 2 : 3;
   wait_for_previous();
   launch_dependents();
+  // Row and place in it go on by steps, without a division for each vector.
   const int64_t total = rows * vecs, step = static_cast<int64_t>(gridDim.x) * kPartThreads;
-  for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kPartThreads + threadIdx.x; i0 < total; i0 += kLoads * step) {
-    uint4 v[kLoads][3] = {};
+  const unsigned start = blockIdx.x * kPartThreads + threadIdx.x, step_r = gridDim.x * kPartThreads / static_cast<unsigned>(vecs);
+  const int step_c = static_cast<int>(gridDim.x * kPartThreads - step_r * vecs);
+  int64_t r = start / static_cast<unsigned>(vecs);
+  int c = static_cast<int>(start % static_cast<unsigned>(vecs));
+  for (int64_t i0 = start; i0 < total; i0 += kLoads * step) {
+    uint4 v[kLoads][kGate ? 3 : 2] = {};
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
-      const int64_t i = i0 + k * step, r = i / vecs, c = i - r * vecs;
-      if (i >= total) continue;
-      v[k][0] = row8(dout, r, s_dout, c);
-      v[k][1] = row8(gate, r, s_gate, c);
-      v[k][2] = row8(up, r, s_up, c);
+      if (i0 + k * step < total) {
+        v[k][0] = row8(dout, r, s_dout, c);
+        v[k][1] = row8(gate, r, s_gate, c);
+        if constexpr (kGate) v[k][2] = row8(up, r, s_up, c);
+      }
+      r += step_r;
+      c += step_c;
+      if (c >= vecs) {
+        c -= vecs;
+        ++r;
+      }
     }
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
@@ -517,46 +530,52 @@ __global__ void __launch_bounds__(kPartThreads)
       float d[8], g[8], u[8];
       unpack8(v[k][0], d);
       unpack8(v[k][1], g);
-      unpack8(v[k][2], u);
+      if constexpr (kGate) unpack8(v[k][2], u);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float value, slope;
         activate_grad(act, g[e], &value, &slope);
-        g[e] = d[e] * u[e] * slope;
-        u[e] = d[e] * value;
+        if constexpr (kGate) {
+          g[e] = d[e] * u[e] * slope;
+          u[e] = d[e] * value;
+        } else {
+          g[e] = d[e] * slope;
+        }
       }
       dgate[i] = pack8(g);
-      dup[i] = pack8(u);
+      if constexpr (kGate) dup[i] = pack8(u);
     }
   }
 }
 
-// dz = dout act'(pre) (not written without an activation), and sums of its columns: 64 columns a
-// CTA, 32 rows at a time, four of them a thread in flight. The CTAs of a cluster share a run of rows,
-// whose sums its first one adds up in their order: to `sums`, or, where there is one run, to `dbias`.
-__global__ void __launch_bounds__(kPartThreads)
-    linear_parts_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* pre, int64_t s_dout, int64_t s_pre, int act, int64_t rows,
-                        int64_t rows_per_cta, int vecs, uint4* dz, float* sums, void* dbias, int bias_bf16) {
-  constexpr int kLoads = 4, kLanes = kPartThreads / 8;  // rows at a time
-  __shared__ float part[kLanes][64 + 1], total[64];
+// dz = dout act'(pre) (not written without an activation), and the sums of its columns: 8 kLanes
+// columns a CTA, 256 / kLanes rows at a time, four of them a thread in flight. The CTAs of a cluster
+// share a run of rows, whose sums its first one adds up in their order: to `sums`, or, where there is one
+// run, to `dbias`.
+template <int kLanes>
+__global__ void __launch_bounds__(kPartThreads, 4)
+    bias_parts_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* pre, int64_t s_dout, int64_t s_pre, int act, int64_t rows,
+                      int64_t rows_per_cta, int vecs, uint4* dz, float* sums, void* dbias, int bias_bf16) {
+  constexpr int kLoads = 4, kRowsOnce = kPartThreads / kLanes, kCols = 8 * kLanes;
+  __shared__ float part[kRowsOnce][kCols + 1], total[kCols];
   wait_for_previous();
   launch_dependents();
-  const int lane = threadIdx.x & 7, row = threadIdx.x >> 3;
+  const int lane = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
   const int ranks = static_cast<int>(cg::this_cluster().num_blocks()), rank = static_cast<int>(cg::this_cluster().block_rank());
-  const int64_t strip = blockIdx.x / ranks, c = strip * 8 + lane, run = static_cast<int64_t>(blockIdx.y) * ranks + rank;
+  const int64_t strip = blockIdx.x / ranks, c = strip * kLanes + lane, run = static_cast<int64_t>(blockIdx.y) * ranks + rank;
   const int64_t r0 = run * rows_per_cta, r1 = r0 + rows_per_cta < rows ? r0 + rows_per_cta : rows;
   float sum[8] = {};
-  for (int64_t r = r0 + row; r < r1 && c < vecs; r += kLoads * kLanes) {
+  for (int64_t r = r0 + row; r < r1 && c < vecs; r += kLoads * kRowsOnce) {
     uint4 d4[kLoads] = {}, z4[kLoads] = {};
 #pragma unroll
     for (int k = 0; k < kLoads; ++k)
-      if (r + k * kLanes < r1) {
-        d4[k] = row8(dout, r + k * kLanes, s_dout, c);
-        if (pre) z4[k] = row8(pre, r + k * kLanes, s_pre, c);
+      if (r + k * kRowsOnce < r1) {
+        d4[k] = row8(dout, r + k * kRowsOnce, s_dout, c);
+        if (pre) z4[k] = row8(pre, r + k * kRowsOnce, s_pre, c);
       }
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
-      if (r + k * kLanes >= r1) continue;
+      if (r + k * kRowsOnce >= r1) continue;
       float d[8];
       unpack8(d4[k], d);
       if (pre) {
@@ -568,25 +587,24 @@ __global__ void __launch_bounds__(kPartThreads)
           activate_grad(act, z[e], &value, &slope);
           d[e] *= slope;
         }
-        dz[(r + k * kLanes) * vecs + c] = pack8(d);
+        dz[(r + k * kRowsOnce) * vecs + c] = pack8(d);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += d[e];
     }
   }
-  if (!sums && !dbias) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) part[row][8 * lane + e] = sum[e];
   __syncthreads();
-  if (threadIdx.x < 64) {
+  if (threadIdx.x < kCols) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < kLanes; ++i) s += part[i][threadIdx.x];
+    for (int i = 0; i < kRowsOnce; ++i) s += part[i][threadIdx.x];
     total[threadIdx.x] = s;
   }
   cg::this_cluster().sync();
-  const int64_t cols = static_cast<int64_t>(vecs) * 8, col = strip * 64 + threadIdx.x;
-  if (rank == 0 && threadIdx.x < 64 && col < cols) {
+  const int64_t cols = static_cast<int64_t>(vecs) * 8, col = strip * kCols + threadIdx.x;
+  if (rank == 0 && threadIdx.x < kCols && col < cols) {
     float s = 0.f;
     for (int i = 0; i < ranks; ++i) s += *cg::this_cluster().map_shared_rank(total + threadIdx.x, i);
     if (sums)
@@ -748,25 +766,29 @@ size_t take(size_t* at, size_t bytes) {
 
 int64_t pad_rows(int64_t n) { return ceil_div(n, 64) * 64; }
 
-// How the rows are split for the sums of dz's columns: CTAs of a cluster, of 64 rows each or more,
-// and runs, whose sums are kept (one run needs no second launch): eight CTAs an SM in all.
+// How the sums of dz's columns are split: strips of 8 `lanes` columns; runs of rows, whose sums are kept
+// (one run needs no second launch); CTAs of a cluster that share a run. As many CTAs as run at once,
+// four an SM, with 64 rows each or more: with twice as many 16384 x 8192 took 159 us. Pieces of 512
+// bytes of a row instead of 128 pay where there is much to read, with clusters only to keep the runs few
+// (16384 x 8192: 132 us, 805 MB at 6.1 TB/s, against 152; 2048 x 2048: 9.8 against 8.4).
 struct BiasSplit {
+  int lanes;
   int64_t runs;
   int ranks;
 };
 BiasSplit bias_split(int64_t N, int64_t m) {
-  const int64_t want = ceil_div(8 * 152, ceil_div(m, 64)), most = ceil_div(N, 64), all = want < most ? want : most;
+  constexpr int64_t kCtas = 4 * 152, kMuch = 2048, kMostRuns = 64;
+  const int64_t most = ceil_div(N, 64);
   int ranks = 1;
+  if (ceil_div(m, 256) * most >= kMuch) {
+    int64_t all = kCtas / ceil_div(m, 256);
+    all = all < 1 ? 1 : all < most ? all : most;
+    while (ranks < 8 && all / ranks > kMostRuns) ranks *= 2;
+    return {32, all / ranks, ranks};
+  }
+  const int64_t want = ceil_div(kCtas, ceil_div(m, 64)), all = want < most ? want : most;
   while (ranks < 8 && ranks * 2 <= all) ranks *= 2;
-  return {all > 64 ? ceil_div(all, ranks) : 1, ranks};
-}
-
-// Runs of rows where there are no sums: 128 rows a CTA, fewer where that leaves SMs empty.
-int64_t part_runs(int64_t N, int64_t m) {
-  int64_t rows = 128;
-  while (rows > 32 && ceil_div(N, rows) * ceil_div(m, 64) < 4 * 152) rows /= 2;
-  const int64_t runs = ceil_div(N, rows);
-  return runs < 1 << 15 ? runs : 1 << 15;
+  return {8, all > 64 ? ceil_div(all, ranks) : 1, ranks};
 }
 
 struct GradLayout {
@@ -779,6 +801,17 @@ GradLayout grad_layout(int64_t N, int64_t m, int64_t d, int matrices) {
   l.turned = take(&l.bytes, static_cast<size_t>(d) * pad_rows(N) * 2);
   if (matrices == 1) l.sums = take(&l.bytes, static_cast<size_t>(bias_split(N, m).runs) * m * 4);
   return l;
+}
+
+// dgate and dup, or (kGate false, g the projection's pre) dgate alone.
+template <bool kGate>
+int launch_parts(const Matrix& dout, const Matrix& g, const Matrix& up, int act, void* dgate, void* dup, cudaStream_t stream) {
+  const int64_t ctas = ceil_div(g.rows * (g.cols / 8), kPartThreads), most = static_cast<int64_t>(sm_count()) * 8;
+  return launched(launch_overlapped(parts_kernel<kGate>, dim3(static_cast<unsigned>(ctas < most ? ctas : most)), kPartThreads, 0, stream, 1,
+                                    true, static_cast<const __nv_bfloat16*>(dout.data), static_cast<const __nv_bfloat16*>(g.data),
+                                    static_cast<const __nv_bfloat16*>(up.data), dout.stride, g.stride, up.stride, act, g.rows,
+                                    static_cast<int>(g.cols / 8), static_cast<uint4*>(dgate), static_cast<uint4*>(dup)),
+                  "gradient parts");
 }
 
 int launch_transpose(const Matrix& x, void* out, Matrix* turned, cudaStream_t stream) {
@@ -885,14 +918,7 @@ int launch_gated_grad(const GatedArgs& a, cudaStream_t stream) {
   const GradLayout l = grad_layout(N, f, d, 2);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   const Matrix dz[2] = {{ws + l.dz, N, f, f}, {ws + l.second, N, f, f}}, w[2] = {a.w_gate, a.w_up}, dw[2] = {a.dw_gate, a.dw_up};
-  const int64_t vecs = N * (f / 8), most = static_cast<int64_t>(sm_count()) * 8;
-  const int64_t ctas = ceil_div(vecs, kPartThreads);
-  int st = launched(launch_overlapped(gated_parts_kernel, dim3(static_cast<unsigned>(ctas < most ? ctas : most)), kPartThreads, 0, stream,
-                                      1, true, static_cast<const __nv_bfloat16*>(a.dout.data),
-                                      static_cast<const __nv_bfloat16*>(a.gate.data), static_cast<const __nv_bfloat16*>(a.up.data),
-                                      a.dout.stride, a.gate.stride, a.up.stride, a.act, N, static_cast<int>(f / 8),
-                                      static_cast<uint4*>(dz[0].data), static_cast<uint4*>(dz[1].data)),
-                    "gradient parts");
+  const int st = launch_parts<true>(a.dout, a.gate, a.up, a.act, dz[0].data, dz[1].data, stream);
   if (st != DLM_OK) return st;
   Epilogue ep = {};
   ep.residual = a.add;
@@ -919,16 +945,16 @@ int launch_linear_grad(const LinearArgs& a, cudaStream_t stream) {
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   Matrix dz = a.dout;
   int st;
-  if (a.pre.data || a.dbias) {
-    const BiasSplit split = a.dbias ? bias_split(N, m) : BiasSplit{part_runs(N, m), 1};
+  if (a.pre.data) dz = {ws + l.dz, N, m, m};
+  if (a.dbias) {
+    const BiasSplit split = bias_split(N, m);
     const int64_t rows = ceil_div(N, split.runs * split.ranks);
-    float* sums = a.dbias && split.runs > 1 ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
-    if (a.pre.data) dz = {ws + l.dz, N, m, m};
-    const dim3 grid(static_cast<unsigned>(ceil_div(m, 64) * split.ranks), static_cast<unsigned>(split.runs));
-    st = launched(launch_overlapped(linear_parts_kernel, grid, kPartThreads, 0, stream, split.ranks, true,
-                                    static_cast<const __nv_bfloat16*>(a.dout.data), static_cast<const __nv_bfloat16*>(a.pre.data),
-                                    a.dout.stride, a.pre.stride, a.ep.act, N, rows, static_cast<int>(m / 8),
-                                    reinterpret_cast<uint4*>(ws + l.dz), sums, a.dbias, a.ep.bias_bf16),
+    float* sums = split.runs > 1 ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
+    const dim3 grid(static_cast<unsigned>(ceil_div(m, 8 * split.lanes) * split.ranks), static_cast<unsigned>(split.runs));
+    st = launched(launch_overlapped(split.lanes == 32 ? bias_parts_kernel<32> : bias_parts_kernel<8>, grid, kPartThreads, 0, stream,
+                                    split.ranks, true, static_cast<const __nv_bfloat16*>(a.dout.data),
+                                    static_cast<const __nv_bfloat16*>(a.pre.data), a.dout.stride, a.pre.stride, a.ep.act, N, rows,
+                                    static_cast<int>(m / 8), reinterpret_cast<uint4*>(ws + l.dz), sums, a.dbias, a.ep.bias_bf16),
                   "gradient parts");
     if (st != DLM_OK) return st;
     if (sums) {
@@ -938,6 +964,8 @@ int launch_linear_grad(const LinearArgs& a, cudaStream_t stream) {
                     "bias gradient");
       if (st != DLM_OK) return st;
     }
+  } else if (a.pre.data) {
+    if ((st = launch_parts<false>(a.dout, a.pre, Matrix{}, a.ep.act, dz.data, nullptr, stream)) != DLM_OK) return st;
   }
   Epilogue ep = a.ep;  // of d x
   ep.act = DLM_ACT_NONE;
