@@ -856,15 +856,15 @@ int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue
   // In one launch, or apart, whichever is fitted as faster, by the sizes alone, so that each has the
   // same bits without the other. In one launch the longer one takes its time and the shorter one a
   // tenth of its own, where all CTAs run at once, two an SM (64 x 2048 x 8192 with a gate: 43.2 -> 35.5 us
-  // with 128 CTAs for dx; 256 x 2048 x 8192: 64.7 -> 48.1 with 128, 65.5 with 256), and few CTAs that read
-  // leave HBM to those that write (1 x 2048 x 8192: 34.3 us with 64 for dx, 40.0 with 128).
+  // with 128 CTAs for dx; 256 x 2048 x 8192: 64.7 -> 48.1 with 128, 65.5 with 256). CTAs that read cost
+  // those that write a little each.
   FewPlan fx = {}, fw = {};
   double both = 1e300;
   for (int s = 1; s <= 8; s *= 2) {
     const FewPlan a = plan_few(x.rows, x_tiles, x_kblocks, 1, false, s), b = plan_few(z[0].cols, x_tiles, w_kblocks, count, true, s, true);
     const int64_t x_ctas = x_tiles * ceil_div(x.rows, a.n) * s;
     if (x_ctas + few_outer_ctas(z[0].cols, x_tiles, count, b) > 2 * 152) continue;
-    const double us = (a.us > b.us ? a.us + 0.1 * b.us : b.us + 0.1 * a.us) + 0.015 * static_cast<double>(x_ctas);
+    const double us = (a.us > b.us ? a.us + 0.1 * b.us : b.us + 0.1 * a.us) + 0.01 * static_cast<double>(x_ctas);
     if (us >= both) continue;
     both = us;
     fx = a;

@@ -583,7 +583,7 @@ FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices,
         const double tiles = static_cast<double>(all), k = static_cast<double>(kblocks), round = 0.5 * k > 0.92 ? 0.5 * k : 0.92;
         double us = 3.6 + 0.35 * k;                                        // an SM for each tile, six stages
         if (all > kSms) us = 3.0 + (tiles > 304 ? tiles / 304 : 1) * (k > 2 ? 1.3 + 0.38 * k : 2.2);  // two CTAs an SM, three stages
-        if (splits) us = 4.5 + static_cast<double>(ceil_div(all, kSms)) * round;  // one an SM beside those of dx
+        if (splits) us = 3.5 + static_cast<double>(ceil_div(all, kSms)) * round;  // one an SM beside those of dx
         if (us < best.us - 1e-9) best = {n, s, us};
         continue;
       }
