@@ -18,6 +18,8 @@
 //          stores, residuals and biases are 32 columns of a row side by side, and need no
 //          alignment
 //   rows:  A is dz's columns (MN-major), B x transposed once, before, to K-major
+// The tensor pipe bounds it. 16384 rows, 2048 x 8192: gated (1.1 TFLOP) 631-645 us, cols 332-340, under
+// the power cap (1.62-1.74 PFLOP/s); a gated block's d x and dW 590 each in single launches (1.86).
 // Every wait is bounded; on expiry the kernel sets DLM_DEVERR_TIMEOUT, lets what it has on
 // its way land (in both CTAs) and exits.
 #include <cooperative_groups.h>
@@ -633,7 +635,7 @@ __global__ void __launch_bounds__(kPartThreads) bias_sum_kernel(const float* sum
 }
 
 // x [rows, cols] transposed, [cols, pad]: 64 x 64 a CTA (what lies behind the last row is left
-// as it is: the map of the result ends there).
+// as it is: the map of the result ends there). HBM bounds it: 16384 x 2048 21 us (134 MB, 6.3 TB/s).
 __global__ void __launch_bounds__(kPartThreads)
     transpose_kernel(const __nv_bfloat16* x, int64_t stride, int64_t rows, int cols, int64_t pad, uint4* out) {
   __shared__ uint32_t tile[64][33];  // rows of 32 pairs of columns
