@@ -43,21 +43,24 @@ __device__ __forceinline__ void activate_grad(int act, float x, float* value, fl
   *slope = p * fmaf(c * (1.f - p), ds, 1.f);
 }
 
-// Eight neighbouring columns of a row; wide: 16-byte aligned.
-__device__ __forceinline__ void load8(const __nv_bfloat16* src, bool wide, float (&x)[8]) {
-  if (wide) {
-    const uint4 u = *reinterpret_cast<const uint4*>(src);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      x[2 * k] = __uint_as_float(w[k] << 16);
-      x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = __bfloat162float(src[k]);
+  for (int k = 0; k < 4; ++k) {
+    x[2 * k] = __uint_as_float(w[k] << 16);
+    x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
   }
 }
+// Eight neighbouring columns of a row; wide: 16-byte aligned.
+__device__ __forceinline__ uint4 load8_raw(const __nv_bfloat16* src, bool wide) {
+  if (wide) return *reinterpret_cast<const uint4*>(src);
+  const unsigned short* h = reinterpret_cast<const unsigned short*>(src);
+  uint32_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = h[2 * k] | static_cast<uint32_t>(h[2 * k + 1]) << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* src, bool wide, float (&x)[8]) { unpack8(load8_raw(src, wide), x); }
 __device__ __forceinline__ void store8(__nv_bfloat16* dst, bool wide, const float (&x)[8]) {
   if (wide) {
     *reinterpret_cast<uint4*>(dst) =

@@ -315,14 +315,37 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     for (int t = worker; t < tiles; t += workers, ++tile) {
       const Tile tl = tile_of(p, t);
       const int acc = tile & 1;
+      const int m0 = tl.m * kRows + rank * kBM + qw * 32;  // of this warp's lanes
+      const int groups = (kForm == kGated ? p.bn / 2 : p.bn) / 64;
+      // cols: eight columns a lane, their biases, and the residuals of the next 32 rows, on their way
+      // while these are computed (loaded where they are added each waits for memory by itself: 2224 rows of
+      // 32 x 8192 took 74 us, not 38).
+      const int col = m0 + 8 * (lane & 3);
+      const bool on = col < p.cols;  // (a multiple of 8)
+      float bias[8] = {};
+      uint4 ahead[4] = {};
+      const auto fetch_residual = [&](int row0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t row = static_cast<int64_t>(row0) + 8 * k + (lane >> 2);
+          if (row < p.n && on) ahead[k] = load8_raw(p.residual + row * p.s_residual + col, p.wide);
+        }
+      };
+      if ((kForm == kCols || kForm == kColsTurned) && half < groups) {
+        if (p.residual) fetch_residual(tl.n * p.bn + 64 * half);
+        if (kForm == kCols && p.bias && on) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            bias[k] = p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[col + k])
+                                  : static_cast<const float*>(p.bias)[col + k];
+        }
+      }
       if (!warp_wait(&sm.acc_full[acc], (tile >> 1) & 1, abort, p.err, p.wait_ns)) {
         ok = false;
         break;
       }
       tc_fence_after();
       const uint32_t base = tmem + lane_base + acc * kMaxBN;
-      const int m0 = tl.m * kRows + rank * kBM + qw * 32;  // of this warp's lanes
-      const int groups = (kForm == kGated ? p.bn / 2 : p.bn) / 64;
       if (half >= groups) release(acc);
 #pragma unroll 1
       for (int g = half; g < groups; g += 2) {
@@ -381,18 +404,13 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           // 32 rows of the result at a time, of which the lanes hold a column each, turned in shared
           // memory: eight columns a lane of every eighth row (16-byte pieces swapped by the row, so
           // that neither side meets a bank twice).
-          const int col = m0 + 8 * (lane & 3);
-          const bool on = col < p.cols;  // (a multiple of 8)
-          float bias[8] = {};
-          if (kForm == kCols && p.bias && on) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              bias[k] = p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[col + k])
-                                    : static_cast<const float*>(p.bias)[col + k];
-          }
 #pragma unroll 1
           for (int c = 0; c < 2; ++c) {
             const int row0 = tl.n * p.bn + 64 * g + 32 * c;
+            uint4 extra[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) extra[k] = ahead[k];
+            if (p.residual && (c == 0 || !last)) fetch_residual(row0 + (c == 0 ? 32 : 96));
             uint32_t x[32];
             tmem_ld32(base + 64 * g + 32 * c, x);
             tmem_wait_ld(x);
@@ -404,12 +422,15 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             for (int pass = 0; pass < 4; ++pass) {
               const int e = 8 * pass + (lane >> 2);
               const int64_t row = row0 + e;
+              const uint4 mine = extra[0];
+#pragma unroll
+              for (int k = 0; k < 3; ++k) extra[k] = extra[k + 1];
               if (row >= p.n || !on) continue;
               const int piece = 2 * (lane & 3), swap = e & 7;
               const float4 lo = *reinterpret_cast<const float4*>(buf + e * 128 + ((piece ^ swap) << 4));
               const float4 hi = *reinterpret_cast<const float4*>(buf + e * 128 + (((piece + 1) ^ swap) << 4));
-              float z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, add[8] = {};
-              if (p.residual) load8(p.residual + row * p.s_residual + col, p.wide, add);
+              float z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, add[8];
+              unpack8(mine, add);
               if (kForm == kCols) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) z[k] += bias[k];
@@ -476,14 +497,6 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 
 // ---------------------------------------------------------------- gradients' element-wise parts
 
-__device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    x[2 * k] = __uint_as_float(w[k] << 16);
-    x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-  }
-}
 __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
@@ -678,17 +691,20 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Columns of a tile and the time as fitted to measurements (us): 256, or 128 where those leave pairs
 // without a tile or much of the last one empty. A K step takes 0.27 to 0.29 us, 0.205 of 128 columns
-// (0.245 with an MN-major A), a tile no less than its epilogue, which the last one adds.
+// (0.245 with an MN-major A), a tile no less than its epilogue, which the last one adds: those that are
+// turned in shared memory take longer.
 struct PairPlan {
   int bn;
   double us;
 };
 constexpr double kTurnUs = 3.0;  // the launch that transposes x for the weights' gradients
-PairPlan plan_pairs(int64_t cols, int64_t row_tiles, int64_t kblocks, int workers, bool a_mn) {
+PairPlan plan_pairs(Form form, int64_t cols, int64_t row_tiles, int64_t kblocks, int workers) {
+  const bool a_mn = form == kColsTurned || form == kRowsForm, turned = form == kCols || form == kColsTurned;
   PairPlan best = {256, 1e300};
   for (int bn = 256; bn >= 128 && workers > 0; bn /= 2) {
     const double rounds = static_cast<double>(ceil_div(ceil_div(cols, bn) * row_tiles, workers));
-    const double step = bn == 256 ? 0.28 : a_mn ? 0.245 : 0.205, epilogue = bn == 256 ? 2.4 : 1.5, k = static_cast<double>(kblocks) * step;
+    const double step = bn == 256 ? 0.28 : a_mn ? 0.245 : 0.205, k = static_cast<double>(kblocks) * step;
+    const double epilogue = bn == 256 ? (turned ? 4.0 : 2.4) : (turned ? 2.4 : 1.5);
     const double us = 3.2 + rounds * (k > epilogue ? k : epilogue) + epilogue;
     if (us < best.us - 1e-9) best = {bn, us};
   }
@@ -730,7 +746,7 @@ int launch_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const E
   const int64_t N = x[0].rows, M = turned ? w[0].cols : w[0].rows;
   const int64_t kblocks = ceil_div(x[0].cols, kBK);
   const int workers = turned ? pairs_of<kColsTurned>() : pairs_of<kCols>();
-  const PairPlan plan = plan_pairs(N, ceil_div(M, kRows), runs * kblocks, workers, turned);
+  const PairPlan plan = plan_pairs(turned ? kColsTurned : kCols, N, ceil_div(M, kRows), runs * kblocks, workers);
   const FewPlan few = plan_few(N, ceil_div(M, kBM), runs * kblocks, 1, false);
   if (few.us < plan.us) return launch_few_cols(x, w, runs, turned, ep, few, stream);
   Params p = {};
@@ -828,7 +844,7 @@ int launch_transpose(const Matrix& x, void* out, Matrix* turned, cudaStream_t st
 int launch_rows(const Matrix* z, const Matrix& x, void* turned, const Matrix* out, int count, cudaStream_t stream) {
   const int workers = pairs_of<kRowsForm>();
   const int64_t row_tiles = count * ceil_div(z[0].cols, kRows), kblocks = ceil_div(x.rows, kBK);
-  const PairPlan plan = plan_pairs(x.cols, row_tiles, kblocks, workers, true);
+  const PairPlan plan = plan_pairs(kRowsForm, x.cols, row_tiles, kblocks, workers);
   const FewPlan few = plan_few(z[0].cols, ceil_div(x.cols, kBM), kblocks, count, true);
   if (few.us < plan.us + kTurnUs) return launch_few_outer(z, x, out, count, few, stream);
   Matrix xt;
@@ -872,8 +888,8 @@ int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue
     fx = a;
     fw = b;
   }
-  const double pairs_x = plan_pairs(x.rows, ceil_div(x.cols, kRows), x_kblocks, pairs_of<kColsTurned>(), true).us;
-  const double pairs_w = plan_pairs(x.cols, count * ceil_div(z[0].cols, kRows), w_kblocks, pairs_of<kRowsForm>(), true).us + kTurnUs;
+  const double pairs_x = plan_pairs(kColsTurned, x.rows, ceil_div(x.cols, kRows), x_kblocks, pairs_of<kColsTurned>()).us;
+  const double pairs_w = plan_pairs(kRowsForm, x.cols, count * ceil_div(z[0].cols, kRows), w_kblocks, pairs_of<kRowsForm>()).us + kTurnUs;
   const double few_x = plan_few(x.rows, x_tiles, x_kblocks, 1, false).us, few_w = plan_few(z[0].cols, x_tiles, w_kblocks, count, true).us;
   const double apart = (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w) + 3.0;
   if (both < apart) {
@@ -890,7 +906,7 @@ int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue
 int launch_gated(const GatedArgs& a, cudaStream_t stream) {
   const int64_t f = a.w_gate.rows, row_tiles = ceil_div(a.x.rows, kRows), kblocks = ceil_div(a.x.cols, kBK);
   const int workers = pairs_of<kGated>();
-  const PairPlan plan = plan_pairs(2 * f, row_tiles, kblocks, workers, false);
+  const PairPlan plan = plan_pairs(kGated, 2 * f, row_tiles, kblocks, workers);
   const FewPlan few = plan_few(a.x.rows, ceil_div(f, 64), kblocks, 1, false);
   if (few.us < plan.us) return launch_few_gated(a, few, stream);
   Params p = {};

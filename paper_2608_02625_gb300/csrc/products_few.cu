@@ -40,8 +40,10 @@ constexpr int kThreads = 256;          // warp 0 TMA, warp 1 MMA; all of them th
 constexpr int kABytes = kBM * kBK * 2;
 constexpr int kBoxBytes = 64 * 128;    // an MN-major box: 64 K rows of 64 columns
 constexpr int kSms = 152;
-constexpr int kMaxStages = 6;
+constexpr int kClustered = 256;  // CTAs in clusters of four or eight that find room at once, two an SM
+constexpr int kMaxStages = 8;
 constexpr int kStageRoom = 108 * 1024;  // of a CTA, so that two fit on an SM
+constexpr int kAloneRoom = 192 * 1024;  // of a CTA with an SM to itself
 
 enum Form { kGated, kCols, kTurned, kOuter };
 
@@ -68,7 +70,7 @@ struct Params {
   int splits, stages;
   int rows, cols;              // extents of the result
   int act, bias_bf16;
-  int wide;                    // rows of out, pre and residual are 16-byte aligned; 2 (outer): of out 32-byte
+  int wide;                    // rows of out, pre and residual are 16-byte aligned
   const void* bias;
   const __nv_bfloat16* residual;
   __nv_bfloat16* out[3];
@@ -458,12 +460,18 @@ __device__ __forceinline__ void few_weights(const Maps& maps, const Params& p, i
           uint32_t w[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) w[k] = pack_bf16x2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
-          if (p.wide == 2 && n == 32) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 16 * k), "r"(w[8 * k]), "r"(w[8 * k + 1]),
-                           "r"(w[8 * k + 2]), "r"(w[8 * k + 3]), "r"(w[8 * k + 4]), "r"(w[8 * k + 5]), "r"(w[8 * k + 6]), "r"(w[8 * k + 7])
-                           : "memory");
+          const auto sector = [&](__nv_bfloat16* to, int k) {  // 16 columns from the (2 k)th on
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]),
+                         "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7])
+                         : "memory");
+          };
+          if (n == 32 && reinterpret_cast<uintptr_t>(dst) % 32 == 0) {
+            sector(dst, 0);
+            sector(dst + 16, 8);
+          } else if (n == 32) {  // 16 bytes behind a sector's start
+            *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+            sector(dst + 8, 4);
+            *reinterpret_cast<uint4*>(dst + 24) = make_uint4(w[12], w[13], w[14], w[15]);
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -546,9 +554,18 @@ Launch complete_weights(Params* to, int room, int most) {
 
 template <int kForm>
 int launch_few(const Maps& m, Params p, int64_t row_tiles, const FewPlan& plan, cudaStream_t stream) {
-  const Launch l = complete(&p, row_tiles, plan, kStageRoom);
   const auto kernel = few_kernel<kForm>;
-  cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel), kStageRoom + 1024);
+  cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel), kAloneRoom + 1024);
+  Launch l = complete(&p, row_tiles, plan, kStageRoom);
+  if (e == cudaSuccess && ceil_div(p.kblocks, p.splits) > p.stages) {
+    // A deeper ring where an SM for each CTA is to be had, clusters and all.
+    Params alone = p;
+    const Launch la = complete(&alone, row_tiles, plan, kAloneRoom);
+    if (la.ctas <= static_cast<int64_t>(p.splits) * active_clusters(reinterpret_cast<const void*>(kernel), p.splits, kThreads, la.smem)) {
+      p = alone;
+      l = la;
+    }
+  }
   if (e == cudaSuccess)
     e = launch_overlapped(kernel, dim3(static_cast<unsigned>(l.ctas)), kThreads, l.smem, stream, p.splits, true, m, p);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
@@ -588,10 +605,10 @@ FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices,
         continue;
       }
       const int64_t ctas = row_tiles * matrices * ceil_div(rows, n) * s;
-      if (s > 1 && ctas > 2 * kSms) break;
+      if (s > 1 && ctas > (s > 2 ? kClustered : 2 * kSms)) break;
       const bool shared = ctas > kSms;
       const double rounds = static_cast<double>(ceil_div(ctas, 2 * kSms)), steps = static_cast<double>(ceil_div(kblocks, s));
-      const double epilogue = s == 1 ? 0.012 * n : 0.5 + 0.03 * n * (shared ? 2 : 1);
+      const double join = 0.5 + 0.06 * s + (n == 128 && s == 8 ? 3.0 : 0.0), epilogue = s == 1 ? 0.012 * n : join + 0.03 * n * (shared ? 2 : 1);
       const double us = 3.0 + rounds * (steps * (shared ? kShared : kStep)[i] + epilogue) + 1.8 * (rounds - 1);
       if (us < best.us - 1e-9) best = {n, s, us};
     }
@@ -657,15 +674,13 @@ int set_up_outer(const Matrix* z, const Matrix& x, const Matrix* out, int count,
   p.first_tiles = static_cast<int>(ceil_div(p.rows, p.n));
   p.col_tiles = count * p.first_tiles;
   p.kblocks = p.first_kblocks = static_cast<int>(ceil_div(x.rows, kBK));
-  bool sectors = true;
+  p.wide = 1;
   int st;
   for (int i = 0; i < count; ++i) {
     p.out[i] = static_cast<__nv_bfloat16*>(out[i].data);
     p.s_out[i] = out[i].stride;
-    sectors = sectors && reinterpret_cast<uintptr_t>(out[i].data) % 32 == 0 && out[i].stride % 16 == 0;
     if ((st = operand_map(&maps->b[i], z[i], 64)) != DLM_OK) return st;
   }
-  p.wide = sectors ? 2 : 1;
   return operand_map(&maps->a[0], x, 64);
 }
 
@@ -689,8 +704,8 @@ int launch_few_outer(const Matrix* z, const Matrix& x, const Matrix* out, int co
   if (plan.splits > 1) return launch_few<kOuter>(m, p, ceil_div(p.cols, kBM), plan, stream);
   // Six stages where a CTA has an SM to itself, three where two share one.
   const bool alone = ceil_div(p.cols, kBM) * p.col_tiles <= kSms;
-  const Launch l = complete_weights(&p, alone ? 6 * 2 * kABytes : kStageRoom, 2 * kSms);
-  cudaError_t e = allow_smem(reinterpret_cast<const void*>(few_weights_kernel), 6 * 2 * kABytes + 1024);
+  const Launch l = complete_weights(&p, alone ? kAloneRoom : kStageRoom, 2 * kSms);
+  cudaError_t e = allow_smem(reinterpret_cast<const void*>(few_weights_kernel), kAloneRoom + 1024);
   if (e == cudaSuccess)
     e = launch_overlapped(few_weights_kernel, dim3(static_cast<unsigned>(l.ctas)), kThreads, l.smem, stream, 1, true, m, p);
   return e == cudaSuccess ? DLM_OK : fail(DLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
