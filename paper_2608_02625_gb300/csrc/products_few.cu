@@ -164,6 +164,23 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
   volatile int* abort = &bars.abort;
   wait_for_previous();
 
+  // This CTA's rows of the tile, eight columns a thread, and the residuals of a thread's next rows, on
+  // their way from the start.
+  const int valid = min(p.n, p.rows - n0);
+  const int c0 = static_cast<int>(static_cast<int64_t>(valid) * rank / p.splits);
+  const int c1 = static_cast<int>(static_cast<int64_t>(valid) * (rank + 1) / p.splits);
+  constexpr int kGroups = kForm == kGated ? 8 : 16;  // of eight columns
+  constexpr int kRowsOnce = kThreads / kGroups;
+  const int i = 8 * (threadIdx.x % kGroups), col = m0 + i, first = c0 + threadIdx.x / kGroups;
+  const bool adds = (kForm == kCols || kForm == kTurned) && p.residual && col < p.cols;  // (a multiple of 8)
+  constexpr int kAhead = 2;
+  uint4 ahead[kAhead] = {};
+  const auto residual_of = [&](int c) {
+    return adds && c < c1 ? load8_raw(p.residual + (static_cast<int64_t>(n0) + c) * p.s_residual + col, p.wide) : make_uint4(0, 0, 0, 0);
+  };
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) ahead[k] = residual_of(first + k * kRowsOnce);
+
   if (warp == 0) {
     // ================================================================ TMA producer
     Ring ring;
@@ -235,7 +252,6 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
   // [row of the tile][lane], over the stages, which nothing uses any more. (Rows are as many as
   // fill a load; what is behind the valid ones is not read.)
   const uint32_t sums = smem_u32(smem);
-  const int valid = min(p.n, p.rows - n0);  // rows of the result in this tile
   for (int c = (warp >> 2) * 32; c < valid; c += 64) {
     uint32_t x[32];
     tmem_ld32(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + c, x);
@@ -256,8 +272,6 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
 
   // ================================================================ epilogue: this CTA's rows
   // Eight columns a thread. (Two: 69 instructions for them, and 10000 cycles for 128 rows.)
-  const int c0 = static_cast<int>(static_cast<int64_t>(valid) * rank / p.splits);
-  const int c1 = static_cast<int>(static_cast<int64_t>(valid) * (rank + 1) / p.splits);
   // The cluster's rank of the first CTA of this tile (the cluster is larger than the splits where one
   // launch computes both gradients).
   const uint32_t first_rank = cg::this_cluster().block_rank() - static_cast<uint32_t>(rank);
@@ -284,8 +298,6 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
       z[4 * h + 3] = s.w;
     }
   };
-  constexpr int kGroups = kForm == kGated ? 8 : 16;  // of eight columns
-  const int i = 8 * (threadIdx.x % kGroups), col = m0 + i;
   if (col < p.cols) {  // (a multiple of 8)
     const bool wide = p.wide;
     float bias[8] = {};
@@ -296,10 +308,15 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
                               : static_cast<const float*>(p.bias)[col + k];
     }
 #pragma unroll 1
-    for (int c = c0 + threadIdx.x / kGroups; c < c1; c += kThreads / kGroups) {
+    for (int c = first; c < c1; c += kRowsOnce) {
       const int64_t row = static_cast<int64_t>(n0) + c;
-      float add[8] = {};
-      if ((kForm == kCols || kForm == kTurned) && p.residual) load8(p.residual + row * p.s_residual + col, wide, add);
+      float add[8];
+      if (kForm == kCols || kForm == kTurned) {
+        unpack8(ahead[0], add);
+#pragma unroll
+        for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
+        ahead[kAhead - 1] = residual_of(c + kAhead * kRowsOnce);
+      }
       float z[8];
       joined(sums + (c * kBM + i) * 4, z);
       if (kForm == kGated) {
