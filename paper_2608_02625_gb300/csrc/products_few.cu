@@ -605,6 +605,12 @@ int64_t few_outer_ctas(int64_t rows, int64_t row_tiles, int matrices, const FewP
 // what the first one has done under the launch before. With splits one round only.
 FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices, bool outer, int splits, bool or_one) {
   constexpr double kStep[4] = {0.22, 0.225, 0.27, 0.35}, kShared[4] = {0.34, 0.36, 0.40, 0.50};  // n = 16, 32, 64, 128
+  // Operands that L2 does not hold reach the SMs at some 12 TB/s in all, 32 KB a tile and K step of 128 x 128
+  // (7471 x 520 x 6832: dx 164 us, dW 186; planned without it as 112 and 84).
+  const double operands = static_cast<double>((outer ? matrices : 1) * rows + row_tiles * kBM) * static_cast<double>(kblocks) * kBK * 2;
+  const auto least = [&](int64_t tiles, int n) {
+    return operands < 80e6 ? 0.0 : 3.0 + static_cast<double>(tiles * kblocks) * (kABytes + n * kBK * 2) / 12e6;
+  };
   FewPlan best = {128, 1, 1e300};
   for (int i = outer ? 2 : 0; i < 4; ++i) {
     const int n = 16 << i;
@@ -618,6 +624,7 @@ FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices,
         double us = 3.6 + 0.35 * k;                                        // an SM for each tile, six stages
         if (all > kSms) us = 3.0 + (tiles > 304 ? tiles / 304 : 1) * (k > 2 ? 1.3 + 0.38 * k : 2.2);  // two CTAs an SM, three stages
         if (splits) us = 3.5 + static_cast<double>(ceil_div(all, kSms)) * round;  // one an SM beside those of dx
+        if (us < least(all, n)) us = least(all, n);
         if (us < best.us - 1e-9) best = {n, s, us};
         continue;
       }
@@ -626,7 +633,8 @@ FewPlan plan_few(int64_t rows, int64_t row_tiles, int64_t kblocks, int matrices,
       const bool shared = ctas > kSms;
       const double rounds = static_cast<double>(ceil_div(ctas, 2 * kSms)), steps = static_cast<double>(ceil_div(kblocks, s));
       const double join = 0.5 + 0.06 * s + (n == 128 && s == 8 ? 3.0 : 0.0), epilogue = s == 1 ? 0.012 * n : join + 0.03 * n * (shared ? 2 : 1);
-      const double us = 3.0 + rounds * (steps * (shared ? kShared : kStep)[i] + epilogue) + 1.8 * (rounds - 1);
+      double us = 3.0 + rounds * (steps * (shared ? kShared : kStep)[i] + epilogue) + 1.8 * (rounds - 1);
+      if (us < least(ctas / s, n)) us = least(ctas / s, n);
       if (us < best.us - 1e-9) best = {n, s, us};
     }
   }
