@@ -537,8 +537,9 @@ typedef struct dlm_adamw_params {
  * from 2^-6 of the scale up, 2^-10 of the scale below); a sqrt(v) above 0 is held as the
  * smallest code at least, so that no weight is divided by eps alone on the next step. The
  * step itself uses m and v before that rounding. With 8-bit states a v below fp32's normal range
- * counts as 0, and a block whose scale is below it is held as zeros. A NaN or an infinity in a gradient makes its weight NaN, and
- * where states are held in 8 bits those of its whole block.
+ * counts as 0, a block whose scale is below it is held as zeros, and an eps below 2^-100 is taken
+ * as that (so 0 / 0 is 0 there). A NaN or an infinity in a gradient makes its weight NaN, and where
+ * states are held in 8 bits those of its whole block.
  */
 int dlm_adamw(const dlm_tensor* params, const dlm_tensor* masters, const dlm_tensor* grads, const dlm_tensor* m,
               const dlm_tensor* v, const dlm_tensor* m_scales, const dlm_tensor* v_scales, int32_t count,

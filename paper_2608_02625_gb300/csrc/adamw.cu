@@ -7,7 +7,8 @@
 // One pass: a warp takes 256 elements, eight a lane, loads everything that belongs to
 // them, computes in fp32 (two elements an instruction) and stores. HBM bounds it: 213 M weights with
 // bf16 copies, bf16 gradients and 32-bit states 911 us (6.56 TB/s, 97 % of a copy), bf16 weights with
-// 8-bit states 323 us (6.64 TB/s, 98 %). 8-bit states are e4m3 codes of m and of sqrt(v) (whose range,
+// 8-bit states 330 us (6.5 TB/s, 96 %; 323 with an approximate square root held, of whose codes
+// half as many again lie on the wrong side of a border). 8-bit states are e4m3 codes of m and of sqrt(v) (whose range,
 // 2^17 within a block with half a step of 2^-4 over most of it, is twice that in powers of two of v), in
 // blocks of 256 elements with a scale of their own: the largest magnitude over 448. A block is a
 // warp's 256 elements, so a scale is a reduction over the warp. The step itself uses the new m and v
@@ -234,7 +235,7 @@ __device__ __forceinline__ void store_codes(uint8_t* dst, int lane, int n, const
   }
 }
 
-// sqrt(x), off by 2^-23 relative at most, and a / b, off by 2^-22. kFlush: what is below fp32's normal
+// sqrt(x), off by 2^-23 relative at most (quotients by 2^-22). kFlush: what is below fp32's normal
 // range counts as 0, which saves the instructions that scale it (8-bit states, which hold no more).
 template <bool kFlush>
 __device__ __forceinline__ float sqrt_approx(float x) {
@@ -245,15 +246,19 @@ __device__ __forceinline__ float sqrt_approx(float x) {
     asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-template <bool kFlush>
-__device__ __forceinline__ float quotient(float a, float b) {
-  if constexpr (kFlush) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
-    return a * y;
-  } else {
-    return __fdividef(a, b);
-  }
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float2 ffma2_flush(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.ftz.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
 }
 
 template <bool kEight, int kKind, typename G>
@@ -292,7 +297,16 @@ struct Block {
       vn[k] = fadd2(fmul2(v0, both(b.beta2)), fmul2(fmul2(x, x), both(b.rest2)));
       rn[k] = make_float2(sqrt_approx<kEight>(vn[k].x), sqrt_approx<kEight>(vn[k].y));
       const float2 d = ffma2(rn[k], both(s.root), both(b.eps));
-      const float2 change = make_float2(quotient<kEight>(mn[k].x, d.x), quotient<kEight>(mn[k].y, d.y));
+      float2 change;
+      if constexpr (kEight) {
+        // The reciprocal serves the square root too, which is a step of Newton's nearer behind: what is held
+        // is that of the rounded root (half a last place, where the approximation alone is off by one).
+        const float2 y = make_float2(rcp_approx(d.x), rcp_approx(d.y));
+        change = fmul2(mn[k], y);
+        rn[k] = ffma2_flush(ffma2_flush(fmul2(rn[k], both(-1.f)), rn[k], vn[k]), fmul2(y, both(0.5f * s.root)), rn[k]);
+      } else {
+        change = make_float2(__fdividef(mn[k].x, d.x), __fdividef(mn[k].y, d.y));
+      }
       pn[k] = ffma2(pair_of(p, k), both(s.keep), fmul2(change, both(-s.alpha)));
     }
     if (kKind == kMaster) store<kVec>(t.master + at, lane, n, pn);
@@ -463,6 +477,7 @@ int launch_tables(const AdamwArgs& a, cudaStream_t stream) {
   Table<kTensors> tab;
   tab.betas = {static_cast<float>(a.beta1), static_cast<float>(1.0 - a.beta1), static_cast<float>(a.beta2),
                static_cast<float>(1.0 - a.beta2), static_cast<float>(a.eps)};
+  if (kEight && tab.betas.eps < 0x1p-100f) tab.betas.eps = 0x1p-100f;  // no division by 0 reaches a state
   tab.log_beta1 = std::log(a.beta1);
   tab.log_beta2 = std::log(a.beta2);
   tab.decay = a.weight_decay;

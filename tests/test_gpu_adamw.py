@@ -184,6 +184,22 @@ def test_a_block_without_gradients_stays_zero():
     assert float(c.ms[0][1]) == 0.0 and float(c.vs[0][1]) == 0.0 and not c.m[0][256:512].any()
 
 
+def test_no_eps():
+    """eps 0: with 8-bit states an element that has had no gradient keeps its states of 0 and only
+    decays; those beside it step by lr."""
+    c = Case([600, 40], "f32", F32, True, t=1, zeros=True, weight_decay=0.5, lr=1e-2, eps=0.0)
+    for g in c.grads:
+        g[::2] = 0.0
+    p = [x.double().clone() for x in c.params]
+    c.run()
+    c.gd.check()
+    for i, g in enumerate(c.grads):
+        off = g == 0
+        assert not c.m[i][off].any() and not c.v[i][off].any() and bool((c.v[i][~off] > 0).all())
+        want = p[i] * (1 - 5e-3) - 1e-2 * g.double().sign()
+        assert float((c.params[i].double() - want).abs().max()) <= 64 * U32 * 0.2
+
+
 def test_small_second_moments():
     """Gradients 2^-30 of their block's largest: sqrt(v) falls below the codes, is held as the
     smallest one, and the next steps move those weights by no more than they should."""
