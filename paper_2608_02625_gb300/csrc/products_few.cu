@@ -578,7 +578,7 @@ int launch_few(const Maps& m, Params p, int64_t row_tiles, const FewPlan& plan, 
     // A deeper ring where an SM for each CTA is to be had, clusters and all.
     Params alone = p;
     const Launch la = complete(&alone, row_tiles, plan, kAloneRoom);
-    if (la.ctas <= static_cast<int64_t>(p.splits) * active_clusters(reinterpret_cast<const void*>(kernel), p.splits, kThreads, la.smem)) {
+    if (la.ctas <= static_cast<int64_t>(p.splits) * active_clusters(reinterpret_cast<const void*>(kernel), p.splits, kThreads, kAloneRoom + 1024)) {
       p = alone;
       l = la;
     }
