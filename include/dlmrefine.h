@@ -536,10 +536,12 @@ typedef struct dlm_adamw_params {
  * Arithmetic in fp32. 8-bit states round to the nearest code (half a step: 2^-4 relative
  * from 2^-6 of the scale up, 2^-10 of the scale below); a sqrt(v) above 0 is held as the
  * smallest code at least, so that no weight is divided by eps alone on the next step. The
- * step itself uses m and v before that rounding. With 8-bit states a v below fp32's normal range
- * counts as 0, a block whose scale is below it is held as zeros, and an eps below 2^-100 is taken
- * as that (so 0 / 0 is 0 there). A NaN or an infinity in a gradient makes its weight NaN, and where
- * states are held in 8 bits those of its whole block.
+ * step itself uses m and v before that rounding. With 8-bit states a block whose scale is below
+ * fp32's normal range is held as zeros, and an eps below 2^-74 / sqrt(1 - beta2^t) is taken as
+ * that: as much as fp32 may lose of a sqrt(v / (1 - beta2^t)), so that with eps 0 too a v that is
+ * lost moves its weight by no more than the v itself would, and 0 / 0 is 0. (32-bit states divide
+ * by what eps is.) A NaN or an infinity in a gradient makes its weight NaN, and where states are
+ * held in 8 bits those of its whole block.
  */
 int dlm_adamw(const dlm_tensor* params, const dlm_tensor* masters, const dlm_tensor* grads, const dlm_tensor* m,
               const dlm_tensor* v, const dlm_tensor* m_scales, const dlm_tensor* v_scales, int32_t count,

@@ -6,9 +6,9 @@
 //
 // One pass: a warp takes 256 elements, eight a lane, loads everything that belongs to
 // them, computes in fp32 (two elements an instruction) and stores. HBM bounds it: 213 M weights with
-// bf16 copies, bf16 gradients and 32-bit states 911 us (6.56 TB/s, 97 % of a copy), bf16 weights with
-// 8-bit states 330 us (6.5 TB/s, 96 %; 323 with an approximate square root held, of whose codes
-// half as many again lie on the wrong side of a border). 8-bit states are e4m3 codes of m and of sqrt(v) (whose range,
+// bf16 copies, bf16 gradients and 32-bit states 929 us (6.43 TB/s, 95 % of a copy), bf16 weights with
+// 8-bit states 342 us (6.28 TB/s, 93 %; 334 with a square root that flushes what is below the normal
+// range, which left such a v's m to be divided by eps alone). 8-bit states are e4m3 codes of m and of sqrt(v) (whose range,
 // 2^17 within a block with half a step of 2^-4 over most of it, is twice that in powers of two of v), in
 // blocks of 256 elements with a scale of their own: the largest magnitude over 448. A block is a
 // warp's 256 elements, so a scale is a reduction over the warp. The step itself uses the new m and v
@@ -54,7 +54,7 @@ struct Tensor {
 
 // The coefficients of m and v.
 struct Betas {
-  float beta1, rest1, beta2, rest2, eps;
+  float beta1, rest1, beta2, rest2;
 };
 
 template <int kTensors>
@@ -64,6 +64,7 @@ struct Table {
   int count, chunk;  // tensors, elements a chunk (a multiple of 2048)
   Betas betas;
   double log_beta1, log_beta2, decay, max_norm;
+  float eps;
   const float* lr;
   const int32_t* step;
   const float* norm;  // may be null
@@ -72,10 +73,10 @@ struct Table {
 
 // What the step's scalars come to.
 struct Step {
-  float clip, keep, alpha, root;  // c, 1 - lr wd, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  float clip, keep, alpha, root, eps;  // c, 1 - lr wd, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
 };
 
-template <typename Tab>
+template <bool kEight, typename Tab>
 __device__ Step step_of(const Tab& tab) {
   Step s;
   int t = *tab.step;
@@ -89,6 +90,10 @@ __device__ Step step_of(const Tab& tab) {
   s.keep = static_cast<float>(1.0 - static_cast<double>(lr) * tab.decay);
   s.alpha = lr / one1;
   s.root = 1.f / sqrtf(one2);
+  // With 8-bit states no m is divided by less than what its v may have lost: g^2, its product, the v held and
+  // theirs are rounded by up to 2^-150 each below the normal range, which is a root of up to 2^-74. So a v
+  // that is 0 for that moves its weight by no more than the v itself would, and 0 / 0 is 0.
+  s.eps = kEight ? fmaxf(tab.eps, 0x1p-74f * s.root) : tab.eps;
   s.clip = 1.f;
   if (tab.norm) {
     const double c = tab.max_norm / (static_cast<double>(*tab.norm) + 1e-6);
@@ -235,15 +240,11 @@ __device__ __forceinline__ void store_codes(uint8_t* dst, int lane, int n, const
   }
 }
 
-// sqrt(x), off by 2^-23 relative at most (quotients by 2^-22). kFlush: what is below fp32's normal
-// range counts as 0, which saves the instructions that scale it (8-bit states, which hold no more).
-template <bool kFlush>
+// sqrt(x), off by 2^-23 relative at most (quotients by 2^-22), below fp32's normal range too: a v flushed to
+// 0 there leaves m to be divided by eps alone.
 __device__ __forceinline__ float sqrt_approx(float x) {
   float y;
-  if constexpr (kFlush)
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  else
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -251,16 +252,6 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float2 ffma2_flush(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
-      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-      "fma.rn.ftz.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-
 template <bool kEight, int kKind, typename G>
 struct Block {
   using State = typename std::conditional<kEight, uint8_t, float>::type;
@@ -295,15 +286,16 @@ struct Block {
       }
       mn[k] = fadd2(fmul2(m0, both(b.beta1)), fmul2(x, both(b.rest1)));
       vn[k] = fadd2(fmul2(v0, both(b.beta2)), fmul2(fmul2(x, x), both(b.rest2)));
-      rn[k] = make_float2(sqrt_approx<kEight>(vn[k].x), sqrt_approx<kEight>(vn[k].y));
-      const float2 d = ffma2(rn[k], both(s.root), both(b.eps));
+      rn[k] = make_float2(sqrt_approx(vn[k].x), sqrt_approx(vn[k].y));
+      const float2 d = ffma2(rn[k], both(s.root), both(s.eps));
       float2 change;
       if constexpr (kEight) {
-        // The reciprocal serves the square root too, which is a step of Newton's nearer behind: what is held
-        // is that of the rounded root (half a last place, where the approximation alone is off by one).
+        // The reciprocal serves the square root too, for a step of Newton's: off by some half a last place then
+        // where eps is far below the corrected root, and, as the step is scaled by root r / (root r + eps),
+        // by the approximation's own last place where eps is far above it.
         const float2 y = make_float2(rcp_approx(d.x), rcp_approx(d.y));
         change = fmul2(mn[k], y);
-        rn[k] = ffma2_flush(ffma2_flush(fmul2(rn[k], both(-1.f)), rn[k], vn[k]), fmul2(y, both(0.5f * s.root)), rn[k]);
+        rn[k] = ffma2(ffma2(fmul2(rn[k], both(-1.f)), rn[k], vn[k]), fmul2(y, both(0.5f * s.root)), rn[k]);
       } else {
         change = make_float2(__fdividef(mn[k].x, d.x), __fdividef(mn[k].y, d.y));
       }
@@ -410,7 +402,7 @@ template <int kTensors, bool kEight>
 __global__ void __launch_bounds__(kThreads, kPerSm) adamw_kernel(const __grid_constant__ Table<kTensors> tab) {
   __shared__ Step shared;
   wait_for_previous();
-  if (threadIdx.x == 0) shared = step_of(tab);
+  if (threadIdx.x == 0) shared = step_of<kEight>(tab);
   __syncthreads();
   const Step s = shared;
   for (int64_t c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
@@ -476,8 +468,8 @@ int launch_tables(const AdamwArgs& a, cudaStream_t stream) {
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   Table<kTensors> tab;
   tab.betas = {static_cast<float>(a.beta1), static_cast<float>(1.0 - a.beta1), static_cast<float>(a.beta2),
-               static_cast<float>(1.0 - a.beta2), static_cast<float>(a.eps)};
-  if (kEight && tab.betas.eps < 0x1p-100f) tab.betas.eps = 0x1p-100f;  // no division by 0 reaches a state
+               static_cast<float>(1.0 - a.beta2)};
+  tab.eps = static_cast<float>(a.eps);
   tab.log_beta1 = std::log(a.beta1);
   tab.log_beta2 = std::log(a.beta2);
   tab.decay = a.weight_decay;
