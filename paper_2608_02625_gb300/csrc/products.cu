@@ -689,28 +689,6 @@ int sm_count() {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Columns of a tile and the time as fitted to measurements (us): 256, or 128 where those leave pairs
-// without a tile or much of the last one empty. A K step takes 0.27 to 0.29 us, 0.205 of 128 columns
-// (0.245 with an MN-major A), a tile no less than its epilogue, which the last one adds: those that are
-// turned in shared memory take longer.
-struct PairPlan {
-  int bn;
-  double us;
-};
-constexpr double kTurnUs = 3.0;  // the launch that transposes x for the weights' gradients
-PairPlan plan_pairs(Form form, int64_t cols, int64_t row_tiles, int64_t kblocks, int workers) {
-  const bool a_mn = form == kColsTurned || form == kRowsForm, turned = form == kCols || form == kColsTurned;
-  PairPlan best = {256, 1e300};
-  for (int bn = 256; bn >= 128 && workers > 0; bn /= 2) {
-    const double rounds = static_cast<double>(ceil_div(ceil_div(cols, bn) * row_tiles, workers));
-    const double step = bn == 256 ? 0.28 : a_mn ? 0.245 : 0.205, k = static_cast<double>(kblocks) * step;
-    const double epilogue = bn == 256 ? (turned ? 4.0 : 2.4) : (turned ? 2.4 : 1.5);
-    const double us = 3.2 + rounds * (k > epilogue ? k : epilogue) + epilogue;
-    if (us < best.us - 1e-9) best = {bn, us};
-  }
-  return best;
-}
-
 bool aligned(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
 
 template <int kForm>
@@ -746,9 +724,8 @@ int launch_cols(const Matrix* x, const Matrix* w, int runs, bool turned, const E
   const int64_t N = x[0].rows, M = turned ? w[0].cols : w[0].rows;
   const int64_t kblocks = ceil_div(x[0].cols, kBK);
   const int workers = turned ? pairs_of<kColsTurned>() : pairs_of<kCols>();
-  const PairPlan plan = plan_pairs(turned ? kColsTurned : kCols, N, ceil_div(M, kRows), runs * kblocks, workers);
-  const FewPlan few = plan_few(N, ceil_div(M, kBM), runs * kblocks, 1, false);
-  if (few.us < plan.us) return launch_few_cols(x, w, runs, turned, ep, few, stream);
+  const ProductPlan plan = plan_cols(N, M, runs * kblocks, turned, workers);
+  if (!plan.pairs) return launch_few_cols(x, w, runs, turned, ep, plan.few, stream);
   Params p = {};
   p.row_tiles = static_cast<int>(ceil_div(M, kRows));
   p.bn = plan.bn;
@@ -783,31 +760,6 @@ size_t take(size_t* at, size_t bytes) {
 }
 
 int64_t pad_rows(int64_t n) { return ceil_div(n, 64) * 64; }
-
-// How the sums of dz's columns are split: strips of 8 `lanes` columns; runs of rows, whose sums are kept
-// (one run needs no second launch); CTAs of a cluster that share a run. As many CTAs as run at once,
-// four an SM, with 64 rows each or more: with twice as many 16384 x 8192 took 159 us. Pieces of 512
-// bytes of a row instead of 128 pay where there is much to read, with clusters only to keep the runs few
-// (16384 x 8192: 132 us, 805 MB at 6.1 TB/s, against 152; 2048 x 2048: 9.8 against 8.4).
-struct BiasSplit {
-  int lanes;
-  int64_t runs;
-  int ranks;
-};
-BiasSplit bias_split(int64_t N, int64_t m) {
-  constexpr int64_t kCtas = 4 * 152, kMuch = 2048, kMostRuns = 64;
-  const int64_t most = ceil_div(N, 64);
-  int ranks = 1;
-  if (ceil_div(m, 256) * most >= kMuch) {
-    int64_t all = kCtas / ceil_div(m, 256);
-    all = all < 1 ? 1 : all < most ? all : most;
-    while (ranks < 8 && all / ranks > kMostRuns) ranks *= 2;
-    return {32, all / ranks, ranks};
-  }
-  const int64_t want = ceil_div(kCtas, ceil_div(m, 64)), all = want < most ? want : most;
-  while (ranks < 8 && ranks * 2 <= all) ranks *= 2;
-  return {8, all > 64 ? ceil_div(all, ranks) : 1, ranks};
-}
 
 struct GradLayout {
   size_t dz, second, turned, sums, bytes;
@@ -844,9 +796,8 @@ int launch_transpose(const Matrix& x, void* out, Matrix* turned, cudaStream_t st
 int launch_rows(const Matrix* z, const Matrix& x, void* turned, const Matrix* out, int count, cudaStream_t stream) {
   const int workers = pairs_of<kRowsForm>();
   const int64_t row_tiles = count * ceil_div(z[0].cols, kRows), kblocks = ceil_div(x.rows, kBK);
-  const PairPlan plan = plan_pairs(kRowsForm, x.cols, row_tiles, kblocks, workers);
-  const FewPlan few = plan_few(z[0].cols, ceil_div(x.cols, kBM), kblocks, count, true);
-  if (few.us < plan.us + kTurnUs) return launch_few_outer(z, x, out, count, few, stream);
+  const ProductPlan plan = plan_rows(z[0].cols, x.cols, kblocks, count, workers);
+  if (!plan.pairs) return launch_few_outer(z, x, out, count, plan.few, stream);
   Matrix xt;
   int st;
   if ((st = launch_transpose(x, turned, &xt, stream)) != DLM_OK) return st;
@@ -870,31 +821,11 @@ int launch_rows(const Matrix* z, const Matrix& x, void* turned, const Matrix* ou
 // dx = sum z[i] w[i] + what ep adds (none without ep.out), dw[i] = z[i]^T x (none without data).
 int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue& ep, const Matrix& x, void* turned, const Matrix* dw,
                      cudaStream_t stream) {
-  const int64_t x_tiles = ceil_div(x.cols, kBM), x_kblocks = count * ceil_div(z[0].cols, kBK), w_kblocks = ceil_div(x.rows, kBK);
-  // In one launch, or apart, whichever is fitted as faster, by the sizes alone, so that each has the
-  // same bits without the other. In one launch the longer one takes its time and the shorter one a
-  // tenth of its own, where all CTAs run at once, two an SM (64 x 2048 x 8192 with a gate: 43.2 -> 35.5 us
-  // with 128 CTAs for dx; 256 x 2048 x 8192: 64.7 -> 48.1 with 128, 65.5 with 256). CTAs that read cost
-  // those that write a little each.
-  FewPlan fx = {}, fw = {};
-  double both = 1e300;
-  for (int s = 1; s <= 8; s *= 2) {
-    const FewPlan a = plan_few(x.rows, x_tiles, x_kblocks, 1, false, s), b = plan_few(z[0].cols, x_tiles, w_kblocks, count, true, s, true);
-    const int64_t x_ctas = x_tiles * ceil_div(x.rows, a.n) * s;
-    if (x_ctas + few_outer_ctas(z[0].cols, x_tiles, count, b) > 2 * 152) continue;
-    const double us = (a.us > b.us ? a.us + 0.1 * b.us : b.us + 0.1 * a.us) + 0.01 * static_cast<double>(x_ctas);
-    if (us >= both) continue;
-    both = us;
-    fx = a;
-    fw = b;
-  }
-  const double pairs_x = plan_pairs(kColsTurned, x.rows, ceil_div(x.cols, kRows), x_kblocks, pairs_of<kColsTurned>()).us;
-  const double pairs_w = plan_pairs(kRowsForm, x.cols, count * ceil_div(z[0].cols, kRows), w_kblocks, pairs_of<kRowsForm>()).us + kTurnUs;
-  const double few_x = plan_few(x.rows, x_tiles, x_kblocks, 1, false).us, few_w = plan_few(z[0].cols, x_tiles, w_kblocks, count, true).us;
-  const double apart = (few_x < pairs_x ? few_x : pairs_x) + (few_w < pairs_w ? few_w : pairs_w) + 3.0;
-  if (both < apart) {
-    if (ep.out && dw[0].data) return launch_few_gradients(z, w, count, ep, fx, x, dw, fw, stream);
-    return ep.out ? launch_few_cols(z, w, count, true, ep, fx, stream) : dw[0].data ? launch_few_outer(z, x, dw, count, fw, stream) : DLM_OK;
+  const GradientsPlan plan = plan_gradients(x.rows, z[0].cols, x.cols, count, pairs_of<kColsTurned>(), pairs_of<kRowsForm>());
+  if (plan.together) {
+    if (ep.out && dw[0].data) return launch_few_gradients(z, w, count, ep, plan.x.few, x, dw, plan.w.few, stream);
+    return ep.out ? launch_few_cols(z, w, count, true, ep, plan.x.few, stream)
+                  : dw[0].data ? launch_few_outer(z, x, dw, count, plan.w.few, stream) : DLM_OK;
   }
   int st;
   if (ep.out && (st = launch_cols(z, w, count, true, ep, stream)) != DLM_OK) return st;
@@ -903,12 +834,110 @@ int launch_gradients(const Matrix* z, const Matrix* w, int count, const Epilogue
 
 }  // namespace
 
+// ---------------------------------------------------------------- which form a call takes
+
+namespace {
+
+// Columns of a tile and the time as fitted to measurements (us): 256, or 128 where those leave pairs
+// without a tile or much of the last one empty. A K step takes 0.27 to 0.29 us, 0.205 of 128 columns
+// (0.245 with an MN-major A), a tile no less than its epilogue, which the last one adds: those that are
+// turned in shared memory take longer.
+struct PairPlan {
+  int bn;
+  double us;
+};
+constexpr double kTurnUs = 3.0;  // the launch that transposes x for the weights' gradients
+PairPlan plan_pairs(Form form, int64_t cols, int64_t row_tiles, int64_t kblocks, int workers) {
+  const bool a_mn = form == kColsTurned || form == kRowsForm, turned = form == kCols || form == kColsTurned;
+  PairPlan best = {256, 1e300};
+  for (int bn = 256; bn >= 128 && workers > 0; bn /= 2) {
+    const double rounds = static_cast<double>(ceil_div(ceil_div(cols, bn) * row_tiles, workers));
+    const double step = bn == 256 ? 0.28 : a_mn ? 0.245 : 0.205, k = static_cast<double>(kblocks) * step;
+    const double epilogue = bn == 256 ? (turned ? 4.0 : 2.4) : (turned ? 2.4 : 1.5);
+    const double us = 3.2 + rounds * (k > epilogue ? k : epilogue) + epilogue;
+    if (us < best.us - 1e-9) best = {bn, us};
+  }
+  return best;
+}
+
+ProductPlan faster(const PairPlan& pairs, double extra, const FewPlan& few) {
+  const bool some = few.us < pairs.us + extra;
+  return {!some, pairs.bn, few, some ? few.us : pairs.us + extra};
+}
+
+}  // namespace
+
+ProductPairs product_pairs() { return {pairs_of<kGated>(), pairs_of<kCols>(), pairs_of<kColsTurned>(), pairs_of<kRowsForm>()}; }
+
+ProductPlan plan_gated(int64_t N, int64_t f, int64_t kblocks, int workers) {
+  return faster(plan_pairs(kGated, 2 * f, ceil_div(N, kRows), kblocks, workers), 0.0, plan_few(N, ceil_div(f, 64), kblocks, 1, false));
+}
+
+ProductPlan plan_cols(int64_t N, int64_t M, int64_t kblocks, bool turned, int workers) {
+  return faster(plan_pairs(turned ? kColsTurned : kCols, N, ceil_div(M, kRows), kblocks, workers), 0.0,
+                plan_few(N, ceil_div(M, kBM), kblocks, 1, false));
+}
+
+ProductPlan plan_rows(int64_t M, int64_t d, int64_t kblocks, int count, int workers) {
+  return faster(plan_pairs(kRowsForm, d, count * ceil_div(M, kRows), kblocks, workers), kTurnUs,
+                plan_few(M, ceil_div(d, kBM), kblocks, count, true));
+}
+
+GradientsPlan plan_gradients(int64_t N, int64_t m, int64_t d, int count, int x_workers, int w_workers) {
+  const int64_t x_tiles = ceil_div(d, kBM), x_kblocks = count * ceil_div(m, kBK), w_kblocks = ceil_div(N, kBK);
+  // In one launch, or apart, whichever is fitted as faster, by the sizes alone, so that each has the
+  // same bits without the other. In one launch the longer one takes its time and the shorter one a
+  // tenth of its own, where all CTAs run at once, two an SM (64 x 2048 x 8192 with a gate: 43.2 -> 35.5 us
+  // with 128 CTAs for dx; 256 x 2048 x 8192: 64.7 -> 48.1 with 128, 65.5 with 256). CTAs that read cost
+  // those that write a little each.
+  GradientsPlan plan = {};
+  FewPlan fx = {}, fw = {};
+  double both = 1e300;
+  for (int s = 1; s <= 8; s *= 2) {
+    const FewPlan a = plan_few(N, x_tiles, x_kblocks, 1, false, s), b = plan_few(m, x_tiles, w_kblocks, count, true, s, true);
+    const int64_t x_ctas = x_tiles * ceil_div(N, a.n) * s;
+    if (x_ctas + few_outer_ctas(m, x_tiles, count, b) > 2 * 152) continue;
+    const double us = (a.us > b.us ? a.us + 0.1 * b.us : b.us + 0.1 * a.us) + 0.01 * static_cast<double>(x_ctas);
+    if (us >= both) continue;
+    both = us;
+    fx = a;
+    fw = b;
+  }
+  plan.x = plan_cols(N, d, x_kblocks, true, x_workers);
+  plan.w = plan_rows(m, d, w_kblocks, count, w_workers);
+  plan.together = both < plan.x.us + plan.w.us + 3.0;
+  if (plan.together) {
+    plan.x = {false, 0, fx, fx.us};
+    plan.w = {false, 0, fw, fw.us};
+  }
+  return plan;
+}
+
+// How the sums of dz's columns are split: strips of 8 `lanes` columns; runs of rows, whose sums are kept
+// (one run needs no second launch); CTAs of a cluster that share a run. As many CTAs as run at once,
+// four an SM, with 64 rows each or more: with twice as many 16384 x 8192 took 159 us. Pieces of 512
+// bytes of a row instead of 128 pay where there is much to read, with clusters only to keep the runs few
+// (16384 x 8192: 132 us, 805 MB at 6.1 TB/s, against 152; 2048 x 2048: 9.8 against 8.4).
+BiasSplit bias_split(int64_t N, int64_t m) {
+  constexpr int64_t kCtas = 4 * 152, kMuch = 2048, kManyRuns = 64;  // (608 CTAs in clusters of eight: 76 runs at most)
+  const int64_t most = ceil_div(N, 64);
+  int ranks = 1;
+  if (ceil_div(m, 256) * most >= kMuch) {
+    int64_t all = kCtas / ceil_div(m, 256);
+    all = all < 1 ? 1 : all < most ? all : most;
+    while (ranks < 8 && all / ranks > kManyRuns) ranks *= 2;
+    return {32, all / ranks, ranks};
+  }
+  const int64_t want = ceil_div(kCtas, ceil_div(m, 64)), all = want < most ? want : most;
+  while (ranks < 8 && ranks * 2 <= all) ranks *= 2;
+  return {8, all > 64 ? ceil_div(all, ranks) : 1, ranks};
+}
+
 int launch_gated(const GatedArgs& a, cudaStream_t stream) {
   const int64_t f = a.w_gate.rows, row_tiles = ceil_div(a.x.rows, kRows), kblocks = ceil_div(a.x.cols, kBK);
   const int workers = pairs_of<kGated>();
-  const PairPlan plan = plan_pairs(kGated, 2 * f, row_tiles, kblocks, workers);
-  const FewPlan few = plan_few(a.x.rows, ceil_div(f, 64), kblocks, 1, false);
-  if (few.us < plan.us) return launch_few_gated(a, few, stream);
+  const ProductPlan plan = plan_gated(a.x.rows, f, kblocks, workers);
+  if (!plan.pairs) return launch_few_gated(a, plan.few, stream);
   Params p = {};
   p.row_tiles = static_cast<int>(row_tiles);
   p.bn = plan.bn;
