@@ -20,9 +20,10 @@ extern "C" {
  * DLM_DEVERR_TIMEOUT, lets the copies and MMAs it issued land, frees its
  * tensor memory and returns, leaving its outputs undefined. Calls made after
  * setting the budget back to 2e9 are unaffected. A checked build times every
- * wait, also one that completes at its first try, against the GPU's global
- * timer, whose resolution is about a microsecond: waits shorter than that may
- * not run out.
+ * wait against the GPU's global timer. In the feed-forward products waits of
+ * any length count; in the other kernels the time that a wait's last try is
+ * suspended for (1 to 2 us at most) is not counted, and a wait that its first
+ * try completes does not run out.
  */
 int dlm_checked_set_wait_budget(int64_t budget_ns);
 

@@ -150,16 +150,18 @@ constexpr uint64_t kWaitBudgetNs = 2000000000ull;  // 2 s
 // (returns false) when *abort is set by another thread of the block or when
 // `budget_ns` of wall-clock time has passed; in the latter case sets *abort
 // and DLM_DEVERR_TIMEOUT in the error word.
+//
+// Checked builds time every wait: a budget of a few hundred ns then makes the waits of a real
+// pipeline run out, in tests. Each try that does not complete is counted, but of the last one nothing: the
+// timer is read while mbarrier.try_wait still suspends the thread (1 to 2 us at most). With
+// kPolled, checked builds ask without being suspended, so that waits of any length count.
+template <bool kPolled = false>
 __device__ __forceinline__ bool mbar_wait_for(uint64_t* bar, uint32_t parity, volatile int* abort, int* err,
                                               uint64_t budget_ns) {
   if constexpr (kCheckBounds) {
-    // Checked builds time every wait, also one whose phase completes within
-    // the first try (mbarrier.try_wait suspends the thread in hardware for a
-    // while, so short waits never reach the loop below): a budget of a few
-    // hundred ns then makes the waits of a real pipeline run out, in tests.
     const uint64_t t0 = global_timer_ns();
     for (uint32_t it = 1;; ++it) {
-      const bool done = mbar_try_wait(bar, parity);
+      const bool done = kPolled ? mbar_test(bar, parity) : mbar_try_wait(bar, parity);
       if (global_timer_ns() - t0 > budget_ns) {
         *abort = 1;
         set_device_error(err, DLM_DEVERR_TIMEOUT);

@@ -94,7 +94,7 @@ struct Params {
 };
 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* err, uint64_t budget_ns) {
-  const bool ok = mbar_wait_for(bar, parity, abort, err, budget_ns);
+  const bool ok = mbar_wait_for<true>(bar, parity, abort, err, budget_ns);
   return __all_sync(0xffffffffu, ok);
 }
 
