@@ -333,7 +333,8 @@ size_t dlm_gated_linear_grad_workspace_bytes(int64_t rows, int64_t f, int64_t d)
  *   pre        z, in the shape of out, BF16, rows evenly strided, any alignment (dlm_linear_grad reads
  *              it, aligned); or NULL
  *   workspace  >= dlm_linear_workspace_bytes(N, m, k) bytes, 16-byte aligned, no initial contents
- *              needed; not used where that is 0. Calls sharing it must not overlap on the GPU.
+ *              needed; not used where that is 0, as it is for every size in this version.
+ *              Calls sharing it must not overlap on the GPU.
  * k and m are multiples of 8 up to 2^20, N up to 2^28, N k and N m up to 2^40. The base pointers
  * and row strides of x and weight are multiples of 16 bytes, strides below 2^40 bytes. No output
  * may overlap another tensor but as said. bf16 products, fp32 sums, one rounding of each output.

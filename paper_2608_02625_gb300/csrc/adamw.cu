@@ -31,7 +31,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kPerSm = 3;            // CTAs an SM: 80 registers a thread (four of 64: 6 % slower with 8 bits)
+constexpr int kPerSm = 3;            // CTAs an SM: 80 registers a thread, two more of which 8-bit states spill (four of 64: 6 % slower)
 constexpr int kBlock = kAdamwBlock;  // elements of a warp's turn, and of a scale
 constexpr int kPer = kBlock / 32;    // elements a lane
 constexpr float kTop = 448.f;        // the largest e4m3 value

@@ -1,8 +1,10 @@
 // Activations of a feed-forward block, x sigmoid(s):
 //   SiLU         s = x
 //   GELU (tanh)  s = 2 sqrt(2 / pi) (x + 0.044715 x^3)   (x (1 + tanh(s / 2)) / 2)
-// sigmoid(s) = 1 / (1 + 2^(-s log2 e)) with the approximate exponential and reciprocal: off
-// by some 2^-21 relative for |s| up to 20, far below the rounding to bf16 behind it.
+// sigmoid(s) = 1 / (1 + 2^(-s log2 e)) with the approximate exponential and reciprocal: off by
+// 2^-20 + 2^-21 min(|s|, 90) relative at most (their own 2^-22 each; s log2 e is rounded, and GELU's s
+// three times before, which the exponential turns into relative errors), 2^-14.4 at the far end, where the
+// rounding to bf16 behind it is 2^-8.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -60,7 +62,6 @@ __device__ __forceinline__ uint4 load8_raw(const __nv_bfloat16* src, bool wide) 
   for (int k = 0; k < 4; ++k) w[k] = h[2 * k] | static_cast<uint32_t>(h[2 * k + 1]) << 16;
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void load8(const __nv_bfloat16* src, bool wide, float (&x)[8]) { unpack8(load8_raw(src, wide), x); }
 __device__ __forceinline__ void store8(__nv_bfloat16* dst, bool wide, const float (&x)[8]) {
   if (wide) {
     *reinterpret_cast<uint4*>(dst) =

@@ -271,7 +271,7 @@ __device__ __forceinline__ void few_product(const Maps& maps, const Params& p, i
   if (p.splits > 1) cg::this_cluster().sync();
 
   // ================================================================ epilogue: this CTA's rows
-  // Eight columns a thread. (Two: 69 instructions for them, and 10000 cycles for 128 rows.)
+  // Eight columns a thread. (With two, 128 rows took 10000 cycles.)
   // The cluster's rank of the first CTA of this tile (the cluster is larger than the splits where one
   // launch computes both gradients).
   const uint32_t first_rank = cg::this_cluster().block_rank() - static_cast<uint32_t>(rank);
